@@ -597,6 +597,164 @@ int foremoe_plan_rank_slots(const int32_t* copy_rank, int32_t E, int32_t C_max, 
                             int32_t* S_out, int32_t* W_out);
 
 /*
+ * The operators around the expert layer in a policy-update step: the router
+ * that makes the layer's ids and gates and takes its dgates, the
+ * log-probabilities that recompute is for and that the update's backward
+ * starts from, and the AdamW step that takes the accumulated gradients.
+ *
+ * Logits are matrices with rows `ld` elements apart (ld >= the row length,
+ * any alignment that the type has).
+ *
+ * Router (Sec. 2.1: the router scores E experts and picks the top K; Sec. 5:
+ * recorded ids are replayed in recompute and policy update).
+ *   scores: FOREMOE_SOFTMAX s = softmax(l), FOREMOE_SIGMOID s = 1 / (1 + e^-l);
+ *   pi = s / sum(s), the distribution of the balance loss.
+ *   A token takes part if mask is NULL or mask[t] != 0, and some logit of it
+ *   is not -inf. A token that does not: ids -1, gates 0, no counts,
+ *   gradient 0.
+ *   ids_in NULL: the K experts of the largest logits, or with bias (sigmoid
+ *   scores only) of the largest s + bias, in descending order, ties to the
+ *   lower id. An expert whose logit is -inf or NaN is never picked; places
+ *   left over are empty: id -1, gate 0.
+ *   ids_in [T, K]: the recorded ids; a place whose id is outside [0, E), or
+ *   whose logit is -inf, is empty.
+ *   gates = scale * s of the picked, or with renorm scale * s / (sum of the
+ *   picked s) (0 where that sum is 0).
+ *   Statistics over the tokens that take part (all four pointers, or none):
+ *   counts[e] picks of expert e, n_tokens[0] tokens, prob_mean[e] the mean
+ *   of pi_e (0 without tokens), and with f_e = counts[e] / sum(counts)
+ *   balance_loss[0] = E * sum_e f_e * prob_mean[e], 1 for an even load.
+ *   A NaN or +inf logit makes pi NaN, and the gates that it enters; ids
+ *   stay in range.
+ * logits [T, E] of dtype; bias [E] fp32 or NULL; mask [T] bytes or NULL;
+ * ids [T, K] out (may be ids_in); gates [T, K] fp32 out. 1 <= E <=
+ * FOREMOE_MAX_EXPERTS, 1 <= K <= min(E, FOREMOE_MAX_TOPK), T*K < 2^31.
+ * ws, ws_bytes: needed with statistics, foremoe_router_workspace_size(E)
+ * bytes, 256-byte aligned, zero-filled before its first use (the call leaves
+ * its counter at zero). Calls that share one must not overlap in time.
+ */
+typedef enum foremoe_score {
+  FOREMOE_SOFTMAX = 0,
+  FOREMOE_SIGMOID = 1
+} foremoe_score;
+size_t foremoe_router_workspace_size(int32_t E);
+int foremoe_router_fwd(const void* logits, foremoe_dtype dtype, int64_t ld, int64_t T, int32_t E,
+                       int32_t K, foremoe_score score, int32_t renorm, float scale,
+                       const float* bias, const uint8_t* mask, const int32_t* ids_in,
+                       int32_t* ids, float* gates, int32_t* counts, int32_t* n_tokens,
+                       float* prob_mean, float* balance_loss, void* ws, size_t ws_bytes,
+                       void* stream);
+
+/*
+ * Backward of the router: the gradient of the logits (at fixed ids) from the
+ * gates' gradient, plus balance_coef times the gradient of balance_loss (at
+ * fixed counts). ids are those that foremoe_router_fwd wrote. dgates may be
+ * NULL (the gates' part is 0); counts and n_tokens are needed where
+ * balance_coef is not 0, and may be sums over several ranks' tokens.
+ * dlogits [T, E] of the logits' dtype, rows ld_out elements apart; it may be
+ * the logits themselves (the same address and ld).
+ */
+int foremoe_router_bwd(const void* logits, foremoe_dtype dtype, int64_t ld, int64_t T, int32_t E,
+                       int32_t K, foremoe_score score, int32_t renorm, float scale,
+                       const uint8_t* mask, const int32_t* ids, const float* dgates,
+                       const int32_t* counts, const int32_t* n_tokens, float balance_coef,
+                       void* dlogits, int64_t ld_out, void* stream);
+
+/*
+ * Log-probabilities of given tokens. With x = logits / temperature, per row:
+ *   lse = log sum_j e^x_j, logp = x_target - lse,
+ *   entropy = lse - sum_j p_j x_j, p = e^(x - lse), and the n_top largest
+ *   logits in descending order, ties to the lower id: top_ids, and
+ *   top_logp = x - lse. A logit of -inf or NaN is never among them; places
+ *   left over hold id -1 and -inf.
+ * targets [N] int32 or NULL. A row whose target is outside [0, V) is ignored
+ *   and not read: logp, entropy and lse 0, its top places left over. Without
+ *   targets every row counts, and logp must be NULL.
+ * logits / temperature are within the range of fp32. A row of -inf only: lse
+ * -inf, logp -inf, entropy 0. A NaN or +inf logit makes its row's logp,
+ * entropy and lse NaN.
+ * logits [N, V] of dtype; logp, entropy, lse [N] fp32 out, each or NULL;
+ * top_ids [N, n_top] int32, top_logp [N, n_top] fp32 out, NULL with
+ * n_top = 0. temperature > 0, 1 <= V < 2^31, 0 <= n_top <= min(V,
+ * FOREMOE_MAX_TOP), N < 2^31.
+ * ws (optional): NULL, or foremoe_logprobs_workspace_size() bytes, 256-byte
+ * aligned, zero-filled before its first use (each call leaves its counters
+ * at zero): rows too few to fill the GPU are then cut into pieces. The sums'
+ * order depends on that, and on N and V, but not on the run. Calls that
+ * share one must not overlap in time.
+ */
+#define FOREMOE_MAX_TOP 32
+size_t foremoe_logprobs_workspace_size(void);
+int foremoe_token_logprobs(const void* logits, foremoe_dtype dtype, int64_t ld, int64_t N,
+                           int64_t V, const int32_t* targets, float temperature, int32_t n_top,
+                           float* logp, float* entropy, float* lse, int32_t* top_ids,
+                           float* top_logp, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Backward of the log-probabilities and entropies:
+ *   dlogits_j = (dlogp (1[j = target] - p_j) - dentropy p_j (log p_j + entropy))
+ *               / temperature
+ * with p from the forward's lse; 0 where p_j is 0 (but for the target) and
+ * in ignored rows. dlogp [N] or NULL (needs targets); dentropy [N] or NULL
+ * (needs entropy [N], the forward's). dlogits [N, V] of the logits' dtype,
+ * rows ld_out apart; it may be the logits themselves (same address and ld).
+ */
+int foremoe_token_logprobs_bwd(const void* logits, foremoe_dtype dtype, int64_t ld, int64_t N,
+                               int64_t V, const int32_t* targets, float temperature,
+                               const float* lse, const float* entropy, const float* dlogp,
+                               const float* dentropy, void* dlogits, int64_t ld_out, void* stream);
+
+/*
+ * One AdamW step over many tensors, step = 1, 2, ...:
+ *   g = grad * grad_scale[0]  (grad_scale NULL: 1)
+ *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2
+ *   p = p (1 - lr weight_decay)
+ *       - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
+ * in fp32; where the last quotient is 0 / 0 (eps = 0, no gradient yet) it is
+ * 0. p is master where the record has one (param, of bf16, then gets
+ * its rounded copy), else param itself. zero_grads != 0: grad is zero
+ * afterwards (the accumulators of the weight gradients start anew).
+ * state_bits 32: m and v are fp32 [n]; m_scale, v_scale NULL.
+ * state_bits 8: m and v are bytes [n] with an fp32 scale for every
+ *   FOREMOE_ADAMW_BLOCK consecutive elements, [ceil(n / block)] each. The
+ *   scale is the block's largest |m|, or sqrt(v). A byte of m is a sign bit
+ *   and the rounded top bits of |m| / scale as a float, 3 bits of fraction,
+ *   127 standing for 1; a byte of v is the same of sqrt(v) / scale with 4
+ *   bits of fraction, 255 standing for 1. Byte 0 is zero; a v above zero
+ *   never becomes byte 0. Values below 2^-16 of the scale go to byte 0 (m)
+ *   or 1 (v). The step itself uses the unrounded m and v. A NaN or infinite
+ *   element makes its block's scale NaN or infinite, so the whole block
+ *   shows it at the next step. Zero-filled states are the start.
+ * tensors: HOST array, read during the call only; pointers aligned to their
+ * types. n = 0: skipped. One launch for every FOREMOE_ADAMW_LAUNCH tensors.
+ */
+#define FOREMOE_ADAMW_BLOCK 256
+#define FOREMOE_ADAMW_LAUNCH 48
+typedef struct foremoe_adamw_tensor {
+  void* param;         /* [n] of param_dtype                     */
+  void* grad;          /* [n] of grad_dtype                      */
+  float* master;       /* [n] fp32 or NULL; bf16 parameters only */
+  void* m;             /* [n] fp32, or bytes                     */
+  void* v;
+  float* m_scale;      /* [ceil(n / FOREMOE_ADAMW_BLOCK)], 8 bits */
+  float* v_scale;
+  int64_t n;
+  double weight_decay;
+} foremoe_adamw_tensor;
+int foremoe_adamw_step(const foremoe_adamw_tensor* tensors, int32_t n_tensors,
+                       foremoe_dtype param_dtype, foremoe_dtype grad_dtype, int32_t state_bits,
+                       double lr, double beta1, double beta2, double eps, int64_t step,
+                       const float* grad_scale, int32_t zero_grads, void* stream);
+
+/*
+ * The values that 8-bit states stand for: m_out, v_out [n] fp32 from m, v
+ * [n] bytes and their scales.
+ */
+int foremoe_adamw_state_values(const uint8_t* m, const float* m_scale, const uint8_t* v,
+                               const float* v_scale, int64_t n, float* m_out, float* v_out,
+                               void* stream);
+
+/*
  * Timed forms of the four row-GEMM calls (a measurement aid, not an
  * operation of the method): the same arguments, work and results as
  * foremoe_ffn_gate_up_fwd, foremoe_ffn_down_fwd, foremoe_ffn_down_dgrad and

@@ -27,8 +27,13 @@ XFER_GRADS = 2
 XFER_ASSIGN = 0
 XFER_ADD = 1
 MAX_XFER_RECORDS = 64
+SOFTMAX = 0
+SIGMOID = 1
+MAX_TOP = 32
+ADAMW_BLOCK = 256
 
 c_i32, c_i64, c_sz, c_p = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_void_p
+c_f32, c_f64 = ctypes.c_float, ctypes.c_double
 
 
 class Plan(ctypes.Structure):
@@ -55,6 +60,14 @@ class WgradStep(ctypes.Structure):
 
 
 PWgradStep = ctypes.POINTER(WgradStep)
+
+
+class AdamWTensor(ctypes.Structure):
+    _fields_ = [("param", c_p), ("grad", c_p), ("master", c_p), ("m", c_p), ("v", c_p), ("m_scale", c_p),
+                ("v_scale", c_p), ("n", c_i64), ("weight_decay", c_f64)]
+
+
+PAdamWTensor = ctypes.POINTER(AdamWTensor)
 
 # name -> (restype, argtypes)
 SIGNATURES = {
@@ -106,6 +119,19 @@ SIGNATURES = {
     "foremoe_plan_base": (ctypes.c_int, [c_p, c_i32, PMachine, c_i64, c_i64, c_p]),
     "foremoe_plan_micro_step": (ctypes.c_int, [c_p, c_i32, PMachine, c_p, c_i32, c_p, c_p, c_p]),
     "foremoe_plan_rank_slots": (ctypes.c_int, [c_p, c_i32, c_i32, c_i32, c_i32, c_p, c_p, c_p, c_p, c_p, c_p, c_p]),
+    "foremoe_router_workspace_size": (c_sz, [c_i32]),
+    "foremoe_router_fwd": (ctypes.c_int, [c_p, c_i32, c_i64, c_i64, c_i32, c_i32, c_i32, c_i32, c_f32, c_p, c_p, c_p,
+                                          c_p, c_p, c_p, c_p, c_p, c_p, c_p, c_sz, c_p]),
+    "foremoe_router_bwd": (ctypes.c_int, [c_p, c_i32, c_i64, c_i64, c_i32, c_i32, c_i32, c_i32, c_f32, c_p, c_p, c_p,
+                                          c_p, c_p, c_f32, c_p, c_i64, c_p]),
+    "foremoe_logprobs_workspace_size": (c_sz, []),
+    "foremoe_token_logprobs": (ctypes.c_int, [c_p, c_i32, c_i64, c_i64, c_i64, c_p, c_f32, c_i32, c_p, c_p, c_p, c_p,
+                                              c_p, c_p, c_sz, c_p]),
+    "foremoe_token_logprobs_bwd": (ctypes.c_int, [c_p, c_i32, c_i64, c_i64, c_i64, c_p, c_f32, c_p, c_p, c_p, c_p,
+                                                  c_p, c_i64, c_p]),
+    "foremoe_adamw_step": (ctypes.c_int, [PAdamWTensor, c_i32, c_i32, c_i32, c_i32, c_f64, c_f64, c_f64, c_f64, c_i64,
+                                          c_p, c_i32, c_p]),
+    "foremoe_adamw_state_values": (ctypes.c_int, [c_p, c_p, c_p, c_p, c_i64, c_p, c_p, c_p]),
     "foremoe_ffn_gate_up_fwd_timed": (ctypes.c_int, [c_p, c_i32, c_i32, c_i32, c_i32, c_p, c_p, c_i32, c_p,
                                                      c_i64, c_p, c_p, c_p, c_sz, c_p, c_p, c_p]),
     "foremoe_ffn_down_fwd_timed": (ctypes.c_int, [c_p, c_i32, c_i32, c_i32, c_i32, c_p, c_p, c_i32, c_p, c_i64,

@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes
 from dataclasses import dataclass
-from typing import Optional, Tuple
+from typing import NamedTuple, Optional, Tuple
 
 import numpy as np
 import torch
@@ -351,6 +351,212 @@ def permute_bwd(dx_perm: torch.Tensor, pair_to_row: torch.Tensor, T: int, K: int
                                           dx.data_ptr(), _DT[out_dtype], _stream(dx_perm.device)),
           "foremoe_permute_bwd")
     return dx
+
+
+# ---------------------------------------------------------------------------
+# Router, token log-probabilities and optimizer states, the operators around
+# the layer (see include/foremoe.h)
+# ---------------------------------------------------------------------------
+_SCORES = {"softmax": _lib.SOFTMAX, "sigmoid": _lib.SIGMOID}
+
+
+def _rows(t: torch.Tensor, name: str) -> int:
+    """Checks a [rows, columns] device tensor whose rows are contiguous and do
+    not overlap; returns the elements from one row to the next."""
+    if not t.is_cuda:
+        raise ValueError(f"{name}: expected a device tensor")
+    if t.dim() != 2:
+        raise ValueError(f"{name}: expected [rows, columns]")
+    rows, cols = t.shape
+    by_row, by_col = t.stride()
+    if by_col != 1 and cols > 1:
+        raise ValueError(f"{name}: rows must be contiguous")
+    if rows <= 1:
+        return max(cols, 1)
+    if by_row < cols:
+        raise ValueError(f"{name}: rows overlap")
+    return by_row
+
+
+def _vec(t: Optional[torch.Tensor], n: int, dtype: torch.dtype, name: str, device: torch.device) -> Optional[int]:
+    """The address of a contiguous device tensor of n elements of dtype."""
+    if t is None:
+        return None
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}")
+    if t.numel() != n:
+        raise ValueError(f"{name}: {t.numel()} elements, {n} expected")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not {device}")
+    return _ptr(t)
+
+
+def _mask(mask: Optional[torch.Tensor], n: int, device: torch.device) -> Optional[int]:
+    if mask is None:
+        return None
+    if mask.dtype not in (torch.bool, torch.uint8):
+        raise TypeError("mask must be bool or uint8")
+    return _vec(mask, n, mask.dtype, "mask", device)
+
+
+class Routing(NamedTuple):
+    """What router_fwd returns (the last four None without statistics)."""
+    ids: torch.Tensor                      # [T, K] int32, -1: an empty place
+    gates: torch.Tensor                    # [T, K] fp32
+    counts: Optional[torch.Tensor]         # [E] int32
+    n_tokens: Optional[torch.Tensor]       # [1] int32
+    prob_mean: Optional[torch.Tensor]      # [E] fp32
+    balance_loss: Optional[torch.Tensor]   # [1] fp32
+
+
+def router_workspace(E: int, device) -> torch.Tensor:
+    """Scratch of the router's statistics (foremoe_router_workspace_size(E)
+    bytes), zero-filled as its counter must be before first use."""
+    n = _lib.load().foremoe_router_workspace_size(E)
+    if n == 0:
+        raise ValueError("invalid number of experts")
+    return torch.zeros(n, dtype=torch.uint8, device=device)
+
+
+def _score(score: str) -> int:
+    if score not in _SCORES:
+        raise ValueError(f"score must be one of {sorted(_SCORES)}")
+    return _SCORES[score]
+
+
+def router_fwd(logits: torch.Tensor, K: int, *, score: str = "softmax", renorm: bool = True, scale: float = 1.0,
+               bias: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None,
+               ids: Optional[torch.Tensor] = None, stats: bool = True, ws: Optional[torch.Tensor] = None) -> Routing:
+    """Ids and gates of T tokens from the logits [T, E] (fp32 or bf16; rows
+    may be apart), as histogram_assign, permute and combine take them.
+
+    ids: recorded ids [T, K] to replay instead of picking. mask [T]: false for
+    tokens that take no part. bias [E]: added to sigmoid scores for picking.
+    stats: also the per-expert counts and the balance loss; needs ws from
+    router_workspace (one is made when missing)."""
+    ld = _rows(logits, "logits")
+    T, E = logits.shape
+    dev = logits.device
+    out_ids = torch.empty((T, K), dtype=torch.int32, device=dev)
+    gates = torch.empty((T, K), dtype=torch.float32, device=dev)
+    counts = n_tokens = prob_mean = loss = None
+    if ids is not None and tuple(ids.shape) != (T, K):
+        raise ValueError("ids must be [T, K]")
+    if stats:
+        counts = torch.empty(E, dtype=torch.int32, device=dev)
+        n_tokens = torch.empty(1, dtype=torch.int32, device=dev)
+        prob_mean = torch.empty(E, dtype=torch.float32, device=dev)
+        loss = torch.empty(1, dtype=torch.float32, device=dev)
+        if ws is None:
+            ws = router_workspace(E, dev)
+        sp = (counts.data_ptr(), n_tokens.data_ptr(), prob_mean.data_ptr(), loss.data_ptr(), _ptr(ws), ws.numel())
+    else:
+        sp = (None, None, None, None, None, 0)
+    check(_lib.load().foremoe_router_fwd(
+        logits.data_ptr(), _dt(logits), ld, T, E, K, _score(score), int(renorm), scale,
+        _vec(bias, E, torch.float32, "bias", dev), _mask(mask, T, dev), _vec(ids, T * K, torch.int32, "ids", dev),
+        out_ids.data_ptr(), gates.data_ptr(), *sp, _stream(dev)), "foremoe_router_fwd")
+    return Routing(out_ids, gates, counts, n_tokens, prob_mean, loss)
+
+
+def router_bwd(logits: torch.Tensor, ids: torch.Tensor, dgates: Optional[torch.Tensor], *, score: str = "softmax",
+               renorm: bool = True, scale: float = 1.0, mask: Optional[torch.Tensor] = None,
+               counts: Optional[torch.Tensor] = None, n_tokens: Optional[torch.Tensor] = None,
+               balance_coef: float = 0.0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The gradient of the logits from the gates' gradient (as combine_bwd
+    makes it) plus balance_coef times that of the balance loss, at the ids
+    that router_fwd returned. counts and n_tokens may be sums over ranks.
+    out: where it goes, e.g. the logits themselves."""
+    ld = _rows(logits, "logits")
+    T, E = logits.shape
+    K = ids.shape[1]
+    dev = logits.device
+    if out is None:
+        out = torch.empty((T, E), dtype=logits.dtype, device=dev)
+    elif out.shape != logits.shape or out.dtype != logits.dtype or out.device != dev:
+        raise ValueError("out must be like the logits")
+    check(_lib.load().foremoe_router_bwd(
+        logits.data_ptr(), _dt(logits), ld, T, E, K, _score(score), int(renorm), scale, _mask(mask, T, dev),
+        _vec(ids, T * K, torch.int32, "ids", dev), _vec(dgates, T * K, torch.float32, "dgates", dev),
+        _vec(counts, E, torch.int32, "counts", dev), _vec(n_tokens, 1, torch.int32, "n_tokens", dev), balance_coef,
+        out.data_ptr(), _rows(out, "out"), _stream(dev)), "foremoe_router_bwd")
+    return out
+
+
+class TokenLogprobs(NamedTuple):
+    """What token_logprobs returns."""
+    logp: Optional[torch.Tensor]      # [N] fp32, None without targets
+    entropy: torch.Tensor             # [N] fp32
+    lse: torch.Tensor                 # [N] fp32, what the backward reads
+    top_ids: Optional[torch.Tensor]   # [N, n_top] int32, None with n_top = 0
+    top_logp: Optional[torch.Tensor]  # [N, n_top] fp32
+
+
+def logprobs_workspace(device) -> torch.Tensor:
+    """Scratch that lets token_logprobs cut few rows into pieces
+    (foremoe_logprobs_workspace_size() bytes), zero-filled as its counters
+    must be before first use."""
+    return torch.zeros(_lib.load().foremoe_logprobs_workspace_size(), dtype=torch.uint8, device=device)
+
+
+def token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = None, *, temperature: float = 1.0,
+                   n_top: int = 0, ws: Optional[torch.Tensor] = None) -> TokenLogprobs:
+    """Log-probabilities of the targets [N] (int32; outside [0, V): the row is
+    ignored) under softmax(logits / temperature), with every row's entropy and
+    its n_top likeliest tokens. logits [N, V], fp32 or bf16; rows may be
+    apart. ws: from logprobs_workspace."""
+    ld = _rows(logits, "logits")
+    N, V = logits.shape
+    dev = logits.device
+    lse = torch.empty(N, dtype=torch.float32, device=dev)
+    entropy = torch.empty(N, dtype=torch.float32, device=dev)
+    logp = torch.empty(N, dtype=torch.float32, device=dev) if targets is not None else None
+    top_ids = top_logp = None
+    if n_top > 0:
+        top_ids = torch.empty((N, n_top), dtype=torch.int32, device=dev)
+        top_logp = torch.empty((N, n_top), dtype=torch.float32, device=dev)
+    p = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    check(_lib.load().foremoe_token_logprobs(
+        logits.data_ptr(), _dt(logits), ld, N, V, _vec(targets, N, torch.int32, "targets", dev), temperature, n_top,
+        p(logp), entropy.data_ptr(), lse.data_ptr(), p(top_ids), p(top_logp), *_ws(ws), _stream(dev)),
+        "foremoe_token_logprobs")
+    return TokenLogprobs(logp, entropy, lse, top_ids, top_logp)
+
+
+def token_logprobs_bwd(logits: torch.Tensor, targets: Optional[torch.Tensor], lse: torch.Tensor,
+                       dlogp: Optional[torch.Tensor], *, entropy: Optional[torch.Tensor] = None,
+                       dentropy: Optional[torch.Tensor] = None, temperature: float = 1.0,
+                       out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The gradient of the logits from those of the log-probabilities and of
+    the entropies (which needs the forward's entropy). out: where it goes,
+    e.g. the logits themselves, which saves their size again."""
+    ld = _rows(logits, "logits")
+    N, V = logits.shape
+    dev = logits.device
+    f32 = torch.float32
+    if out is None:
+        out = torch.empty((N, V), dtype=logits.dtype, device=dev)
+    elif out.shape != logits.shape or out.dtype != logits.dtype or out.device != dev:
+        raise ValueError("out must be like the logits")
+    check(_lib.load().foremoe_token_logprobs_bwd(
+        logits.data_ptr(), _dt(logits), ld, N, V, _vec(targets, N, torch.int32, "targets", dev), temperature,
+        _vec(lse, N, f32, "lse", dev), _vec(entropy, N, f32, "entropy", dev), _vec(dlogp, N, f32, "dlogp", dev),
+        _vec(dentropy, N, f32, "dentropy", dev), out.data_ptr(), _rows(out, "out"), _stream(dev)),
+        "foremoe_token_logprobs_bwd")
+    return out
+
+
+def adamw_state_values(m: torch.Tensor, m_scale: torch.Tensor, v: torch.Tensor, v_scale: torch.Tensor):
+    """The fp32 moments (m, v) that a tensor's 8-bit optimizer states stand for."""
+    n, dev = m.numel(), m.device
+    blocks = -(-n // _lib.ADAMW_BLOCK)
+    m_out = torch.empty(m.shape, dtype=torch.float32, device=dev)
+    v_out = torch.empty(m.shape, dtype=torch.float32, device=dev)
+    check(_lib.load().foremoe_adamw_state_values(
+        _vec(m, n, torch.uint8, "m", dev), _vec(m_scale, blocks, torch.float32, "m_scale", dev),
+        _vec(v, n, torch.uint8, "v", dev), _vec(v_scale, blocks, torch.float32, "v_scale", dev), n, m_out.data_ptr(),
+        v_out.data_ptr(), _stream(dev)), "foremoe_adamw_state_values")
+    return m_out, v_out
 
 
 # ---------------------------------------------------------------------------
