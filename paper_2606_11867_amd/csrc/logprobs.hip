@@ -5,25 +5,58 @@
 
 #include "common.h"
 
+// Fused multiply-adds are written out: a product that is rounded once and
+// used twice has to be the same both times.
+#pragma clang fp contract(off)
+
 namespace foremoe {
 namespace {
+
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+// A row may start at any element, so its 16-byte vectors have the alignment
+// of the type only; the hardware takes those.
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
 
 constexpr int kLpThreads = 256;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLowest = -3.402823466e38f;
+constexpr int kTile = 4;      // vectors that a lane holds at a time
+constexpr int kBuf = 512;     // candidates for the top places that a wavefront keeps
+constexpr int kMaxPieces = 64;     // of one row
+constexpr int kMaxSplit = 1024;    // pieces of all rows
+constexpr int kJoin = kMaxPieces * FOREMOE_MAX_TOP / kLpThreads;  // candidates a lane takes when pieces are joined
+
+struct Sums {
+  float m, s, t;
+};
+struct Candidate {
+  float x;
+  int32_t id;
+};
+struct LpPiece {  // what a piece of a row leaves for the join
+  Sums r;
+  float pad;
+};
 
 struct LogprobArgs {
   const void* logits;
   int64_t ld;
-  int32_t N, V;
+  int32_t first, V;  // first: the launch's first row
   const int32_t* targets;
   float c, inv_temperature;  // c: log2(e) / temperature
   int32_t n_top;
   float *logp, *entropy, *lse;
   int32_t* top_ids;
   float* top_logp;
+  int32_t pieces, piece_vectors;
+  uint32_t* ticket;     // [N]
+  LpPiece* part;        // [N, pieces]
+  Candidate* part_top;  // [N, pieces, n_top]
 };
+
+template <bool BF16>
+constexpr int kVec = BF16 ? 8 : 4;  // elements of a 16-byte vector
 
 template <bool BF16>
 __device__ __forceinline__ float load_lp(const void* p, int64_t i) {
@@ -31,110 +64,393 @@ __device__ __forceinline__ float load_lp(const void* p, int64_t i) {
   return ((const float*)p)[i];
 }
 
-// Running maximum m of the logits x, s = sum e, t = sum (x - m) e with
-// e = 2^((x - m) c), so that lse = m / temperature + ln2 log2 s and
-// entropy = ln2 log2 s - t / (s temperature), both terms >= 0. Subtracting
-// before scaling keeps logits up to the type's ends apart. m starts at the
-// lowest finite number, so an x of -inf adds nothing to s.
-struct Sums {
-  float m, s, t;
-};
+template <bool BF16>
+__device__ __forceinline__ u32x4 load_vec(const void* row, uint32_t vector) {
+  return *(const u32x4_any*)((const char*)row + (size_t)vector * 16);
+}
 
-__device__ __forceinline__ float rebased(float t, float d, float s) { return t + fmaxf(d, kLowest) * s; }
+template <bool BF16>
+__device__ __forceinline__ void unpack(u32x4 v, float* x) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (BF16) {
+      x[2 * i] = __uint_as_float(v[i] << 16);
+      x[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+    } else {
+      x[i] = __uint_as_float(v[i]);
+    }
+  }
+}
+
+// Running sums of a row: the maximum m of its logits x, and with
+// y = (x - m) c in base 2, s = sum 2^y and t = sum y 2^y, so that
+//   lse = ln2 (m c + log2 s),  entropy = ln2 (log2 s - t / s),
+// both terms of the entropy >= 0. y is one fused multiply-add, x c - m c with
+// m c rounded once: the same reference everywhere, so that its rounding
+// cancels. m starts at the lowest finite number, so an x of -inf adds nothing
+// to s. Logits so large that m c overflows subtract before they scale.
+__device__ __forceinline__ bool huge(float mc) { return !(fabsf(mc) < 1e38f); }
+
+// 2^y of what is summed under a, seen from the reference m; in y.
+__device__ __forceinline__ float shift(float from, float m, float c) {
+  const float a = from * c, b = m * c;
+  return huge(a) || huge(b) ? (from - m) * c : a - b;
+}
+
+__device__ __forceinline__ void rebase(Sums& a, float m, float c) {
+  const float y = shift(a.m, m, c), e = __builtin_amdgcn_exp2f(y);
+  a.t = e == 0.0f ? 0.0f : e * (a.t + y * a.s);
+  a.s = e == 0.0f ? a.s * 0.0f : a.s * e;  // keeps a NaN
+  a.m = m;
+}
 
 __device__ __forceinline__ Sums join(Sums a, Sums b, float c) {
   const float m = fmaxf(a.m, b.m);
-  const float da = a.m - m, db = b.m - m;
-  const float ea = exp2f(da * c), eb = exp2f(db * c);
-  Sums r;
-  r.m = m;
-  r.s = a.s * ea + b.s * eb;
-  // an e of 0 takes what was below along, however large (d s may overflow)
-  r.t = (ea == 0.0f ? 0.0f : ea * rebased(a.t, da, a.s)) + (eb == 0.0f ? 0.0f : eb * rebased(b.t, db, b.s));
-  return r;
+  rebase(a, m, c);
+  rebase(b, m, c);
+  return Sums{m, a.s + b.s, a.t + b.t};
 }
 
-__device__ __forceinline__ Sums add(Sums a, float x, float c) {
-  if (x > a.m) {
-    const float d = a.m - x, e = exp2f(d * c);
-    a.t = e == 0.0f ? 0.0f : e * rebased(a.t, d, a.s);
-    a.s *= e;
-    a.m = x;
+// Adds n elements of one lane.
+template <int n>
+__device__ __forceinline__ void add(Sums& a, const float (&x)[n], float c) {
+  float top = x[0];
+#pragma unroll
+  for (int i = 1; i < n; ++i) top = fmaxf(top, x[i]);
+  if (top > a.m) rebase(a, top, c);
+  const float mc = a.m * c;
+  float s[2] = {0.0f, 0.0f}, t[2] = {0.0f, 0.0f};
+#pragma unroll
+  for (int i = 0; i < n; ++i) {
+    const float y = fmaf(x[i], c, -mc), e = __builtin_amdgcn_exp2f(y);
+    s[i & 1] += e;
+    t[i & 1] = fmaf(y, e, t[i & 1]);
   }
-  const float d = x - a.m, e = exp2f(d * c);
-  a.s += e;
-  a.t += fmaxf(d, kLowest) * e;
-  return a;
+  s[0] += s[1];
+  t[0] += t[1];
+  // y 2^y of a y of -inf is a NaN above (a masked logit): once more with care
+  if (__builtin_expect(t[0] != t[0] || huge(mc), 0)) {
+    s[0] = t[0] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+      const float y = (x[i] - a.m) * c, e = __builtin_amdgcn_exp2f(y);
+      s[0] += e;
+      t[0] += fmaxf(y, kLowest) * e;
+    }
+  }
+  a.s += s[0];
+  a.t += t[0];
 }
 
 __device__ __forceinline__ bool better(float v, int id, float w, int jd) { return v > w || (v == w && id < jd); }
 
-// One workgroup per row; the top alternatives one after another, each a pass
-// over the row.
-template <bool BF16>
-__global__ __launch_bounds__(kLpThreads) void logprobs_kernel(LogprobArgs a) {
-  __shared__ Sums sh[kLpThreads / 64];
-  __shared__ float sh_v[kLpThreads / 64];
-  __shared__ int sh_i[kLpThreads / 64];
-  const int64_t row = blockIdx.x, base = row * a.ld;
-  const int tid = threadIdx.x, lane = lane_id(), wave = tid >> 6;
+// The candidates of a wavefront for the n top places: everything it has seen
+// that is not behind its threshold (an element with at least n - 1 before it,
+// itself a candidate), in any order.
+//
+// The threshold is the n-th largest of 64 lanes' own maxima, which n lanes
+// reach: of the first elements, then of the kept candidates whenever the
+// buffer is full. A lane holds at most kBuf / 64 = 8 candidates then, so at
+// most 8 n <= 256 pass, and a ballot's 64 always fit behind them.
+struct TopList {
+  Candidate* buf;  // [kBuf] in LDS
+  int n, count;
+  float x;  // threshold
+  int id;
+
+  __device__ __forceinline__ void start(Candidate* b, int places) {
+    buf = b, n = places, count = 0, x = -INFINITY, id = -1;
+  }
+  // an integer in the order of the floats, NaN lowest (0.0 and -0.0 alike)
+  static __device__ __forceinline__ uint32_t ordered(float v) {
+    if (!(v >= -INFINITY)) return 0;
+    const uint32_t b = __float_as_uint(v + 0.0f);
+    return b ^ (b >> 31 ? 0xffffffffu : 0x80000000u);
+  }
+  static __device__ __forceinline__ float of_ordered(uint32_t k) {
+    return __uint_as_float(k ^ (k >> 31 ? 0x80000000u : 0xffffffffu));
+  }
+  // The n-th largest of the lanes' keys.
+  __device__ __forceinline__ uint32_t nth(uint32_t key, int nth) const {
+    uint32_t k = 0;
+#pragma unroll
+    for (int bit = 31; bit >= 0; --bit) {
+      const uint32_t test = k | (1u << bit);
+      if (__popcll(__ballot(key >= test)) >= nth) k = test;
+    }
+    return k;
+  }
+  // Before anything is added: the lanes' largest elements so far.
+  __device__ __forceinline__ void first_threshold(float lane_max) {
+    const float v = of_ordered(max(nth(ordered(lane_max), n), ordered(-INFINITY)));
+    if (v > x) x = v, id = INT_MAX;
+  }
+  __device__ __forceinline__ bool passes(float v, int i) const { return v > x || (v == x && i <= id); }
+  __device__ __forceinline__ void fence() const {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  }
+  __device__ __forceinline__ void put(float v, int i, bool pass) {
+    const uint64_t mask = __ballot(pass);
+    if (pass) buf[count + lanes_below(mask)] = Candidate{v, i};
+    count += __popcll(mask);
+  }
+  __device__ __forceinline__ void prune() {
+    const int lane = lane_id();
+    fence();
+    Candidate e[kBuf / 64], best{-INFINITY, INT_MAX};
+#pragma unroll
+    for (int q = 0; q < kBuf / 64; ++q) {
+      const int at = lane + 64 * q;
+      e[q] = at < count ? buf[at] : Candidate{-INFINITY, INT_MAX};
+      if (better(e[q].x, e[q].id, best.x, best.id)) best = e[q];
+    }
+    const uint32_t key = ordered(best.x), k = nth(key, n);
+    const int above = __popcll(__ballot(key > k));
+    // of the lanes that are equal, those with the lowest ids
+    const bool equal = key == k;
+    int last = INT_MAX;
+    if (__popcll(__ballot(equal)) > n - above)
+      last = (int)~nth(equal ? ~(uint32_t)best.id : 0u, n - above);
+    const float v = of_ordered(max(k, ordered(-INFINITY)));
+    if (better(v, last, x, id)) x = v, id = last;
+    fence();
+    count = 0;
+#pragma unroll
+    for (int q = 0; q < kBuf / 64; ++q) put(e[q].x, e[q].id, e[q].x > -INFINITY && passes(e[q].x, e[q].id));
+    fence();
+  }
+  // All lanes of the wavefront together; x -inf where a lane has nothing.
+  __device__ __forceinline__ void offer(float v, int i) {
+    bool pass = passes(v, i);
+    if (!__any(pass)) return;
+    if (count + __popcll(__ballot(pass)) > kBuf) {
+      prune();
+      pass = passes(v, i);
+    }
+    put(v, i, pass);
+  }
+};
+
+// Sums of the workgroup, in every thread; the order of the joins is fixed.
+template <int WAVES>
+__device__ __forceinline__ Sums join_block(Sums r, Sums* sh, float c) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1)
+    r = join(r, Sums{__shfl_xor(r.m, o, 64), __shfl_xor(r.s, o, 64), __shfl_xor(r.t, o, 64)}, c);
+  if constexpr (WAVES > 1) {
+    if (lane_id() == 0) sh[threadIdx.x >> 6] = r;
+    __syncthreads();
+    r = sh[0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) r = join(r, sh[w], c);
+  }
+  return r;
+}
+
+// The workgroup's candidates by rank: out(place, candidate) for the places
+// below n, and how many there are.
+template <int WAVES, class Out>
+__device__ __forceinline__ int rank_block(TopList& top, const Candidate* buf, int* sh_count, Out&& out) {
+  if (top.count > 64) top.prune();
+  if (lane_id() == 0) sh_count[threadIdx.x >> 6] = top.count;
+  if constexpr (WAVES > 1) __syncthreads();
+  else top.fence();
+  int all = 0;
+  for (int w = 0; w < WAVES; ++w) {
+    const int cw = sh_count[w];
+    for (int j0 = 0; j0 < cw; j0 += 64 * WAVES) {
+      const int j = j0 + threadIdx.x;
+      if (j >= cw) continue;
+      const Candidate me = buf[w * kBuf + j];
+      int rank = 0;
+      for (int q = 0; q < WAVES; ++q)
+        for (int i = 0; i < sh_count[q]; ++i) {
+          const Candidate o = buf[q * kBuf + i];
+          rank += better(o.x, o.id, me.x, me.id);
+        }
+      if (rank < top.n) out(rank, me);
+    }
+    all += cw;
+  }
+  return min(all, top.n);
+}
+
+// A workgroup of WAVES wavefronts takes a piece of a row; where a row has
+// several, the last one to finish joins them.
+template <bool BF16, bool TOP, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void logprobs_kernel(LogprobArgs a) {
+  constexpr int kThreads = 64 * WAVES, VEC = kVec<BF16>;
+  __shared__ Candidate buf[TOP ? WAVES * kBuf : 1];
+  __shared__ Sums sh[WAVES];
+  __shared__ int sh_count[WAVES];
+  __shared__ bool sh_last;
+  const int tid = threadIdx.x, wave = tid >> 6;
+  const int64_t row = a.first + (int64_t)(a.pieces > 1 ? blockIdx.x / (unsigned)a.pieces : blockIdx.x);
+  const int piece = a.pieces > 1 ? (int)(blockIdx.x % (unsigned)a.pieces) : 0;
   const int target = a.targets ? a.targets[row] : 0;
   if ((unsigned)target >= (unsigned)a.V) {
+    if (piece != 0) return;
     if (tid == 0) {
       if (a.logp) a.logp[row] = 0.0f;
       if (a.entropy) a.entropy[row] = 0.0f;
       if (a.lse) a.lse[row] = 0.0f;
     }
-    for (int k = tid; k < a.n_top; k += kLpThreads) {
+    for (int k = tid; k < a.n_top; k += kThreads) {
       a.top_ids[row * a.n_top + k] = -1;
       a.top_logp[row * a.n_top + k] = -INFINITY;
     }
     return;
   }
+  const char* x0 = (const char*)a.logits + (size_t)row * a.ld * (BF16 ? 2 : 4);
+  TopList top;
+  if constexpr (TOP) top.start(buf + wave * kBuf, a.n_top);
+
   Sums r{kLowest, 0.0f, 0.0f};
-  for (int j = tid; j < a.V; j += kLpThreads) r = add(r, load_lp<BF16>(a.logits, base + j), a.c);
+  const uint32_t vectors = (uint32_t)a.V / VEC, beg = (uint32_t)piece * a.piece_vectors;
+  const uint32_t end = min(vectors, beg + a.piece_vectors);
+  uint32_t at = beg;  // the workgroup's next vector
+  bool first = true;
+  for (; at + kTile * kThreads <= end; at += kTile * kThreads) {
+    float x[kTile * VEC];
 #pragma unroll
-  for (int o = 32; o >= 1; o >>= 1)
-    r = join(r, Sums{__shfl_xor(r.m, o, 64), __shfl_xor(r.s, o, 64), __shfl_xor(r.t, o, 64)}, a.c);
-  if (lane == 0) sh[wave] = r;
-  __syncthreads();
-  r = sh[0];
-  for (int w = 1; w < kLpThreads / 64; ++w) r = join(r, sh[w], a.c);
-  const float ls = kLn2 * log2f(r.s);
-  const bool none = r.s == 0.0f;
-  if (tid == 0) {
-    if (a.lse) a.lse[row] = r.m * a.inv_temperature + ls;
-    if (a.entropy) a.entropy[row] = none ? 0.0f : ls - r.t / r.s * a.inv_temperature;
-    if (a.logp)
-      a.logp[row] = none ? -INFINITY : (load_lp<BF16>(a.logits, base + target) - r.m) * a.inv_temperature - ls;
+    for (int u = 0; u < kTile; ++u) unpack<BF16>(load_vec<BF16>(x0, at + u * kThreads + tid), x + u * VEC);
+    add(r, x, a.c);
+    if constexpr (TOP) {
+      float most = x[0];
+#pragma unroll
+      for (int i = 1; i < kTile * VEC; ++i) most = fmaxf(most, x[i]);
+      if (first) top.first_threshold(most), first = false;
+      if (__any(most >= top.x)) {
+#pragma unroll
+        for (int i = 0; i < kTile * VEC; ++i)
+          top.offer(x[i], (int)((at + (i / VEC) * kThreads + tid) * VEC + i % VEC));
+      }
+    }
   }
-  float last = INFINITY;
-  int last_id = -1;
-  for (int k = 0; k < a.n_top; ++k) {
-    float v = -INFINITY;
-    int id = INT_MAX;
-    for (int j = tid; j < a.V; j += kLpThreads) {
-      const float x = load_lp<BF16>(a.logits, base + j);
-      if (x > -INFINITY && better(last, last_id, x, j) && better(x, j, v, id)) v = x, id = j;
+  for (; at < end; at += kThreads) {
+    float x[VEC];
+    const bool in = at + tid < end;
+    if (in) {
+      unpack<BF16>(load_vec<BF16>(x0, at + tid), x);
+      add(r, x, a.c);
     }
+    if constexpr (TOP) {
+      float most = in ? x[0] : -INFINITY;
 #pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) {
-      const float w = __shfl_xor(v, o, 64);
-      const int jd = __shfl_xor(id, o, 64);
-      if (better(w, jd, v, id)) v = w, id = jd;
+      for (int i = 1; i < VEC; ++i) most = in ? fmaxf(most, x[i]) : most;
+      if (first) top.first_threshold(most), first = false;
+      if (__any(most >= top.x)) {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) top.offer(in ? x[i] : -INFINITY, (int)((at + tid) * VEC + i));
+      }
     }
-    __syncthreads();
-    if (lane == 0) sh_v[wave] = v, sh_i[wave] = id;
-    __syncthreads();
-    v = sh_v[0], id = sh_i[0];
-    for (int w = 1; w < kLpThreads / 64; ++w)
-      if (better(sh_v[w], sh_i[w], v, id)) v = sh_v[w], id = sh_i[w];
+  }
+  if (end == vectors) {  // what is left of the row, less than a vector
+    const uint32_t id = vectors * VEC + tid;
+    const bool in = id < (uint32_t)a.V;
+    float x[1] = {-INFINITY};
+    if (in) {
+      x[0] = load_lp<BF16>(x0, id);
+      add(r, x, a.c);
+    }
+    if constexpr (TOP) top.offer(x[0], (int)id);
+  }
+  r = join_block<WAVES>(r, sh, a.c);
+
+  if (a.pieces > 1) {
+    const int64_t me = row * a.pieces + piece;
+    auto keep = [](void* p, uint32_t v) {
+      __hip_atomic_store((uint32_t*)p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    };
+    auto fetch = [](const void* p) {
+      return __hip_atomic_load((const uint32_t*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    };
+    if constexpr (TOP) {
+      Candidate* mine = a.part_top + me * a.n_top;
+      const int got = rank_block<WAVES>(top, buf, sh_count, [&](int k, Candidate e) {
+        keep(&mine[k].x, __float_as_uint(e.x));
+        keep(&mine[k].id, (uint32_t)e.id);
+      });
+      for (int k = got + tid; k < a.n_top; k += kThreads) {
+        keep(&mine[k].x, __float_as_uint(-INFINITY));
+        keep(&mine[k].id, (uint32_t)INT_MAX);
+      }
+    }
     if (tid == 0) {
-      const bool left = id == INT_MAX;
-      a.top_ids[row * a.n_top + k] = left ? -1 : id;
-      a.top_logp[row * a.n_top + k] = left ? -INFINITY : (v - r.m) * a.inv_temperature - ls;
+      keep(&a.part[me].r.m, __float_as_uint(r.m));
+      keep(&a.part[me].r.s, __float_as_uint(r.s));
+      keep(&a.part[me].r.t, __float_as_uint(r.t));
     }
-    last = v, last_id = id;
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): this wavefront's part has reached memory
+    __syncthreads();
+    if (tid == 0) sh_last = atomicAdd(a.ticket + row, 1u) == (unsigned)a.pieces - 1;
+    __syncthreads();
+    if (!sh_last) return;
+    // every piece's part is in memory: join them
+    r = Sums{kLowest, 0.0f, 0.0f};
+    if (tid < a.pieces) {
+      const LpPiece* p = a.part + row * a.pieces + tid;
+      r = Sums{__uint_as_float(fetch(&p->r.m)), __uint_as_float(fetch(&p->r.s)), __uint_as_float(fetch(&p->r.t))};
+    }
+    if constexpr (TOP) {
+      const Candidate* p = a.part_top + row * a.pieces * a.n_top;
+      const int n = a.pieces * a.n_top;
+      Candidate e[kJoin];
+      float most = -INFINITY;
+#pragma unroll
+      for (int q = 0; q < kJoin; ++q) {
+        const int i = tid + q * kThreads;
+        e[q] = Candidate{-INFINITY, INT_MAX};
+        if (i < n) e[q] = Candidate{__uint_as_float(fetch(&p[i].x)), (int32_t)fetch(&p[i].id)};
+        most = fmaxf(most, e[q].x);
+      }
+      top.start(buf + wave * kBuf, a.n_top);
+      top.first_threshold(most);
+#pragma unroll
+      for (int q = 0; q < kJoin; ++q) top.offer(e[q].x, e[q].id);
+    }
+    r = join_block<WAVES>(r, sh, a.c);
+    if (tid == 0) __hip_atomic_store(a.ticket + row, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+
+  const bool none = r.s == 0.0f;  // nothing but -inf
+  const float mc = r.m * a.c, ls = __builtin_amdgcn_logf(r.s);
+  // log2 of the probability of a logit x
+  auto lp = [&](float x) { return (huge(mc) ? (x - r.m) * a.c : fmaf(x, a.c, -mc)) - ls; };
+  if (tid == 0) {
+    if (a.lse) a.lse[row] = huge(mc) ? r.m * a.inv_temperature + kLn2 * ls : kLn2 * (mc + ls);
+    if (a.entropy) a.entropy[row] = none ? 0.0f : kLn2 * (ls - r.t / r.s);
+    if (a.logp) a.logp[row] = none ? -INFINITY : kLn2 * lp(load_lp<BF16>(x0, target));
+  }
+  if constexpr (TOP) {
+    const int got = rank_block<WAVES>(top, buf, sh_count, [&](int k, Candidate e) {
+      a.top_ids[row * a.n_top + k] = e.id;
+      a.top_logp[row * a.n_top + k] = kLn2 * lp(e.x);
+    });
+    for (int k = got + tid; k < a.n_top; k += kThreads) {
+      a.top_ids[row * a.n_top + k] = -1;
+      a.top_logp[row * a.n_top + k] = -INFINITY;
+    }
+  }
+}
+
+constexpr size_t kLpTicketBytes = sizeof(uint32_t) * kMaxSplit;
+constexpr size_t kLpPartBytes = sizeof(LpPiece) * kMaxSplit;
+constexpr size_t kLpWsBytes = kLpTicketBytes + kLpPartBytes + sizeof(Candidate) * FOREMOE_MAX_TOP * kMaxSplit;
+
+template <bool BF16, bool TOP>
+void launch_logprobs(LogprobArgs a, int64_t N, int waves, hipStream_t st) {
+  // a launch has fewer than 2^32 threads
+  constexpr int64_t kRows = 1 << 22;
+  for (int64_t r = 0; r < N; r += kRows) {
+    a.first = (int32_t)r;
+    const dim3 grid((unsigned)((N - r < kRows ? N - r : kRows) * a.pieces));
+    if (waves == 1)
+      hipLaunchKernelGGL((logprobs_kernel<BF16, TOP, 1>), grid, dim3(64), 0, st, a);
+    else
+      hipLaunchKernelGGL((logprobs_kernel<BF16, TOP, kLpThreads / 64>), grid, dim3(kLpThreads), 0, st, a);
   }
 }
 
@@ -173,8 +489,6 @@ __global__ __launch_bounds__(kLpThreads) void logprobs_bwd_kernel(LogprobBwdArgs
       ((float*)a.dlogits)[row * a.ld_out + j] = d;
   }
 }
-
-constexpr size_t kLpWsBytes = 256;
 
 }  // namespace
 }  // namespace foremoe
@@ -218,13 +532,35 @@ int foremoe_token_logprobs(const void* logits, foremoe_dtype dtype, int64_t ld, 
     REQUIRE(ws_bytes >= kLpWsBytes, "token_logprobs: workspace too small (%zu < %zu)", ws_bytes, kLpWsBytes);
   }
   if (N == 0) return FOREMOE_OK;
-  LogprobArgs a{logits, ld, (int32_t)N, (int32_t)V, targets, kLog2e / temperature, 1.0f / temperature, n_top, logp, entropy, lse, top_ids,
-                top_logp};
+  const int vec = dtype == FOREMOE_BF16 ? kVec<true> : kVec<false>;
+  const int64_t vectors = V / vec;
+  // a wavefront where a row has no more than two vectors for each lane of it,
+  // else a workgroup; rows that do not fill the GPU in as many pieces as do,
+  // of at least a vector for every thread
+  const int waves = vectors <= 128 ? 1 : kLpThreads / 64;
+  int64_t pieces = 1;
+  if (ws && waves > 1) {
+    pieces = kMaxSplit / N;
+    if (pieces > kMaxPieces) pieces = kMaxPieces;
+    if (pieces > vectors / kLpThreads) pieces = vectors / kLpThreads;
+    if (pieces < 1) pieces = 1;
+  }
+  LogprobArgs a{};
+  a.logits = logits, a.ld = ld, a.V = (int32_t)V, a.targets = targets;
+  a.c = kLog2e / temperature, a.inv_temperature = 1.0f / temperature, a.n_top = n_top;
+  a.logp = logp, a.entropy = entropy, a.lse = lse, a.top_ids = top_ids, a.top_logp = top_logp;
+  const int64_t per = (vectors + pieces - 1) / pieces;
+  a.piece_vectors = (int32_t)((per + kLpThreads - 1) / kLpThreads * kLpThreads);
+  if (pieces > 1) pieces = (vectors + a.piece_vectors - 1) / a.piece_vectors;
+  a.pieces = (int32_t)pieces;
+  a.ticket = (uint32_t*)ws;
+  a.part = (LpPiece*)((char*)ws + kLpTicketBytes);
+  a.part_top = (Candidate*)((char*)ws + kLpTicketBytes + kLpPartBytes);
   hipStream_t st = (hipStream_t)stream;
   if (dtype == FOREMOE_BF16)
-    hipLaunchKernelGGL(logprobs_kernel<true>, dim3((unsigned)N), dim3(kLpThreads), 0, st, a);
+    n_top ? launch_logprobs<true, true>(a, N, waves, st) : launch_logprobs<true, false>(a, N, waves, st);
   else
-    hipLaunchKernelGGL(logprobs_kernel<false>, dim3((unsigned)N), dim3(kLpThreads), 0, st, a);
+    n_top ? launch_logprobs<false, true>(a, N, waves, st) : launch_logprobs<false, false>(a, N, waves, st);
   return check_launch("token_logprobs");
 }
 
