@@ -26,13 +26,10 @@ constexpr int kBuf = 512;     // candidates for the top places that a wavefront 
 constexpr int kMaxPieces = 64;     // of one row
 constexpr int kMaxSplit = 1024;    // pieces of all rows
 constexpr int kJoin = kMaxPieces * FOREMOE_MAX_TOP / kLpThreads;  // candidates a lane takes when pieces are joined
+static_assert(kJoin * 64 <= kBuf);
 
 struct Sums {
   float m, s, t;
-};
-struct Candidate {
-  float x;
-  int32_t id;
 };
 struct LpPiece {  // what a piece of a row leaves for the join
   Sums r;
@@ -52,7 +49,7 @@ struct LogprobArgs {
   int32_t pieces, piece_vectors;
   uint32_t* ticket;     // [N]
   LpPiece* part;        // [N, pieces]
-  Candidate* part_top;  // [N, pieces, n_top]
+  uint64_t* part_top;   // [N, pieces, n_top]
 };
 
 template <bool BF16>
@@ -142,134 +139,139 @@ __device__ __forceinline__ void add(Sums& a, const float (&x)[n], float c) {
   a.t += t[0];
 }
 
-__device__ __forceinline__ bool better(float v, int id, float w, int jd) { return v > w || (v == w && id < jd); }
+// A logit and its id as one integer in the order of the top places: larger
+// logits first, among equals (0.0 and -0.0 too) the lower id. 0 for a NaN and
+// -inf, which have no place.
+__device__ __forceinline__ uint64_t place_key(float x, uint32_t id) {
+  const uint32_t b = __float_as_uint(x + 0.0f);
+  const uint32_t o = b ^ (b >> 31 ? 0xffffffffu : 0x80000000u);
+  return x > -INFINITY ? (uint64_t)o << 32 | (uint32_t)~id : 0;
+}
+__device__ __forceinline__ float key_logit(uint64_t k) {
+  const uint32_t o = (uint32_t)(k >> 32);
+  return __uint_as_float(o ^ (o >> 31 ? 0x80000000u : 0xffffffffu));
+}
+__device__ __forceinline__ int32_t key_id(uint64_t k) { return (int32_t)~(uint32_t)k; }
 
-// The candidates of a wavefront for the n top places: everything it has seen
-// that is not behind its threshold (an element with at least n - 1 before it,
-// itself a candidate), in any order.
+// The n-th largest of the lanes' values, bit by bit.
+__device__ __forceinline__ uint32_t nth_largest(uint32_t value, int n) {
+  uint32_t k = 0;
+#pragma unroll 1
+  for (uint32_t bit = 1u << 31; bit; bit >>= 1)
+    if (__popcll(__ballot(value >= (k | bit))) >= n) k |= bit;
+  return k;
+}
+
+// The candidates of a wavefront for the n top places: every element it has
+// seen whose key is at least its threshold, in any order.
 //
-// The threshold is the n-th largest of 64 lanes' own maxima, which n lanes
-// reach: of the first elements, then of the kept candidates whenever the
-// buffer is full. A lane holds at most kBuf / 64 = 8 candidates then, so at
-// most 8 n <= 256 pass, and a ballot's 64 always fit behind them.
+// The threshold is the n-th largest of the 64 lanes' own maxima, so n
+// elements reach it: of the first elements, then of the kept candidates
+// whenever the buffer is full. A lane holds kBuf / 64 = 8 candidates then, so
+// at most 8 n <= 256 of them pass, and a ballot's 64 always fit behind them.
 struct TopList {
-  Candidate* buf;  // [kBuf] in LDS
+  uint64_t* buf;  // [kBuf] in LDS
   int n, count;
-  float x;  // threshold
-  int id;
+  uint64_t least;  // the threshold, > 0
+  float x;         // its logit
 
-  __device__ __forceinline__ void start(Candidate* b, int places) {
-    buf = b, n = places, count = 0, x = -INFINITY, id = -1;
+  __device__ __forceinline__ void start(uint64_t* b, int places) {
+    buf = b, n = places, count = 0, least = 1, x = -INFINITY;
   }
-  // an integer in the order of the floats, NaN lowest (0.0 and -0.0 alike)
-  static __device__ __forceinline__ uint32_t ordered(float v) {
-    if (!(v >= -INFINITY)) return 0;
-    const uint32_t b = __float_as_uint(v + 0.0f);
-    return b ^ (b >> 31 ? 0xffffffffu : 0x80000000u);
-  }
-  static __device__ __forceinline__ float of_ordered(uint32_t k) {
-    return __uint_as_float(k ^ (k >> 31 ? 0x80000000u : 0xffffffffu));
-  }
-  // The n-th largest of the lanes' keys.
-  __device__ __forceinline__ uint32_t nth(uint32_t key, int nth) const {
-    uint32_t k = 0;
-#pragma unroll
-    for (int bit = 31; bit >= 0; --bit) {
-      const uint32_t test = k | (1u << bit);
-      if (__popcll(__ballot(key >= test)) >= nth) k = test;
-    }
-    return k;
-  }
-  // Before anything is added: the lanes' largest elements so far.
+  // Before anything is offered: the lanes' largest elements so far.
   __device__ __forceinline__ void first_threshold(float lane_max) {
-    const float v = of_ordered(max(nth(ordered(lane_max), n), ordered(-INFINITY)));
-    if (v > x) x = v, id = INT_MAX;
+    const uint32_t o = nth_largest((uint32_t)(place_key(lane_max, 0) >> 32), n);
+    if (o) least = (uint64_t)o << 32, x = key_logit(least);
   }
-  __device__ __forceinline__ bool passes(float v, int i) const { return v > x || (v == x && i <= id); }
   __device__ __forceinline__ void fence() const {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
   }
-  __device__ __forceinline__ void put(float v, int i, bool pass) {
+  __device__ __forceinline__ void put(uint64_t key) {
+    const bool pass = key >= least;
     const uint64_t mask = __ballot(pass);
-    if (pass) buf[count + lanes_below(mask)] = Candidate{v, i};
+    if (pass) buf[count + lanes_below(mask)] = key;
     count += __popcll(mask);
   }
   __device__ __forceinline__ void prune() {
     const int lane = lane_id();
     fence();
-    Candidate e[kBuf / 64], best{-INFINITY, INT_MAX};
+    uint64_t e[kBuf / 64], best = 0;
 #pragma unroll
     for (int q = 0; q < kBuf / 64; ++q) {
       const int at = lane + 64 * q;
-      e[q] = at < count ? buf[at] : Candidate{-INFINITY, INT_MAX};
-      if (better(e[q].x, e[q].id, best.x, best.id)) best = e[q];
+      e[q] = at < count ? buf[at] : 0;
+      best = e[q] > best ? e[q] : best;
     }
-    const uint32_t key = ordered(best.x), k = nth(key, n);
-    const int above = __popcll(__ballot(key > k));
-    // of the lanes that are equal, those with the lowest ids
-    const bool equal = key == k;
-    int last = INT_MAX;
-    if (__popcll(__ballot(equal)) > n - above)
-      last = (int)~nth(equal ? ~(uint32_t)best.id : 0u, n - above);
-    const float v = of_ordered(max(k, ordered(-INFINITY)));
-    if (better(v, last, x, id)) x = v, id = last;
+    const uint32_t hi = (uint32_t)(best >> 32), o = nth_largest(hi, n);
+    const uint32_t lo = nth_largest(hi == o ? (uint32_t)best : 0, n - __popcll(__ballot(hi > o)));
+    const uint64_t t = (uint64_t)o << 32 | lo;
+    if (t > least) least = t, x = key_logit(t);
     fence();
     count = 0;
 #pragma unroll
-    for (int q = 0; q < kBuf / 64; ++q) put(e[q].x, e[q].id, e[q].x > -INFINITY && passes(e[q].x, e[q].id));
+    for (int q = 0; q < kBuf / 64; ++q) put(e[q]);
     fence();
   }
-  // All lanes of the wavefront together; x -inf where a lane has nothing.
-  __device__ __forceinline__ void offer(float v, int i) {
-    bool pass = passes(v, i);
-    if (!__any(pass)) return;
-    if (count + __popcll(__ballot(pass)) > kBuf) {
-      prune();
-      pass = passes(v, i);
+  // The elements whose bit is set in `mine`; key(bit) gives one's key. All
+  // lanes of the wavefront together.
+  template <class Key>
+  __device__ __forceinline__ void offer(uint32_t mine, Key&& key) {
+    while (__any(mine != 0)) {
+      const uint64_t k = mine ? key(__builtin_ctz(mine)) : 0;
+      mine &= mine - 1;
+      if (count + __popcll(__ballot(k >= least)) > kBuf) prune();
+      put(k);
     }
-    put(v, i, pass);
   }
 };
 
 // Sums of the workgroup, in every thread; the order of the joins is fixed.
 template <int WAVES>
 __device__ __forceinline__ Sums join_block(Sums r, Sums* sh, float c) {
-#pragma unroll
+#pragma unroll 1
   for (int o = 32; o >= 1; o >>= 1)
     r = join(r, Sums{__shfl_xor(r.m, o, 64), __shfl_xor(r.s, o, 64), __shfl_xor(r.t, o, 64)}, c);
   if constexpr (WAVES > 1) {
     if (lane_id() == 0) sh[threadIdx.x >> 6] = r;
     __syncthreads();
     r = sh[0];
-#pragma unroll
+#pragma unroll 1
     for (int w = 1; w < WAVES; ++w) r = join(r, sh[w], c);
   }
   return r;
 }
 
-// The workgroup's candidates by rank: out(place, candidate) for the places
-// below n, and how many there are.
+// The workgroup's candidates by rank: out(place, key) for the places below n,
+// and how many there are.
 template <int WAVES, class Out>
-__device__ __forceinline__ int rank_block(TopList& top, const Candidate* buf, int* sh_count, Out&& out) {
+__device__ __forceinline__ int rank_block(TopList& top, const uint64_t* buf, int* sh_count, Out&& out) {
   if (top.count > 64) top.prune();
+  // filled up to a multiple of 4 with keys that rank behind every other
+  if (lane_id() < 3 && top.count + lane_id() < kBuf) top.buf[top.count + lane_id()] = 0;
   if (lane_id() == 0) sh_count[threadIdx.x >> 6] = top.count;
   if constexpr (WAVES > 1) __syncthreads();
   else top.fence();
   int all = 0;
+#pragma unroll 1
   for (int w = 0; w < WAVES; ++w) {
     const int cw = sh_count[w];
+#pragma unroll 1
     for (int j0 = 0; j0 < cw; j0 += 64 * WAVES) {
       const int j = j0 + threadIdx.x;
       if (j >= cw) continue;
-      const Candidate me = buf[w * kBuf + j];
+      const uint64_t me = buf[w * kBuf + j];
       int rank = 0;
-      for (int q = 0; q < WAVES; ++q)
-        for (int i = 0; i < sh_count[q]; ++i) {
-          const Candidate o = buf[q * kBuf + i];
-          rank += better(o.x, o.id, me.x, me.id);
+#pragma unroll 1
+      for (int q = 0; q < WAVES; ++q) {
+        const int cq = sh_count[q];
+#pragma unroll 1
+        for (int i = 0; i < cq; i += 4) {
+          const uint64_t* o = buf + q * kBuf + i;
+          rank += (o[0] > me) + (o[1] > me) + (o[2] > me) + (o[3] > me);
         }
+      }
       if (rank < top.n) out(rank, me);
     }
     all += cw;
@@ -282,7 +284,7 @@ __device__ __forceinline__ int rank_block(TopList& top, const Candidate* buf, in
 template <bool BF16, bool TOP, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void logprobs_kernel(LogprobArgs a) {
   constexpr int kThreads = 64 * WAVES, VEC = kVec<BF16>;
-  __shared__ Candidate buf[TOP ? WAVES * kBuf : 1];
+  __shared__ uint64_t buf[TOP ? WAVES * kBuf : 1];
   __shared__ Sums sh[WAVES];
   __shared__ int sh_count[WAVES];
   __shared__ bool sh_last;
@@ -310,78 +312,70 @@ __global__ __launch_bounds__(64 * WAVES) void logprobs_kernel(LogprobArgs a) {
   Sums r{kLowest, 0.0f, 0.0f};
   const uint32_t vectors = (uint32_t)a.V / VEC, beg = (uint32_t)piece * a.piece_vectors;
   const uint32_t end = min(vectors, beg + a.piece_vectors);
-  uint32_t at = beg;  // the workgroup's next vector
+  if (end == vectors) {  // the row's last elements, less than a vector
+    const uint32_t id = vectors * VEC + tid;
+    float x[1] = {-INFINITY};
+    if (id < (uint32_t)a.V) {
+      x[0] = load_lp<BF16>(x0, id);
+      add(r, x, a.c);
+    }
+    if constexpr (TOP) top.put(place_key(x[0], id));
+  }
   bool first = true;
-  for (; at + kTile * kThreads <= end; at += kTile * kThreads) {
+  for (uint32_t at = beg; at < end; at += kTile * kThreads) {
     float x[kTile * VEC];
+    uint32_t there = ~0u;  // a bit for every element held
+    if (at + kTile * kThreads <= end) {
 #pragma unroll
-    for (int u = 0; u < kTile; ++u) unpack<BF16>(load_vec<BF16>(x0, at + u * kThreads + tid), x + u * VEC);
-    add(r, x, a.c);
+      for (int u = 0; u < kTile; ++u) unpack<BF16>(load_vec<BF16>(x0, at + u * kThreads + tid), x + u * VEC);
+      add(r, x, a.c);
+    } else {
+#pragma unroll
+      for (int u = 0; u < kTile; ++u) {
+        if (at + u * kThreads + tid < end) {
+          float y[VEC];
+          unpack<BF16>(load_vec<BF16>(x0, at + u * kThreads + tid), y);
+          add(r, y, a.c);
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) x[u * VEC + i] = y[i];
+        } else if constexpr (TOP) {
+          there &= ~(((1u << VEC) - 1) << (u * VEC));
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) x[u * VEC + i] = -INFINITY;
+        }
+      }
+    }
     if constexpr (TOP) {
       float most = x[0];
 #pragma unroll
       for (int i = 1; i < kTile * VEC; ++i) most = fmaxf(most, x[i]);
       if (first) top.first_threshold(most), first = false;
       if (__any(most >= top.x)) {
+        uint32_t mine = 0;
 #pragma unroll
-        for (int i = 0; i < kTile * VEC; ++i)
-          top.offer(x[i], (int)((at + (i / VEC) * kThreads + tid) * VEC + i % VEC));
+        for (int i = 0; i < kTile * VEC; ++i) mine |= x[i] >= top.x ? 1u << i : 0u;
+        top.offer(mine & there, [&](int i) {
+          const uint32_t id = (at + (i / VEC) * kThreads + tid) * VEC + i % VEC;
+          return place_key(load_lp<BF16>(x0, id), id);
+        });
       }
     }
-  }
-  for (; at < end; at += kThreads) {
-    float x[VEC];
-    const bool in = at + tid < end;
-    if (in) {
-      unpack<BF16>(load_vec<BF16>(x0, at + tid), x);
-      add(r, x, a.c);
-    }
-    if constexpr (TOP) {
-      float most = in ? x[0] : -INFINITY;
-#pragma unroll
-      for (int i = 1; i < VEC; ++i) most = in ? fmaxf(most, x[i]) : most;
-      if (first) top.first_threshold(most), first = false;
-      if (__any(most >= top.x)) {
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) top.offer(in ? x[i] : -INFINITY, (int)((at + tid) * VEC + i));
-      }
-    }
-  }
-  if (end == vectors) {  // what is left of the row, less than a vector
-    const uint32_t id = vectors * VEC + tid;
-    const bool in = id < (uint32_t)a.V;
-    float x[1] = {-INFINITY};
-    if (in) {
-      x[0] = load_lp<BF16>(x0, id);
-      add(r, x, a.c);
-    }
-    if constexpr (TOP) top.offer(x[0], (int)id);
   }
   r = join_block<WAVES>(r, sh, a.c);
 
   if (a.pieces > 1) {
     const int64_t me = row * a.pieces + piece;
-    auto keep = [](void* p, uint32_t v) {
-      __hip_atomic_store((uint32_t*)p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    };
-    auto fetch = [](const void* p) {
-      return __hip_atomic_load((const uint32_t*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    };
+    auto keep = [](auto* p, auto v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
+    auto fetch = [](const auto* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
     if constexpr (TOP) {
-      Candidate* mine = a.part_top + me * a.n_top;
-      const int got = rank_block<WAVES>(top, buf, sh_count, [&](int k, Candidate e) {
-        keep(&mine[k].x, __float_as_uint(e.x));
-        keep(&mine[k].id, (uint32_t)e.id);
-      });
-      for (int k = got + tid; k < a.n_top; k += kThreads) {
-        keep(&mine[k].x, __float_as_uint(-INFINITY));
-        keep(&mine[k].id, (uint32_t)INT_MAX);
-      }
+      uint64_t* mine = a.part_top + me * a.n_top;
+      const int got = rank_block<WAVES>(top, buf, sh_count, [&](int k, uint64_t key) { keep(&mine[k], key); });
+      for (int k = got + tid; k < a.n_top; k += kThreads) keep(&mine[k], (uint64_t)0);
     }
     if (tid == 0) {
-      keep(&a.part[me].r.m, __float_as_uint(r.m));
-      keep(&a.part[me].r.s, __float_as_uint(r.s));
-      keep(&a.part[me].r.t, __float_as_uint(r.t));
+      keep(&a.part[me].r.m, r.m);
+      keep(&a.part[me].r.s, r.s);
+      keep(&a.part[me].r.t, r.t);
     }
     __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): this wavefront's part has reached memory
     __syncthreads();
@@ -392,24 +386,22 @@ __global__ __launch_bounds__(64 * WAVES) void logprobs_kernel(LogprobArgs a) {
     r = Sums{kLowest, 0.0f, 0.0f};
     if (tid < a.pieces) {
       const LpPiece* p = a.part + row * a.pieces + tid;
-      r = Sums{__uint_as_float(fetch(&p->r.m)), __uint_as_float(fetch(&p->r.s)), __uint_as_float(fetch(&p->r.t))};
+      r = Sums{fetch(&p->r.m), fetch(&p->r.s), fetch(&p->r.t)};
     }
     if constexpr (TOP) {
-      const Candidate* p = a.part_top + row * a.pieces * a.n_top;
+      const uint64_t* p = a.part_top + row * a.pieces * a.n_top;
       const int n = a.pieces * a.n_top;
-      Candidate e[kJoin];
-      float most = -INFINITY;
+      uint64_t e[kJoin], best = 0;
 #pragma unroll
       for (int q = 0; q < kJoin; ++q) {
-        const int i = tid + q * kThreads;
-        e[q] = Candidate{-INFINITY, INT_MAX};
-        if (i < n) e[q] = Candidate{__uint_as_float(fetch(&p[i].x)), (int32_t)fetch(&p[i].id)};
-        most = fmaxf(most, e[q].x);
+        e[q] = tid + q * kThreads < n ? fetch(p + tid + q * kThreads) : 0;
+        best = e[q] > best ? e[q] : best;
       }
       top.start(buf + wave * kBuf, a.n_top);
-      top.first_threshold(most);
+      const uint32_t o = nth_largest((uint32_t)(best >> 32), a.n_top);
+      if (o) top.least = (uint64_t)o << 32;
 #pragma unroll
-      for (int q = 0; q < kJoin; ++q) top.offer(e[q].x, e[q].id);
+      for (int q = 0; q < kJoin; ++q) top.put(e[q]);  // kJoin x 64: they all fit
     }
     r = join_block<WAVES>(r, sh, a.c);
     if (tid == 0) __hip_atomic_store(a.ticket + row, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -425,9 +417,9 @@ __global__ __launch_bounds__(64 * WAVES) void logprobs_kernel(LogprobArgs a) {
     if (a.logp) a.logp[row] = none ? -INFINITY : kLn2 * lp(load_lp<BF16>(x0, target));
   }
   if constexpr (TOP) {
-    const int got = rank_block<WAVES>(top, buf, sh_count, [&](int k, Candidate e) {
-      a.top_ids[row * a.n_top + k] = e.id;
-      a.top_logp[row * a.n_top + k] = kLn2 * lp(e.x);
+    const int got = rank_block<WAVES>(top, buf, sh_count, [&](int k, uint64_t key) {
+      a.top_ids[row * a.n_top + k] = key_id(key);
+      a.top_logp[row * a.n_top + k] = kLn2 * lp(key_logit(key));
     });
     for (int k = got + tid; k < a.n_top; k += kThreads) {
       a.top_ids[row * a.n_top + k] = -1;
@@ -438,7 +430,7 @@ __global__ __launch_bounds__(64 * WAVES) void logprobs_kernel(LogprobArgs a) {
 
 constexpr size_t kLpTicketBytes = sizeof(uint32_t) * kMaxSplit;
 constexpr size_t kLpPartBytes = sizeof(LpPiece) * kMaxSplit;
-constexpr size_t kLpWsBytes = kLpTicketBytes + kLpPartBytes + sizeof(Candidate) * FOREMOE_MAX_TOP * kMaxSplit;
+constexpr size_t kLpWsBytes = kLpTicketBytes + kLpPartBytes + sizeof(uint64_t) * FOREMOE_MAX_TOP * kMaxSplit;
 
 template <bool BF16, bool TOP>
 void launch_logprobs(LogprobArgs a, int64_t N, int waves, hipStream_t st) {
@@ -555,7 +547,7 @@ int foremoe_token_logprobs(const void* logits, foremoe_dtype dtype, int64_t ld, 
   a.pieces = (int32_t)pieces;
   a.ticket = (uint32_t*)ws;
   a.part = (LpPiece*)((char*)ws + kLpTicketBytes);
-  a.part_top = (Candidate*)((char*)ws + kLpTicketBytes + kLpPartBytes);
+  a.part_top = (uint64_t*)((char*)ws + kLpTicketBytes + kLpPartBytes);
   hipStream_t st = (hipStream_t)stream;
   if (dtype == FOREMOE_BF16)
     n_top ? launch_logprobs<true, true>(a, N, waves, st) : launch_logprobs<true, false>(a, N, waves, st);
