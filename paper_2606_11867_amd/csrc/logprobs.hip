@@ -21,7 +21,6 @@ constexpr int kLpThreads = 256;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLowest = -3.402823466e38f;
-constexpr int kTile = 4;      // vectors that a lane holds at a time
 constexpr int kBuf = 512;     // candidates for the top places that a wavefront keeps
 constexpr int kMaxPieces = 64;     // of one row
 constexpr int kMaxSplit = 1024;    // pieces of all rows
@@ -244,44 +243,41 @@ __device__ __forceinline__ Sums join_block(Sums r, Sums* sh, float c) {
 }
 
 // The workgroup's candidates by rank: out(place, key) for the places below n,
-// and how many there are.
+// and how many there are. A thread counts what is before its candidate.
 template <int WAVES, class Out>
 __device__ __forceinline__ int rank_block(TopList& top, const uint64_t* buf, int* sh_count, Out&& out) {
+  constexpr int kStep = 8;
   if (top.count > 64) top.prune();
-  // filled up to a multiple of 4 with keys that rank behind every other
-  if (lane_id() < 3 && top.count + lane_id() < kBuf) top.buf[top.count + lane_id()] = 0;
+  // filled up to a multiple of kStep with keys that are behind every other
+  if (lane_id() < kStep && top.count + lane_id() < kBuf) top.buf[top.count + lane_id()] = 0;
   if (lane_id() == 0) sh_count[threadIdx.x >> 6] = top.count;
   if constexpr (WAVES > 1) __syncthreads();
   else top.fence();
   int all = 0;
+  for (int w = 0; w < WAVES; ++w) all += sh_count[w];
 #pragma unroll 1
-  for (int w = 0; w < WAVES; ++w) {
-    const int cw = sh_count[w];
+  for (int j = threadIdx.x; j < all; j += 64 * WAVES) {
+    int w = 0, i = j;
+    while (i >= sh_count[w]) i -= sh_count[w++];
+    const uint64_t me = buf[w * kBuf + i];
+    int rank = 0;
 #pragma unroll 1
-    for (int j0 = 0; j0 < cw; j0 += 64 * WAVES) {
-      const int j = j0 + threadIdx.x;
-      if (j >= cw) continue;
-      const uint64_t me = buf[w * kBuf + j];
-      int rank = 0;
+    for (int q = 0; q < WAVES; ++q) {
+      const int cq = sh_count[q];
 #pragma unroll 1
-      for (int q = 0; q < WAVES; ++q) {
-        const int cq = sh_count[q];
-#pragma unroll 1
-        for (int i = 0; i < cq; i += 4) {
-          const uint64_t* o = buf + q * kBuf + i;
-          rank += (o[0] > me) + (o[1] > me) + (o[2] > me) + (o[3] > me);
-        }
+      for (int o = 0; o < cq; o += kStep) {
+#pragma unroll
+        for (int z = 0; z < kStep; ++z) rank += buf[q * kBuf + o + z] > me;
       }
-      if (rank < top.n) out(rank, me);
     }
-    all += cw;
+    if (rank < top.n) out(rank, me);
   }
   return min(all, top.n);
 }
 
 // A workgroup of WAVES wavefronts takes a piece of a row; where a row has
 // several, the last one to finish joins them.
-template <bool BF16, bool TOP, int WAVES>
+template <bool BF16, bool TOP, int WAVES, int TILE>
 __global__ __launch_bounds__(64 * WAVES) void logprobs_kernel(LogprobArgs a) {
   constexpr int kThreads = 64 * WAVES, VEC = kVec<BF16>;
   __shared__ uint64_t buf[TOP ? WAVES * kBuf : 1];
@@ -322,44 +318,42 @@ __global__ __launch_bounds__(64 * WAVES) void logprobs_kernel(LogprobArgs a) {
     if constexpr (TOP) top.put(place_key(x[0], id));
   }
   bool first = true;
-  for (uint32_t at = beg; at < end; at += kTile * kThreads) {
-    float x[kTile * VEC];
-    uint32_t there = ~0u;  // a bit for every element held
-    if (at + kTile * kThreads <= end) {
+  uint32_t at = beg;  // the workgroup's next vector
+  // a lane's elements x, of the vectors at, at + kThreads, ...
+  auto consider = [&](auto& x, bool in) {
+    constexpr int n = sizeof(x) / sizeof(float);
+    float most = x[0];
 #pragma unroll
-      for (int u = 0; u < kTile; ++u) unpack<BF16>(load_vec<BF16>(x0, at + u * kThreads + tid), x + u * VEC);
+    for (int i = 1; i < n; ++i) most = fmaxf(most, x[i]);
+    most = in ? most : -INFINITY;
+    if (first) top.first_threshold(most), first = false;
+    if (__any(most >= top.x)) {
+      uint32_t mine = 0;
+#pragma unroll
+      for (int i = 0; i < n; ++i) mine |= x[i] >= top.x ? 1u << i : 0u;
+      top.offer(in ? mine : 0, [&](int i) {
+        const uint32_t id = (at + (i / VEC) * kThreads + tid) * VEC + i % VEC;
+        return place_key(load_lp<BF16>(x0, id), id);
+      });
+    }
+  };
+  if constexpr (TILE > 1)
+    for (; at + TILE * kThreads <= end; at += TILE * kThreads) {
+      float x[TILE * VEC];
+#pragma unroll
+      for (int u = 0; u < TILE; ++u) unpack<BF16>(load_vec<BF16>(x0, at + u * kThreads + tid), x + u * VEC);
       add(r, x, a.c);
-    } else {
-#pragma unroll
-      for (int u = 0; u < kTile; ++u) {
-        if (at + u * kThreads + tid < end) {
-          float y[VEC];
-          unpack<BF16>(load_vec<BF16>(x0, at + u * kThreads + tid), y);
-          add(r, y, a.c);
-#pragma unroll
-          for (int i = 0; i < VEC; ++i) x[u * VEC + i] = y[i];
-        } else if constexpr (TOP) {
-          there &= ~(((1u << VEC) - 1) << (u * VEC));
-#pragma unroll
-          for (int i = 0; i < VEC; ++i) x[u * VEC + i] = -INFINITY;
-        }
-      }
+      if constexpr (TOP) consider(x, true);
     }
-    if constexpr (TOP) {
-      float most = x[0];
-#pragma unroll
-      for (int i = 1; i < kTile * VEC; ++i) most = fmaxf(most, x[i]);
-      if (first) top.first_threshold(most), first = false;
-      if (__any(most >= top.x)) {
-        uint32_t mine = 0;
-#pragma unroll
-        for (int i = 0; i < kTile * VEC; ++i) mine |= x[i] >= top.x ? 1u << i : 0u;
-        top.offer(mine & there, [&](int i) {
-          const uint32_t id = (at + (i / VEC) * kThreads + tid) * VEC + i % VEC;
-          return place_key(load_lp<BF16>(x0, id), id);
-        });
-      }
+#pragma unroll 1
+  for (; at < end; at += kThreads) {
+    float x[VEC];
+    const bool in = at + tid < end;
+    if (in) {
+      unpack<BF16>(load_vec<BF16>(x0, at + tid), x);
+      add(r, x, a.c);
     }
+    if constexpr (TOP) consider(x, in);
   }
   r = join_block<WAVES>(r, sh, a.c);
 
@@ -440,9 +434,11 @@ void launch_logprobs(LogprobArgs a, int64_t N, int waves, hipStream_t st) {
     a.first = (int32_t)r;
     const dim3 grid((unsigned)((N - r < kRows ? N - r : kRows) * a.pieces));
     if (waves == 1)
-      hipLaunchKernelGGL((logprobs_kernel<BF16, TOP, 1>), grid, dim3(64), 0, st, a);
+      hipLaunchKernelGGL((logprobs_kernel<BF16, TOP, 1, 1>), grid, dim3(64), 0, st, a);
+    else if (a.pieces > 1)
+      hipLaunchKernelGGL((logprobs_kernel<BF16, TOP, kLpThreads / 64, 1>), grid, dim3(kLpThreads), 0, st, a);
     else
-      hipLaunchKernelGGL((logprobs_kernel<BF16, TOP, kLpThreads / 64>), grid, dim3(kLpThreads), 0, st, a);
+      hipLaunchKernelGGL((logprobs_kernel<BF16, TOP, kLpThreads / 64, 4>), grid, dim3(kLpThreads), 0, st, a);
   }
 }
 
