@@ -21,9 +21,14 @@ constexpr int kLpThreads = 256;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLowest = -3.402823466e38f;
+constexpr int kTile = 4;           // vectors that a lane holds at a time
+constexpr int kBwdTile = 4;        // the same in the backward
 constexpr int kBuf = 512;     // candidates for the top places that a wavefront keeps
 constexpr int kMaxPieces = 64;     // of one row
-constexpr int kMaxSplit = 1024;    // pieces of all rows
+constexpr int kFewRows = 256;       // fewer rows than this are cut into pieces
+constexpr int kSplit = 512;         // and into about so many of all rows
+constexpr int kMaxSplit = kSplit + kFewRows;
+static_assert(kMaxSplit >= kMaxPieces * (kFewRows / kMaxPieces));
 constexpr int kJoin = kMaxPieces * FOREMOE_MAX_TOP / kLpThreads;  // candidates a lane takes when pieces are joined
 static_assert(kJoin * 64 <= kBuf);
 
@@ -107,29 +112,33 @@ __device__ __forceinline__ Sums join(Sums a, Sums b, float c) {
   return Sums{m, a.s + b.s, a.t + b.t};
 }
 
-// Adds n elements of one lane.
+// Adds n elements of one lane; with care where some may be -inf.
 template <int n>
-__device__ __forceinline__ void add(Sums& a, const float (&x)[n], float c) {
+__device__ __forceinline__ void add(Sums& a, const float (&x)[n], float c, bool care) {
   float top = x[0];
 #pragma unroll
   for (int i = 1; i < n; ++i) top = fmaxf(top, x[i]);
   if (top > a.m) rebase(a, top, c);
   const float mc = a.m * c;
   float s[2] = {0.0f, 0.0f}, t[2] = {0.0f, 0.0f};
-#pragma unroll
-  for (int i = 0; i < n; ++i) {
-    const float y = fmaf(x[i], c, -mc), e = __builtin_amdgcn_exp2f(y);
-    s[i & 1] += e;
-    t[i & 1] = fmaf(y, e, t[i & 1]);
-  }
-  s[0] += s[1];
-  t[0] += t[1];
-  // y 2^y of a y of -inf is a NaN above (a masked logit): once more with care
-  if (__builtin_expect(t[0] != t[0] || huge(mc), 0)) {
-    s[0] = t[0] = 0.0f;
+  if (!care) {
 #pragma unroll
     for (int i = 0; i < n; ++i) {
-      const float y = (x[i] - a.m) * c, e = __builtin_amdgcn_exp2f(y);
+      const float y = fmaf(x[i], c, -mc), e = __builtin_amdgcn_exp2f(y);
+      s[i & 1] += e;
+      t[i & 1] = fmaf(y, e, t[i & 1]);
+    }
+    s[0] += s[1];
+    t[0] += t[1];
+    // a y of -inf (a masked logit) makes a NaN of y 2^y
+    care = t[0] != t[0] || huge(mc);
+  }
+  if (care) {
+    s[0] = t[0] = 0.0f;
+    const bool far = huge(mc);
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+      const float y = far ? (x[i] - a.m) * c : fmaf(x[i], c, -mc), e = __builtin_amdgcn_exp2f(y);
       s[0] += e;
       t[0] += fmaxf(y, kLowest) * e;
     }
@@ -152,12 +161,16 @@ __device__ __forceinline__ float key_logit(uint64_t k) {
 }
 __device__ __forceinline__ int32_t key_id(uint64_t k) { return (int32_t)~(uint32_t)k; }
 
-// The n-th largest of the lanes' values, bit by bit.
+// A threshold that at least n lanes' values reach, bit by bit from the top:
+// the first that just n reach, or else the n-th largest value.
 __device__ __forceinline__ uint32_t nth_largest(uint32_t value, int n) {
   uint32_t k = 0;
 #pragma unroll 1
-  for (uint32_t bit = 1u << 31; bit; bit >>= 1)
-    if (__popcll(__ballot(value >= (k | bit))) >= n) k |= bit;
+  for (uint32_t bit = 1u << 31; bit; bit >>= 1) {
+    const int reach = __popcll(__ballot(value >= (k | bit)));
+    if (reach >= n) k |= bit;
+    if (reach == n) break;
+  }
   return k;
 }
 
@@ -203,6 +216,7 @@ struct TopList {
       e[q] = at < count ? buf[at] : 0;
       best = e[q] > best ? e[q] : best;
     }
+    // n lanes reach t: those above o, and of those at o the ones with the lowest ids
     const uint32_t hi = (uint32_t)(best >> 32), o = nth_largest(hi, n);
     const uint32_t lo = nth_largest(hi == o ? (uint32_t)best : 0, n - __popcll(__ballot(hi > o)));
     const uint64_t t = (uint64_t)o << 32 | lo;
@@ -313,47 +327,51 @@ __global__ __launch_bounds__(64 * WAVES) void logprobs_kernel(LogprobArgs a) {
     float x[1] = {-INFINITY};
     if (id < (uint32_t)a.V) {
       x[0] = load_lp<BF16>(x0, id);
-      add(r, x, a.c);
+      add(r, x, a.c, true);
     }
     if constexpr (TOP) top.put(place_key(x[0], id));
   }
   bool first = true;
-  uint32_t at = beg;  // the workgroup's next vector
-  // a lane's elements x, of the vectors at, at + kThreads, ...
-  auto consider = [&](auto& x, bool in) {
-    constexpr int n = sizeof(x) / sizeof(float);
-    float most = x[0];
+  // the next tile's loads are under way while a tile is summed
+  u32x4 held[TILE];
+  auto load = [&](uint32_t at) {
 #pragma unroll
-    for (int i = 1; i < n; ++i) most = fmaxf(most, x[i]);
-    most = in ? most : -INFINITY;
-    if (first) top.first_threshold(most), first = false;
-    if (__any(most >= top.x)) {
-      uint32_t mine = 0;
-#pragma unroll
-      for (int i = 0; i < n; ++i) mine |= x[i] >= top.x ? 1u << i : 0u;
-      top.offer(in ? mine : 0, [&](int i) {
-        const uint32_t id = (at + (i / VEC) * kThreads + tid) * VEC + i % VEC;
-        return place_key(load_lp<BF16>(x0, id), id);
-      });
-    }
+    for (int u = 0; u < TILE; ++u)
+      if (at + u * kThreads + tid < end) held[u] = load_vec<BF16>(x0, at + u * kThreads + tid);
   };
-  if constexpr (TILE > 1)
-    for (; at + TILE * kThreads <= end; at += TILE * kThreads) {
-      float x[TILE * VEC];
-#pragma unroll
-      for (int u = 0; u < TILE; ++u) unpack<BF16>(load_vec<BF16>(x0, at + u * kThreads + tid), x + u * VEC);
-      add(r, x, a.c);
-      if constexpr (TOP) consider(x, true);
-    }
+  load(beg);
 #pragma unroll 1
-  for (; at < end; at += kThreads) {
-    float x[VEC];
-    const bool in = at + tid < end;
-    if (in) {
-      unpack<BF16>(load_vec<BF16>(x0, at + tid), x);
-      add(r, x, a.c);
+  for (uint32_t at = beg; at < end; at += TILE * kThreads) {
+    float x[TILE * VEC];
+    const bool whole = at + TILE * kThreads <= end;
+#pragma unroll
+    for (int u = 0; u < TILE; ++u) unpack<BF16>(held[u], x + u * VEC);
+    if (!whole) {  // -inf adds nothing and has no place
+#pragma unroll
+      for (int i = 0; i < TILE * VEC; ++i)
+        if (at + (i / VEC) * kThreads + tid >= end) x[i] = -INFINITY;
     }
-    if constexpr (TOP) consider(x, in);
+    load(at + TILE * kThreads);
+    add(r, x, a.c, !whole);
+    if constexpr (TOP) {
+      float most = x[0];
+#pragma unroll
+      for (int i = 1; i < TILE * VEC; ++i) most = fmaxf(most, x[i]);
+      if (first) top.first_threshold(most), first = false;
+      if (__any(most >= top.x)) {
+        uint32_t mine = 0;
+#pragma unroll
+        for (int i = 0; i < TILE * VEC; ++i) mine |= x[i] > -INFINITY && x[i] >= top.x ? 1u << i : 0u;
+        top.offer(mine, [&](int i) {
+          const uint32_t id = (at + (i / VEC) * kThreads + tid) * VEC + i % VEC;
+          if constexpr (TILE > 1) return place_key(load_lp<BF16>(x0, id), id);
+          float v = x[0];
+#pragma unroll
+          for (int j = 1; j < VEC; ++j) v = j == i ? x[j] : v;
+          return place_key(v, id);
+        });
+      }
+    }
   }
   r = join_block<WAVES>(r, sh, a.c);
 
@@ -435,17 +453,17 @@ void launch_logprobs(LogprobArgs a, int64_t N, int waves, hipStream_t st) {
     const dim3 grid((unsigned)((N - r < kRows ? N - r : kRows) * a.pieces));
     if (waves == 1)
       hipLaunchKernelGGL((logprobs_kernel<BF16, TOP, 1, 1>), grid, dim3(64), 0, st, a);
-    else if (a.pieces > 1)
+    else if (a.piece_vectors <= kLpThreads)
       hipLaunchKernelGGL((logprobs_kernel<BF16, TOP, kLpThreads / 64, 1>), grid, dim3(kLpThreads), 0, st, a);
     else
-      hipLaunchKernelGGL((logprobs_kernel<BF16, TOP, kLpThreads / 64, 4>), grid, dim3(kLpThreads), 0, st, a);
+      hipLaunchKernelGGL((logprobs_kernel<BF16, TOP, kLpThreads / 64, kTile>), grid, dim3(kLpThreads), 0, st, a);
   }
 }
 
 struct LogprobBwdArgs {
   const void* logits;
   int64_t ld;
-  int32_t N, V;
+  int32_t V;
   const int32_t* targets;
   float inv_temperature;
   const float *lse, *entropy, *dlogp, *dentropy;
@@ -453,28 +471,68 @@ struct LogprobBwdArgs {
   int64_t ld_out;
 };
 
+// One row's gradient: d = -p (a + b (y + h)), y = x / temperature - lse.
+struct RowGrad {
+  float it, lse, a, b, h;
+  __device__ __forceinline__ float operator()(float x) const {
+    const float y = fmaf(x, it, -lse), p = __builtin_amdgcn_exp2f(y * kLog2e);
+    const float d = -p * fmaf(b, y + h, a);
+    return p == 0.0f ? 0.0f : d;  // y is -inf where the logit is
+  }
+};
+
+// A workgroup takes kBwdTile vectors per thread of one row; every element is
+// read and then written by one thread, so the gradient may replace the logits.
 template <bool BF16>
 __global__ __launch_bounds__(kLpThreads) void logprobs_bwd_kernel(LogprobBwdArgs a) {
+  constexpr int VEC = kVec<BF16>;
   const int64_t row = blockIdx.y;
+  const int tid = threadIdx.x;
+  const char* x0 = (const char*)a.logits + (size_t)row * a.ld * (BF16 ? 2 : 4);
+  char* d0 = (char*)a.dlogits + (size_t)row * a.ld_out * (BF16 ? 2 : 4);
+  const uint32_t vectors = (uint32_t)a.V / VEC, at = blockIdx.x * (kBwdTile * kLpThreads) + tid;
   const int target = a.targets ? a.targets[row] : -1;
   const bool keep = !a.targets || (unsigned)target < (unsigned)a.V;
+  u32x4 held[kBwdTile];
+  if (keep) {
+#pragma unroll
+    for (int u = 0; u < kBwdTile; ++u)
+      if (at + u * kLpThreads < vectors) held[u] = load_vec<BF16>(x0, at + u * kLpThreads);
+  }
+  RowGrad g;
   // a row of -inf only: every p is 0
-  const float lse = a.lse[row] == -INFINITY ? INFINITY : a.lse[row];
+  g.it = a.inv_temperature, g.lse = a.lse[row] == -INFINITY ? INFINITY : a.lse[row];
   const float dlp = a.dlogp ? a.dlogp[row] * a.inv_temperature : 0.0f;
-  const float dh = a.dentropy ? a.dentropy[row] * a.inv_temperature : 0.0f;
-  const float h = a.dentropy ? a.entropy[row] : 0.0f;
-  for (int j = blockIdx.x * kLpThreads + threadIdx.x; j < a.V; j += gridDim.x * kLpThreads) {
-    float d = 0.0f;
+  g.a = dlp;
+  g.b = a.dentropy ? a.dentropy[row] * a.inv_temperature : 0.0f;
+  g.h = a.dentropy ? a.entropy[row] : 0.0f;
+#pragma unroll
+  for (int u = 0; u < kBwdTile; ++u) {
+    const uint32_t v = at + u * kLpThreads;
+    if (v >= vectors) continue;
+    u32x4 out = {0, 0, 0, 0};
     if (keep) {
-      const float y = fmaf(load_lp<BF16>(a.logits, row * a.ld + j), a.inv_temperature, -lse);
-      const float p = exp2f(y * kLog2e);
-      if (!(p == 0.0f)) d = -p * (dlp + dh * (y + h));
-      if (j == target) d += dlp;
+      float x[VEC];
+      unpack<BF16>(held[u], x);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) x[i] = g(x[i]);
+      if (a.dlogp && (uint32_t)target / VEC == v) {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) x[i] += (uint32_t)target % VEC == i ? dlp : 0.0f;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) out[i] = BF16 ? pack_bf2(x[2 * i % VEC], x[(2 * i + 1) % VEC]) : __float_as_uint(x[i]);
     }
+    *(u32x4_any*)(d0 + (size_t)v * 16) = out;
+  }
+  const uint32_t id = vectors * VEC + tid;  // the row's last elements, less than a vector
+  if (blockIdx.x == 0 && id < (uint32_t)a.V) {
+    float d = 0.0f;
+    if (keep) d = g(load_lp<BF16>(x0, id)) + (a.dlogp && target == (int)id ? dlp : 0.0f);
     if constexpr (BF16)
-      ((uint16_t*)a.dlogits)[row * a.ld_out + j] = (uint16_t)pack_bf2(d, 0.0f);
+      ((uint16_t*)d0)[id] = (uint16_t)pack_bf2(d, 0.0f);
     else
-      ((float*)a.dlogits)[row * a.ld_out + j] = d;
+      ((float*)d0)[id] = d;
   }
 }
 
@@ -527,10 +585,12 @@ int foremoe_token_logprobs(const void* logits, foremoe_dtype dtype, int64_t ld, 
   // of at least a vector for every thread
   const int waves = vectors <= 128 ? 1 : kLpThreads / 64;
   int64_t pieces = 1;
-  if (ws && waves > 1) {
-    pieces = kMaxSplit / N;
+  if (ws && waves > 1 && N < kFewRows) {
+    const bool one = N <= kFewRows / kMaxPieces;  // a vector for every thread
+    pieces = one ? kMaxPieces : (kSplit + N - 1) / N;
+    const int64_t most = vectors / (kLpThreads * (one ? 1 : n_top ? kTile : 2 * kTile));
+    if (pieces > most) pieces = most;
     if (pieces > kMaxPieces) pieces = kMaxPieces;
-    if (pieces > vectors / kLpThreads) pieces = vectors / kLpThreads;
     if (pieces < 1) pieces = 1;
   }
   LogprobArgs a{};
@@ -571,12 +631,12 @@ int foremoe_token_logprobs_bwd(const void* logits, foremoe_dtype dtype, int64_t 
   const size_t item = dtype == FOREMOE_BF16 ? 2 : 4;
   for (int64_t r = 0; r < N; r += 65535) {
     const int64_t n = N - r < 65535 ? N - r : 65535;
-    LogprobBwdArgs a{(const char*)logits + (size_t)r * ld * item, ld, (int32_t)n, (int32_t)V,
+    LogprobBwdArgs a{(const char*)logits + (size_t)r * ld * item, ld, (int32_t)V,
                      targets ? targets + r : nullptr, 1.0f / temperature, lse + r,
                      entropy ? entropy + r : nullptr, dlogp ? dlogp + r : nullptr, dentropy ? dentropy + r : nullptr,
                      (char*)dlogits + (size_t)r * ld_out * item, ld_out};
-    const unsigned gx = (unsigned)((V + kLpThreads * 8 - 1) / (kLpThreads * 8));
-    const dim3 grid(gx < 64 ? gx : 64, (unsigned)n);
+    const int64_t per = kLpThreads * kBwdTile, vectors = V / (dtype == FOREMOE_BF16 ? kVec<true> : kVec<false>);
+    const dim3 grid((unsigned)(vectors < 1 ? 1 : (vectors + per - 1) / per), (unsigned)n);
     if (dtype == FOREMOE_BF16)
       hipLaunchKernelGGL(logprobs_bwd_kernel<true>, grid, dim3(kLpThreads), 0, st, a);
     else
