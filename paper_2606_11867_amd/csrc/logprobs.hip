@@ -112,28 +112,25 @@ __device__ __forceinline__ Sums join(Sums a, Sums b, float c) {
   return Sums{m, a.s + b.s, a.t + b.t};
 }
 
-// Adds n elements of one lane; with care where some may be -inf.
+// Adds n elements of one lane.
 template <int n>
-__device__ __forceinline__ void add(Sums& a, const float (&x)[n], float c, bool care) {
+__device__ __forceinline__ void add(Sums& a, const float* x, float c) {
   float top = x[0];
 #pragma unroll
   for (int i = 1; i < n; ++i) top = fmaxf(top, x[i]);
   if (top > a.m) rebase(a, top, c);
   const float mc = a.m * c;
   float s[2] = {0.0f, 0.0f}, t[2] = {0.0f, 0.0f};
-  if (!care) {
 #pragma unroll
-    for (int i = 0; i < n; ++i) {
-      const float y = fmaf(x[i], c, -mc), e = __builtin_amdgcn_exp2f(y);
-      s[i & 1] += e;
-      t[i & 1] = fmaf(y, e, t[i & 1]);
-    }
-    s[0] += s[1];
-    t[0] += t[1];
-    // a y of -inf (a masked logit) makes a NaN of y 2^y
-    care = t[0] != t[0] || huge(mc);
+  for (int i = 0; i < n; ++i) {
+    const float y = fmaf(x[i], c, -mc), e = __builtin_amdgcn_exp2f(y);
+    s[i & 1] += e;
+    t[i & 1] = fmaf(y, e, t[i & 1]);
   }
-  if (care) {
+  s[0] += s[1];
+  t[0] += t[1];
+  // a y of -inf (a masked logit) has made a NaN of y 2^y: again with care
+  if (__builtin_expect(t[0] != t[0] || huge(mc), 0)) {
     s[0] = t[0] = 0.0f;
     const bool far = huge(mc);
 #pragma unroll
@@ -324,54 +321,70 @@ __global__ __launch_bounds__(64 * WAVES) void logprobs_kernel(LogprobArgs a) {
   const uint32_t end = min(vectors, beg + a.piece_vectors);
   if (end == vectors) {  // the row's last elements, less than a vector
     const uint32_t id = vectors * VEC + tid;
-    float x[1] = {-INFINITY};
+    float x = -INFINITY;
     if (id < (uint32_t)a.V) {
-      x[0] = load_lp<BF16>(x0, id);
-      add(r, x, a.c, true);
+      x = load_lp<BF16>(x0, id);
+      add<1>(r, &x, a.c);
     }
-    if constexpr (TOP) top.put(place_key(x[0], id));
+    if constexpr (TOP) top.put(place_key(x, id));
   }
   bool first = true;
-  // the next tile's loads are under way while a tile is summed
-  u32x4 held[TILE];
-  auto load = [&](uint32_t at) {
+  uint32_t at = beg;  // the workgroup's next vector
+  // a lane's elements x of the vectors at, at + kThreads, ...
+  auto consider = [&](const auto& x) {
+    constexpr int n = sizeof(x) / sizeof(float);
+    float most = x[0];
+#pragma unroll
+    for (int i = 1; i < n; ++i) most = fmaxf(most, x[i]);
+    if (first) top.first_threshold(most), first = false;
+    if (__any(most >= top.x)) {
+      uint32_t mine = 0;
+#pragma unroll
+      for (int i = 0; i < n; ++i) mine |= x[i] > -INFINITY && x[i] >= top.x ? 1u << i : 0u;
+      top.offer(mine, [&](int i) {
+        const uint32_t id = (at + (i / VEC) * kThreads + tid) * VEC + i % VEC;
+        if constexpr (n > VEC) return place_key(load_lp<BF16>(x0, id), id);
+        float v = x[0];
+#pragma unroll
+        for (int j = 1; j < VEC; ++j) v = j == i ? x[j] : v;
+        return place_key(v, id);
+      });
+    }
+  };
+  if constexpr (TILE > 1) {
+    u32x4 next[TILE];  // under way while a tile is summed
+    const uint32_t whole = end - (end - beg) % (TILE * kThreads);
 #pragma unroll
     for (int u = 0; u < TILE; ++u)
-      if (at + u * kThreads + tid < end) held[u] = load_vec<BF16>(x0, at + u * kThreads + tid);
-  };
-  load(beg);
+      if (at < whole) next[u] = load_vec<BF16>(x0, at + u * kThreads + tid);
 #pragma unroll 1
-  for (uint32_t at = beg; at < end; at += TILE * kThreads) {
-    float x[TILE * VEC];
-    const bool whole = at + TILE * kThreads <= end;
+    for (; at < whole; at += TILE * kThreads) {
+      float x[TILE * VEC];
 #pragma unroll
-    for (int u = 0; u < TILE; ++u) unpack<BF16>(held[u], x + u * VEC);
-    if (!whole) {  // -inf adds nothing and has no place
+      for (int u = 0; u < TILE; ++u) unpack<BF16>(next[u], x + u * VEC);
+      if (at + TILE * kThreads < whole) {
 #pragma unroll
-      for (int i = 0; i < TILE * VEC; ++i)
-        if (at + (i / VEC) * kThreads + tid >= end) x[i] = -INFINITY;
-    }
-    load(at + TILE * kThreads);
-    add(r, x, a.c, !whole);
-    if constexpr (TOP) {
-      float most = x[0];
-#pragma unroll
-      for (int i = 1; i < TILE * VEC; ++i) most = fmaxf(most, x[i]);
-      if (first) top.first_threshold(most), first = false;
-      if (__any(most >= top.x)) {
-        uint32_t mine = 0;
-#pragma unroll
-        for (int i = 0; i < TILE * VEC; ++i) mine |= x[i] > -INFINITY && x[i] >= top.x ? 1u << i : 0u;
-        top.offer(mine, [&](int i) {
-          const uint32_t id = (at + (i / VEC) * kThreads + tid) * VEC + i % VEC;
-          if constexpr (TILE > 1) return place_key(load_lp<BF16>(x0, id), id);
-          float v = x[0];
-#pragma unroll
-          for (int j = 1; j < VEC; ++j) v = j == i ? x[j] : v;
-          return place_key(v, id);
-        });
+        for (int u = 0; u < TILE; ++u) next[u] = load_vec<BF16>(x0, at + (TILE + u) * kThreads + tid);
       }
+      add<TILE * VEC>(r, x, a.c);
+      if constexpr (TOP) consider(x);
     }
+  }
+  // what is left of the piece, at most TILE vectors for a thread
+  u32x4 one;
+  if (at + tid < end) one = load_vec<BF16>(x0, at + tid);
+#pragma unroll 1
+  for (; at < end; at += kThreads) {
+    float x[VEC];
+    unpack<BF16>(one, x);
+    if (at + kThreads + tid < end) one = load_vec<BF16>(x0, at + kThreads + tid);
+    if (at + tid < end) {
+      add<VEC>(r, x, a.c);
+    } else if constexpr (TOP) {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) x[i] = -INFINITY;  // has no place
+    }
+    if constexpr (TOP) consider(x);
   }
   r = join_block<WAVES>(r, sh, a.c);
 
@@ -452,7 +465,7 @@ void launch_logprobs(LogprobArgs a, int64_t N, int waves, hipStream_t st) {
     a.first = (int32_t)r;
     const dim3 grid((unsigned)((N - r < kRows ? N - r : kRows) * a.pieces));
     if (waves == 1)
-      hipLaunchKernelGGL((logprobs_kernel<BF16, TOP, 1, 1>), grid, dim3(64), 0, st, a);
+      hipLaunchKernelGGL((logprobs_kernel<BF16, TOP, 1, kTile>), grid, dim3(64), 0, st, a);
     else if (a.piece_vectors <= kLpThreads)
       hipLaunchKernelGGL((logprobs_kernel<BF16, TOP, kLpThreads / 64, 1>), grid, dim3(kLpThreads), 0, st, a);
     else
@@ -580,10 +593,14 @@ int foremoe_token_logprobs(const void* logits, foremoe_dtype dtype, int64_t ld, 
   if (N == 0) return FOREMOE_OK;
   const int vec = dtype == FOREMOE_BF16 ? kVec<true> : kVec<false>;
   const int64_t vectors = V / vec;
-  // a wavefront where a row has no more than two vectors for each lane of it,
-  // else a workgroup; rows that do not fill the GPU in as many pieces as do,
-  // of at least a vector for every thread
-  const int waves = vectors <= 128 ? 1 : kLpThreads / 64;
+  // A wavefront for a row, or a workgroup: a workgroup's barriers and joins
+  // cost more than they give where rows are short, or many and wanted with
+  // top places (us, workgroup -> wavefront: 16384 x 8000 bf16 81 -> 54, 600 x
+  // 4096 5.3 -> 4.5, 16384 x 16000 123 -> 101, 8192 x 131072 with 20 places
+  // 494 -> 415; without places 365 -> 378, 2048 x 131072 with 5 118 -> 143).
+  // Rows that do not fill the GPU are cut into pieces, of at least a vector
+  // for every thread.
+  const int waves = vectors <= 1024 || (N >= 4096 && (n_top || vectors <= 2048)) ? 1 : kLpThreads / 64;
   int64_t pieces = 1;
   if (ws && waves > 1 && N < kFewRows) {
     const bool one = N <= kFewRows / kMaxPieces;  // a vector for every thread
