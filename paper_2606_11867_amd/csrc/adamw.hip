@@ -4,6 +4,8 @@
 #include <limits.h>
 #include <math.h>
 
+#include <type_traits>
+
 #include "common.h"
 
 // 8-bit states round what the formulas give, operation by operation: a
@@ -13,9 +15,13 @@
 namespace foremoe {
 namespace {
 
-constexpr int kAdamThreads = FOREMOE_ADAMW_BLOCK;
+constexpr int kAdamThreads = 256;
+constexpr int kAdamBlocks = 2;  // blocks of 256 elements that a wavefront takes, 4 elements a lane
+constexpr int kAdamChunk = kAdamThreads / 64 * kAdamBlocks * FOREMOE_ADAMW_BLOCK;  // elements of a workgroup
+static_assert(FOREMOE_ADAMW_BLOCK == 64 * 4);
 // elements of a record that one launch takes: fewer than 2^32 threads
 constexpr int64_t kAdamPiece = (int64_t)1 << 30;
+static_assert(kAdamPiece % kAdamChunk == 0);
 
 struct AdamRecord {
   void* param;
@@ -27,17 +33,46 @@ struct AdamRecord {
   float* v_scale;
   int64_t n;
   float decay;
-  uint32_t first;  // its first workgroup
 };
 
 struct AdamArgs {
   AdamRecord rec[FOREMOE_ADAMW_LAUNCH];
+  uint32_t first[FOREMOE_ADAMW_LAUNCH];  // a record's first workgroup
   int32_t n_rec;
   int32_t zero_grads;
   float beta1, one_beta1, beta2, one_beta2, eps, alpha, root;
   const float* grad_scale;
 };
 static_assert(sizeof(AdamArgs) <= 4096, "kernel arguments");
+
+// Four consecutive elements as they lie in memory. Tensors may start at any
+// element, so the vectors have the alignment of the type only.
+template <class T>
+struct Four {
+  typedef T any __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+  T e[4];
+  __device__ __forceinline__ void load(const void* p, int64_t i, int64_t n) {
+    const T* at = (const T*)p + i;
+    if (i + 4 <= n) {
+      const any x = *(const any*)at;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) e[k] = x[k];
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) e[k] = i + k < n ? at[k] : T(0);
+    }
+  }
+  __device__ __forceinline__ void store(void* p, int64_t i, int64_t n) const {
+    T* at = (T*)p + i;
+    if (i + 4 <= n) {
+      *(any*)at = any{e[0], e[1], e[2], e[3]};
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (i + k < n) at[k] = e[k];
+    }
+  }
+};
 
 // ---------------------------------------------------------------------------
 // 8-bit codes: x in [0, 1] as the top bits of its fp32 pattern, rounded to
@@ -72,79 +107,135 @@ __device__ __forceinline__ float decode_v(uint32_t c, float scale) {
 }
 __device__ __forceinline__ float inverse(float scale) { return scale >= 0x1p-126f ? 1.0f / scale : 0.0f; }
 
-// The largest of non-negative values over the workgroup, by their patterns:
-// a NaN is above every number, so it wins.
-__device__ __forceinline__ float block_max(float v, uint32_t* sh) {
-  uint32_t b = __float_as_uint(v) & 0x7fffffffu;
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) b = max(b, (uint32_t)__shfl_xor((int)b, o, 64));
-  __syncthreads();
-  if (lane_id() == 0) sh[threadIdx.x >> 6] = b;
-  __syncthreads();
-  for (int w = 0; w < kAdamThreads / 64; ++w) b = max(b, sh[w]);
-  return __uint_as_float(b);
+// The largest of the wavefront's patterns. Of non-negative floats: a NaN is
+// above every number, so it wins.
+__device__ __forceinline__ float wave_max_pattern(uint32_t b) {
+  // within rows of 16 lanes, then the rows' last lanes onwards: lane 63 has it
+#define FOREMOE_DPP_MAX(ctrl, rows) b = max(b, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)b, ctrl, rows, 0xf, true))
+  FOREMOE_DPP_MAX(0x111, 0xf);  // row_shr:1
+  FOREMOE_DPP_MAX(0x112, 0xf);  // row_shr:2
+  FOREMOE_DPP_MAX(0x114, 0xf);  // row_shr:4
+  FOREMOE_DPP_MAX(0x118, 0xf);  // row_shr:8
+  FOREMOE_DPP_MAX(0x142, 0xa);  // row_bcast:15
+  FOREMOE_DPP_MAX(0x143, 0xc);  // row_bcast:31
+#undef FOREMOE_DPP_MAX
+  return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)b, 63));
 }
 
+// A wavefront takes kAdamBlocks blocks of 256 elements, 4 consecutive ones a
+// lane, loads them all and then works on one after another; a block's scale
+// is then one maximum over the wavefront.
 template <bool PBF16, bool GBF16, bool BITS8>
 __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(AdamArgs a) {
-  __shared__ uint32_t sh[kAdamThreads / 64];
+  typedef typename std::conditional<PBF16, uint16_t, float>::type P;
+  typedef typename std::conditional<GBF16, uint16_t, float>::type G;
+  typedef typename std::conditional<BITS8, uint8_t, float>::type S;
   int r = 0;
-  while (r + 1 < a.n_rec && a.rec[r + 1].first <= blockIdx.x) ++r;
+#pragma unroll
+  for (int step = 32; step; step >>= 1)
+    if (r + step < a.n_rec && a.first[r + step] <= blockIdx.x) r += step;
   const AdamRecord& rec = a.rec[r];
-  const int64_t block = blockIdx.x - rec.first, i = block * kAdamThreads + threadIdx.x;
-  const bool in = i < rec.n;
-  float m = 0.0f, v = 0.0f;
-  if (in) {
-    float g = GBF16 ? bf2f(((uint16_t*)rec.grad)[i]) : ((float*)rec.grad)[i];
-    if (a.grad_scale) g = g * *a.grad_scale;
-    if constexpr (BITS8) {
-      m = decode_m(((uint8_t*)rec.m)[i], rec.m_scale[block]);
-      v = decode_v(((uint8_t*)rec.v)[i], rec.v_scale[block]);
-    } else {
-      m = ((float*)rec.m)[i];
-      v = ((float*)rec.v)[i];
-    }
-    m = m * a.beta1 + g * a.one_beta1;
-    v = v * a.beta2 + g * g * a.one_beta2;
-  }
-  const float u = sqrtf(v);
-  if (in) {
-    float p = rec.master ? rec.master[i] : PBF16 ? bf2f(((uint16_t*)rec.param)[i]) : ((float*)rec.param)[i];
-    const float den = u * a.root + a.eps;
-    p = p * rec.decay - (den == 0.0f ? 0.0f : m / den) * a.alpha;
-    if (rec.master) rec.master[i] = p;
-    if constexpr (PBF16)
-      ((uint16_t*)rec.param)[i] = (uint16_t)pack_bf2(p, 0.0f);
+  const int64_t n = rec.n;
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t block0 = ((int64_t)(blockIdx.x - a.first[r]) * (kAdamThreads / 64) + wave) * kAdamBlocks;
+  const float gs = a.grad_scale ? *a.grad_scale : 1.0f;
+  Four<G> g[kAdamBlocks];
+  Four<P> p[kAdamBlocks];
+  Four<float> w[kAdamBlocks];
+  Four<S> m[kAdamBlocks], v[kAdamBlocks];
+  float m_scale[kAdamBlocks], v_scale[kAdamBlocks];
+#pragma unroll
+  for (int q = 0; q < kAdamBlocks; ++q) {
+    const int64_t i = (block0 + q) * FOREMOE_ADAMW_BLOCK + lane * 4;
+    if ((block0 + q) * FOREMOE_ADAMW_BLOCK >= n) continue;
+    g[q].load(rec.grad, i, n);
+    if (rec.master)
+      w[q].load(rec.master, i, n);
     else
-      ((float*)rec.param)[i] = p;
-    if (a.zero_grads) {
-      if constexpr (GBF16)
-        ((uint16_t*)rec.grad)[i] = 0;
-      else
-        ((float*)rec.grad)[i] = 0.0f;
-    }
+      p[q].load(rec.param, i, n);
+    m[q].load(rec.m, i, n);
+    v[q].load(rec.v, i, n);
+    if constexpr (BITS8) m_scale[q] = rec.m_scale[block0 + q], v_scale[q] = rec.v_scale[block0 + q];
   }
-  if constexpr (BITS8) {
-    const float ms = block_max(m, sh), vs = block_max(u, sh);
-    if (in) {
-      ((uint8_t*)rec.m)[i] = (uint8_t)encode_m(m, inverse(ms));
-      ((uint8_t*)rec.v)[i] = (uint8_t)encode_v(u, inverse(vs));
+#pragma unroll
+  for (int q = 0; q < kAdamBlocks; ++q) {
+    const int64_t i = (block0 + q) * FOREMOE_ADAMW_BLOCK + lane * 4;
+    if ((block0 + q) * FOREMOE_ADAMW_BLOCK >= n) continue;
+    float mm[4], uu[4];
+    uint32_t m_most = 0, u_most = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      float grad, mk, vk, wk;
+      if constexpr (GBF16) grad = bf2f(g[q].e[k]);
+      else grad = g[q].e[k];
+      if (a.grad_scale) grad = grad * gs;
+      if constexpr (BITS8) {
+        mk = decode_m(m[q].e[k], m_scale[q]);
+        vk = decode_v(v[q].e[k], v_scale[q]);
+      } else {
+        mk = m[q].e[k];
+        vk = v[q].e[k];
+      }
+      mk = mk * a.beta1 + grad * a.one_beta1;
+      vk = vk * a.beta2 + grad * grad * a.one_beta2;
+      const float u = BITS8 ? sqrtf(vk) : __builtin_amdgcn_sqrtf(vk);
+      if (rec.master) wk = w[q].e[k];
+      else if constexpr (PBF16) wk = bf2f(p[q].e[k]);
+      else wk = p[q].e[k];
+      // the reciprocal and the square root are within a unit in the last
+      // place (8 bits: the square root is exact, it makes the code)
+      const float den = u * a.root + a.eps;
+      wk = wk * rec.decay - (den == 0.0f ? 0.0f : mk * __builtin_amdgcn_rcpf(den)) * a.alpha;
+      if (rec.master) w[q].e[k] = wk;
+      if constexpr (!PBF16) p[q].e[k] = wk;
+      else p[q].e[k] = (uint16_t)pack_bf2(wk, 0.0f);
+      if constexpr (BITS8) {
+        mm[k] = mk, uu[k] = u;
+        m_most = max(m_most, __float_as_uint(mk) & 0x7fffffffu);
+        u_most = max(u_most, __float_as_uint(u) & 0x7fffffffu);
+      } else {
+        m[q].e[k] = mk, v[q].e[k] = vk;
+      }
     }
-    __syncthreads();  // every thread has read the old scales
-    if (threadIdx.x == 0) rec.m_scale[block] = ms, rec.v_scale[block] = vs;
-  } else if (in) {
-    ((float*)rec.m)[i] = m;
-    ((float*)rec.v)[i] = v;
+    if constexpr (BITS8) {
+      const float ms = wave_max_pattern(m_most), us = wave_max_pattern(u_most);
+      const float mi = inverse(ms), ui = inverse(us);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        m[q].e[k] = (uint8_t)encode_m(mm[k], mi);
+        v[q].e[k] = (uint8_t)encode_v(uu[k], ui);
+      }
+      if (lane == 0) rec.m_scale[block0 + q] = ms, rec.v_scale[block0 + q] = us;
+    }
+    if (rec.master) w[q].store(rec.master, i, n);
+    p[q].store(rec.param, i, n);
+    m[q].store(rec.m, i, n);
+    v[q].store(rec.v, i, n);
+    if (a.zero_grads) {
+      Four<G> z{};
+      z.store(rec.grad, i, n);
+    }
   }
 }
 
 __global__ __launch_bounds__(kAdamThreads) void adamw_values_kernel(const uint8_t* m, const float* m_scale,
                                                                     const uint8_t* v, const float* v_scale, int64_t n,
                                                                     float* m_out, float* v_out) {
-  const int64_t block = blockIdx.x + (int64_t)blockIdx.y * gridDim.x, i = block * kAdamThreads + threadIdx.x;
+  const int64_t block = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (kAdamThreads / 64) + (threadIdx.x >> 6);
+  const int64_t i = block * FOREMOE_ADAMW_BLOCK + lane_id() * 4;
   if (i >= n) return;
-  m_out[i] = decode_m(m[i], m_scale[block]);
-  v_out[i] = decode_v(v[i], v_scale[block]);
+  Four<uint8_t> cm, cv;
+  Four<float> fm, fv;
+  cm.load(m, i, n);
+  cv.load(v, i, n);
+  const float ms = m_scale[block], vs = v_scale[block];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    fm.e[k] = decode_m(cm.e[k], ms);
+    fv.e[k] = decode_v(cv.e[k], vs);
+  }
+  fm.store(m_out, i, n);
+  fv.store(v_out, i, n);
 }
 
 }  // namespace
@@ -217,15 +308,16 @@ int foremoe_adamw_step(const foremoe_adamw_tensor* tensors, int32_t n_tensors, f
     const foremoe_adamw_tensor& t = tensors[i];
     for (int64_t at = 0; at < t.n; at += kAdamPiece) {
       const int64_t n = t.n - at < kAdamPiece ? t.n - at : kAdamPiece;
-      const uint64_t nb = (uint64_t)(n + kAdamThreads - 1) / kAdamThreads;
+      const uint64_t nb = (uint64_t)(n + kAdamChunk - 1) / kAdamChunk;
       if (a.n_rec == FOREMOE_ADAMW_LAUNCH || (blocks + nb) * kAdamThreads > (uint64_t)2 * kAdamPiece) flush();
+      a.first[a.n_rec] = (uint32_t)blocks;
       AdamRecord& r = a.rec[a.n_rec++];
       r.param = (char*)t.param + at * pb, r.grad = (char*)t.grad + at * gb;
       r.master = t.master ? t.master + at : nullptr;
       r.m = (char*)t.m + at * sb, r.v = (char*)t.v + at * sb;
       r.m_scale = state_bits == 8 ? t.m_scale + at / FOREMOE_ADAMW_BLOCK : nullptr;
       r.v_scale = state_bits == 8 ? t.v_scale + at / FOREMOE_ADAMW_BLOCK : nullptr;
-      r.n = n, r.decay = (float)(1 - lr * t.weight_decay), r.first = (uint32_t)blocks;
+      r.n = n, r.decay = (float)(1 - lr * t.weight_decay);
       blocks += nb;
     }
   }
@@ -240,7 +332,7 @@ int foremoe_adamw_state_values(const uint8_t* m, const float* m_scale, const uin
   REQUIRE(m && m_scale && v && v_scale && m_out && v_out, "adamw_state_values: NULL pointer");
   REQUIRE(!misaligned(m_scale, 4) && !misaligned(v_scale, 4) && !misaligned(m_out, 4) && !misaligned(v_out, 4),
           "adamw_state_values: misaligned pointer");
-  const int64_t nb = (n + kAdamThreads - 1) / kAdamThreads;
+  const int64_t nb = (n + kAdamThreads * 4 - 1) / (kAdamThreads * 4);
   const int64_t gx = nb < (1 << 20) ? nb : 1 << 20, gy = (nb + gx - 1) / gx;
   hipLaunchKernelGGL(adamw_values_kernel, dim3((unsigned)gx, (unsigned)gy), dim3(kAdamThreads), 0,
                      (hipStream_t)stream, m, m_scale, v, v_scale, n, m_out, v_out);
