@@ -45,31 +45,36 @@ struct AdamArgs {
 };
 static_assert(sizeof(AdamArgs) <= 4096, "kernel arguments");
 
-// Four consecutive elements as they lie in memory. Tensors may start at any
-// element, so the vectors have the alignment of the type only.
+// A lane's four elements of a block, as they lie in memory. Tensors may start
+// at any element, so the vectors have the alignment of the type only. Every
+// byte is read once and written once: both carry the nontemporal hint.
+// `block` is uniform; `left` elements of the block exist (FULL: all).
 template <class T>
 struct Four {
   typedef T any __attribute__((ext_vector_type(4), aligned(sizeof(T))));
   T e[4];
-  __device__ __forceinline__ void load(const void* p, int64_t i, int64_t n) {
-    const T* at = (const T*)p + i;
-    if (i + 4 <= n) {
-      const any x = *(const any*)at;
+  template <bool FULL>
+  __device__ __forceinline__ void load(const void* block, int lane, int left) {
+    const T* at = (const T*)block + (uint32_t)lane * 4;
+    if (FULL || lane * 4 + 4 <= left) {
+      const any x = __builtin_nontemporal_load((const any*)at);
 #pragma unroll
       for (int k = 0; k < 4; ++k) e[k] = x[k];
     } else {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) e[k] = i + k < n ? at[k] : T(0);
+      for (int k = 0; k < 4; ++k) e[k] = lane * 4 + k < left ? at[k] : T(0);
     }
   }
-  __device__ __forceinline__ void store(void* p, int64_t i, int64_t n) const {
-    T* at = (T*)p + i;
-    if (i + 4 <= n) {
-      *(any*)at = any{e[0], e[1], e[2], e[3]};
+  template <bool FULL>
+  __device__ __forceinline__ void store(void* block, int lane, int left) const {
+    T* at = (T*)block + (uint32_t)lane * 4;
+    if (FULL || lane * 4 + 4 <= left) {
+      const any x = {e[0], e[1], e[2], e[3]};
+      __builtin_nontemporal_store(x, (any*)at);
     } else {
 #pragma unroll
       for (int k = 0; k < 4; ++k)
-        if (i + k < n) at[k] = e[k];
+        if (lane * 4 + k < left) at[k] = e[k];
     }
   }
 };
@@ -81,7 +86,8 @@ struct Four {
 template <int SHIFT, int ONE>
 __device__ __forceinline__ int top_bits(float x) {
   const uint32_t b = __float_as_uint(x);
-  return (int)((b + ((1u << (SHIFT - 1)) - 1) + ((b >> SHIFT) & 1)) >> SHIFT) - ((0x3F800000 >> SHIFT) - ONE);
+  constexpr uint32_t kZero = ((0x3F800000u >> SHIFT) - ONE) << SHIFT;  // the pattern of code 0
+  return (int)(b + ((b >> SHIFT) & 1) + (((1u << (SHIFT - 1)) - 1) - kZero)) >> SHIFT;
 }
 template <int SHIFT, int ONE>
 __device__ __forceinline__ float of_top_bits(uint32_t c) {
@@ -122,22 +128,23 @@ __device__ __forceinline__ float wave_max_pattern(uint32_t b) {
   return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)b, 63));
 }
 
-// A wavefront takes kAdamBlocks blocks of 256 elements, 4 consecutive ones a
-// lane, loads them all and then works on one after another; a block's scale
-// is then one maximum over the wavefront.
-template <bool PBF16, bool GBF16, bool BITS8>
-__global__ __launch_bounds__(kAdamThreads) void adamw_kernel(AdamArgs a) {
+// One wavefront's kAdamBlocks blocks of 256 elements, 4 consecutive ones a
+// lane: all are loaded, then worked on one after another; a block's scale is
+// then one maximum over the wavefront. left: elements from its first block on.
+template <bool PBF16, bool GBF16, bool BITS8, bool FULL>
+__device__ __forceinline__ void adamw_blocks(const AdamArgs& a, const AdamRecord& rec, int64_t block0, int left) {
   typedef typename std::conditional<PBF16, uint16_t, float>::type P;
   typedef typename std::conditional<GBF16, uint16_t, float>::type G;
   typedef typename std::conditional<BITS8, uint8_t, float>::type S;
-  int r = 0;
-#pragma unroll
-  for (int step = 32; step; step >>= 1)
-    if (r + step < a.n_rec && a.first[r + step] <= blockIdx.x) r += step;
-  const AdamRecord& rec = a.rec[r];
-  const int64_t n = rec.n;
-  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t block0 = ((int64_t)(blockIdx.x - a.first[r]) * (kAdamThreads / 64) + wave) * kAdamBlocks;
+  constexpr int B = FOREMOE_ADAMW_BLOCK;
+  const int lane = lane_id();
+  const bool master = PBF16 && rec.master;
+  const int64_t i0 = block0 * B;
+  G* const grad0 = (G*)rec.grad + i0;
+  P* const param0 = (P*)rec.param + i0;
+  float* const master0 = master ? rec.master + i0 : nullptr;
+  S* const m0 = (S*)rec.m + i0;
+  S* const v0 = (S*)rec.v + i0;
   const float gs = a.grad_scale ? *a.grad_scale : 1.0f;
   Four<G> g[kAdamBlocks];
   Four<P> p[kAdamBlocks];
@@ -146,21 +153,19 @@ __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(AdamArgs a) {
   float m_scale[kAdamBlocks], v_scale[kAdamBlocks];
 #pragma unroll
   for (int q = 0; q < kAdamBlocks; ++q) {
-    const int64_t i = (block0 + q) * FOREMOE_ADAMW_BLOCK + lane * 4;
-    if ((block0 + q) * FOREMOE_ADAMW_BLOCK >= n) continue;
-    g[q].load(rec.grad, i, n);
-    if (rec.master)
-      w[q].load(rec.master, i, n);
+    if (!FULL && q * B >= left) break;
+    g[q].template load<FULL>(grad0 + q * B, lane, left - q * B);
+    if (master)
+      w[q].template load<FULL>(master0 + q * B, lane, left - q * B);
     else
-      p[q].load(rec.param, i, n);
-    m[q].load(rec.m, i, n);
-    v[q].load(rec.v, i, n);
+      p[q].template load<FULL>(param0 + q * B, lane, left - q * B);
+    m[q].template load<FULL>(m0 + q * B, lane, left - q * B);
+    v[q].template load<FULL>(v0 + q * B, lane, left - q * B);
     if constexpr (BITS8) m_scale[q] = rec.m_scale[block0 + q], v_scale[q] = rec.v_scale[block0 + q];
   }
 #pragma unroll
   for (int q = 0; q < kAdamBlocks; ++q) {
-    const int64_t i = (block0 + q) * FOREMOE_ADAMW_BLOCK + lane * 4;
-    if ((block0 + q) * FOREMOE_ADAMW_BLOCK >= n) continue;
+    if (!FULL && q * B >= left) break;
     float mm[4], uu[4];
     uint32_t m_most = 0, u_most = 0;
 #pragma unroll
@@ -179,14 +184,14 @@ __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(AdamArgs a) {
       mk = mk * a.beta1 + grad * a.one_beta1;
       vk = vk * a.beta2 + grad * grad * a.one_beta2;
       const float u = BITS8 ? sqrtf(vk) : __builtin_amdgcn_sqrtf(vk);
-      if (rec.master) wk = w[q].e[k];
+      if (master) wk = w[q].e[k];
       else if constexpr (PBF16) wk = bf2f(p[q].e[k]);
       else wk = p[q].e[k];
       // the reciprocal and the square root are within a unit in the last
       // place (8 bits: the square root is exact, it makes the code)
       const float den = u * a.root + a.eps;
       wk = wk * rec.decay - (den == 0.0f ? 0.0f : mk * __builtin_amdgcn_rcpf(den)) * a.alpha;
-      if (rec.master) w[q].e[k] = wk;
+      if (master) w[q].e[k] = wk;
       if constexpr (!PBF16) p[q].e[k] = wk;
       else p[q].e[k] = (uint16_t)pack_bf2(wk, 0.0f);
       if constexpr (BITS8) {
@@ -207,35 +212,53 @@ __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(AdamArgs a) {
       }
       if (lane == 0) rec.m_scale[block0 + q] = ms, rec.v_scale[block0 + q] = us;
     }
-    if (rec.master) w[q].store(rec.master, i, n);
-    p[q].store(rec.param, i, n);
-    m[q].store(rec.m, i, n);
-    v[q].store(rec.v, i, n);
+    if (master) w[q].template store<FULL>(master0 + q * B, lane, left - q * B);
+    p[q].template store<FULL>(param0 + q * B, lane, left - q * B);
+    m[q].template store<FULL>(m0 + q * B, lane, left - q * B);
+    v[q].template store<FULL>(v0 + q * B, lane, left - q * B);
     if (a.zero_grads) {
       Four<G> z{};
-      z.store(rec.grad, i, n);
+      z.template store<FULL>(grad0 + q * B, lane, left - q * B);
     }
   }
+}
+
+template <bool PBF16, bool GBF16, bool BITS8>
+__global__ __launch_bounds__(kAdamThreads) void adamw_kernel(AdamArgs a) {
+  int r = 0;
+#pragma unroll
+  for (int step = 32; step; step >>= 1)
+    if (r + step < a.n_rec && a.first[r + step] <= blockIdx.x) r += step;
+  const AdamRecord& rec = a.rec[r];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t block0 = ((int64_t)(blockIdx.x - a.first[r]) * (kAdamThreads / 64) + wave) * kAdamBlocks;
+  const int64_t left = rec.n - block0 * FOREMOE_ADAMW_BLOCK;
+  if (left >= kAdamBlocks * FOREMOE_ADAMW_BLOCK)
+    adamw_blocks<PBF16, GBF16, BITS8, true>(a, rec, block0, kAdamBlocks * FOREMOE_ADAMW_BLOCK);
+  else if (left > 0)
+    adamw_blocks<PBF16, GBF16, BITS8, false>(a, rec, block0, (int)left);
 }
 
 __global__ __launch_bounds__(kAdamThreads) void adamw_values_kernel(const uint8_t* m, const float* m_scale,
                                                                     const uint8_t* v, const float* v_scale, int64_t n,
                                                                     float* m_out, float* v_out) {
-  const int64_t block = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (kAdamThreads / 64) + (threadIdx.x >> 6);
-  const int64_t i = block * FOREMOE_ADAMW_BLOCK + lane_id() * 4;
-  if (i >= n) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = lane_id();
+  const int64_t block = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (kAdamThreads / 64) + wave;
+  const int64_t i0 = block * FOREMOE_ADAMW_BLOCK;
+  if (i0 >= n) return;
+  const int left = (int)(n - i0 < FOREMOE_ADAMW_BLOCK ? n - i0 : FOREMOE_ADAMW_BLOCK);
   Four<uint8_t> cm, cv;
   Four<float> fm, fv;
-  cm.load(m, i, n);
-  cv.load(v, i, n);
+  cm.load<false>(m + i0, lane, left);
+  cv.load<false>(v + i0, lane, left);
   const float ms = m_scale[block], vs = v_scale[block];
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     fm.e[k] = decode_m(cm.e[k], ms);
     fv.e[k] = decode_v(cv.e[k], vs);
   }
-  fm.store(m_out, i, n);
-  fv.store(v_out, i, n);
+  fm.store<false>(m_out + i0, lane, left);
+  fv.store<false>(v_out + i0, lane, left);
 }
 
 }  // namespace
