@@ -12,7 +12,9 @@ namespace {
 constexpr int kRouterThreads = 256;
 constexpr int kRouterWaves = kRouterThreads / 64;
 constexpr int kRouterBlocks = 512;  // most workgroups that leave partial statistics
+constexpr int kStatColumns = 16;    // experts that a workgroup of the statistics kernel sums
 constexpr float kNegInf = -INFINITY;
+constexpr float kLog2e = 1.4426950408889634f;
 
 struct RouterArgs {
   const void* logits;
@@ -44,146 +46,236 @@ __device__ __forceinline__ float load_logit(const void* p, int64_t i) {
   return ((const float*)p)[i];
 }
 
-__device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+// ---------------------------------------------------------------------------
+// A token is worked on by L lanes, 16 (four tokens to a wavefront) up to 256
+// experts and all 64 above. Register j of lane l holds expert
+// 4 (L (j / 4) + l) + j % 4, so that four registers are one load.
+// ---------------------------------------------------------------------------
+template <int L>
+__device__ __forceinline__ int expert_of(int lane, int j) {
+  return 4 * (L * (j / 4) + lane) + j % 4;
+}
+
+// Reductions over a token's lanes; every lane gets the same bits. Within 16
+// lanes by rotations, which cost no more than the operation itself.
+template <int CTRL>
+__device__ __forceinline__ int rotated(int v) {
+  return __builtin_amdgcn_update_dpp(v, v, CTRL, 0xf, 0xf, false);
+}
+template <int L, class Op>
+__device__ __forceinline__ float reduce(float v, Op&& op) {
+  v = op(v, __int_as_float(rotated<0x128>(__float_as_int(v))));  // row_ror:8, 4, 2, 1
+  v = op(v, __int_as_float(rotated<0x124>(__float_as_int(v))));
+  v = op(v, __int_as_float(rotated<0x122>(__float_as_int(v))));
+  v = op(v, __int_as_float(rotated<0x121>(__float_as_int(v))));
+  if constexpr (L == 64) {
+    v = op(v, __shfl_xor(v, 16, 64));
+    v = op(v, __shfl_xor(v, 32, 64));
+  }
   return v;
 }
-__device__ __forceinline__ int wave_min(int v) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) v = min(v, __shfl_xor(v, o, 64));
+template <int L>
+__device__ __forceinline__ float lanes_max(float v) {
+  return reduce<L>(v, [](float a, float b) { return fmaxf(a, b); });
+}
+template <int L>
+__device__ __forceinline__ float lanes_sum(float v) {
+  return reduce<L>(v, [](float a, float b) { return a + b; });
+}
+template <int L>
+__device__ __forceinline__ int lanes_min(int v) {
+  v = min(v, rotated<0x128>(v));
+  v = min(v, rotated<0x124>(v));
+  v = min(v, rotated<0x122>(v));
+  v = min(v, rotated<0x121>(v));
+  if constexpr (L == 64) {
+    v = min(v, __shfl_xor(v, 16, 64));
+    v = min(v, __shfl_xor(v, 32, 64));
+  }
   return v;
 }
 
+// e^d for d <= 0, and the sigmoid: within |d| 2^-24 + 2 units in the last place.
+__device__ __forceinline__ float fast_exp(float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
+__device__ __forceinline__ float fast_sigmoid(float v) {
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v * -kLog2e));
+}
+// The same rounded operation by operation, where a score plus a bias decides:
+// the score of the definition's four fp32 operations.
 __device__ __forceinline__ float sigmoid(float v) { return 1.0f / (1.0f + expf(-v)); }
 
-// One token's scores: s[j] (softmax numerators or sigmoids) of the experts
-// lane + 64 j, and their sum.
-template <int VPL>
-__device__ __forceinline__ float token_scores(const float (&v)[VPL], bool sig, float (&s)[VPL]) {
-  float m = kNegInf;
+// A token's row of logits, -inf beyond the last expert.
+template <bool BF16, int L, int V>
+__device__ __forceinline__ void load_row(const RouterArgs& a, int64_t t, int lane, float (&v)[V]) {
+  typedef float f32x4 __attribute__((ext_vector_type(4), aligned(4)));
+  typedef uint16_t u16x4 __attribute__((ext_vector_type(4), aligned(2)));
+  const char* row = (const char*)a.logits + (size_t)t * a.ld * (BF16 ? 2 : 4);
 #pragma unroll
-  for (int j = 0; j < VPL; ++j) m = fmaxf(m, v[j]);
-  m = wave_max(m);
-  if (m == kNegInf) m = 0.0f;
-  float sum = 0.0f;
+  for (int j = 0; j < V; j += 4) {
+    const int e = expert_of<L>(lane, j);
+    if (e + 4 <= a.E) {
+      if constexpr (BF16) {
+        const u16x4 x = *(const u16x4*)(row + 2 * e);
 #pragma unroll
-  for (int j = 0; j < VPL; ++j) {
-    s[j] = sig ? sigmoid(v[j]) : expf(v[j] - m);
+        for (int i = 0; i < 4; ++i) v[j + i] = bf2f(x[i]);
+      } else {
+        const f32x4 x = *(const f32x4*)(row + 4 * e);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[j + i] = x[i];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[j + i] = e + i < a.E ? load_logit<BF16>(row, e + i) : kNegInf;
+    }
+  }
+}
+
+// Whether some logit is not -inf (a NaN is not), the row's maximum (0 where
+// there is none), its scores s and their sum.
+template <int L, int V>
+__device__ __forceinline__ bool row_scores(const float (&v)[V], bool sig, float (&s)[V], float& top, float& sum) {
+  float m = v[0];
+  bool some = false;
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    m = fmaxf(m, v[j]);
+    some |= v[j] != kNegInf;
+  }
+  m = lanes_max<L>(m);
+  top = m > kNegInf ? m : 0.0f;
+  sum = 0.0f;
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    s[j] = sig ? fast_sigmoid(v[j]) : fast_exp(v[j] - top);
     sum += s[j];
   }
-  return wave_sum(sum);
+  sum = lanes_sum<L>(sum);
+  return lanes_max<L>(some ? 1.0f : 0.0f) != 0.0f;
 }
 
-// The score of a picked place (x its logit) over the sum that its gate
-// divides by, for the place this lane holds; `empty` places give 0.
-__device__ __forceinline__ float place_gate(float x, bool empty, bool sig, bool renorm, float row_max,
-                                            float row_sum, float* denom) {
-  float q;
-  if (sig) {
-    q = empty ? 0.0f : sigmoid(x);
-    *denom = renorm ? wave_sum(q) : 1.0f;
-  } else if (renorm) {
-    float mx = wave_max(empty ? kNegInf : x);
-    if (mx == kNegInf) mx = 0.0f;
-    q = empty ? 0.0f : expf(x - mx);
-    *denom = wave_sum(q);
-  } else {
-    q = empty ? 0.0f : expf(x - row_max);
-    *denom = row_sum;
+// The C * L places of a token, place lane + c L in register c: the scores q
+// of the picked logits x over the sum that the gates divide by.
+template <int L, int C>
+__device__ __forceinline__ float place_scores(const float (&x)[C], const int (&id)[C], bool sig, bool renorm,
+                                              float top, float sum, float (&q)[C]) {
+  if (!sig && renorm) {  // the softmax over the picked logits alone
+    top = kNegInf;
+#pragma unroll
+    for (int c = 0; c < C; ++c) top = fmaxf(top, id[c] < 0 ? kNegInf : x[c]);
+    top = lanes_max<L>(top);
+    if (!(top > kNegInf)) top = 0.0f;
   }
-  return *denom == 0.0f ? 0.0f : q / *denom;
+  float total = 0.0f;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    q[c] = id[c] < 0 ? 0.0f : sig ? fast_sigmoid(x[c]) : fast_exp(x[c] - top);
+    total += q[c];
+  }
+  if (renorm) return lanes_sum<L>(total);
+  return sig ? 1.0f : sum;
 }
 
-// One wavefront per token, expert e = lane + 64 j in register j.
-template <bool BF16, int VPL>
+template <bool BF16, int L, int V, int C>
 __global__ __launch_bounds__(kRouterThreads) void router_fwd_kernel(RouterArgs a) {
+  constexpr int kTokens = 64 / L;  // of a wavefront
   extern __shared__ char smem[];
-  float* sh_prob = (float*)smem;                             // [waves][E]
+  float* sh_prob = (float*)smem;                                // [waves, E]
   int32_t* sh_count = (int32_t*)(sh_prob + kRouterWaves * a.E);  // [E]
   int32_t* sh_tokens = sh_count + a.E;
-  const int lane = lane_id(), wave = threadIdx.x >> 6;
-  const bool stats = a.prob_part != nullptr;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x % L, sub = lane_id() / L;
+  const bool stats = a.prob_part != nullptr, sig = a.sigmoid != 0, renorm = a.renorm != 0;
+  // replayed gates that need the picked logits alone
+  const bool rows = stats || !a.ids_in || (!sig && !renorm);
   if (stats) {
     for (int e = threadIdx.x; e < a.E; e += kRouterThreads) sh_count[e] = 0;
     if (threadIdx.x == 0) *sh_tokens = 0;
     __syncthreads();
   }
-  float acc[VPL] = {};
+  float acc[V] = {};
   int tokens = 0;
-  const bool sig = a.sigmoid != 0;
-  for (int64_t t = (int64_t)blockIdx.x * kRouterWaves + wave; t < a.T; t += (int64_t)gridDim.x * kRouterWaves) {
-    float v[VPL], s[VPL];
-    bool some = false;
-#pragma unroll
-    for (int j = 0; j < VPL; ++j) {
-      const int e = lane + 64 * j;
-      v[j] = e < a.E ? load_logit<BF16>(a.logits, t * a.ld + e) : kNegInf;
-      some |= v[j] != kNegInf;  // true for a NaN
-    }
-    const bool alive = __any(some) && (!a.mask || a.mask[t]);
-    const float sum = token_scores<VPL>(v, sig, s);
-    int id = -1;  // this lane's place, k = lane
+  // every lane of a wavefront stays in the loop while one of its tokens is left
+  for (int64_t t0 = ((int64_t)blockIdx.x * kRouterWaves + wave) * kTokens; t0 < a.T;
+       t0 += (int64_t)gridDim.x * kRouterWaves * kTokens) {
+    const bool in = t0 + sub < a.T;
+    const int64_t t = in ? t0 + sub : a.T - 1;
+    bool alive = in && (!a.mask || a.mask[t]);
+    float v[V], s[V], top = 0.0f, sum = 1.0f;
+    int id[C];
     if (a.ids_in) {
-      if (lane < a.K) id = a.ids_in[t * a.K + lane];
-      if ((unsigned)id >= (unsigned)a.E) id = -1;
-    } else {
-      float key[VPL];
 #pragma unroll
-      for (int j = 0; j < VPL; ++j) {
-        const int e = lane + 64 * j;
+      for (int c = 0; c < C; ++c) id[c] = lane + c * L < a.K ? a.ids_in[t * a.K + lane + c * L] : -1;
+    }
+    if (rows) {
+      load_row<BF16, L, V>(a, t, lane, v);
+      alive &= row_scores<L, V>(v, sig, s, top, sum);
+    }
+    if (!a.ids_in) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) id[c] = -1;
+      float key[V];
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
         key[j] = v[j];
-        if (a.bias && e < a.E) key[j] = s[j] + a.bias[e];
+        const int e = expert_of<L>(lane, j);
+        if (a.bias && e < a.E) key[j] = sigmoid(v[j]) + a.bias[e];
         if (!(v[j] > kNegInf) || !(key[j] > kNegInf)) key[j] = kNegInf;
       }
-      for (int k = 0; k < a.K; ++k) {
-        float best = kNegInf;
 #pragma unroll
-        for (int j = 0; j < VPL; ++j) best = fmaxf(best, key[j]);
-        best = wave_max(best);
-        if (best == kNegInf) break;
-        int at = INT_MAX;
+      for (int c = 0; c < C; ++c) {
+#pragma unroll 1
+        for (int k = 0; k < L && c * L + k < a.K; ++k) {
+          float best = key[0];
 #pragma unroll
-        for (int j = VPL - 1; j >= 0; --j)
-          if (key[j] == best) at = lane + 64 * j;
-        at = wave_min(at);
-        if (lane == k) id = at;
+          for (int j = 1; j < V; ++j) best = fmaxf(best, key[j]);
+          best = lanes_max<L>(best);
+          int at = INT_MAX;
 #pragma unroll
-        for (int j = 0; j < VPL; ++j)
-          if (lane + 64 * j == at) key[j] = kNegInf;
+          for (int j = V - 1; j >= 0; --j) at = key[j] == best ? expert_of<L>(lane, j) : at;
+          at = lanes_min<L>(at);
+#pragma unroll
+          for (int j = 0; j < V; ++j) key[j] = expert_of<L>(lane, j) == at ? kNegInf : key[j];
+          if (lane == k) id[c] = best > kNegInf ? at : -1;
+        }
       }
     }
-    if (!alive) id = -1;
-    const float x = id >= 0 ? load_logit<BF16>(a.logits, t * a.ld + id) : kNegInf;
-    if (x == kNegInf) id = -1;
-    float m = kNegInf;
+    float x[C], q[C];
 #pragma unroll
-    for (int j = 0; j < VPL; ++j) m = fmaxf(m, v[j]);
-    m = wave_max(m);
-    float denom;
-    const float g = place_gate(x, id < 0, sig, a.renorm != 0, m == kNegInf ? 0.0f : m, sum, &denom);
-    if (lane < a.K) {
-      a.ids[t * a.K + lane] = id;
-      a.gates[t * a.K + lane] = id < 0 ? 0.0f : a.scale * g;
+    for (int c = 0; c < C; ++c) {
+      if (!alive || (unsigned)id[c] >= (unsigned)a.E) id[c] = -1;
+      x[c] = id[c] >= 0 ? load_logit<BF16>(a.logits, t * a.ld + id[c]) : kNegInf;
+      if (x[c] == kNegInf) id[c] = -1;
+    }
+    const float denom = place_scores<L, C>(x, id, sig, renorm, top, sum, q);
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int k = lane + c * L;
+      if (!in || k >= a.K) continue;
+      a.ids[t * a.K + k] = id[c];
+      a.gates[t * a.K + k] = id[c] < 0 || denom == 0.0f ? 0.0f : a.scale * (q[c] / denom);
+      if (stats && id[c] >= 0) atomicAdd(&sh_count[id[c]], 1);
     }
     if (stats && alive) {
       const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
 #pragma unroll
-      for (int j = 0; j < VPL; ++j) acc[j] += s[j] * inv;
+      for (int j = 0; j < V; ++j) acc[j] += s[j] * inv;
       ++tokens;
-      if (lane < a.K && id >= 0) atomicAdd(&sh_count[id], 1);
     }
   }
   if (!stats) return;
 #pragma unroll
-  for (int j = 0; j < VPL; ++j) {
-    const int e = lane + 64 * j;
-    if (e < a.E) sh_prob[wave * a.E + e] = acc[j];
+  for (int j = 0; j < V; ++j) {
+    if constexpr (L == 16) {
+      acc[j] += __shfl_xor(acc[j], 16, 64);
+      acc[j] += __shfl_xor(acc[j], 32, 64);
+    }
+    const int e = expert_of<L>(lane, j);
+    if (sub == 0 && e < a.E) sh_prob[wave * a.E + e] = acc[j];
   }
   if (lane == 0) atomicAdd(sh_tokens, tokens);
   __syncthreads();
   for (int e = threadIdx.x; e < a.E; e += kRouterThreads) {
     float p = 0.0f;
+#pragma unroll
     for (int w = 0; w < kRouterWaves; ++w) p += sh_prob[w * a.E + e];
     a.prob_part[(size_t)blockIdx.x * a.E + e] = p;
     a.count_part[(size_t)blockIdx.x * a.E + e] = sh_count[e];
@@ -191,54 +283,74 @@ __global__ __launch_bounds__(kRouterThreads) void router_fwd_kernel(RouterArgs a
   if (threadIdx.x == 0) a.token_part[blockIdx.x] = *sh_tokens;
 }
 
-// The workgroups' partial statistics summed in their order.
-__global__ __launch_bounds__(1024) void router_stats_kernel(int E, int blocks, const float* prob_part,
-                                                            const int32_t* count_part, const int32_t* token_part,
-                                                            int32_t* counts, int32_t* n_tokens, float* prob_mean,
-                                                            float* loss) {
-  __shared__ float sh_loss[16];
-  __shared__ int sh_total[16];
-  const int e = threadIdx.x, lane = lane_id(), wave = threadIdx.x >> 6;
-  int n = 0, c = 0;
+// The workgroups' partial statistics summed in a fixed order: 16 experts to a
+// workgroup, 16 threads to an expert. The last workgroup to finish adds up the
+// balance loss.
+__global__ __launch_bounds__(256) void router_stats_kernel(int E, int blocks, const float* prob_part,
+                                                           const int32_t* count_part, const int32_t* token_part,
+                                                           int32_t* counts, int32_t* n_tokens, float* prob_mean,
+                                                           float* loss, uint32_t* ticket) {
+  __shared__ float sh_p[256];
+  __shared__ int sh_c[256], sh_n[4];
+  __shared__ bool sh_last;
+  const int tid = threadIdx.x, e = blockIdx.x * kStatColumns + tid % kStatColumns, row = tid / kStatColumns;
+  int c = 0, n = 0;
   float p = 0.0f;
-  for (int b = 0; b < blocks; ++b) {
-    n += token_part[b];
-    if (e < E) {
+  for (int b = tid; b < blocks; b += 256) n += token_part[b];
+  if (e < E) {
+#pragma unroll 8
+    for (int b = row; b < blocks; b += 256 / kStatColumns) {
       p += prob_part[(size_t)b * E + e];
       c += count_part[(size_t)b * E + e];
     }
   }
-  const float mean = p / (float)max(n, 1);
-  if (e < E) {
-    counts[e] = c;
-    prob_mean[e] = mean;
-  }
-  const float part = wave_sum((float)c * mean);
-  int total = c;
-  for (int o = 32; o >= 1; o >>= 1) total += __shfl_xor(total, o, 64);
-  if (lane == 0) {
-    sh_loss[wave] = part;
-    sh_total[wave] = total;
-  }
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) n += __shfl_xor(n, o, 64);
+  if (lane_id() == 0) sh_n[tid >> 6] = n;
+  sh_p[tid] = p, sh_c[tid] = c;
   __syncthreads();
-  if (e == 0) {
-    float l = 0.0f;
-    int all = 0;
-    for (int w = 0; w < 16; ++w) {
-      l += sh_loss[w];
-      all += sh_total[w];
-    }
+  n = sh_n[0] + sh_n[1] + sh_n[2] + sh_n[3];
+  if (tid < kStatColumns && e < E) {
+    for (int r = 1; r < 256 / kStatColumns; ++r) p += sh_p[r * kStatColumns + tid], c += sh_c[r * kStatColumns + tid];
+    __hip_atomic_store(counts + e, c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __hip_atomic_store(prob_mean + e, p / (float)max(n, 1), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): these results have reached memory
+  __syncthreads();
+  if (tid == 0) sh_last = atomicAdd(ticket, 1u) == gridDim.x - 1;
+  __syncthreads();
+  if (!sh_last) return;
+  float l = 0.0f;
+  int all = 0;
+  for (int i = tid; i < E; i += 256) {
+    const int ci = __hip_atomic_load(counts + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    l += (float)ci * __hip_atomic_load(prob_mean + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    all += ci;
+  }
+  l = wave_sum(l);
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) all += __shfl_xor(all, o, 64);
+  if (lane_id() == 0) sh_p[tid >> 6] = l, sh_c[tid >> 6] = all;
+  __syncthreads();
+  if (tid == 0) {
+    l = sh_p[0] + sh_p[1] + sh_p[2] + sh_p[3];
+    all = sh_c[0] + sh_c[1] + sh_c[2] + sh_c[3];
     *n_tokens = n;
     *loss = (float)E * (l / (float)max(all, 1));
+    __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
 }
 
-template <bool BF16, int VPL>
+template <bool BF16, int L, int V, int C>
 __global__ __launch_bounds__(kRouterThreads) void router_bwd_kernel(RouterArgs a) {
+  constexpr int kTokens = 64 / L;
+  typedef float f32x4 __attribute__((ext_vector_type(4), aligned(4)));
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2), aligned(2)));
   __shared__ int sh_total;
-  const int lane = lane_id(), wave = threadIdx.x >> 6;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x % L, sub = lane_id() / L;
   const bool sig = a.sigmoid != 0, renorm = a.renorm != 0, balance = a.coef != 0.0f;
-  float c[VPL] = {};
+  const bool through_pi = !sig && !renorm;  // the gates' gradient goes through the whole softmax
+  float push[V] = {};  // balance gradient of pi
   if (balance) {
     if (threadIdx.x == 0) sh_total = 0;
     __syncthreads();
@@ -248,77 +360,100 @@ __global__ __launch_bounds__(kRouterThreads) void router_bwd_kernel(RouterArgs a
     __syncthreads();
     const float k = a.coef * (float)a.E / (float)max(*a.n_tokens, 1) / (float)max(sh_total, 1);
 #pragma unroll
-    for (int j = 0; j < VPL; ++j) {
-      const int e = lane + 64 * j;
-      if (e < a.E) c[j] = k * (float)a.counts[e];
+    for (int j = 0; j < V; ++j) {
+      const int e = expert_of<L>(lane, j);
+      if (e < a.E) push[j] = k * (float)a.counts[e];
     }
   }
-  for (int64_t t = (int64_t)blockIdx.x * kRouterWaves + wave; t < a.T; t += (int64_t)gridDim.x * kRouterWaves) {
-    float v[VPL], s[VPL], d[VPL];
-    bool some = false;
+  for (int64_t t0 = ((int64_t)blockIdx.x * kRouterWaves + wave) * kTokens; t0 < a.T;
+       t0 += (int64_t)gridDim.x * kRouterWaves * kTokens) {
+    const bool in = t0 + sub < a.T;
+    const int64_t t = in ? t0 + sub : a.T - 1;
+    float v[V], s[V], top, sum;
+    int id[C];
+    float dg[C], x[C], w[C];
 #pragma unroll
-    for (int j = 0; j < VPL; ++j) {
-      const int e = lane + 64 * j;
-      v[j] = e < a.E ? load_logit<BF16>(a.logits, t * a.ld + e) : kNegInf;
-      some |= v[j] != kNegInf;
-      d[j] = 0.0f;
+    for (int c = 0; c < C; ++c) {
+      id[c] = -1, dg[c] = w[c] = 0.0f;
+      if (a.dgates && lane + c * L < a.K) {
+        id[c] = a.ids[t * a.K + lane + c * L];
+        dg[c] = a.scale * a.dgates[t * a.K + lane + c * L];
+      }
+      if ((unsigned)id[c] >= (unsigned)a.E) id[c] = -1;
     }
-    if (__any(some) && (!a.mask || a.mask[t])) {
-      const float sum = token_scores<VPL>(v, sig, s);
-      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-      float w = 0.0f;
-      int id = -1;
-      if (a.dgates) {
-        if (lane < a.K) id = a.ids[t * a.K + lane];
-        if ((unsigned)id >= (unsigned)a.E) id = -1;
-        const float x = id >= 0 ? load_logit<BF16>(a.logits, t * a.ld + id) : kNegInf;
-        const float dg = id >= 0 ? a.scale * a.dgates[t * a.K + lane] : 0.0f;
-        w = dg;
-        if (renorm) {
-          float denom;
-          const float q = place_gate(x, id < 0, sig, true, 0.0f, 0.0f, &denom);
-          const float dot = wave_sum(q * dg);
-          w = id < 0 || denom == 0.0f ? 0.0f : sig ? (dg - dot) / denom : q * (dg - dot);
+    load_row<BF16, L, V>(a, t, lane, v);
+    const bool alive = row_scores<L, V>(v, sig, s, top, sum) && (!a.mask || a.mask[t]);
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    float ds[V] = {};  // of the score, or of the logit (softmax renormalised)
+    if (a.dgates) {
+      if (renorm) {
+        float q[C], dot = 0.0f;
+#pragma unroll
+        for (int c = 0; c < C; ++c) x[c] = id[c] >= 0 ? load_logit<BF16>(a.logits, t * a.ld + id[c]) : kNegInf;
+        const float denom = place_scores<L, C>(x, id, sig, true, 0.0f, 0.0f, q);
+        const float over = denom == 0.0f ? 0.0f : 1.0f / denom;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          q[c] *= over;
+          if (id[c] >= 0) dot += q[c] * dg[c];
+        }
+        dot = lanes_sum<L>(dot);
+#pragma unroll
+        for (int c = 0; c < C; ++c) w[c] = id[c] < 0 ? 0.0f : (sig ? over : q[c]) * (dg[c] - dot);
+      } else {
+#pragma unroll
+        for (int c = 0; c < C; ++c) w[c] = id[c] < 0 ? 0.0f : dg[c];
+      }
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+#pragma unroll 1
+        for (int k = 0; k < L && c * L + k < a.K; ++k) {
+          const int ik = __shfl(id[c], k, L);
+          const float wk = __shfl(w[c], k, L);
+#pragma unroll
+          for (int j = 0; j < V; ++j) ds[j] += expert_of<L>(lane, j) == ik ? wk : 0.0f;
         }
       }
-      float ds[VPL] = {};  // what the gates give: of the score, or of the logit (softmax renormalised)
-      if (a.dgates)
-        for (int k = 0; k < a.K; ++k) {
-          const int ik = __shfl(id, k, 64);
-          const float wk = __shfl(w, k, 64);
+    }
+    float pc = 0.0f;  // sum of pi times its gradient
+    if (balance || through_pi) {
 #pragma unroll
-          for (int j = 0; j < VPL; ++j)
-            if (lane + 64 * j == ik) ds[j] += wk;
-        }
-      float pc = 0.0f;  // sum of pi times its gradient
-      const bool through_pi = !sig && !renorm;
-#pragma unroll
-      for (int j = 0; j < VPL; ++j) pc += s[j] * inv * (c[j] + (through_pi ? ds[j] : 0.0f));
-      if (balance || through_pi) pc = wave_sum(pc);
-#pragma unroll
-      for (int j = 0; j < VPL; ++j) {
-        const float pi = s[j] * inv;
-        float r = 0.0f;
-        if (through_pi) {
-          r = pi * (c[j] + ds[j] - pc);
-        } else if (sig) {
-          r = s[j] * (1.0f - s[j]) * ds[j];
-          if (balance) r += pi * (1.0f - s[j]) * (c[j] - pc);
-        } else {
-          r = ds[j];
-          if (balance) r += pi * (c[j] - pc);
-        }
-        d[j] = r;
-      }
+      for (int j = 0; j < V; ++j) pc += s[j] * (push[j] + (through_pi ? ds[j] : 0.0f));
+      pc = lanes_sum<L>(pc) * inv;
     }
 #pragma unroll
-    for (int j = 0; j < VPL; ++j) {
-      const int e = lane + 64 * j;
-      if (e >= a.E) continue;
-      if constexpr (BF16)
-        ((uint16_t*)a.dlogits)[t * a.ld_out + e] = (uint16_t)pack_bf2(d[j], 0.0f);
-      else
-        ((float*)a.dlogits)[t * a.ld_out + e] = d[j];
+    for (int j = 0; j < V; ++j) {
+      const float pi = s[j] * inv;
+      float d;
+      if (through_pi) {
+        d = pi * (push[j] + ds[j] - pc);
+      } else if (sig) {
+        d = (1.0f - s[j]) * (s[j] * ds[j] + (balance ? pi * (push[j] - pc) : 0.0f));
+      } else {
+        d = ds[j] + (balance ? pi * (push[j] - pc) : 0.0f);
+      }
+      ds[j] = alive ? d : 0.0f;
+    }
+    if (!in) continue;
+    char* row = (char*)a.dlogits + (size_t)t * a.ld_out * (BF16 ? 2 : 4);
+#pragma unroll
+    for (int j = 0; j < V; j += 4) {
+      const int e = expert_of<L>(lane, j);
+      if (e + 4 <= a.E) {
+        if constexpr (BF16)
+          *(u32x2*)(row + 2 * e) = u32x2{pack_bf2(ds[j], ds[j + 1]), pack_bf2(ds[j + 2], ds[j + 3])};
+        else
+          *(f32x4*)(row + 4 * e) = f32x4{ds[j], ds[j + 1], ds[j + 2], ds[j + 3]};
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (e + i >= a.E) break;
+          if constexpr (BF16)
+            ((uint16_t*)row)[e + i] = (uint16_t)pack_bf2(ds[j + i], 0.0f);
+          else
+            ((float*)row)[e + i] = ds[j + i];
+        }
+      }
     }
   }
 }
@@ -327,18 +462,24 @@ size_t router_ws_bytes(int32_t E) {
   return align_up(256 + sizeof(int32_t) * (size_t)kRouterBlocks * (2 * (size_t)E + 1), 256);
 }
 
-// launch(VPL as a constant): registers for E experts over 64 lanes.
+template <int L_, int V_, int C_>
+struct Shape {
+  static constexpr int L = L_, V = V_, C = C_;
+};
+
+// launch(the lanes of a token, registers for E experts and K places over them)
 template <class Launch>
-void by_experts(int E, Launch&& launch) {
-  if (E <= 64) launch(std::integral_constant<int, 1>{});
-  else if (E <= 128) launch(std::integral_constant<int, 2>{});
-  else if (E <= 256) launch(std::integral_constant<int, 4>{});
-  else if (E <= 512) launch(std::integral_constant<int, 8>{});
-  else launch(std::integral_constant<int, 16>{});
+void by_shape(int E, int K, Launch&& launch) {
+  if (E > 512) launch(Shape<64, 16, 1>{});
+  else if (E > 256) launch(Shape<64, 8, 1>{});
+  else if (K > 16) E <= 128 ? launch(Shape<16, 8, 4>{}) : launch(Shape<16, 16, 4>{});
+  else if (E <= 64) launch(Shape<16, 4, 1>{});
+  else if (E <= 128) launch(Shape<16, 8, 1>{});
+  else launch(Shape<16, 16, 1>{});
 }
 
-unsigned router_grid(int64_t T, int64_t most) {
-  const int64_t g = (T + kRouterWaves - 1) / kRouterWaves;
+unsigned router_grid(int64_t T, int L, int64_t most) {
+  const int64_t tokens = kRouterWaves * (64 / L), g = (T + tokens - 1) / tokens;
   return (unsigned)(g < 1 ? 1 : g < most ? g : most);
 }
 
@@ -394,7 +535,6 @@ int foremoe_router_fwd(const void* logits, foremoe_dtype dtype, int64_t ld, int6
   a.logits = logits, a.ld = ld, a.T = T, a.E = E, a.K = K;
   a.sigmoid = score == FOREMOE_SIGMOID, a.renorm = renorm, a.scale = scale;
   a.bias = ids_in ? nullptr : bias, a.mask = mask, a.ids_in = ids_in, a.ids = ids, a.gates = gates;
-  const unsigned grid = router_grid(T, n_stats ? kRouterBlocks : 1 << 16);
   size_t smem = 0;
   if (n_stats) {
     a.prob_part = (float*)((char*)ws + 256);
@@ -403,16 +543,18 @@ int foremoe_router_fwd(const void* logits, foremoe_dtype dtype, int64_t ld, int6
     smem = sizeof(float) * ((size_t)(kRouterWaves + 1) * E + 1);
   }
   hipStream_t st = (hipStream_t)stream;
-  by_experts(E, [&](auto vpl) {
+  by_shape(E, K, [&](auto s) {
+    constexpr int L = decltype(s)::L, V = decltype(s)::V, C = decltype(s)::C;
+    const unsigned grid = router_grid(T, L, n_stats ? kRouterBlocks : 1 << 16);
     if (dtype == FOREMOE_BF16)
-      hipLaunchKernelGGL((router_fwd_kernel<true, decltype(vpl)::value>), dim3(grid), dim3(kRouterThreads), smem, st, a);
+      hipLaunchKernelGGL((router_fwd_kernel<true, L, V, C>), dim3(grid), dim3(kRouterThreads), smem, st, a);
     else
-      hipLaunchKernelGGL((router_fwd_kernel<false, decltype(vpl)::value>), dim3(grid), dim3(kRouterThreads), smem, st,
-                         a);
+      hipLaunchKernelGGL((router_fwd_kernel<false, L, V, C>), dim3(grid), dim3(kRouterThreads), smem, st, a);
+    if (n_stats)
+      hipLaunchKernelGGL(router_stats_kernel, dim3((E + kStatColumns - 1) / kStatColumns), dim3(256), 0, st, E,
+                         (int)grid, a.prob_part, a.count_part, a.token_part, counts, n_tokens, prob_mean, balance_loss,
+                         (uint32_t*)ws);
   });
-  if (n_stats)
-    hipLaunchKernelGGL(router_stats_kernel, dim3(1), dim3(1024), 0, st, E, (int)grid, a.prob_part, a.count_part,
-                       a.token_part, counts, n_tokens, prob_mean, balance_loss);
   return check_launch("router_fwd");
 }
 
@@ -435,13 +577,14 @@ int foremoe_router_bwd(const void* logits, foremoe_dtype dtype, int64_t ld, int6
   a.sigmoid = score == FOREMOE_SIGMOID, a.renorm = renorm, a.scale = scale;
   a.mask = mask, a.ids = const_cast<int32_t*>(ids), a.dgates = dgates, a.counts = counts, a.n_tokens = n_tokens;
   a.coef = balance_coef, a.dlogits = dlogits, a.ld_out = ld_out;
-  const unsigned grid = router_grid(T, 4096);
   hipStream_t st = (hipStream_t)stream;
-  by_experts(E, [&](auto vpl) {
+  by_shape(E, K, [&](auto s) {
+    constexpr int L = decltype(s)::L, V = decltype(s)::V, C = decltype(s)::C;
+    const unsigned grid = router_grid(T, L, 4096);
     if (dtype == FOREMOE_BF16)
-      hipLaunchKernelGGL((router_bwd_kernel<true, decltype(vpl)::value>), dim3(grid), dim3(kRouterThreads), 0, st, a);
+      hipLaunchKernelGGL((router_bwd_kernel<true, L, V, C>), dim3(grid), dim3(kRouterThreads), 0, st, a);
     else
-      hipLaunchKernelGGL((router_bwd_kernel<false, decltype(vpl)::value>), dim3(grid), dim3(kRouterThreads), 0, st, a);
+      hipLaunchKernelGGL((router_bwd_kernel<false, L, V, C>), dim3(grid), dim3(kRouterThreads), 0, st, a);
   });
   return check_launch("router_bwd");
 }

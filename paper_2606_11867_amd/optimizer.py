@@ -62,10 +62,12 @@ class AdamW:
             masters = None
         elif not bf16:
             raise ValueError("masters go with bf16 parameters")
-        self.masters: Optional[List[torch.Tensor]] = None if masters is None else list(masters)
+        # tensors of its own over the same memory: only params and grads can be
+        # given other memory from outside
+        self.masters: Optional[List[torch.Tensor]] = None if masters is None else [t.detach() for t in masters]
         if states is None:
             states = [self._zero_state(p) for p in self.params]
-        self.states = [tuple(s) for s in states]
+        self.states = [tuple(t.detach() for t in s) for s in states]
         if len(self.states) != n or (self.masters is not None and len(self.masters) != n):
             raise ValueError("masters and states: one per parameter")
         self._records = (_lib.AdamWTensor * n)()
@@ -93,8 +95,8 @@ class AdamW:
                 _vec(p, n, pd, f"params[{i}]", dev), _vec(g, n, gd, f"grads[{i}]", dev),
                 _vec(self.masters[i], n, F32, f"masters[{i}]", dev) if self.masters is not None else None,
                 *a, *([None] * (4 - len(a))), n, self.weight_decay[i])
-        self._tensors = self.params + self.grads + (self.masters or []) + [t for s in self.states for t in s]
-        self._at = [t.data_ptr() for t in self._tensors]
+        self._tensors = self.params + self.grads
+        self._at = list(map(torch.Tensor.data_ptr, self._tensors))
 
     def step(self, lr: Optional[float] = None, grad_scale: Optional[torch.Tensor] = None) -> None:
         """One step on the current stream. lr: from now on. grad_scale: a
@@ -102,7 +104,7 @@ class AdamW:
         loss scaling)."""
         if lr is not None:
             self.lr = lr
-        if [t.data_ptr() for t in self._tensors] != self._at:  # a tensor was given other memory
+        if list(map(torch.Tensor.data_ptr, self._tensors)) != self._at:  # a tensor was given other memory
             self._fill()
         _lib.check(self.lib.foremoe_adamw_step(
             self._records, len(self.params), self._pdt, self._gdt, self.state_bits, self.lr, *self.betas, self.eps,
