@@ -9,7 +9,7 @@
 namespace foremoe {
 namespace {
 
-constexpr int kRouterThreads = 256;
+constexpr int kRouterThreads = 512;
 constexpr int kRouterWaves = kRouterThreads / 64;
 constexpr int kRouterBlocks = 512;  // most workgroups that leave partial statistics
 constexpr int kStatColumns = 16;    // experts that a workgroup of the statistics kernel sums
@@ -95,6 +95,15 @@ __device__ __forceinline__ int lanes_min(int v) {
   return v;
 }
 
+typedef float f32x4_a __attribute__((ext_vector_type(4)));
+
+// Orders a wavefront's own LDS accesses.
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // e^d for d <= 0, and the sigmoid: within |d| 2^-24 + 2 units in the last place.
 __device__ __forceinline__ float fast_exp(float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
 __device__ __forceinline__ float fast_sigmoid(float v) {
@@ -102,7 +111,13 @@ __device__ __forceinline__ float fast_sigmoid(float v) {
 }
 // The same rounded operation by operation, where a score plus a bias decides:
 // the score of the definition's four fp32 operations.
-__device__ __forceinline__ float sigmoid(float v) { return 1.0f / (1.0f + expf(-v)); }
+// The quotient by a residual correction, which is correctly rounded up to
+// 2^120 (P. Markstein's method; as the division for every such number).
+__device__ __forceinline__ float sigmoid(float v) {
+  const float d = 1.0f + expf(-v), r = __builtin_amdgcn_rcpf(d);
+  const float q = fmaf(fmaf(-d, r, 1.0f), r, r);
+  return d <= 0x1p120f ? q : 1.0f / d;
+}
 
 // A token's row of logits, -inf beyond the last expert.
 template <bool BF16, int L, int V>
@@ -110,45 +125,62 @@ __device__ __forceinline__ void load_row(const RouterArgs& a, int64_t t, int lan
   typedef float f32x4 __attribute__((ext_vector_type(4), aligned(4)));
   typedef uint16_t u16x4 __attribute__((ext_vector_type(4), aligned(2)));
   const char* row = (const char*)a.logits + (size_t)t * a.ld * (BF16 ? 2 : 4);
+  auto four = [&](int j, int e) {
+    if constexpr (BF16) {
+      const u16x4 x = *(const u16x4*)(row + 2 * e);
 #pragma unroll
-  for (int j = 0; j < V; j += 4) {
-    const int e = expert_of<L>(lane, j);
-    if (e + 4 <= a.E) {
-      if constexpr (BF16) {
-        const u16x4 x = *(const u16x4*)(row + 2 * e);
+      for (int i = 0; i < 4; ++i) v[j + i] = bf2f(x[i]);
+    } else {
+      const f32x4 x = *(const f32x4*)(row + 4 * e);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[j + i] = bf2f(x[i]);
-      } else {
-        const f32x4 x = *(const f32x4*)(row + 4 * e);
+      for (int i = 0; i < 4; ++i) v[j + i] = x[i];
+    }
+  };
+  if (a.E == L * V) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[j + i] = x[i];
-      }
+    for (int j = 0; j < V; j += 4) four(j, expert_of<L>(lane, j));
+  } else {
+#pragma unroll
+    for (int j = 0; j < V; ++j) v[j] = kNegInf;
+    if (a.E % 4 == 0) {
+#pragma unroll
+      for (int j = 0; j < V; j += 4)
+        if (expert_of<L>(lane, j) < a.E) four(j, expert_of<L>(lane, j));
     } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[j + i] = e + i < a.E ? load_logit<BF16>(row, e + i) : kNegInf;
+      for (int j = 0; j < V; ++j)
+        if (expert_of<L>(lane, j) < a.E) v[j] = load_logit<BF16>(row, expert_of<L>(lane, j));
     }
   }
 }
 
 // Whether some logit is not -inf (a NaN is not), the row's maximum (0 where
-// there is none), its scores s and their sum.
+// there is none), its scores s and their sum. exact: sigmoids that decide.
 template <int L, int V>
-__device__ __forceinline__ bool row_scores(const float (&v)[V], bool sig, float (&s)[V], float& top, float& sum) {
-  float m = v[0];
+__device__ __forceinline__ bool row_scores(const float (&v)[V], bool sig, bool exact, float (&s)[V], float& top,
+                                           float& sum) {
   bool some = false;
 #pragma unroll
-  for (int j = 0; j < V; ++j) {
-    m = fmaxf(m, v[j]);
-    some |= v[j] != kNegInf;
+  for (int j = 0; j < V; ++j) some |= v[j] != kNegInf;
+  top = 0.0f;
+  if (exact) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) s[j] = sigmoid(v[j]);
+  } else if (sig) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) s[j] = fast_sigmoid(v[j]);
+  } else {
+    float m = v[0];
+#pragma unroll
+    for (int j = 1; j < V; ++j) m = fmaxf(m, v[j]);
+    m = lanes_max<L>(m);
+    top = m > kNegInf ? m : 0.0f;
+#pragma unroll
+    for (int j = 0; j < V; ++j) s[j] = fast_exp(v[j] - top);
   }
-  m = lanes_max<L>(m);
-  top = m > kNegInf ? m : 0.0f;
   sum = 0.0f;
 #pragma unroll
-  for (int j = 0; j < V; ++j) {
-    s[j] = sig ? fast_sigmoid(v[j]) : fast_exp(v[j] - top);
-    sum += s[j];
-  }
+  for (int j = 0; j < V; ++j) sum += s[j];
   sum = lanes_sum<L>(sum);
   return lanes_max<L>(some ? 1.0f : 0.0f) != 0.0f;
 }
@@ -176,7 +208,7 @@ __device__ __forceinline__ float place_scores(const float (&x)[C], const int (&i
 }
 
 template <bool BF16, int L, int V, int C>
-__global__ __launch_bounds__(kRouterThreads) void router_fwd_kernel(RouterArgs a) {
+__global__ __launch_bounds__(kRouterThreads, 4) void router_fwd_kernel(RouterArgs a) {
   constexpr int kTokens = 64 / L;  // of a wavefront
   extern __shared__ char smem[];
   float* sh_prob = (float*)smem;                                // [waves, E]
@@ -191,8 +223,13 @@ __global__ __launch_bounds__(kRouterThreads) void router_fwd_kernel(RouterArgs a
     if (threadIdx.x == 0) *sh_tokens = 0;
     __syncthreads();
   }
-  float acc[V] = {};
+  float acc[V] = {}, bias[V] = {};
   int tokens = 0;
+  if (a.bias) {
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+      if (expert_of<L>(lane, j) < a.E) bias[j] = a.bias[expert_of<L>(lane, j)];
+  }
   // every lane of a wavefront stays in the loop while one of its tokens is left
   for (int64_t t0 = ((int64_t)blockIdx.x * kRouterWaves + wave) * kTokens; t0 < a.T;
        t0 += (int64_t)gridDim.x * kRouterWaves * kTokens) {
@@ -207,18 +244,21 @@ __global__ __launch_bounds__(kRouterThreads) void router_fwd_kernel(RouterArgs a
     }
     if (rows) {
       load_row<BF16, L, V>(a, t, lane, v);
-      alive &= row_scores<L, V>(v, sig, s, top, sum);
+      alive &= row_scores<L, V>(v, sig, a.bias != nullptr, s, top, sum);
     }
     if (!a.ids_in) {
 #pragma unroll
       for (int c = 0; c < C; ++c) id[c] = -1;
       float key[V];
+      if (a.bias) {
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        key[j] = v[j];
-        const int e = expert_of<L>(lane, j);
-        if (a.bias && e < a.E) key[j] = sigmoid(v[j]) + a.bias[e];
-        if (!(v[j] > kNegInf) || !(key[j] > kNegInf)) key[j] = kNegInf;
+        for (int j = 0; j < V; ++j) {
+          key[j] = s[j] + bias[j];
+          if (!(v[j] > kNegInf) || !(key[j] > kNegInf)) key[j] = kNegInf;
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) key[j] = v[j] > kNegInf ? v[j] : kNegInf;
       }
 #pragma unroll
       for (int c = 0; c < C; ++c) {
@@ -347,6 +387,7 @@ __global__ __launch_bounds__(kRouterThreads) void router_bwd_kernel(RouterArgs a
   typedef float f32x4 __attribute__((ext_vector_type(4), aligned(4)));
   typedef uint32_t u32x2 __attribute__((ext_vector_type(2), aligned(2)));
   __shared__ int sh_total;
+  __shared__ f32x4_a sh_w[C == 1 && L == 16 ? kRouterWaves : 1][kTokens][L * V / 4];  // a token's gradients by expert
   const int wave = threadIdx.x >> 6, lane = threadIdx.x % L, sub = lane_id() / L;
   const bool sig = a.sigmoid != 0, renorm = a.renorm != 0, balance = a.coef != 0.0f;
   const bool through_pi = !sig && !renorm;  // the gates' gradient goes through the whole softmax
@@ -382,7 +423,7 @@ __global__ __launch_bounds__(kRouterThreads) void router_bwd_kernel(RouterArgs a
       if ((unsigned)id[c] >= (unsigned)a.E) id[c] = -1;
     }
     load_row<BF16, L, V>(a, t, lane, v);
-    const bool alive = row_scores<L, V>(v, sig, s, top, sum) && (!a.mask || a.mask[t]);
+    const bool alive = row_scores<L, V>(v, sig, false, s, top, sum) && (!a.mask || a.mask[t]);
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     float ds[V] = {};  // of the score, or of the logit (softmax renormalised)
     if (a.dgates) {
@@ -404,55 +445,88 @@ __global__ __launch_bounds__(kRouterThreads) void router_bwd_kernel(RouterArgs a
 #pragma unroll
         for (int c = 0; c < C; ++c) w[c] = id[c] < 0 ? 0.0f : dg[c];
       }
+      // every place's w to its expert's register: through LDS, or, where an
+      // id comes twice in a token (the sum's order has to be the same every
+      // time) or places take several registers, one place after another
+      bool twice = C > 1 || L > 16;
+      if constexpr (C == 1 && L == 16) {
+        const int mine = id[0] >= 0 ? id[0] : -1 - lane;  // no two empty places alike
+        twice |= mine == rotated<0x121>(mine) || mine == rotated<0x122>(mine) || mine == rotated<0x123>(mine) ||
+                 mine == rotated<0x124>(mine) || mine == rotated<0x125>(mine) || mine == rotated<0x126>(mine) ||
+                 mine == rotated<0x127>(mine) || mine == rotated<0x128>(mine);
+      }
+      if (C > 1 || L > 16 || __any(twice)) {
 #pragma unroll
-      for (int c = 0; c < C; ++c) {
+        for (int c = 0; c < C; ++c) {
 #pragma unroll 1
-        for (int k = 0; k < L && c * L + k < a.K; ++k) {
-          const int ik = __shfl(id[c], k, L);
-          const float wk = __shfl(w[c], k, L);
+          for (int k = 0; k < L && c * L + k < a.K; ++k) {
+            const int ik = __shfl(id[c], k, L);
+            const float wk = __shfl(w[c], k, L);
 #pragma unroll
-          for (int j = 0; j < V; ++j) ds[j] += expert_of<L>(lane, j) == ik ? wk : 0.0f;
+            for (int j = 0; j < V; ++j) ds[j] += expert_of<L>(lane, j) == ik ? wk : 0.0f;
+          }
         }
+      } else {
+        f32x4_a* mine = sh_w[C == 1 && L == 16 ? wave : 0][sub];
+#pragma unroll
+        for (int j = 0; j < V / 4; ++j) mine[L * j + lane] = f32x4_a{0.0f, 0.0f, 0.0f, 0.0f};
+        wave_fence();
+        if (id[0] >= 0) ((float*)mine)[id[0]] = w[0];
+        wave_fence();
+#pragma unroll
+        for (int j = 0; j < V / 4; ++j) {
+          const f32x4_a x4 = mine[L * j + lane];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) ds[4 * j + i] = x4[i];
+        }
+        wave_fence();
       }
     }
     float pc = 0.0f;  // sum of pi times its gradient
     if (balance || through_pi) {
 #pragma unroll
-      for (int j = 0; j < V; ++j) pc += s[j] * (push[j] + (through_pi ? ds[j] : 0.0f));
+      for (int j = 0; j < V; ++j) pc += s[j] * push[j];
+      if (through_pi) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) pc += s[j] * ds[j];
+      }
       pc = lanes_sum<L>(pc) * inv;
     }
+    if (through_pi) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const float pi = s[j] * inv;
-      float d;
-      if (through_pi) {
-        d = pi * (push[j] + ds[j] - pc);
-      } else if (sig) {
-        d = (1.0f - s[j]) * (s[j] * ds[j] + (balance ? pi * (push[j] - pc) : 0.0f));
-      } else {
-        d = ds[j] + (balance ? pi * (push[j] - pc) : 0.0f);
-      }
-      ds[j] = alive ? d : 0.0f;
+      for (int j = 0; j < V; ++j) ds[j] = s[j] * inv * (push[j] + ds[j] - pc);
+    } else if (sig) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) ds[j] = (1.0f - s[j]) * s[j] * (ds[j] + inv * (push[j] - pc));
+    } else if (balance) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) ds[j] += s[j] * inv * (push[j] - pc);
+    }
+    if (!alive) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) ds[j] = 0.0f;
     }
     if (!in) continue;
     char* row = (char*)a.dlogits + (size_t)t * a.ld_out * (BF16 ? 2 : 4);
+    auto four = [&](int j, int e) {
+      if constexpr (BF16)
+        *(u32x2*)(row + 2 * e) = u32x2{pack_bf2(ds[j], ds[j + 1]), pack_bf2(ds[j + 2], ds[j + 3])};
+      else
+        *(f32x4*)(row + 4 * e) = f32x4{ds[j], ds[j + 1], ds[j + 2], ds[j + 3]};
+    };
+    if (a.E % 4 == 0) {
 #pragma unroll
-    for (int j = 0; j < V; j += 4) {
-      const int e = expert_of<L>(lane, j);
-      if (e + 4 <= a.E) {
+      for (int j = 0; j < V; j += 4)
+        if (expert_of<L>(lane, j) < a.E) four(j, expert_of<L>(lane, j));
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const int e = expert_of<L>(lane, j);
+        if (e >= a.E) continue;
         if constexpr (BF16)
-          *(u32x2*)(row + 2 * e) = u32x2{pack_bf2(ds[j], ds[j + 1]), pack_bf2(ds[j + 2], ds[j + 3])};
+          ((uint16_t*)row)[e] = (uint16_t)pack_bf2(ds[j], 0.0f);
         else
-          *(f32x4*)(row + 4 * e) = f32x4{ds[j], ds[j + 1], ds[j + 2], ds[j + 3]};
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (e + i >= a.E) break;
-          if constexpr (BF16)
-            ((uint16_t*)row)[e + i] = (uint16_t)pack_bf2(ds[j + i], 0.0f);
-          else
-            ((float*)row)[e + i] = ds[j + i];
-        }
+          ((float*)row)[e] = ds[j];
       }
     }
   }
