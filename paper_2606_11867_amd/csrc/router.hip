@@ -13,6 +13,7 @@ constexpr int kRouterThreads = 512;
 constexpr int kRouterWaves = kRouterThreads / 64;
 constexpr int kRouterBlocks = 512;  // most workgroups that leave partial statistics
 constexpr int kStatColumns = 16;    // experts that a workgroup of the statistics kernel sums
+constexpr int kStatThreads = 1024;
 constexpr float kNegInf = -INFINITY;
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -81,6 +82,18 @@ __device__ __forceinline__ float lanes_max(float v) {
 template <int L>
 __device__ __forceinline__ float lanes_sum(float v) {
   return reduce<L>(v, [](float a, float b) { return a + b; });
+}
+template <int L>
+__device__ __forceinline__ int lanes_sum_int(int v) {
+  v += rotated<0x128>(v);
+  v += rotated<0x124>(v);
+  v += rotated<0x122>(v);
+  v += rotated<0x121>(v);
+  if constexpr (L == 64) {
+    v += __shfl_xor(v, 16, 64);
+    v += __shfl_xor(v, 32, 64);
+  }
+  return v;
 }
 template <int L>
 __device__ __forceinline__ int lanes_min(int v) {
@@ -324,45 +337,60 @@ __global__ __launch_bounds__(kRouterThreads, 4) void router_fwd_kernel(RouterArg
 }
 
 // The workgroups' partial statistics summed in a fixed order: 16 experts to a
-// workgroup, 16 threads to an expert. The last workgroup to finish adds up the
-// balance loss.
-__global__ __launch_bounds__(256) void router_stats_kernel(int E, int blocks, const float* prob_part,
-                                                           const int32_t* count_part, const int32_t* token_part,
-                                                           int32_t* counts, int32_t* n_tokens, float* prob_mean,
-                                                           float* loss, uint32_t* ticket) {
-  __shared__ float sh_p[256];
-  __shared__ int sh_c[256], sh_n[4];
+// workgroup, 64 threads to an expert, so that all loads of 512 workgroups'
+// parts are under way at once. The last workgroup to finish adds up the
+// balance loss; the results that it reads have reached memory before their
+// workgroup took its ticket, past the XCDs' caches.
+__global__ __launch_bounds__(kStatThreads) void router_stats_kernel(int E, int blocks, const float* prob_part,
+                                                                    const int32_t* count_part,
+                                                                    const int32_t* token_part, int32_t* counts,
+                                                                    int32_t* n_tokens, float* prob_mean, float* loss,
+                                                                    uint32_t* ticket) {
+  constexpr int kRows = kStatThreads / kStatColumns, kWaves = kStatThreads / 64;
+  __shared__ float sh_p[kWaves][kStatColumns];
+  __shared__ int sh_c[kWaves][kStatColumns], sh_n[kWaves];
   __shared__ bool sh_last;
-  const int tid = threadIdx.x, e = blockIdx.x * kStatColumns + tid % kStatColumns, row = tid / kStatColumns;
+  const int tid = threadIdx.x, wave = tid >> 6;
+  const int column = tid % kStatColumns, e = blockIdx.x * kStatColumns + column;
   int c = 0, n = 0;
   float p = 0.0f;
-  for (int b = tid; b < blocks; b += 256) n += token_part[b];
+  for (int b = tid; b < blocks; b += kStatThreads) n += token_part[b];
   if (e < E) {
 #pragma unroll 8
-    for (int b = row; b < blocks; b += 256 / kStatColumns) {
+    for (int b = tid / kStatColumns; b < blocks; b += kRows) {
       p += prob_part[(size_t)b * E + e];
       c += count_part[(size_t)b * E + e];
     }
   }
 #pragma unroll
+  for (int o = kStatColumns; o < 64; o <<= 1) {
+    p += __shfl_xor(p, o, 64);
+    c += __shfl_xor(c, o, 64);
+  }
+#pragma unroll
   for (int o = 32; o >= 1; o >>= 1) n += __shfl_xor(n, o, 64);
-  if (lane_id() == 0) sh_n[tid >> 6] = n;
-  sh_p[tid] = p, sh_c[tid] = c;
+  if (lane_id() == 0) sh_n[wave] = n;
+  if (lane_id() < kStatColumns) sh_p[wave][column] = p, sh_c[wave][column] = c;
   __syncthreads();
-  n = sh_n[0] + sh_n[1] + sh_n[2] + sh_n[3];
+  n = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) n += sh_n[w];
   if (tid < kStatColumns && e < E) {
-    for (int r = 1; r < 256 / kStatColumns; ++r) p += sh_p[r * kStatColumns + tid], c += sh_c[r * kStatColumns + tid];
+    p = 0.0f, c = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) p += sh_p[w][tid], c += sh_c[w][tid];
     __hip_atomic_store(counts + e, c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __hip_atomic_store(prob_mean + e, p / (float)max(n, 1), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): they have reached memory
   }
-  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): these results have reached memory
   __syncthreads();
   if (tid == 0) sh_last = atomicAdd(ticket, 1u) == gridDim.x - 1;
   __syncthreads();
-  if (!sh_last) return;
+  if (!sh_last || wave != 0) return;
   float l = 0.0f;
   int all = 0;
-  for (int i = tid; i < E; i += 256) {
+#pragma unroll 4
+  for (int i = tid; i < E; i += 64) {
     const int ci = __hip_atomic_load(counts + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     l += (float)ci * __hip_atomic_load(prob_mean + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     all += ci;
@@ -370,11 +398,7 @@ __global__ __launch_bounds__(256) void router_stats_kernel(int E, int blocks, co
   l = wave_sum(l);
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) all += __shfl_xor(all, o, 64);
-  if (lane_id() == 0) sh_p[tid >> 6] = l, sh_c[tid >> 6] = all;
-  __syncthreads();
   if (tid == 0) {
-    l = sh_p[0] + sh_p[1] + sh_p[2] + sh_p[3];
-    all = sh_c[0] + sh_c[1] + sh_c[2] + sh_c[3];
     *n_tokens = n;
     *loss = (float)E * (l / (float)max(all, 1));
     __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -386,25 +410,25 @@ __global__ __launch_bounds__(kRouterThreads) void router_bwd_kernel(RouterArgs a
   constexpr int kTokens = 64 / L;
   typedef float f32x4 __attribute__((ext_vector_type(4), aligned(4)));
   typedef uint32_t u32x2 __attribute__((ext_vector_type(2), aligned(2)));
-  __shared__ int sh_total;
   __shared__ f32x4_a sh_w[C == 1 && L == 16 ? kRouterWaves : 1][kTokens][L * V / 4];  // a token's gradients by expert
   const int wave = threadIdx.x >> 6, lane = threadIdx.x % L, sub = lane_id() / L;
   const bool sig = a.sigmoid != 0, renorm = a.renorm != 0, balance = a.coef != 0.0f;
   const bool through_pi = !sig && !renorm;  // the gates' gradient goes through the whole softmax
   float push[V] = {};  // balance gradient of pi
   if (balance) {
-    if (threadIdx.x == 0) sh_total = 0;
-    __syncthreads();
-    int mine = 0;
-    for (int e = threadIdx.x; e < a.E; e += kRouterThreads) mine += a.counts[e];
-    atomicAdd(&sh_total, mine);
-    __syncthreads();
-    const float k = a.coef * (float)a.E / (float)max(*a.n_tokens, 1) / (float)max(sh_total, 1);
+    // a token's lanes hold all the counts
+    int count[V], total = 0;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
       const int e = expert_of<L>(lane, j);
-      if (e < a.E) push[j] = k * (float)a.counts[e];
+      count[j] = e < a.E ? a.counts[e] : 0;
+      total += count[j];
     }
+    const int n = *a.n_tokens;
+    total = lanes_sum_int<L>(total);
+    const float k = a.coef * (float)a.E / (float)max(n, 1) / (float)max(total, 1);
+#pragma unroll
+    for (int j = 0; j < V; ++j) push[j] = k * (float)count[j];
   }
   for (int64_t t0 = ((int64_t)blockIdx.x * kRouterWaves + wave) * kTokens; t0 < a.T;
        t0 += (int64_t)gridDim.x * kRouterWaves * kTokens) {
@@ -625,7 +649,7 @@ int foremoe_router_fwd(const void* logits, foremoe_dtype dtype, int64_t ld, int6
     else
       hipLaunchKernelGGL((router_fwd_kernel<false, L, V, C>), dim3(grid), dim3(kRouterThreads), smem, st, a);
     if (n_stats)
-      hipLaunchKernelGGL(router_stats_kernel, dim3((E + kStatColumns - 1) / kStatColumns), dim3(256), 0, st, E,
+      hipLaunchKernelGGL(router_stats_kernel, dim3((E + kStatColumns - 1) / kStatColumns), dim3(kStatThreads), 0, st, E,
                          (int)grid, a.prob_part, a.count_part, a.token_part, counts, n_tokens, prob_mean, balance_loss,
                          (uint32_t*)ws);
   });
