@@ -63,16 +63,24 @@ template <int CTRL>
 __device__ __forceinline__ int rotated(int v) {
   return __builtin_amdgcn_update_dpp(v, v, CTRL, 0xf, 0xf, false);
 }
+// v of the other 16 lanes of a pair of rows, or of the other half, combined.
+template <class Op>
+__device__ __forceinline__ int across_rows(int v, Op&& op) {
+  const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = op((int)a[0], (int)a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return op((int)b[0], (int)b[1]);
+}
 template <int L, class Op>
 __device__ __forceinline__ float reduce(float v, Op&& op) {
   v = op(v, __int_as_float(rotated<0x128>(__float_as_int(v))));  // row_ror:8, 4, 2, 1
   v = op(v, __int_as_float(rotated<0x124>(__float_as_int(v))));
   v = op(v, __int_as_float(rotated<0x122>(__float_as_int(v))));
   v = op(v, __int_as_float(rotated<0x121>(__float_as_int(v))));
-  if constexpr (L == 64) {
-    v = op(v, __shfl_xor(v, 16, 64));
-    v = op(v, __shfl_xor(v, 32, 64));
-  }
+  if constexpr (L == 64)
+    v = __int_as_float(across_rows(__float_as_int(v), [&](int a, int b) {
+      return __float_as_int(op(__int_as_float(a), __int_as_float(b)));
+    }));
   return v;
 }
 template <int L>
@@ -89,10 +97,7 @@ __device__ __forceinline__ int lanes_sum_int(int v) {
   v += rotated<0x124>(v);
   v += rotated<0x122>(v);
   v += rotated<0x121>(v);
-  if constexpr (L == 64) {
-    v += __shfl_xor(v, 16, 64);
-    v += __shfl_xor(v, 32, 64);
-  }
+  if constexpr (L == 64) v = across_rows(v, [](int a, int b) { return a + b; });
   return v;
 }
 template <int L>
@@ -101,10 +106,7 @@ __device__ __forceinline__ int lanes_min(int v) {
   v = min(v, rotated<0x124>(v));
   v = min(v, rotated<0x122>(v));
   v = min(v, rotated<0x121>(v));
-  if constexpr (L == 64) {
-    v = min(v, __shfl_xor(v, 16, 64));
-    v = min(v, __shfl_xor(v, 32, 64));
-  }
+  if constexpr (L == 64) v = across_rows(v, [](int a, int b) { return min(a, b); });
   return v;
 }
 
