@@ -101,6 +101,16 @@ __device__ __forceinline__ int lanes_sum_int(int v) {
   return v;
 }
 template <int L>
+__device__ __forceinline__ uint32_t lanes_max_uint(uint32_t v) {
+  v = max(v, (uint32_t)rotated<0x128>((int)v));
+  v = max(v, (uint32_t)rotated<0x124>((int)v));
+  v = max(v, (uint32_t)rotated<0x122>((int)v));
+  v = max(v, (uint32_t)rotated<0x121>((int)v));
+  if constexpr (L == 64)
+    v = (uint32_t)across_rows((int)v, [](int a, int b) { return (int)max((uint32_t)a, (uint32_t)b); });
+  return v;
+}
+template <int L>
 __device__ __forceinline__ int lanes_min(int v) {
   v = min(v, rotated<0x128>(v));
   v = min(v, rotated<0x124>(v));
@@ -222,7 +232,67 @@ __device__ __forceinline__ float place_scores(const float (&x)[C], const int (&i
   return sig ? 1.0f : sum;
 }
 
-template <bool BF16, int L, int V, int C>
+// The K largest keys in descending order, ties to the lower id; place k goes
+// to lane k % L. Every pick compares and takes out one key by one.
+template <int L, int V, int C>
+__device__ __forceinline__ void pick_keys(float (&key)[V], int K, int lane, int (&id)[C]) {
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+#pragma unroll 1
+    for (int k = 0; k < L && c * L + k < K; ++k) {
+      float best = key[0];
+#pragma unroll
+      for (int j = 1; j < V; ++j) best = fmaxf(best, key[j]);
+      best = lanes_max<L>(best);
+      int at = INT_MAX;
+#pragma unroll
+      for (int j = V - 1; j >= 0; --j) at = key[j] == best ? expert_of<L>(lane, j) : at;
+      at = lanes_min<L>(at);
+#pragma unroll
+      for (int j = 0; j < V; ++j) key[j] = expert_of<L>(lane, j) == at ? kNegInf : key[j];
+      if (lane == k) id[c] = best > kNegInf ? at : -1;
+    }
+  }
+}
+
+// The same for keys of 16 bits, each in one 32-bit integer with its expert:
+// the key's bits in the order of the floats, the expert's complement below; 0
+// for a key that is never picked. All of a token's integers differ, so the
+// next one below the last pick is last + max(p - last) modulo 2^32 (what is
+// not below wraps round to less): a subtraction and half a maximum for each,
+// and nothing to take out. (32768 x 256: 19.7 -> 15.3 us. With the leading 24
+// bits of fp32 keys, and pick_keys where those do not decide, the kernel's
+// registers spilled: 8.1 -> 12.8 us for a replay.)
+template <int L, int V, int C>
+__device__ __forceinline__ void pick_packed(const float (&key)[V], int K, int lane, int (&id)[C]) {
+  constexpr uint32_t kIds = L == 16 ? 0xff : 0x3ff;
+  static_assert(L * V <= kIds + 1);
+  uint32_t p[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const int32_t b = __float_as_int(key[j] + 0.0f);  // 0.0 and -0.0 tie
+    const uint32_t o = (uint32_t)b ^ ((uint32_t)(b >> 31) | 0x80000000u);
+    p[j] = key[j] > kNegInf ? (o & ~kIds) | (kIds - expert_of<L>(lane, j)) : 0;
+  }
+  uint32_t last = 0;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+#pragma unroll 1
+    for (int k = 0; k < L && c * L + k < K; ++k) {
+      uint32_t most = 0;
+#pragma unroll
+      for (int j = 0; j < V; ++j) most = max(most, p[j] - last);
+      const uint32_t best = last + lanes_max_uint<L>(most);
+      if (lane == k) id[c] = best ? (int)(kIds - (best & kIds)) : -1;
+      last = best ? best : 1;  // from 1 the next is 0 again
+    }
+  }
+}
+
+// How a kernel finds its ids; each its own kernel, for the registers.
+enum Pick { kReplay, kLogits, kBiased };
+
+template <bool BF16, int PICK, int L, int V, int C>
 __global__ __launch_bounds__(kRouterThreads, 4) void router_fwd_kernel(RouterArgs a) {
   constexpr int kTokens = 64 / L;  // of a wavefront
   extern __shared__ char smem[];
@@ -232,7 +302,7 @@ __global__ __launch_bounds__(kRouterThreads, 4) void router_fwd_kernel(RouterArg
   const int wave = threadIdx.x >> 6, lane = threadIdx.x % L, sub = lane_id() / L;
   const bool stats = a.prob_part != nullptr, sig = a.sigmoid != 0, renorm = a.renorm != 0;
   // replayed gates that need the picked logits alone
-  const bool rows = stats || !a.ids_in || (!sig && !renorm);
+  const bool rows = stats || PICK != kReplay || (!sig && !renorm);
   if (stats) {
     for (int e = threadIdx.x; e < a.E; e += kRouterThreads) sh_count[e] = 0;
     if (threadIdx.x == 0) *sh_tokens = 0;
@@ -240,7 +310,7 @@ __global__ __launch_bounds__(kRouterThreads, 4) void router_fwd_kernel(RouterArg
   }
   float acc[V] = {}, bias[V] = {};
   int tokens = 0;
-  if (a.bias) {
+  if constexpr (PICK == kBiased) {
 #pragma unroll
     for (int j = 0; j < V; ++j)
       if (expert_of<L>(lane, j) < a.E) bias[j] = a.bias[expert_of<L>(lane, j)];
@@ -253,19 +323,25 @@ __global__ __launch_bounds__(kRouterThreads, 4) void router_fwd_kernel(RouterArg
     bool alive = in && (!a.mask || a.mask[t]);
     float v[V], s[V], top = 0.0f, sum = 1.0f;
     int id[C];
-    if (a.ids_in) {
+    if constexpr (PICK == kReplay) {
 #pragma unroll
       for (int c = 0; c < C; ++c) id[c] = lane + c * L < a.K ? a.ids_in[t * a.K + lane + c * L] : -1;
     }
     if (rows) {
       load_row<BF16, L, V>(a, t, lane, v);
-      alive &= row_scores<L, V>(v, sig, a.bias != nullptr, s, top, sum);
+      alive &= row_scores<L, V>(v, sig, PICK == kBiased, s, top, sum);
     }
-    if (!a.ids_in) {
+    if (stats && alive) {
+      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+      for (int j = 0; j < V; ++j) acc[j] += s[j] * inv;
+      ++tokens;
+    }
+    if constexpr (PICK != kReplay) {
 #pragma unroll
       for (int c = 0; c < C; ++c) id[c] = -1;
       float key[V];
-      if (a.bias) {
+      if constexpr (PICK == kBiased) {
 #pragma unroll
         for (int j = 0; j < V; ++j) {
           key[j] = s[j] + bias[j];
@@ -275,23 +351,10 @@ __global__ __launch_bounds__(kRouterThreads, 4) void router_fwd_kernel(RouterArg
 #pragma unroll
         for (int j = 0; j < V; ++j) key[j] = v[j] > kNegInf ? v[j] : kNegInf;
       }
-#pragma unroll
-      for (int c = 0; c < C; ++c) {
-#pragma unroll 1
-        for (int k = 0; k < L && c * L + k < a.K; ++k) {
-          float best = key[0];
-#pragma unroll
-          for (int j = 1; j < V; ++j) best = fmaxf(best, key[j]);
-          best = lanes_max<L>(best);
-          int at = INT_MAX;
-#pragma unroll
-          for (int j = V - 1; j >= 0; --j) at = key[j] == best ? expert_of<L>(lane, j) : at;
-          at = lanes_min<L>(at);
-#pragma unroll
-          for (int j = 0; j < V; ++j) key[j] = expert_of<L>(lane, j) == at ? kNegInf : key[j];
-          if (lane == k) id[c] = best > kNegInf ? at : -1;
-        }
-      }
+      if constexpr (BF16 && PICK == kLogits)
+        pick_packed<L, V, C>(key, a.K, lane, id);
+      else
+        pick_keys<L, V, C>(key, a.K, lane, id);
     }
     float x[C], q[C];
 #pragma unroll
@@ -308,12 +371,6 @@ __global__ __launch_bounds__(kRouterThreads, 4) void router_fwd_kernel(RouterArg
       a.ids[t * a.K + k] = id[c];
       a.gates[t * a.K + k] = id[c] < 0 || denom == 0.0f ? 0.0f : a.scale * (q[c] / denom);
       if (stats && id[c] >= 0) atomicAdd(&sh_count[id[c]], 1);
-    }
-    if (stats && alive) {
-      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-#pragma unroll
-      for (int j = 0; j < V; ++j) acc[j] += s[j] * inv;
-      ++tokens;
     }
   }
   if (!stats) return;
@@ -646,10 +703,15 @@ int foremoe_router_fwd(const void* logits, foremoe_dtype dtype, int64_t ld, int6
   by_shape(E, K, [&](auto s) {
     constexpr int L = decltype(s)::L, V = decltype(s)::V, C = decltype(s)::C;
     const unsigned grid = router_grid(T, L, n_stats ? kRouterBlocks : 1 << 16);
+    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(kRouterThreads), smem, st, a); };
     if (dtype == FOREMOE_BF16)
-      hipLaunchKernelGGL((router_fwd_kernel<true, L, V, C>), dim3(grid), dim3(kRouterThreads), smem, st, a);
+      ids_in ? launch(router_fwd_kernel<true, kReplay, L, V, C>)
+      : bias ? launch(router_fwd_kernel<true, kBiased, L, V, C>)
+             : launch(router_fwd_kernel<true, kLogits, L, V, C>);
     else
-      hipLaunchKernelGGL((router_fwd_kernel<false, L, V, C>), dim3(grid), dim3(kRouterThreads), smem, st, a);
+      ids_in ? launch(router_fwd_kernel<false, kReplay, L, V, C>)
+      : bias ? launch(router_fwd_kernel<false, kBiased, L, V, C>)
+             : launch(router_fwd_kernel<false, kLogits, L, V, C>);
     if (n_stats)
       hipLaunchKernelGGL(router_stats_kernel, dim3((E + kStatColumns - 1) / kStatColumns), dim3(kStatThreads), 0, st, E,
                          (int)grid, a.prob_part, a.count_part, a.token_part, counts, n_tokens, prob_mean, balance_loss,
