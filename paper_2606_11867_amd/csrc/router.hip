@@ -134,14 +134,43 @@ __device__ __forceinline__ float fast_exp(float d) { return __builtin_amdgcn_exp
 __device__ __forceinline__ float fast_sigmoid(float v) {
   return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v * -kLog2e));
 }
-// The same rounded operation by operation, where a score plus a bias decides:
-// the score of the definition's four fp32 operations.
-// The quotient by a residual correction, which is correctly rounded up to
-// 2^120 (P. Markstein's method; as the division for every such number).
-__device__ __forceinline__ float sigmoid(float v) {
-  const float d = 1.0f + expf(-v), r = __builtin_amdgcn_rcpf(d);
-  const float q = fmaf(fmaf(-d, r, 1.0f), r, r);
-  return d <= 0x1p120f ? q : 1.0f / d;
+// The sigmoid of the definition's four fp32 operations, each rounded, where a
+// score plus a bias decides. The quotient is the hardware's reciprocal
+// corrected by its residual, correctly rounded up to 2^120 (P. Markstein's
+// method; equal to the division for every such number).
+template <int V>
+__device__ __forceinline__ void exact_sigmoids(const float (&v)[V], float (&s)[V]) {
+  bool far = false;
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const float d = 1.0f + expf(-v[j]), r = __builtin_amdgcn_rcpf(d);
+    s[j] = d > 0x1p120f ? 0.0f : fmaf(fmaf(-d, r, 1.0f), r, r);
+    far |= d > 0x1p120f && d < INFINITY;
+  }
+  if (__any(far)) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) s[j] = 1.0f / (1.0f + expf(-v[j]));
+  }
+}
+
+// Whole numbers or floats [E] of a lane's experts, 0 beyond the last.
+template <int L, int V, class T>
+__device__ __forceinline__ void load_experts(const T* p, int E, int lane, T (&out)[V]) {
+  typedef T four __attribute__((ext_vector_type(4), aligned(4)));
+#pragma unroll
+  for (int j = 0; j < V; j += 4) {
+    const int e = expert_of<L>(lane, j);
+    four x = {0, 0, 0, 0};
+    if (e + 4 <= E) {
+      x = *(const four*)(p + e);
+    } else if (E % 4 != 0) {
+#pragma unroll
+      for (int i = 0; i < 3; ++i)
+        if (e + i < E) x[i] = p[e + i];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[j + i] = x[i];
+  }
 }
 
 // A token's row of logits, -inf beyond the last expert.
@@ -189,8 +218,7 @@ __device__ __forceinline__ bool row_scores(const float (&v)[V], bool sig, bool e
   for (int j = 0; j < V; ++j) some |= v[j] != kNegInf;
   top = 0.0f;
   if (exact) {
-#pragma unroll
-    for (int j = 0; j < V; ++j) s[j] = sigmoid(v[j]);
+    exact_sigmoids<V>(v, s);
   } else if (sig) {
 #pragma unroll
     for (int j = 0; j < V; ++j) s[j] = fast_sigmoid(v[j]);
@@ -310,11 +338,7 @@ __global__ __launch_bounds__(kRouterThreads, 4) void router_fwd_kernel(RouterArg
   }
   float acc[V] = {}, bias[V] = {};
   int tokens = 0;
-  if constexpr (PICK == kBiased) {
-#pragma unroll
-    for (int j = 0; j < V; ++j)
-      if (expert_of<L>(lane, j) < a.E) bias[j] = a.bias[expert_of<L>(lane, j)];
-  }
+  if constexpr (PICK == kBiased) load_experts<L, V>(a.bias, a.E, lane, bias);
   // every lane of a wavefront stays in the loop while one of its tokens is left
   for (int64_t t0 = ((int64_t)blockIdx.x * kRouterWaves + wave) * kTokens; t0 < a.T;
        t0 += (int64_t)gridDim.x * kRouterWaves * kTokens) {
@@ -477,12 +501,9 @@ __global__ __launch_bounds__(kRouterThreads) void router_bwd_kernel(RouterArgs a
   if (balance) {
     // a token's lanes hold all the counts
     int count[V], total = 0;
+    load_experts<L, V>(a.counts, a.E, lane, count);
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const int e = expert_of<L>(lane, j);
-      count[j] = e < a.E ? a.counts[e] : 0;
-      total += count[j];
-    }
+    for (int j = 0; j < V; ++j) total += count[j];
     const int n = *a.n_tokens;
     total = lanes_sum_int<L>(total);
     const float k = a.coef * (float)a.E / (float)max(n, 1) / (float)max(total, 1);
