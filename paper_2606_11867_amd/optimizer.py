@@ -85,16 +85,23 @@ class AdamW:
         """The call's records, checked."""
         dev, pd, gd = self.device, self.params[0].dtype, self.grads[0].dtype
         kinds = (F32, F32) if self.state_bits == 32 else (torch.uint8, torch.uint8, F32, F32)
+        none = [None] * (4 - len(kinds))
+
+        def at(t, n, dtype, name, i):
+            if t.dtype == dtype and t.numel() == n and t.device == dev and t.is_cuda and t.is_contiguous():
+                return t.data_ptr()
+            return _vec(t, n, dtype, f"{name}[{i}]", dev)  # says what is wrong
+
         for i, (p, g, st) in enumerate(zip(self.params, self.grads, self.states)):
             n = p.numel()
             if len(st) != len(kinds):
                 raise ValueError(f"states[{i}]: {len(kinds)} tensors expected")
             blocks = -(-n // _lib.ADAMW_BLOCK)
-            a = [_vec(t, n if j < 2 else blocks, k, f"states[{i}][{j}]", dev) for j, (t, k) in enumerate(zip(st, kinds))]
             self._records[i] = _lib.AdamWTensor(
-                _vec(p, n, pd, f"params[{i}]", dev), _vec(g, n, gd, f"grads[{i}]", dev),
-                _vec(self.masters[i], n, F32, f"masters[{i}]", dev) if self.masters is not None else None,
-                *a, *([None] * (4 - len(a))), n, self.weight_decay[i])
+                at(p, n, pd, "params", i), at(g, n, gd, "grads", i),
+                at(self.masters[i], n, F32, "masters", i) if self.masters is not None else None,
+                *[at(t, n if j < 2 else blocks, k, "states", i) for j, (t, k) in enumerate(zip(st, kinds))], *none,
+                n, self.weight_decay[i])
         self._tensors = self.params + self.grads
         self._at = list(map(torch.Tensor.data_ptr, self._tensors))
 
