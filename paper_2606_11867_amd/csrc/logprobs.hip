@@ -8,8 +8,8 @@
 // logits is read once: HBM-bound where rows fill the GPU, about 9 vector
 // instruction slots an element (4 of them the exponential) against 13 that
 // fit in the time of 2 bytes. Measured on MI355X:
-//   8192 x 131072 bf16, a fifth ignored   291 us, 5.9 TB/s (dense rows 365, 5.9)
-//   2045 x 32003 fp32                      51 us, 5.2 TB/s
+//   8192 x 131072 bf16, a fifth ignored   267-270 us, 6.4 TB/s
+//   2045 x 32003 fp32                     51 us, 5.2 TB/s
 //   8192 x 131072 bf16, 20 alternatives   415 us, 5.2 TB/s
 //   1 x 131072 bf16: 6.0 us, with 20 alternatives 13.8 us: latency (pieces, their
 //   join and two rankings)
@@ -18,7 +18,8 @@
 // their order, so that results do not depend on the run.
 //
 // Backward: every gradient from its logit and four numbers of the row, one
-// read and one write: HBM-bound, 4096 x 131072 bf16 323 us, 6.0 TB/s.
+// read and one write: HBM-bound, forward and backward of 4096 x 131072 bf16
+// 467 us (2.8 GB, 6.0 TB/s).
 #include <limits.h>
 #include <math.h>
 
@@ -42,6 +43,19 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLowest = -3.402823466e38f;
 constexpr int kTile = 4;         // vectors that a lane holds at a time
 constexpr int kBwdTile = 4;      // the same in the backward
+// A gradient of this many bytes does not stay in the Infinity Cache (256 MB)
+// until it is used, and is better kept out of it, and its logits' last read
+// with it: forward and backward of 2045 x 32003 fp32 152 -> 123 us, of 4096 x
+// 131072 bf16 518 -> 468. A smaller one is used from there: 512 x 32000 bf16 (33
+// MB) with a product behind it 136 -> 153 us with the hint, 300 x 131072 (79
+// MB) 308 -> 307.
+constexpr size_t kStreamBytes = (size_t)128 << 20;
+// The forward keeps logits of this many bytes out too, where no top places are
+// wanted (their candidates are read again): 8192 x 131072 bf16 302 -> 270 us,
+// with the backward 937 -> 926. Of smaller ones a backward that follows finds
+// part there: forward and backward of 4096 x 131072 (1 GB) 467 us, 474 with
+// the hint, of 2045 x 32003 fp32 123 and 136.
+constexpr size_t kStreamLogits = (size_t)3 << 29;
 constexpr int kBuf = 512;        // candidates for the top places that a wavefront keeps
 constexpr int kMaxPieces = 64;   // of one row
 constexpr int kFewRows = 256;    // fewer rows than this are cut into pieces
@@ -83,9 +97,11 @@ __device__ __forceinline__ float load_lp(const void* p, int64_t i) {
   return ((const float*)p)[i];
 }
 
-template <bool BF16>
+template <bool STREAM>
 __device__ __forceinline__ u32x4 load_vec(const void* row, uint32_t vector) {
-  return *(const u32x4_any*)((const char*)row + (size_t)vector * 16);
+  const u32x4_any* p = (const u32x4_any*)((const char*)row + (size_t)vector * 16);
+  if constexpr (STREAM) return __builtin_nontemporal_load(p);
+  return *p;
 }
 
 template <bool BF16>
@@ -305,8 +321,9 @@ __device__ __forceinline__ int rank_block(TopList& top, const uint64_t* buf, int
 }
 
 // A workgroup of WAVES wavefronts takes a piece of a row; where a row has
-// several, the last one to finish joins them.
-template <bool BF16, bool TOP, int WAVES, int TILE>
+// several, the last one to finish joins them. STREAM: its loads carry the
+// nontemporal hint.
+template <bool BF16, bool TOP, int WAVES, int TILE, bool STREAM>
 __global__ __launch_bounds__(64 * WAVES) void logprobs_kernel(LogprobArgs a) {
   constexpr int kThreads = 64 * WAVES, VEC = kVec<BF16>;
   __shared__ uint64_t buf[TOP ? WAVES * kBuf : 1];
@@ -374,7 +391,7 @@ __global__ __launch_bounds__(64 * WAVES) void logprobs_kernel(LogprobArgs a) {
     const uint32_t whole = end - (end - beg) % (TILE * kThreads);
 #pragma unroll
     for (int u = 0; u < TILE; ++u)
-      if (at < whole) next[u] = load_vec<BF16>(x0, at + u * kThreads + tid);
+      if (at < whole) next[u] = load_vec<STREAM>(x0, at + u * kThreads + tid);
 #pragma unroll 1
     for (; at < whole; at += TILE * kThreads) {
       float x[TILE * VEC];
@@ -382,7 +399,7 @@ __global__ __launch_bounds__(64 * WAVES) void logprobs_kernel(LogprobArgs a) {
       for (int u = 0; u < TILE; ++u) unpack<BF16>(next[u], x + u * VEC);
       if (at + TILE * kThreads < whole) {
 #pragma unroll
-        for (int u = 0; u < TILE; ++u) next[u] = load_vec<BF16>(x0, at + (TILE + u) * kThreads + tid);
+        for (int u = 0; u < TILE; ++u) next[u] = load_vec<STREAM>(x0, at + (TILE + u) * kThreads + tid);
       }
       add<TILE * VEC>(r, x, a.c);
       if constexpr (TOP) consider(x);
@@ -390,12 +407,12 @@ __global__ __launch_bounds__(64 * WAVES) void logprobs_kernel(LogprobArgs a) {
   }
   // what is left of the piece, at most TILE vectors for a thread
   u32x4 one;
-  if (at + tid < end) one = load_vec<BF16>(x0, at + tid);
+  if (at + tid < end) one = load_vec<STREAM>(x0, at + tid);
 #pragma unroll 1
   for (; at < end; at += kThreads) {
     float x[VEC];
     unpack<BF16>(one, x);
-    if (at + kThreads + tid < end) one = load_vec<BF16>(x0, at + kThreads + tid);
+    if (at + kThreads + tid < end) one = load_vec<STREAM>(x0, at + kThreads + tid);
     if (at + tid < end) {
       add<VEC>(r, x, a.c);
     } else if constexpr (TOP) {
@@ -478,17 +495,22 @@ constexpr size_t kLpWsBytes = kLpTicketBytes + kLpPartBytes + sizeof(uint64_t) *
 
 template <bool BF16, bool TOP>
 void launch_logprobs(LogprobArgs a, int64_t N, int waves, hipStream_t st) {
+  const bool stream_through = !TOP && (size_t)N * a.V * (BF16 ? 2 : 4) >= kStreamLogits;
   // a launch has fewer than 2^32 threads
   constexpr int64_t kRows = 1 << 22;
   for (int64_t r = 0; r < N; r += kRows) {
     a.first = (int32_t)r;
     const dim3 grid((unsigned)((N - r < kRows ? N - r : kRows) * a.pieces));
+    auto launch = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, st, a); };
+    constexpr int kWaves = kLpThreads / 64;
     if (waves == 1)
-      hipLaunchKernelGGL((logprobs_kernel<BF16, TOP, 1, kTile>), grid, dim3(64), 0, st, a);
-    else if (a.piece_vectors <= kLpThreads)
-      hipLaunchKernelGGL((logprobs_kernel<BF16, TOP, kLpThreads / 64, 1>), grid, dim3(kLpThreads), 0, st, a);
+      stream_through ? launch(logprobs_kernel<BF16, TOP, 1, kTile, !TOP>, 64)
+                     : launch(logprobs_kernel<BF16, TOP, 1, kTile, false>, 64);
+    else if (a.piece_vectors <= kLpThreads)  // few rows
+      launch(logprobs_kernel<BF16, TOP, kWaves, 1, false>, kLpThreads);
     else
-      hipLaunchKernelGGL((logprobs_kernel<BF16, TOP, kLpThreads / 64, kTile>), grid, dim3(kLpThreads), 0, st, a);
+      stream_through ? launch(logprobs_kernel<BF16, TOP, kWaves, kTile, !TOP>, kLpThreads)
+                     : launch(logprobs_kernel<BF16, TOP, kWaves, kTile, false>, kLpThreads);
   }
 }
 
@@ -515,7 +537,8 @@ struct RowGrad {
 
 // A workgroup takes kBwdTile vectors per thread of one row; every element is
 // read and then written by one thread, so the gradient may replace the logits.
-template <bool BF16>
+// STREAM: its accesses carry the nontemporal hint.
+template <bool BF16, bool STREAM>
 __global__ __launch_bounds__(kLpThreads) void logprobs_bwd_kernel(LogprobBwdArgs a) {
   constexpr int VEC = kVec<BF16>;
   const int64_t row = blockIdx.y;
@@ -529,7 +552,7 @@ __global__ __launch_bounds__(kLpThreads) void logprobs_bwd_kernel(LogprobBwdArgs
   if (keep) {
 #pragma unroll
     for (int u = 0; u < kBwdTile; ++u)
-      if (at + u * kLpThreads < vectors) held[u] = load_vec<BF16>(x0, at + u * kLpThreads);
+      if (at + u * kLpThreads < vectors) held[u] = load_vec<STREAM>(x0, at + u * kLpThreads);
   }
   RowGrad g;
   // a row of -inf only: every p is 0
@@ -555,7 +578,11 @@ __global__ __launch_bounds__(kLpThreads) void logprobs_bwd_kernel(LogprobBwdArgs
 #pragma unroll
       for (int i = 0; i < 4; ++i) out[i] = BF16 ? pack_bf2(x[2 * i % VEC], x[(2 * i + 1) % VEC]) : __float_as_uint(x[i]);
     }
-    *(u32x4_any*)(d0 + (size_t)v * 16) = out;
+    u32x4_any* to = (u32x4_any*)(d0 + (size_t)v * 16);
+    if constexpr (STREAM)
+      __builtin_nontemporal_store(out, to);
+    else
+      *to = out;
   }
   const uint32_t id = vectors * VEC + tid;  // the row's last elements, less than a vector
   if (blockIdx.x == 0 && id < (uint32_t)a.V) {
@@ -673,10 +700,12 @@ int foremoe_token_logprobs_bwd(const void* logits, foremoe_dtype dtype, int64_t 
                      (char*)dlogits + (size_t)r * ld_out * item, ld_out};
     const int64_t per = kLpThreads * kBwdTile, vectors = V / (dtype == FOREMOE_BF16 ? kVec<true> : kVec<false>);
     const dim3 grid((unsigned)(vectors < 1 ? 1 : (vectors + per - 1) / per), (unsigned)n);
+    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kLpThreads), 0, st, a); };
+    const bool stream_through = (size_t)N * V * item >= kStreamBytes;
     if (dtype == FOREMOE_BF16)
-      hipLaunchKernelGGL(logprobs_bwd_kernel<true>, grid, dim3(kLpThreads), 0, st, a);
+      stream_through ? launch(logprobs_bwd_kernel<true, true>) : launch(logprobs_bwd_kernel<true, false>);
     else
-      hipLaunchKernelGGL(logprobs_bwd_kernel<false>, grid, dim3(kLpThreads), 0, st, a);
+      stream_through ? launch(logprobs_bwd_kernel<false, true>) : launch(logprobs_bwd_kernel<false, false>);
   }
   return check_launch("token_logprobs_bwd");
 }

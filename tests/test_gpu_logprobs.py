@@ -252,3 +252,39 @@ def test_logprobs_in_a_graph(gpu):
         torch.cuda.synchronize()
         for a, b in zip(out, step()):
             assert torch.equal(a, b), i
+
+
+@pytest.mark.parametrize("N,V,dt", [(8200, 100003, "bf16"), (1400, 30001, "f32")], ids=["1.6GB-bf16", "168MB-f32"])
+def test_logprobs_larger_than_the_cache(gpu, N, V, dt):
+    """Logits and gradients that are kept out of the cache: rows from the
+    start, the middle and the end against the oracle, every row's gradient
+    summing to zero."""
+    from paper_2606_11867_amd import api
+    dtype = torch.bfloat16 if dt == "bf16" else torch.float32
+    print(f"\n[case] logprobs N={N} V={V} {dt}", flush=True)
+    gen = torch.Generator(device=gpu).manual_seed(N)
+    x = torch.empty(N, V, dtype=dtype, device=gpu)
+    for a in range(0, N, 1024):
+        x[a:a + 1024] = 3 * torch.randn(min(1024, N - a), V, generator=gen, device=gpu)
+    t = torch.randint(0, V, (N,), generator=gen, device=gpu).to(torch.int32)
+    t[5::7] = -1
+    a, b = torch.randn(N, generator=gen, device=gpu), torch.randn(N, generator=gen, device=gpu)
+    rows = np.array([0, 1, 5, N // 2, N // 2 + 1, N - 2, N - 1])
+    pick = torch.from_numpy(rows).to(gpu)
+    l, tt = x[pick].double().cpu().numpy(), t[pick].cpu().numpy()
+    ref = S.token_logprobs(l, tt)
+    tol = U * (16 * np.abs(l).max() + V / 256 + 128)
+    r = api.token_logprobs(x, t, ws=api.logprobs_workspace(gpu))
+    _close("lse", r.lse[pick], ref["lse"], tol)
+    _close("logp", r.logp[pick], ref["logp"], tol)
+    _close("entropy", r.entropy[pick], ref["entropy"], tol * (2 + ref["entropy"]))
+    an, bn = a[pick].cpu().numpy(), b[pick].cpu().numpy()
+    want = S.token_logprobs_backward(l, tt, an, bn)
+    size = (np.abs(an) + np.abs(bn) * (2 + ref["entropy"]) * 2)[:, None]
+    d = api.token_logprobs_bwd(x, t, r.lse, a, entropy=r.entropy, dentropy=b, out=x)
+    _close("dlogits", d[pick], want, 4 * tol * size)
+    assert torch.all(d[5::7] == 0)
+    # the terms of a row, each within 2^-8 of itself, have magnitudes that sum to less than
+    # 2 |a| + |b| sum p |log p + H| <= 2 |a| + 2 |b| H
+    H = r.entropy.abs()
+    assert torch.all(d.float().sum(1).abs() <= 2.0 ** -8 * (2 * a.abs() + 2 * b.abs() * H) + 1e-3)
