@@ -19,6 +19,10 @@
  *   plus foremoe_combine_bwd / foremoe_permute_bwd for the policy-update
  *   backward (Sec. 7.1: the backward repeats dispatch and combine).
  *
+ *   plus the operators around the layer in a policy-update step:
+ *   foremoe_router_* (ids, gates, balance loss), foremoe_token_logprobs*
+ *   and foremoe_adamw_*.
+ *
  * Conventions (all entry points):
  *  - Every pointer argument is a DEVICE pointer unless stated otherwise; the
  *    caller owns every buffer. The library never allocates device memory and
