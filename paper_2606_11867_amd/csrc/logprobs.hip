@@ -8,10 +8,10 @@
 // logits is read once: HBM-bound where rows fill the GPU, about 9 vector
 // instruction slots an element (4 of them the exponential) against 13 that
 // fit in the time of 2 bytes. Measured on MI355X:
-//   8192 x 131072 bf16, a fifth ignored   267-270 us, 6.4 TB/s
+//   8192 x 131072 bf16, a fifth ignored   258-270 us, 6.4-6.6 TB/s
 //   2045 x 32003 fp32                     51 us, 5.2 TB/s
 //   8192 x 131072 bf16, 20 alternatives   415 us, 5.2 TB/s
-//   1 x 131072 bf16: 6.0 us, with 20 alternatives 13.8 us: latency (pieces, their
+//   1 x 131072 bf16: 6.1 us, with 20 alternatives 14.1 us: latency (pieces, their
 //   join and two rankings)
 // A row of few is cut into pieces; each leaves its sums and its sorted top
 // places in the workspace, and the last to finish, by a ticket, joins them in
@@ -57,7 +57,9 @@ constexpr size_t kStreamBytes = (size_t)128 << 20;
 // the hint, of 2045 x 32003 fp32 123 and 136.
 constexpr size_t kStreamLogits = (size_t)3 << 29;
 constexpr int kBuf = 512;        // candidates for the top places that a wavefront keeps
-constexpr int kMaxPieces = 64;   // of one row
+// pieces of one row (us at 64 and 16, with 20 places: 1 x 131072 14.1 and
+// 14.2, 4 x 131072 15.8 and 14.3)
+constexpr int kMaxPieces = 16;
 constexpr int kFewRows = 256;    // fewer rows than this are cut into pieces
 // and into about so many of all rows (us at 256, 512, 1024: 64 x 131072 bf16
 // 10.5, 10.8, 13.4, with 20 places 23.0, 22.1, 22.1; 130 x 70001 fp32 with 20
@@ -323,7 +325,7 @@ __device__ __forceinline__ int rank_block(TopList& top, const uint64_t* buf, int
 // A workgroup of WAVES wavefronts takes a piece of a row; where a row has
 // several, the last one to finish joins them. STREAM: its loads carry the
 // nontemporal hint.
-template <bool BF16, bool TOP, int WAVES, int TILE, bool STREAM>
+template <bool BF16, bool TOP, int WAVES, bool STREAM>
 __global__ __launch_bounds__(64 * WAVES) void logprobs_kernel(LogprobArgs a) {
   constexpr int kThreads = 64 * WAVES, VEC = kVec<BF16>;
   __shared__ uint64_t buf[TOP ? WAVES * kBuf : 1];
@@ -386,26 +388,24 @@ __global__ __launch_bounds__(64 * WAVES) void logprobs_kernel(LogprobArgs a) {
       });
     }
   };
-  if constexpr (TILE > 1) {
-    u32x4 next[TILE];  // under way while a tile is summed
-    const uint32_t whole = end - (end - beg) % (TILE * kThreads);
+  u32x4 next[kTile];  // under way while a tile is summed
+  const uint32_t whole = end - (end - beg) % (kTile * kThreads);
 #pragma unroll
-    for (int u = 0; u < TILE; ++u)
-      if (at < whole) next[u] = load_vec<STREAM>(x0, at + u * kThreads + tid);
+  for (int u = 0; u < kTile; ++u)
+    if (at < whole) next[u] = load_vec<STREAM>(x0, at + u * kThreads + tid);
 #pragma unroll 1
-    for (; at < whole; at += TILE * kThreads) {
-      float x[TILE * VEC];
+  for (; at < whole; at += kTile * kThreads) {
+    float x[kTile * VEC];
 #pragma unroll
-      for (int u = 0; u < TILE; ++u) unpack<BF16>(next[u], x + u * VEC);
-      if (at + TILE * kThreads < whole) {
+    for (int u = 0; u < kTile; ++u) unpack<BF16>(next[u], x + u * VEC);
+    if (at + kTile * kThreads < whole) {
 #pragma unroll
-        for (int u = 0; u < TILE; ++u) next[u] = load_vec<STREAM>(x0, at + (TILE + u) * kThreads + tid);
-      }
-      add<TILE * VEC>(r, x, a.c);
-      if constexpr (TOP) consider(x);
+      for (int u = 0; u < kTile; ++u) next[u] = load_vec<STREAM>(x0, at + (kTile + u) * kThreads + tid);
     }
+    add<kTile * VEC>(r, x, a.c);
+    if constexpr (TOP) consider(x);
   }
-  // what is left of the piece, at most TILE vectors for a thread
+  // what is left of the piece, at most kTile vectors for a thread
   u32x4 one;
   if (at + tid < end) one = load_vec<STREAM>(x0, at + tid);
 #pragma unroll 1
@@ -504,13 +504,11 @@ void launch_logprobs(LogprobArgs a, int64_t N, int waves, hipStream_t st) {
     auto launch = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, st, a); };
     constexpr int kWaves = kLpThreads / 64;
     if (waves == 1)
-      stream_through ? launch(logprobs_kernel<BF16, TOP, 1, kTile, !TOP>, 64)
-                     : launch(logprobs_kernel<BF16, TOP, 1, kTile, false>, 64);
-    else if (a.piece_vectors <= kLpThreads)  // few rows
-      launch(logprobs_kernel<BF16, TOP, kWaves, 1, false>, kLpThreads);
+      stream_through ? launch(logprobs_kernel<BF16, TOP, 1, !TOP>, 64)
+                     : launch(logprobs_kernel<BF16, TOP, 1, false>, 64);
     else
-      stream_through ? launch(logprobs_kernel<BF16, TOP, kWaves, kTile, !TOP>, kLpThreads)
-                     : launch(logprobs_kernel<BF16, TOP, kWaves, kTile, false>, kLpThreads);
+      stream_through ? launch(logprobs_kernel<BF16, TOP, kWaves, !TOP>, kLpThreads)
+                     : launch(logprobs_kernel<BF16, TOP, kWaves, false>, kLpThreads);
   }
 }
 
@@ -644,14 +642,15 @@ int foremoe_token_logprobs(const void* logits, foremoe_dtype dtype, int64_t ld, 
   // top places (us, workgroup -> wavefront: 16384 x 8000 bf16 81 -> 54, 600 x
   // 4096 5.3 -> 4.5, 16384 x 16000 123 -> 101, 8192 x 131072 with 20 places
   // 494 -> 415; without places 365 -> 378, 2048 x 131072 with 5 118 -> 143).
-  // Rows that do not fill the GPU are cut into pieces, of at least a vector
-  // for every thread.
+  // Rows that do not fill the GPU are cut into pieces.
   const int waves = vectors <= 1024 || (N >= 4096 && (n_top || vectors <= 2048)) ? 1 : kLpThreads / 64;
   int64_t pieces = 1;
   if (ws && waves > 1 && N < kFewRows) {
-    const bool one = N <= kFewRows / kMaxPieces;  // a vector for every thread
-    pieces = one ? kMaxPieces : (kSplit + N - 1) / N;
-    const int64_t most = vectors / (kLpThreads * (one ? 1 : n_top ? kTile : 2 * kTile));
+    // at least a vector for every thread, where there are more rows a tile
+    // (without top places two)
+    const bool few = N <= kFewRows / kMaxPieces;
+    const int64_t most = vectors / (kLpThreads * (few ? 1 : n_top ? kTile : 2 * kTile));
+    pieces = (kSplit + N - 1) / N;
     if (pieces > most) pieces = most;
     if (pieces > kMaxPieces) pieces = kMaxPieces;
     if (pieces < 1) pieces = 1;
