@@ -23,7 +23,8 @@ class AdamW:
     elements; all params of one dtype, all grads of one dtype (fp32 or bf16).
     step() reads the gradients from these tensors each time, so they stay in
     place (as PolicyUpdate's dw_gate_up and dw_down do). With zero_grads it
-    leaves them zero.
+    leaves them zero. A param or grad may be given other memory (.data = ...)
+    of the same size and type; step() raises where it was given another type.
     weight_decay: one for all, or one per tensor.
     masters: fp32 copies that hold the values of bf16 params; True makes them,
     False does without (every step then rounds to bf16), or a list of tensors.
@@ -55,6 +56,8 @@ class AdamW:
         dev = self.params[0].device
         self.device = dev
         bf16 = self.params[0].dtype == torch.bfloat16
+        # the call's types: a tensor that is given other memory keeps its own
+        self._dtypes = self.params[0].dtype, self.grads[0].dtype
         self._pdt, self._gdt = _dt(self.params[0]), _dt(self.grads[0])
         if masters is True:
             masters = [p.detach().to(F32) for p in self.params] if bf16 else None
@@ -83,7 +86,7 @@ class AdamW:
 
     def _fill(self) -> None:
         """The call's records, checked."""
-        dev, pd, gd = self.device, self.params[0].dtype, self.grads[0].dtype
+        dev, (pd, gd) = self.device, self._dtypes
         kinds = (F32, F32) if self.state_bits == 32 else (torch.uint8, torch.uint8, F32, F32)
         none = [None] * (4 - len(kinds))
 
