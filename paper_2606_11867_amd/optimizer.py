@@ -73,7 +73,6 @@ class AdamW:
         self.states = [tuple(t.detach() for t in s) for s in states]
         if len(self.states) != n or (self.masters is not None and len(self.masters) != n):
             raise ValueError("masters and states: one per parameter")
-        self._records = (_lib.AdamWTensor * n)()
         self._fill()
 
     def _zero_state(self, p: torch.Tensor) -> tuple:
@@ -85,7 +84,7 @@ class AdamW:
                 torch.zeros(blocks, dtype=F32, device=p.device), torch.zeros(blocks, dtype=F32, device=p.device))
 
     def _fill(self) -> None:
-        """The call's records, checked."""
+        """The call's records, checked: whole, or those before."""
         dev, (pd, gd) = self.device, self._dtypes
         kinds = (F32, F32) if self.state_bits == 32 else (torch.uint8, torch.uint8, F32, F32)
         none = [None] * (4 - len(kinds))
@@ -95,16 +94,18 @@ class AdamW:
                 return t.data_ptr()
             return _vec(t, n, dtype, f"{name}[{i}]", dev)  # says what is wrong
 
+        records = (_lib.AdamWTensor * len(self.params))()
         for i, (p, g, st) in enumerate(zip(self.params, self.grads, self.states)):
             n = p.numel()
             if len(st) != len(kinds):
                 raise ValueError(f"states[{i}]: {len(kinds)} tensors expected")
             blocks = -(-n // _lib.ADAMW_BLOCK)
-            self._records[i] = _lib.AdamWTensor(
+            records[i] = _lib.AdamWTensor(
                 at(p, n, pd, "params", i), at(g, n, gd, "grads", i),
                 at(self.masters[i], n, F32, "masters", i) if self.masters is not None else None,
                 *[at(t, n if j < 2 else blocks, k, "states", i) for j, (t, k) in enumerate(zip(st, kinds))], *none,
                 n, self.weight_decay[i])
+        self._records = records
         self._tensors = self.params + self.grads
         self._at = list(map(torch.Tensor.data_ptr, self._tensors))
 

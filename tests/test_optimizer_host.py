@@ -67,6 +67,22 @@ def test_new_memory_of_another_type_is_refused(lib, which, old, new):
     assert [r["grad"] for r in lib.calls[-1]["records"]] == [g.data_ptr() for g in gs]
 
 
+def test_a_refused_step_leaves_the_records_whole(lib):
+    """The first gradient moved, the second became wrong; both go back to
+    where they were: the next call uses that memory, not the one between."""
+    ps, gs, opt = _made()
+    opt.step()
+    kept = [g.data for g in gs]
+    gs[0].data = torch.zeros(300)
+    gs[1].data = torch.zeros(71)
+    with pytest.raises(ValueError):
+        opt.step()
+    for g, k in zip(gs, kept):
+        g.data = k
+    opt.step()
+    assert [r["grad"] for r in lib.calls[-1]["records"]] == [g.data_ptr() for g in gs]
+
+
 @pytest.mark.gpu
 def test_new_memory_of_another_type_is_refused_on_the_device(gpu):
     p, g = torch.zeros(300, device=gpu), torch.ones(300, device=gpu)
