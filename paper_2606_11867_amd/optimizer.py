@@ -24,7 +24,8 @@ class AdamW:
     step() reads the gradients from these tensors each time, so they stay in
     place (as PolicyUpdate's dw_gate_up and dw_down do). With zero_grads it
     leaves them zero. A param or grad may be given other memory (.data = ...)
-    of the same size and type; step() raises where it was given another type.
+    of the same size and type, and the old memory is released by the next step;
+    step() raises where it was given another type.
     weight_decay: one for all, or one per tensor.
     masters: fp32 copies that hold the values of bf16 params; True makes them,
     False does without (every step then rounds to bf16), or a list of tensors.
@@ -106,6 +107,10 @@ class AdamW:
                 *[at(t, n if j < 2 else blocks, k, "states", i) for j, (t, k) in enumerate(zip(st, kinds))], *none,
                 n, self.weight_decay[i])
         self._records = records
+        # what the records point to stays allocated as long as they do: other
+        # memory is then at another address, which is what step() looks at
+        self._held = [t.detach() for t in (*self.params, *self.grads, *(self.masters or ()),
+                                           *(t for st in self.states for t in st))]
         self._tensors = self.params + self.grads
         self._at = list(map(torch.Tensor.data_ptr, self._tensors))
 

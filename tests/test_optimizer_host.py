@@ -83,6 +83,22 @@ def test_a_refused_step_leaves_the_records_whole(lib):
     assert [r["grad"] for r in lib.calls[-1]["records"]] == [g.data_ptr() for g in gs]
 
 
+def test_moved_tensors_keep_their_old_memory_until_the_next_step(lib):
+    """A freed block could come back at the same address as something
+    smaller, which addresses would not show."""
+    array = np.ones(300, dtype=np.float32)
+    ps, gs = [torch.zeros(300)], [torch.from_numpy(array)]
+    opt = optimizer.AdamW(ps, gs)
+    alive = weakref.ref(array)
+    del array
+    gs[0].data = torch.full((300,), 2.0)
+    gc.collect()
+    assert alive() is not None
+    opt.step()
+    gc.collect()
+    assert alive() is None and lib.calls[-1]["records"][0]["grad"] == gs[0].data_ptr()
+
+
 @pytest.mark.gpu
 def test_new_memory_of_another_type_is_refused_on_the_device(gpu):
     p, g = torch.zeros(300, device=gpu), torch.ones(300, device=gpu)
