@@ -50,10 +50,7 @@ class AdamW:
             raise ValueError("state_bits must be 8 or 32")
         self.lr, self.betas, self.eps = lr, tuple(betas), eps
         self.state_bits, self.n_steps, self.zero_grads = state_bits, int(step), bool(zero_grads)
-        self.weight_decay = [float(weight_decay)] * n if isinstance(weight_decay, (int, float)) else \
-            [float(w) for w in weight_decay]
-        if len(self.weight_decay) != n:
-            raise ValueError("weight_decay: one for all, or one per tensor")
+        self.weight_decay = weight_decay
         dev = self.params[0].device
         self.device = dev
         bf16 = self.params[0].dtype == torch.bfloat16
@@ -75,6 +72,19 @@ class AdamW:
         if len(self.states) != n or (self.masters is not None and len(self.masters) != n):
             raise ValueError("masters and states: one per parameter")
         self._fill()
+
+    @property
+    def weight_decay(self) -> List[float]:
+        """One per tensor; like lr, betas and eps what the next step uses."""
+        return self._weight_decay
+
+    @weight_decay.setter
+    def weight_decay(self, value: Union[float, Sequence[float]]) -> None:
+        n = len(self.params)
+        decay = [float(value)] * n if isinstance(value, (int, float)) else [float(w) for w in value]
+        if len(decay) != n:
+            raise ValueError("weight_decay: one for all, or one per tensor")
+        self._weight_decay = decay
 
     def _zero_state(self, p: torch.Tensor) -> tuple:
         if self.state_bits == 32:
@@ -105,7 +115,7 @@ class AdamW:
                 at(p, n, pd, "params", i), at(g, n, gd, "grads", i),
                 at(self.masters[i], n, F32, "masters", i) if self.masters is not None else None,
                 *[at(t, n if j < 2 else blocks, k, "states", i) for j, (t, k) in enumerate(zip(st, kinds))], *none,
-                n, self.weight_decay[i])
+                n, self._weight_decay[i])
         self._records = records
         # what the records point to stays allocated as long as they do: other
         # memory is then at another address, which is what step() looks at
@@ -113,6 +123,7 @@ class AdamW:
                                            *(t for st in self.states for t in st))]
         self._tensors = self.params + self.grads
         self._at = list(map(torch.Tensor.data_ptr, self._tensors))
+        self._decay = list(self._weight_decay)
 
     def step(self, lr: Optional[float] = None, grad_scale: Optional[torch.Tensor] = None) -> None:
         """One step on the current stream. lr: from now on. grad_scale: a
@@ -120,7 +131,8 @@ class AdamW:
         loss scaling)."""
         if lr is not None:
             self.lr = lr
-        if list(map(torch.Tensor.data_ptr, self._tensors)) != self._at:  # a tensor was given other memory
+        # a tensor was given other memory, or a weight decay was changed
+        if list(map(torch.Tensor.data_ptr, self._tensors)) != self._at or self._weight_decay != self._decay:
             self._fill()
         _lib.check(self.lib.foremoe_adamw_step(
             self._records, len(self.params), self._pdt, self._gdt, self.state_bits, self.lr, *self.betas, self.eps,

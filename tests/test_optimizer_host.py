@@ -99,6 +99,24 @@ def test_moved_tensors_keep_their_old_memory_until_the_next_step(lib):
     assert alive() is None and lib.calls[-1]["records"][0]["grad"] == gs[0].data_ptr()
 
 
+def test_weight_decay_counts_from_the_next_step(lib):
+    ps, gs, opt = _made(weight_decay=0.1)
+    opt.step()
+    opt.weight_decay[1] = 0.3
+    opt.step()
+    opt.weight_decay = [0.0, 0.5]
+    opt.lr = 0.7
+    opt.step()
+    got = [[r["weight_decay"] for r in c["records"]] for c in lib.calls]
+    assert got == [[0.1, 0.1], [0.1, 0.3], [0.0, 0.5]]
+    assert [c["lr"] for c in lib.calls] == [1e-3, 1e-3, 0.7]
+    opt.weight_decay = 0.25  # one for all
+    opt.step()
+    assert [r["weight_decay"] for r in lib.calls[-1]["records"]] == [0.25, 0.25]
+    with pytest.raises(ValueError):
+        opt.weight_decay = [1.0]
+
+
 @pytest.mark.gpu
 def test_new_memory_of_another_type_is_refused_on_the_device(gpu):
     p, g = torch.zeros(300, device=gpu), torch.ones(300, device=gpu)
