@@ -32,6 +32,8 @@ class AdamW:
     state_bits: 32 (fp32 moments) or 8 (a byte each and a scale for every 256
     elements). states: per tensor (m, v), or (m, v, m_scale, v_scale) with 8
     bits, used in place; None starts from zero. step: steps done so far.
+    params, grads, masters and states stay the tensors that they are: to load
+    others' values, copy_ into them.
     """
 
     def __init__(self, params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], *, lr: float = 1e-3,
@@ -40,7 +42,7 @@ class AdamW:
                  masters: Union[bool, Sequence[torch.Tensor]] = True, states: Optional[Sequence[tuple]] = None,
                  step: int = 0, zero_grads: bool = False):
         self.lib = _lib.load()
-        self.params, self.grads = list(params), list(grads)
+        self._params, self._grads = tuple(params), tuple(grads)
         n = len(self.params)
         if n == 0:
             raise ValueError("no parameters")
@@ -49,7 +51,7 @@ class AdamW:
         if state_bits not in (8, 32):
             raise ValueError("state_bits must be 8 or 32")
         self.lr, self.betas, self.eps = lr, tuple(betas), eps
-        self.state_bits, self.n_steps, self.zero_grads = state_bits, int(step), bool(zero_grads)
+        self._state_bits, self.n_steps, self.zero_grads = state_bits, int(step), bool(zero_grads)
         self.weight_decay = weight_decay
         dev = self.params[0].device
         self.device = dev
@@ -65,13 +67,35 @@ class AdamW:
             raise ValueError("masters go with bf16 parameters")
         # tensors of its own over the same memory: only params and grads can be
         # given other memory from outside
-        self.masters: Optional[List[torch.Tensor]] = None if masters is None else [t.detach() for t in masters]
+        self._masters = None if masters is None else tuple(t.detach() for t in masters)
         if states is None:
             states = [self._zero_state(p) for p in self.params]
-        self.states = [tuple(t.detach() for t in s) for s in states]
+        self._states = tuple(tuple(t.detach() for t in s) for s in states)
         if len(self.states) != n or (self.masters is not None and len(self.masters) != n):
             raise ValueError("masters and states: one per parameter")
         self._fill()
+
+    # The tensors that the call's records were made of. They stay: values are
+    # loaded into them (copy_).
+    @property
+    def params(self) -> Tuple[torch.Tensor, ...]:
+        return self._params
+
+    @property
+    def grads(self) -> Tuple[torch.Tensor, ...]:
+        return self._grads
+
+    @property
+    def masters(self) -> Optional[Tuple[torch.Tensor, ...]]:
+        return self._masters
+
+    @property
+    def states(self) -> Tuple[Tuple[torch.Tensor, ...], ...]:
+        return self._states
+
+    @property
+    def state_bits(self) -> int:
+        return self._state_bits
 
     @property
     def weight_decay(self) -> List[float]:

@@ -117,6 +117,20 @@ def test_weight_decay_counts_from_the_next_step(lib):
         opt.weight_decay = [1.0]
 
 
+@pytest.mark.parametrize("name", ["params", "grads", "masters", "states"])
+def test_tensors_are_exchanged_by_new_memory_only(lib, name):
+    """A tensor put in another's place would not be seen, and the old one's
+    memory, which the records hold, could be freed."""
+    ps, gs, opt = _made(dtype=BF16)
+    held = getattr(opt, name)
+    with pytest.raises(TypeError):
+        held[0] = held[1]
+    with pytest.raises(AttributeError):
+        setattr(opt, name, held)
+    with pytest.raises(AttributeError):  # records of the other width are read differently
+        opt.state_bits = 8
+
+
 @pytest.mark.gpu
 def test_new_memory_of_another_type_is_refused_on_the_device(gpu):
     p, g = torch.zeros(300, device=gpu), torch.ones(300, device=gpu)
