@@ -214,7 +214,8 @@ __device__ __forceinline__ void adamw_blocks(const AdamArgs& a, const AdamRecord
       vv[k] = vv[k] * a.beta2 + grad * grad * a.one_beta2;
       // within a unit in the last place; exact where it makes the code
       u[k] = BITS8 ? exact_sqrt(vv[k]) : __builtin_amdgcn_sqrtf(vv[k]);
-      small |= vv[k] < kExactFrom;
+      // the root of an infinity by the residual is a NaN
+      small |= !(vv[k] >= kExactFrom && vv[k] < INFINITY);
     }
     if (BITS8 && __any(small)) {
 #pragma unroll

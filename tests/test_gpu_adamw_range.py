@@ -1,0 +1,61 @@
+"""The AdamW step at the ends of fp32's range and at the last bit of its
+reciprocals and square roots.
+
+Bounds, u = 2^-24: a move is a quotient of the stored moments times two
+factors rounded to fp32: within 32 u of itself, as for ordinary values.
+"""
+import numpy as np
+import pytest
+import torch
+
+import oracle.foremoe_step as S
+
+U = 2.0 ** -24
+F32 = torch.float32
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("param", ["f32", "bf16"])
+@pytest.mark.parametrize("big", [1e20, -3e38])
+def test_finite_gradient_whose_square_is_not(gpu, bits, param, big):
+    """v is infinite, m finite: m / inf = 0, so the parameter stays."""
+    from paper_2606_11867_amd.optimizer import AdamW
+    p = torch.ones(1000, device=gpu, dtype=torch.bfloat16 if param == "bf16" else F32)
+    g = torch.full((1000,), 0.1, device=gpu)
+    g[300] = big
+    opt = AdamW([p], [g], lr=0.1, state_bits=bits)
+    opt.step()
+    where = torch.arange(1000, device=gpu) == 300
+    for t in [p, *(opt.masters or ())]:
+        assert torch.isfinite(t).all() and t[300] == 1.0 and torch.all(t[~where] < 0.95)
+    if bits == 32:
+        assert torch.isfinite(opt.states[0][0]).all() and torch.isinf(opt.states[0][1][300])
+        opt.step()
+        assert torch.isfinite(p).all() and p[300] == 1.0
+
+
+# ---------------------------------------------------------------------------
+# The last bit. A quotient 1 / x and a square root of fp32 numbers, taken in
+# 64 bits and rounded to 32, are correctly rounded (64 bits have more than
+# twice the digits of 32, and two more).
+# ---------------------------------------------------------------------------
+BLOCK = 256
+CHUNK = 1 << 15  # blocks of a call
+
+
+def _rounded_codes(x, shift, one, least):
+    """Codes of ratios x >= 0, to nearest, ties to even patterns."""
+    b = x.view(torch.int32)
+    c = ((b + ((1 << (shift - 1)) - 1) + ((b >> shift) & 1)) >> shift) - ((0x3F800000 >> shift) - one)
+    return torch.where(x > 0, c.clamp(least, one), torch.zeros_like(c)).to(torch.uint8)
+
+
+def _beside_the_boundaries(scale, table):
+    """[blocks, 256]: the scale, then numbers at its ratios halfway between
+    two codes and one step to either side."""
+    mid = (table[1:-1] + table[2:]) / 2
+    mid = torch.from_numpy(np.sort(mid[np.linspace(0, len(mid) - 1, 85).astype(int)])).to(scale.device)
+    a = (scale.double()[:, None] * mid).float()
+    bits = a.view(torch.int32)
+    return torch.cat([scale[:, None], a, (bits - 1).view(F32), (bits + 1).view(F32)], 1)
