@@ -714,10 +714,12 @@ int foremoe_token_logprobs_bwd(const void* logits, foremoe_dtype dtype, int64_t 
  *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2
  *   p = p (1 - lr weight_decay)
  *       - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
- * in fp32; where the last quotient is 0 / 0 (eps = 0, no gradient yet) it is
- * 0. p is master where the record has one (param, of bf16, then gets
- * its rounded copy), else param itself. zero_grads != 0: grad is zero
- * afterwards (the accumulators of the weight gradients start anew).
+ * in fp32, v down to its subnormal numbers. Where the denominator is 0 (eps =
+ * 0, no gradient yet, or one whose square is 0 in fp32) there is no move; an
+ * eps below 2^-126 counts as 0. p is master where the record has one (param,
+ * of bf16, then gets its rounded copy), else param itself. zero_grads != 0:
+ * grad is zero afterwards (the accumulators of the weight gradients start
+ * anew).
  * state_bits 32: m and v are fp32 [n]; m_scale, v_scale NULL.
  * state_bits 8: m and v are bytes [n] with an fp32 scale for every
  *   FOREMOE_ADAMW_BLOCK consecutive elements, [ceil(n / block)] each. The

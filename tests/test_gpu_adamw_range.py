@@ -35,6 +35,48 @@ def test_finite_gradient_whose_square_is_not(gpu, bits, param, big):
         assert torch.isfinite(p).all() and p[300] == 1.0
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [32, 8])
+def test_second_moments_below_the_normal_numbers(gpu, bits):
+    """eps = 0 and gradients whose squares are subnormal: the move is about lr
+    all the same. Where the square is 0 in fp32, so is the denominator, and
+    the element does not move."""
+    from paper_2606_11867_amd.optimizer import AdamW
+    sizes = np.array([1e-18, 5e-19, 1e-19, 3e-20, 1e-21, 1e-22, 1e-25, 0.0], dtype=np.float32)
+    signs = np.where(np.arange(1024) % 3 == 0, -1, 1).astype(np.float32)
+    gn = np.repeat(sizes, 128) * signs
+    g = torch.from_numpy(gn).to(gpu)
+    p = torch.zeros(1024, device=gpu)
+    lr, b1, b2 = 0.1, 0.9, 0.95
+    opt = AdamW([p], [g], lr=lr, betas=(b1, b2), eps=0.0, state_bits=bits)
+    opt.step()
+    f = np.float32
+    m, v = gn * f(1 - b1), (gn * gn) * f(1 - b2)
+    if bits == 32:
+        assert np.array_equal(opt.states[0][1].cpu().numpy(), v)
+    m, v = m.astype(np.float64), v.astype(np.float64)
+    with np.errstate(divide="ignore", invalid="ignore"):
+        want = np.where(v > 0, -lr * m / (1 - b1) / np.sqrt(v / (1 - b2)), 0.0)
+    assert np.count_nonzero(v) == 5 * 128 and np.abs(want[v > 0]).min() > 0.09
+    got = p.double().cpu().numpy()
+    assert np.all(np.abs(got - want) <= 32 * U * np.abs(want)), np.abs(got - want).reshape(8, 128).max(1)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [32, 8])
+def test_eps_below_the_normal_numbers(gpu, bits):
+    from paper_2606_11867_amd.optimizer import AdamW
+    eps = 1e-40
+    g = torch.zeros(600, device=gpu)
+    g[::3] = 1e-3
+    p = torch.zeros(600, device=gpu)
+    opt = AdamW([p], [g], lr=0.1, eps=eps, state_bits=bits)
+    opt.step()
+    want = torch.zeros(600, device=gpu)
+    want[::3] = -0.1
+    assert torch.all((p - want).abs() <= 64 * U * want.abs())
+
+
 # ---------------------------------------------------------------------------
 # The last bit. A quotient 1 / x and a square root of fp32 numbers, taken in
 # 64 bits and rounded to 32, are correctly rounded (64 bits have more than
