@@ -125,27 +125,44 @@ __device__ __forceinline__ void unpack(u32x4 v, float* x) {
 // both terms of the entropy >= 0. y is one fused multiply-add, x c - m c with
 // m c rounded once: the same reference everywhere, so that its rounding
 // cancels. m starts at the lowest finite number, so an x of -inf adds nothing
-// to s. Logits so large that m c overflows subtract before they scale.
-__device__ __forceinline__ bool huge(float mc) { return !(fabsf(mc) < 1e38f); }
+// to s. Where m c is so large that its rounding is no small part of a y (a row
+// that a mask fills with -1e9, or the type's ends), x - m is taken first and
+// then scaled: m c itself is the reference.
+__device__ __forceinline__ bool huge(float mc) { return !(fabsf(mc) < 0x1p24f); }
 
-// 2^y of what is summed under a, seen from the reference m; in y.
-__device__ __forceinline__ float shift(float from, float m, float c) {
-  const float a = from * c, b = m * c;
-  return huge(a) || huge(b) ? (from - m) * c : a - b;
+// Either kind of reference, exactly.
+__device__ __forceinline__ double reference(float m, float c) {
+  const float mc = m * c;
+  return huge(mc) ? (double)m * (double)c : (double)mc;
+}
+
+// The sums seen from a reference that lies -y above their own.
+__device__ __forceinline__ void lower(Sums& a, float y) {
+  const float e = __builtin_amdgcn_exp2f(y);
+  a.t = e == 0.0f ? 0.0f : e * (a.t + y * a.s);
+  a.s = e == 0.0f ? a.s * 0.0f : a.s * e;  // keeps a NaN
 }
 
 __device__ __forceinline__ void rebase(Sums& a, float m, float c) {
-  const float y = shift(a.m, m, c), e = __builtin_amdgcn_exp2f(y);
-  a.t = e == 0.0f ? 0.0f : e * (a.t + y * a.s);
-  a.s = e == 0.0f ? a.s * 0.0f : a.s * e;  // keeps a NaN
+  const float from = a.m * c, to = m * c;
+  float y = from - to;
+  if (a.s == 0.0f) {
+    y = -INFINITY;  // nothing yet: under the lowest number
+  } else if (__builtin_expect(huge(from) || huge(to), 0)) {
+    y = (float)(reference(a.m, c) - reference(m, c));
+  }
+  lower(a, y);
   a.m = m;
 }
 
+// (In 64 bits for every join: branches as in rebase would cost one 0.1 us.)
 __device__ __forceinline__ Sums join(Sums a, Sums b, float c) {
-  const float m = fmaxf(a.m, b.m);
-  rebase(a, m, c);
-  rebase(b, m, c);
-  return Sums{m, a.s + b.s, a.t + b.t};
+  if (b.m > a.m) {
+    const Sums x = a;
+    a = b, b = x;
+  }
+  lower(b, (float)(reference(b.m, c) - reference(a.m, c)));
+  return Sums{a.m, a.s + b.s, a.t + b.t};
 }
 
 // Adds n elements of one lane.

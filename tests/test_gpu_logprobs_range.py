@@ -1,0 +1,63 @@
+"""Log-probabilities of rows far from zero, and of more rows than one launch
+takes, against the fp64 oracle.
+
+Bounds, u = 2^-24. Where logits are so large that a scaled one has no fraction
+left, differences from the row's maximum are taken before they are scaled:
+exact, or rounded once, then scaled by a constant rounded once. A
+log-probability d - log s is then within 8 u |d| + u (V / 256 + 128), an
+entropy within that times (2 + H), lse within 8 u of itself.
+"""
+import numpy as np
+import pytest
+import torch
+
+import oracle.foremoe_step as S
+import test_gpu_logprobs as base
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+INF = float("inf")
+
+
+def _far_rows(V, dtype, rng):
+    """Rows of one value, of values a few steps of the type apart, and of far
+    values beside a masked half."""
+    rows = []
+    top = float(torch.finfo(dtype).max)
+    for base_value in (-1e4, -1e7, -1e8, -1e9, -1e12, -1e30, -top, 1e6, 3e7, 1e10, 1e20, top):
+        v = float(torch.tensor(base_value).to(dtype))
+        rows.append(np.full(V, v))
+        step = 2.0 ** (np.floor(np.log2(abs(v))) - (7 if dtype == torch.bfloat16 else 23))
+        rows.append(v - np.sign(v) * step * rng.integers(0, 4, V))
+        rows.append(np.where(np.arange(V) % 2 == 0, v, -INF))
+    return np.stack(rows)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("V", [5, 3001, 40003])
+@pytest.mark.parametrize("temperature", [1.0, 0.7, 1.3, 50.0])
+@pytest.mark.parametrize("split", [True, False], ids=["ws", "no-ws"])
+def test_rows_far_from_zero(gpu, dtype, V, temperature, split):
+    from paper_2606_11867_amd import api
+    rng = np.random.default_rng(V)
+    x = torch.from_numpy(_far_rows(V, dtype, rng).astype(np.float32)).to(dtype)
+    l = x.double().numpy()
+    N = len(l)
+    T = float(np.float32(temperature))
+    l = l[np.abs(np.where(np.isfinite(l), l, 0)).max(1) / T <= np.finfo(np.float32).max]  # x / T in fp32's range
+    x = torch.from_numpy(l).to(dtype)
+    assert len(l) >= N - 6
+    N = len(l)
+    t = np.array([2 * rng.integers(0, (V + 1) // 2) for _ in range(N)], dtype=np.int32)
+    n_top = min(V, 3)
+    ref = S.token_logprobs(l, t, temperature=T, n_top=n_top)
+    ws = api.logprobs_workspace(gpu) if split else None
+    r = api.token_logprobs(x.to(gpu), torch.from_numpy(t).to(gpu), temperature=temperature, n_top=n_top, ws=ws)
+    tol = U * (V / 256 + 128)
+    base._close("logp", r.logp, ref["logp"], tol + 8 * U * np.abs(ref["logp"]))
+    base._close("entropy", r.entropy, ref["entropy"], (tol + 64 * U) * (2 + ref["entropy"]))
+    base._close("lse", r.lse, ref["lse"], tol + 8 * U * np.abs(ref["lse"]))
+    assert np.array_equal(r.top_ids.cpu().numpy(), ref["top_ids"])
+    near = np.where(np.isfinite(ref["top_logp"]), ref["top_logp"], 0.0)
+    base._close("top_logp", r.top_logp, ref["top_logp"], tol + 8 * U * np.abs(near))
