@@ -699,7 +699,9 @@ int foremoe_token_logprobs(const void* logits, foremoe_dtype dtype, int64_t ld, 
  *   dlogits_j = (dlogp (1[j = target] - p_j) - dentropy p_j (log p_j + entropy))
  *               / temperature
  * with p from the forward's lse; 0 where p_j is 0 (but for the target) and
- * in ignored rows. dlogp [N] or NULL (needs targets); dentropy [N] or NULL
+ * in ignored rows. p is as exact as fp32 holds lse, its relative error a few
+ * times |lse| 2^-24, and never above 1. (Of a row that a mask fills with -1e9,
+ * lse keeps nothing of log V: its gradient is finite, but no more.) dlogp [N] or NULL (needs targets); dentropy [N] or NULL
  * (needs entropy [N], the forward's). dlogits [N, V] of the logits' dtype,
  * rows ld_out apart; it may be the logits themselves (same address and ld).
  */

@@ -540,11 +540,15 @@ struct LogprobBwdArgs {
   int64_t ld_out;
 };
 
-// One row's gradient: d = -p (a + b (y + h)), y = x / temperature - lse.
+// One row's gradient: d = -p (a + b (y + h)), y = x / temperature - lse. An
+// lse that rounding has left below the largest x / temperature, by 32 at 1e9,
+// gives no p above 1.
 struct RowGrad {
   float it, lse, a, b, h;
   __device__ __forceinline__ float operator()(float x) const {
-    const float y = fmaf(x, it, -lse), p = __builtin_amdgcn_exp2f(y * kLog2e);
+    float y = fmaf(x, it, -lse);
+    y = y > 0.0f ? 0.0f : y;  // keeps a NaN
+    const float p = __builtin_amdgcn_exp2f(y * kLog2e);
     const float d = -p * fmaf(b, y + h, a);
     return p == 0.0f ? 0.0f : d;  // y is -inf where the logit is
   }

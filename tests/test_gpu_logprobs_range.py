@@ -61,3 +61,27 @@ def test_rows_far_from_zero(gpu, dtype, V, temperature, split):
     assert np.array_equal(r.top_ids.cpu().numpy(), ref["top_ids"])
     near = np.where(np.isfinite(ref["top_logp"]), ref["top_logp"], 0.0)
     base._close("top_logp", r.top_logp, ref["top_logp"], tol + 8 * U * np.abs(near))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("temperature", [1.0, 0.7, 1.3, 50.0])
+def test_gradients_of_rows_far_from_zero_are_bounded(gpu, dtype, temperature):
+    """An fp32 lse of 1e9 does not hold the logarithm of a sum any more, and
+    a gradient from it is not the formula's; but no p exceeds 1, so it stays
+    within the formula's largest terms."""
+    from paper_2606_11867_amd import api
+    V = 1001
+    rng = np.random.default_rng(3)
+    l = _far_rows(V, dtype, rng)
+    l = l[np.abs(np.where(np.isfinite(l), l, 0)).max(1) / temperature <= np.finfo(np.float32).max]
+    x = torch.from_numpy(l).to(dtype).to(gpu)
+    N = len(l)
+    t = torch.zeros(N, dtype=torch.int32, device=gpu)
+    a = torch.from_numpy(rng.standard_normal(N).astype(np.float32)).to(gpu)
+    b = torch.from_numpy(rng.standard_normal(N).astype(np.float32)).to(gpu)
+    r = api.token_logprobs(x, t, temperature=temperature)
+    d = api.token_logprobs_bwd(x, t, r.lse, a, entropy=r.entropy, dentropy=b, temperature=temperature).float()
+    # |dlogp| (1 + p) + |dentropy| (p |log p| + p H), p |log p| <= 1 / e
+    most = (2 * a.abs() + b.abs() * (0.5 + r.entropy)) / temperature
+    assert torch.isfinite(d).all()
+    assert torch.all(d.abs() <= 1.01 * most[:, None])
