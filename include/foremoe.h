@@ -701,9 +701,10 @@ int foremoe_token_logprobs(const void* logits, foremoe_dtype dtype, int64_t ld, 
  * with p from the forward's lse; 0 where p_j is 0 (but for the target) and
  * in ignored rows. p is as exact as fp32 holds lse, its relative error a few
  * times |lse| 2^-24, and never above 1. (Of a row that a mask fills with -1e9,
- * lse keeps nothing of log V: its gradient is finite, but no more.) dlogp [N] or NULL (needs targets); dentropy [N] or NULL
- * (needs entropy [N], the forward's). dlogits [N, V] of the logits' dtype,
- * rows ld_out apart; it may be the logits themselves (same address and ld).
+ * lse keeps nothing of log V: its gradient is finite, but no more.)
+ * dlogp [N] or NULL (needs targets); dentropy [N] or NULL (needs entropy [N],
+ * the forward's). dlogits [N, V] of the logits' dtype, rows ld_out apart; it
+ * may be the logits themselves (same address and ld).
  */
 int foremoe_token_logprobs_bwd(const void* logits, foremoe_dtype dtype, int64_t ld, int64_t N,
                                int64_t V, const int32_t* targets, float temperature,

@@ -225,6 +225,14 @@ __device__ __forceinline__ void load_row(const RouterArgs& a, int64_t t, int lan
   }
 }
 
+template <int L, int V>
+__device__ __forceinline__ float row_max(const float (&v)[V]) {
+  float most = v[0];
+#pragma unroll
+  for (int j = 1; j < V; ++j) most = fmaxf(most, v[j]);
+  return lanes_max<L>(most);
+}
+
 // Whether some logit is not -inf (a NaN is not), the row's maximum (0 where
 // there is none), its scores s and their sum. exact: sigmoids that decide.
 template <int L, int V>
@@ -240,10 +248,7 @@ __device__ __forceinline__ bool row_scores(const float (&v)[V], bool sig, bool e
 #pragma unroll
     for (int j = 0; j < V; ++j) s[j] = fast_sigmoid(v[j]);
   } else {
-    float m = v[0];
-#pragma unroll
-    for (int j = 1; j < V; ++j) m = fmaxf(m, v[j]);
-    m = lanes_max<L>(m);
+    const float m = row_max<L, V>(v);
     top = m > kNegInf ? m : 0.0f;
 #pragma unroll
     for (int j = 0; j < V; ++j) s[j] = fast_exp(v[j] - top);
@@ -255,22 +260,60 @@ __device__ __forceinline__ bool row_scores(const float (&v)[V], bool sig, bool e
   return lanes_max<L>(some ? 1.0f : 0.0f) != 0.0f;
 }
 
+// Sigmoid scores whose sum lies below this are all e^l to the last bit. Their
+// shares of the sum come from e^(l - max): the scores themselves may be too
+// small for fp32.
+constexpr float kFarSum = 0x1p-60f;
+
+// Adds the shares of such tokens (`far`).
+template <int L, int V>
+__device__ __forceinline__ void add_far_shares(const float (&v)[V], bool far, float (&acc)[V]) {
+  float most = row_max<L, V>(v), all = 0.0f;
+#pragma unroll
+  for (int j = 0; j < V; ++j) all += fast_exp(v[j] - most);
+  all = lanes_sum<L>(all);
+  asm volatile("" : "+v"(most));  // exponentials once more, not V registers that hold them
+  const float inv = 1.0f / all;
+#pragma unroll
+  for (int j = 0; j < V; ++j) acc[j] += far ? fast_exp(v[j] - most) * inv : 0.0f;
+}
+// Puts e^(l - max) in the place of their scores, and its sum; returns what s
+// is to be multiplied by to be the score again.
+template <int L, int V>
+__device__ __forceinline__ float far_scores(const float (&v)[V], bool far, float (&s)[V], float& sum) {
+  const float most = row_max<L, V>(v);
+  float all = 0.0f;
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    s[j] = far ? fast_exp(v[j] - most) : s[j];
+    all += s[j];
+  }
+  all = lanes_sum<L>(all);
+  sum = far ? all : sum;
+  return far ? fast_exp(most) : 1.0f;
+}
+
 // The C * L places of a token, place lane + c L in register c: the scores q
-// of the picked logits x over the sum that the gates divide by.
+// of the picked logits x over the sum that the gates divide by. Renormalised
+// ones are scaled by the largest, so that small ones are not lost.
 template <int L, int C>
 __device__ __forceinline__ float place_scores(const float (&x)[C], const int (&id)[C], bool sig, bool renorm,
                                               float top, float sum, float (&q)[C]) {
-  if (!sig && renorm) {  // the softmax over the picked logits alone
+  if (renorm) {
     top = kNegInf;
 #pragma unroll
     for (int c = 0; c < C; ++c) top = fmaxf(top, id[c] < 0 ? kNegInf : x[c]);
     top = lanes_max<L>(top);
     if (!(top > kNegInf)) top = 0.0f;
   }
+  const float up = renorm ? fminf(top, 0.0f) : 0.0f;
   float total = 0.0f;
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    q[c] = id[c] < 0 ? 0.0f : sig ? fast_sigmoid(x[c]) : fast_exp(x[c] - top);
+    // the sigmoid is e^min(x, 0) / (1 + e^-|x|)
+    q[c] = id[c] < 0 ? 0.0f
+           : sig     ? fast_exp(fminf(x[c], 0.0f) - up) * fast_sigmoid(fabsf(x[c]))
+                     : fast_exp(x[c] - top);
     total += q[c];
   }
   if (renorm) return lanes_sum<L>(total);
@@ -372,11 +415,15 @@ __global__ __launch_bounds__(kRouterThreads, 4) void router_fwd_kernel(RouterArg
       load_row<BF16, L, V>(a, t, lane, v);
       alive &= row_scores<L, V>(v, sig, PICK == kBiased, s, top, sum);
     }
-    if (stats && alive) {
-      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    if (stats) {
+      const bool far = sig && alive && !(sum >= kFarSum);
+      if (__builtin_expect(__any(far), 0)) add_far_shares<L, V>(v, far, acc);
+      if (alive) {
+        const float inv = far ? 0.0f : 1.0f / sum;
 #pragma unroll
-      for (int j = 0; j < V; ++j) acc[j] += s[j] * inv;
-      ++tokens;
+        for (int j = 0; j < V; ++j) acc[j] += s[j] * inv;
+        ++tokens;
+      }
     }
     if constexpr (PICK != kReplay) {
 #pragma unroll
@@ -545,8 +592,11 @@ __global__ __launch_bounds__(kRouterThreads) void router_bwd_kernel(RouterArgs a
     }
     load_row<BF16, L, V>(a, t, lane, v);
     const bool alive = row_scores<L, V>(v, sig, false, s, top, sum) && (!a.mask || a.mask[t]);
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    float ds[V] = {};  // of the score, or of the logit (softmax renormalised)
+    float unit = 1.0f;  // the score over s
+    const bool far = sig && alive && !(sum >= kFarSum);
+    if (__builtin_expect(__any(far), 0)) unit = far_scores<L, V>(v, far, s, sum);
+    const float inv = alive ? 1.0f / sum : 0.0f;
+    float ds[V] = {};  // of the score, or, renormalised, of the logit (a sigmoid's over 1 - s)
     if (a.dgates) {
       if (renorm) {
         float q[C], dot = 0.0f;
@@ -561,7 +611,7 @@ __global__ __launch_bounds__(kRouterThreads) void router_bwd_kernel(RouterArgs a
         }
         dot = lanes_sum<L>(dot);
 #pragma unroll
-        for (int c = 0; c < C; ++c) w[c] = id[c] < 0 ? 0.0f : (sig ? over : q[c]) * (dg[c] - dot);
+        for (int c = 0; c < C; ++c) w[c] = id[c] < 0 ? 0.0f : q[c] * (dg[c] - dot);
       } else {
 #pragma unroll
         for (int c = 0; c < C; ++c) w[c] = id[c] < 0 ? 0.0f : dg[c];
@@ -616,9 +666,13 @@ __global__ __launch_bounds__(kRouterThreads) void router_bwd_kernel(RouterArgs a
     if (through_pi) {
 #pragma unroll
       for (int j = 0; j < V; ++j) ds[j] = s[j] * inv * (push[j] + ds[j] - pc);
+    } else if (sig && renorm) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) ds[j] = fmaf(-unit, s[j], 1.0f) * (ds[j] + s[j] * inv * (push[j] - pc));
     } else if (sig) {
 #pragma unroll
-      for (int j = 0; j < V; ++j) ds[j] = (1.0f - s[j]) * s[j] * (ds[j] + inv * (push[j] - pc));
+      for (int j = 0; j < V; ++j)
+        ds[j] = fmaf(-unit, s[j], 1.0f) * s[j] * (unit * ds[j] + inv * (push[j] - pc));
     } else if (balance) {
 #pragma unroll
       for (int j = 0; j < V; ++j) ds[j] += s[j] * inv * (push[j] - pc);

@@ -1,0 +1,82 @@
+"""The router at far logits, and the sizes that send it through every kernel
+and past the first pass of its loops, against the fp64 oracle.
+
+Bounds as in test_gpu_router, whose cases these continue; u = 2^-24. Gates by
+their last bits: an exponential within 4 u, a score (one addition, one
+reciprocal) within 7 u, a sum over registers and lanes within 8 u more, the
+quotient u: 7 + 7 + 8 + 1 = 23 u. (Logits are multiples of 2^-6, so that their
+differences are exact.)
+"""
+import numpy as np
+import pytest
+import torch
+
+import oracle.foremoe_step as S
+import test_gpu_router as base
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+
+
+def _grid(T, E, seed, low, high):
+    rng = np.random.default_rng(seed)
+    return rng.integers(int(low * 64), int(high * 64), (T, E)).astype(np.float64) / 64, rng
+
+
+@pytest.mark.parametrize("E,K", [(24, 8), (200, 20), (300, 8)])
+@pytest.mark.parametrize("where", ["all", "some"])
+def test_sigmoid_scores_too_small_for_fp32(gpu, E, K, where):
+    """Rows whose every logit is below -90, where a score is subnormal or 0 in
+    fp32: shares and gates are ratios all the same."""
+    from paper_2606_11867_amd import api
+    T = 23
+    l, rng = _grid(T, E, E + 1, -400, -90)
+    l = np.where(np.arange(E) % 2 == 0, l, -90 - rng.integers(0, 640, (T, E)) / 64)
+    if where == "some":
+        l[::2] += 90
+        l[1] += np.where(np.arange(E) == 3, 95, 0)
+    l[5, :] = -np.inf
+    l[7, : E // 2] = -np.inf
+    x = torch.from_numpy(l.astype(np.float32)).to(gpu)
+    dg = rng.standard_normal((T, K)).astype(np.float32)
+    coef = 0.7
+    rel = U * (2 * 400 + E / 8 + 64)
+    ids = np.argsort(rng.random((T, E)), axis=1)[:, :K].astype(np.int32)
+    for replay in (None, ids):
+        for renorm in (True, False):
+            kw = dict(score="sigmoid", renorm=renorm, scale=1.5)
+            ref = S.router_forward(l, K, ids=replay, **kw)
+            r = api.router_fwd(x, K, ids=None if replay is None else torch.from_numpy(ids).to(gpu), **kw)
+            assert np.array_equal(r.ids.cpu().numpy(), ref["ids"])
+            assert np.array_equal(r.counts.cpu().numpy(), ref["counts"])
+            base._check("gates", r.gates, ref["gates"], rel * ref["gates"] + 1e-37)
+            base._check("prob_mean", r.prob_mean, ref["prob_mean"], rel * ref["prob_mean"] + 1e-37)
+            base._check("balance_loss", r.balance_loss, np.array([ref["balance_loss"]]),
+                        (rel + U * (E + 64)) * ref["balance_loss"])
+            lone = api.router_fwd(x, K, ids=r.ids, stats=False, **kw)
+            assert torch.equal(lone.gates, r.gates)
+            c = coef * E / max(1, ref["n_tokens"]) * ref["counts"] / max(1, ref["counts"].sum())
+            for cf, d in ((0.0, dg), (coef, dg), (coef, None)):
+                want = S.router_backward(l, ref["ids"], d, counts=ref["counts"], n_tokens=ref["n_tokens"],
+                                         balance_coef=cf, **kw)
+                got = api.router_bwd(x, r.ids, None if d is None else torch.from_numpy(d).to(gpu), counts=r.counts,
+                                     n_tokens=r.n_tokens, balance_coef=cf, **kw)
+                size = (0.0 if d is None else 1.5 * np.abs(d).max()) + (c.max() if cf else 0.0)
+                base._check("dlogits", got, want, 8 * rel * size)
+            if renorm:  # none of it is lost
+                assert np.abs(ref["gates"].sum(1)[ref["ids"][:, 0] >= 0] - 1.5).max() < 1e-9
+                assert np.abs(want).max() > 0
+
+
+MORE = [
+    # T, E, K, dtype, score, renorm, bias, mask, replay, disabled, pad: places over several registers, few experts
+    (70, 100, 40, "f32", "softmax", True, False, True, False, 0, 0),
+    (50, 256, 64, "bf16", "softmax", True, False, False, False, 0, 0),
+    (33, 20, 20, "f32", "sigmoid", True, False, False, False, 0, 3),
+    (33, 20, 20, "bf16", "softmax", False, False, True, True, 5, 0),
+    (61, 128, 17, "f32", "sigmoid", False, False, False, True, 0, 1),
+    (61, 129, 33, "bf16", "sigmoid", True, False, False, False, 90, 0),
+    (45, 255, 48, "f32", "softmax", False, False, False, False, 0, 0),
+    (45, 250, 64, "f32", "softmax", True, False, True, True, 3, 2),
+]
