@@ -146,10 +146,21 @@ __device__ __forceinline__ void wave_fence() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// e^d for d <= 0, and the sigmoid: within |d| 2^-24 + 2 units in the last place.
+// e^d for d <= 0, and the sigmoid: within |d| 2^-24 + 2 units in the last
+// place. For sums over all experts (shares, the softmax's denominator), where an
+// error counts by its term: sum p |d|, from the maximum, is at most log E.
 __device__ __forceinline__ float fast_exp(float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
 __device__ __forceinline__ float fast_sigmoid(float v) {
   return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v * -kLog2e));
+}
+// e^d for d <= 0 within two units in the last place at any distance: for the
+// gates, of which there are few.
+__device__ __forceinline__ float near_exp(float d) {
+  d = d < -200.0f ? -200.0f : d;  // keeps a NaN
+  const float n = rintf(d * kLog2e);
+  constexpr float kLog2eRest = 1.92596299e-8f;  // log2(e) minus its fp32 value
+  const float f = fmaf(d, kLog2eRest, fmaf(d, kLog2e, -n));
+  return __builtin_amdgcn_ldexpf(__builtin_amdgcn_exp2f(f), (int)n);
 }
 // The sigmoid of the definition's four fp32 operations, each rounded, where a
 // score plus a bias decides. The quotient is the hardware's reciprocal
@@ -312,8 +323,8 @@ __device__ __forceinline__ float place_scores(const float (&x)[C], const int (&i
   for (int c = 0; c < C; ++c) {
     // the sigmoid is e^min(x, 0) / (1 + e^-|x|)
     q[c] = id[c] < 0 ? 0.0f
-           : sig     ? fast_exp(fminf(x[c], 0.0f) - up) * fast_sigmoid(fabsf(x[c]))
-                     : fast_exp(x[c] - top);
+           : sig     ? near_exp(fminf(x[c], 0.0f) - up) * fast_sigmoid(fabsf(x[c]))
+                     : near_exp(x[c] - top);
     total += q[c];
   }
   if (renorm) return lanes_sum<L>(total);

@@ -24,6 +24,21 @@ def _grid(T, E, seed, low, high):
     return rng.integers(int(low * 64), int(high * 64), (T, E)).astype(np.float64) / 64, rng
 
 
+@pytest.mark.parametrize("score,renorm", [("softmax", True), ("sigmoid", False), ("sigmoid", True)])
+@pytest.mark.parametrize("E,K", [(24, 8), (200, 20), (300, 8)])
+def test_gates_to_the_last_bits(gpu, score, renorm, E, K):
+    """Replayed picks with scores down to e^-80 of the largest."""
+    from paper_2606_11867_amd import api
+    l, rng = _grid(40, E, E, -80, 1)
+    ids = np.argsort(rng.random((40, E)), axis=1)[:, :K].astype(np.int32)
+    x = torch.from_numpy(l.astype(np.float32)).to(gpu)
+    ref = S.router_forward(l, K, score=score, renorm=renorm, ids=ids)
+    for stats in (False, True):
+        r = api.router_fwd(x, K, score=score, renorm=renorm, ids=torch.from_numpy(ids).to(gpu), stats=stats)
+        rel = np.abs(r.gates.double().cpu().numpy() / ref["gates"] - 1)
+        assert rel.max() <= 24 * U, rel.max() / U
+
+
 @pytest.mark.parametrize("E,K", [(24, 8), (200, 20), (300, 8)])
 @pytest.mark.parametrize("where", ["all", "some"])
 def test_sigmoid_scores_too_small_for_fp32(gpu, E, K, where):
