@@ -109,15 +109,6 @@ __device__ __forceinline__ float lanes_sum(float v) {
   return reduce<L>(v, [](float a, float b) { return a + b; });
 }
 template <int L>
-__device__ __forceinline__ int lanes_sum_int(int v) {
-  v += rotated<0x128>(v);
-  v += rotated<0x124>(v);
-  v += rotated<0x122>(v);
-  v += rotated<0x121>(v);
-  if constexpr (L == 64) v = across_rows(v, [](int a, int b) { return a + b; });
-  return v;
-}
-template <int L>
 __device__ __forceinline__ uint32_t lanes_max_uint(uint32_t v) {
   v = max(v, (uint32_t)rotated<0x128>((int)v));
   v = max(v, (uint32_t)rotated<0x124>((int)v));
@@ -574,14 +565,16 @@ __global__ __launch_bounds__(kRouterThreads) void router_bwd_kernel(RouterArgs a
   const bool through_pi = !sig && !renorm;  // the gates' gradient goes through the whole softmax
   float push[V] = {};  // balance gradient of pi
   if (balance) {
-    // a token's lanes hold all the counts
-    int count[V], total = 0;
+    // a token's lanes hold all the counts; the total of many ranks' may pass 32
+    // bits as a whole number
+    int count[V];
     load_experts<L, V>(a.counts, a.E, lane, count);
+    float total = 0.0f;
 #pragma unroll
-    for (int j = 0; j < V; ++j) total += count[j];
+    for (int j = 0; j < V; ++j) total += (float)count[j];
     const int n = *a.n_tokens;
-    total = lanes_sum_int<L>(total);
-    const float k = a.coef * (float)a.E / (float)max(n, 1) / (float)max(total, 1);
+    total = lanes_sum<L>(total);
+    const float k = a.coef * (float)a.E / (float)max(n, 1) / fmaxf(total, 1.0f);
 #pragma unroll
     for (int j = 0; j < V; ++j) push[j] = k * (float)count[j];
   }

@@ -84,6 +84,25 @@ def test_sigmoid_scores_too_small_for_fp32(gpu, E, K, where):
                 assert np.abs(want).max() > 0
 
 
+def test_counts_of_many_ranks(gpu):
+    """Counts that fit 32 bits each, their total not."""
+    from paper_2606_11867_amd import api
+    T, E, K = 50, 40, 4
+    x, rng = base._logits(T, E, torch.float32, seed=9)
+    counts = rng.integers(1 << 28, (1 << 31) - 1, E).astype(np.int32)
+    counts[3] = 0
+    n = (1 << 31) - 1
+    l = x.double().numpy()
+    for score in ("softmax", "sigmoid"):
+        want = S.router_backward(l, np.zeros((T, K), np.int32), None, score=score, counts=counts.astype(np.int64),
+                                 n_tokens=n, balance_coef=1e9)
+        got = api.router_bwd(x.to(gpu), torch.zeros(T, K, dtype=torch.int32, device=gpu), None, score=score,
+                             counts=torch.from_numpy(counts).to(gpu),
+                             n_tokens=torch.tensor([n], dtype=torch.int32, device=gpu), balance_coef=1e9)
+        c = 1e9 * E / n * counts / counts.astype(np.int64).sum()
+        base._check("dlogits", got, want, 8 * base._rel(l, E) * c.max())
+
+
 MORE = [
     # T, E, K, dtype, score, renorm, bias, mask, replay, disabled, pad: places over several registers, few experts
     (70, 100, 40, "f32", "softmax", True, False, True, False, 0, 0),
