@@ -213,8 +213,13 @@ def ffn_workspace(device) -> torch.Tensor:
     return torch.zeros(n, dtype=torch.uint8, device=device)
 
 
-def _ws(ws: Optional[torch.Tensor]):
-    return (None, 0) if ws is None else (ws.data_ptr(), ws.numel())
+def _ws(ws: Optional[torch.Tensor], device: torch.device):
+    """A workspace's address and size: memory of the device that the call runs on."""
+    if ws is None:
+        return None, 0
+    if ws.device != device:
+        raise ValueError(f"the workspace is on {ws.device}, not {device}")
+    return _ptr(ws), ws.numel()
 
 
 def grouped_ffn_fwd(x_perm: torch.Tensor, slot_offset: torch.Tensor, slot_widx: torch.Tensor,
@@ -231,7 +236,7 @@ def grouped_ffn_fwd(x_perm: torch.Tensor, slot_offset: torch.Tensor, slot_widx: 
     check(_lib.load().foremoe_grouped_ffn_fwd(_ptr(x_perm), _dt(x_perm), d, F, S, _ptr(slot_offset),
                                               _ptr(slot_widx), W, _ptr(w_gate_up), _ptr(w_down), n_cap,
                                               h.data_ptr(), y_perm.data_ptr(),
-                                              None if save_au is None else save_au.data_ptr(), *_ws(ws),
+                                              None if save_au is None else save_au.data_ptr(), *_ws(ws, dev),
                                               _stream(dev)),
           "foremoe_grouped_ffn_fwd")
     return h, y_perm, save_au
@@ -250,7 +255,7 @@ def grouped_ffn_dgrad(dy_perm: torch.Tensor, save_au: torch.Tensor, slot_offset:
     check(_lib.load().foremoe_grouped_ffn_dgrad(_ptr(dy_perm), _ptr(save_au), _dt(dy_perm), d, F, S,
                                                 _ptr(slot_offset), _ptr(slot_widx), W, _ptr(w_gate_up),
                                                 _ptr(w_down), n_cap, d_au.data_ptr(), dx_perm.data_ptr(),
-                                                *_ws(ws), _stream(dev)), "foremoe_grouped_ffn_dgrad")
+                                                *_ws(ws, dev), _stream(dev)), "foremoe_grouped_ffn_dgrad")
     return d_au, dx_perm
 
 
@@ -451,7 +456,7 @@ def router_fwd(logits: torch.Tensor, K: int, *, score: str = "softmax", renorm: 
         loss = torch.empty_like(n_tokens, dtype=torch.float32)
         if ws is None:
             ws = router_workspace(E, dev)
-        sp = (counts.data_ptr(), n_tokens.data_ptr(), prob_mean.data_ptr(), loss.data_ptr(), _ptr(ws), ws.numel())
+        sp = (counts.data_ptr(), n_tokens.data_ptr(), prob_mean.data_ptr(), loss.data_ptr(), *_ws(ws, dev))
     else:
         sp = (None, None, None, None, None, 0)
     check(_lib.load().foremoe_router_fwd(
@@ -520,7 +525,7 @@ def token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = None,
     p = lambda t: None if t is None else t.data_ptr()  # noqa: E731
     check(_lib.load().foremoe_token_logprobs(
         logits.data_ptr(), _dt(logits), ld, N, V, _vec(targets, N, torch.int32, "targets", dev), temperature, n_top,
-        p(logp), entropy.data_ptr(), lse.data_ptr(), p(top_ids), p(top_logp), *_ws(ws), _stream(dev)),
+        p(logp), entropy.data_ptr(), lse.data_ptr(), p(top_ids), p(top_logp), *_ws(ws, dev), _stream(dev)),
         "foremoe_token_logprobs")
     return TokenLogprobs(logp, entropy, lse, top_ids, top_logp)
 
