@@ -124,9 +124,10 @@ __device__ __forceinline__ float decode_v(uint32_t c, float scale) {
 // Correctly rounded square root and reciprocal of numbers from 2^-90 on (the
 // reciprocal to 2^120): the hardware's, within a unit in the last place,
 // corrected once by a residual that a fused multiply-add gives exactly (P.
-// Markstein's method). Equal to the compiler's sqrtf and division for every
-// one of these numbers, in 11 and 7 instruction slots where those take 18 and
-// 15.
+// Markstein's method), in 11 and 7 instruction slots where the compiler's take
+// 18 and 15. For a reciprocal the method proves all but the significand of all
+// ones, where it depends on the estimate; with this hardware's it is right
+// there too. The tests go over every significand of both.
 constexpr float kExactFrom = 0x1p-90f, kExactTo = 0x1p120f;
 __device__ __forceinline__ float exact_sqrt(float x) {
   const float s = __builtin_amdgcn_sqrtf(x), h = 0.5f * __builtin_amdgcn_rsqf(x);

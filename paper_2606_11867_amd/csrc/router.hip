@@ -155,8 +155,9 @@ __device__ __forceinline__ float near_exp(float d) {
 }
 // The sigmoid of the definition's four fp32 operations, each rounded, where a
 // score plus a bias decides. The quotient is the hardware's reciprocal
-// corrected by its residual, correctly rounded up to 2^120 (P. Markstein's
-// method; equal to the division for every such number).
+// corrected by its residual, correctly rounded up to 2^120 as the optimizer's
+// (P. Markstein's method; adamw.hip has what holds for a significand of all
+// ones).
 template <int V>
 __device__ __forceinline__ void exact_sigmoids(const float (&v)[V], float (&s)[V]) {
   bool far = false;

@@ -77,6 +77,19 @@ def test_eps_below_the_normal_numbers(gpu, bits):
     assert torch.all((p - want).abs() <= 64 * U * want.abs())
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [32, 8])
+def test_no_gradient_and_no_eps_is_no_move(gpu, bits):
+    from paper_2606_11867_amd.optimizer import AdamW
+    ps = [torch.zeros(n, device=gpu) for n in (1, 255, 256, 700)]
+    gs = [torch.zeros_like(p) for p in ps]
+    opt = AdamW(ps, gs, lr=0.5, eps=0.0, state_bits=bits)
+    for _ in range(2):
+        opt.step()
+    for p in ps:
+        assert torch.all(p == 0)
+
+
 # ---------------------------------------------------------------------------
 # The last bit. A quotient 1 / x and a square root of fp32 numbers, taken in
 # 64 bits and rounded to 32, are correctly rounded (64 bits have more than
@@ -101,3 +114,74 @@ def _beside_the_boundaries(scale, table):
     a = (scale.double()[:, None] * mid).float()
     bits = a.view(torch.int32)
     return torch.cat([scale[:, None], a, (bits - 1).view(F32), (bits + 1).view(F32)], 1)
+
+
+def test_boundaries_tell_a_neighbouring_reciprocal():
+    """On the CPU: a reciprocal that is off by one unit in the last place
+    gives other codes of the blocks below, the all-ones significand's too."""
+    rng = np.random.default_rng(5)
+    bits = np.concatenate([rng.integers(0x3F800001, 0x40000000, 200), [0x3FFFFFFF, 0x3F800001]]).astype(np.int32)
+    scale = torch.from_numpy(bits.view(np.float32))
+    a = _beside_the_boundaries(scale, S.TABLE_M)
+    right = (1.0 / scale.double()).float()
+    for step in (-1, 1):
+        off = (right.view(torch.int32) + step).view(F32)
+        same = (_rounded_codes(a * right[:, None], 20, 127, 0) == _rounded_codes(a * off[:, None], 20, 127, 0)).all(1)
+        assert not same.any()
+
+
+@pytest.mark.gpu
+def test_reciprocal_of_every_significand(gpu):
+    """Blocks whose scale has each of the 2^23 significands, with elements at
+    the boundaries of the codes: codes as with 1 / scale rounded once. The
+    method's known exception, a significand of all ones, is among them."""
+    from paper_2606_11867_amd.optimizer import AdamW
+    g = torch.empty(CHUNK * BLOCK, device=gpu)
+    p = torch.zeros_like(g)
+    opt = AdamW([p], [g], lr=0.0, betas=(0.0, 0.0), state_bits=8)  # m = g
+    for first in range(0, 1 << 23, CHUNK):
+        if first % (CHUNK * 64) == 0:
+            print(f"[case] significands from {first}", flush=True)
+        # exponents from 2^-60 to 2^60 in turn
+        i = torch.arange(first, first + CHUNK, device=gpu, dtype=torch.int32)
+        scale = (i | ((127 - 60 + (first // CHUNK) % 121) << 23)).view(F32)
+        a = _beside_the_boundaries(scale, S.TABLE_M)
+        g.copy_(a.reshape(-1))
+        opt.step()
+        want = _rounded_codes((a * (1.0 / scale.double()).float()[:, None]), 20, 127, 0)
+        assert torch.equal(opt.states[0][2], scale)
+        assert torch.equal(opt.states[0][0], want.reshape(-1)), first
+
+
+@pytest.mark.gpu
+def test_square_root_of_every_significand(gpu):
+    """Every second moment from 1 to 4 (each significand at both parities of
+    the exponent), and as many spread over the exponents, made exactly from an
+    old moment and a gradient; its root is the block's scale."""
+    from paper_2606_11867_amd.optimizer import AdamW
+    g = torch.zeros(CHUNK, BLOCK, device=gpu)
+    p = torch.zeros(CHUNK * BLOCK, device=gpu)
+    opt = AdamW([p], [g.view(-1)], lr=0.0, betas=(0.0, 0.5), state_bits=8)
+    m, v, ms, vs = opt.states[0]
+    missed = 0
+    for first in range(0, 1 << 24, CHUNK):
+        if first % (CHUNK * 128) == 0:
+            print(f"[case] patterns from {first}", flush=True)
+        i = torch.arange(first, first + CHUNK, device=gpu, dtype=torch.int32)
+        for spread in (False, True):
+            e = 2 * (((first // CHUNK) * 37) % 100 - 42) if spread else 0  # 2^-84 to 2^114
+            target = (i + 0x3F800000).view(F32) * 2.0 ** e
+            # (s^2 + g^2) / 2, each square rounded
+            s = torch.sqrt(2 * target.double()).float()
+            s = torch.where(s * s > 2 * target, (s.view(torch.int32) - 1).view(F32), s)
+            rest = 2 * target - s * s
+            small = torch.sqrt(rest.double()).float()
+            made = (s * s) * 0.5 + (small * small) * 0.5
+            missed += int((made != target).sum())
+            v.zero_()
+            v.view(CHUNK, BLOCK)[:, 0] = 255
+            vs.copy_(s)
+            g[:, 0] = small
+            opt.step()
+            assert torch.equal(vs, torch.sqrt(made.double()).float()), (first, spread)
+    assert missed == 0
