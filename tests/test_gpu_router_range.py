@@ -114,3 +114,86 @@ MORE = [
     (45, 255, 48, "f32", "softmax", False, False, False, False, 0, 0),
     (45, 250, 64, "f32", "softmax", True, False, True, True, 3, 2),
 ]
+
+
+@pytest.mark.parametrize("case", MORE, ids=lambda c: "T{}-E{}-K{}-{}-{}".format(*c[:5]))
+def test_many_places(gpu, case):
+    base.test_router_forward_and_backward(gpu, case)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("T,E,K", [(37, 300, 8), (21, 1000, 20), (90, 100, 6), (31, 90, 30), (29, 256, 40)])
+def test_picks_by_score_plus_bias(gpu, dt, T, E, K):
+    """Biases and scores that keep the sums of a token apart by more than
+    their rounding."""
+    from paper_2606_11867_amd import api
+    dtype = torch.bfloat16 if dt == "bf16" else torch.float32
+    rng = np.random.default_rng(E + K)
+    # biases 2^-10 apart in a random order, scores within 2^-11 of one half; and a few that stand out
+    bias = (rng.permutation(E) - E / 2).astype(np.float32) * np.float32(2.0 ** -10)
+    x = torch.from_numpy((rng.random((T, E)) * 0.0015).astype(np.float32))
+    for t in range(T):
+        x[t, rng.integers(0, E)] = 3.0
+        x[t, rng.integers(0, E, 5)] = -np.inf
+    x[1] = -np.inf
+    x = x.to(dtype)
+    l = x.double().numpy()
+    key = np.where(l > -np.inf, 1 / (1 + np.exp(-l)) + bias.astype(np.float64), -100.0 - np.arange(E))
+    key = np.sort(key, axis=1)
+    assert np.diff(key, axis=1)[:, -K - 1:].min() > 8 * 2.0 ** -23
+    mask = np.arange(T) % 5 != 2
+    for renorm in (True, False):
+        kw = dict(score="sigmoid", renorm=renorm, scale=2.5)
+        ref = S.router_forward(l, K, bias=bias.astype(np.float64), mask=mask, **kw)
+        r = api.router_fwd(x.to(gpu), K, bias=torch.from_numpy(bias).to(gpu), mask=torch.from_numpy(mask).to(gpu), **kw)
+        assert np.array_equal(r.ids.cpu().numpy(), ref["ids"])
+        assert np.array_equal(r.counts.cpu().numpy(), ref["counts"])
+        rel = base._rel(l, E)
+        base._check("gates", r.gates, ref["gates"], rel * ref["gates"] + 1e-30)
+        base._check("prob_mean", r.prob_mean, ref["prob_mean"], (rel + 65 * U) * ref["prob_mean"] + 1e-30)
+
+
+@pytest.mark.parametrize("T,E,K,dt", [(33003, 8, 2, "f32"), (20000, 24, 3, "bf16"), (5000, 300, 2, "bf16")])
+@pytest.mark.parametrize("replay", [False, True])
+def test_statistics_past_the_first_pass(gpu, T, E, K, dt, replay):
+    """More tokens than the workgroups that leave statistics take at once."""
+    from paper_2606_11867_amd import api
+    print(f"\n[case] statistics T={T} E={E} replay={replay}", flush=True)
+    x, rng = base._logits(T, E, torch.bfloat16 if dt == "bf16" else torch.float32, seed=T)
+    l = x.double().numpy()
+    ids = rng.integers(0, E, (T, K)).astype(np.int32) if replay else None
+    mask = rng.random(T) < 0.9
+    ref = S.router_forward(l, K, ids=ids, mask=mask)
+    r = api.router_fwd(x.to(gpu), K, ids=None if ids is None else torch.from_numpy(ids).to(gpu),
+                       mask=torch.from_numpy(mask).to(gpu))
+    assert np.array_equal(r.ids.cpu().numpy(), ref["ids"])
+    assert np.array_equal(r.counts.cpu().numpy(), ref["counts"])
+    assert int(r.n_tokens) == ref["n_tokens"]
+    rel = base._rel(l, E)
+    sums = rel + U * (T / 256 + 64)
+    base._check("gates", r.gates, ref["gates"], rel * ref["gates"] + 1e-30)
+    base._check("prob_mean", r.prob_mean, ref["prob_mean"], sums * ref["prob_mean"])
+    base._check("balance_loss", r.balance_loss, np.array([ref["balance_loss"]]),
+                (sums + U * (E + 64)) * ref["balance_loss"])
+
+
+@pytest.mark.parametrize("T,E,K,most", [(140000, 8, 2, 131072), (33000, 260, 3, 32768)])
+def test_backward_past_the_first_pass(gpu, T, E, K, most):
+    """More tokens than the backward's workgroups take at once: rows from the
+    start, around the end of the first pass and from the end."""
+    from paper_2606_11867_amd import api
+    x, rng = base._logits(T, E, torch.float32, seed=T)
+    ids = rng.integers(0, E, (T, K)).astype(np.int32)
+    dg = rng.standard_normal((T, K)).astype(np.float32)
+    counts = rng.integers(0, 1000, E).astype(np.int32)
+    rows = np.concatenate([np.arange(40), np.arange(most - 40, most + 40), np.arange(T - 40, T),
+                           rng.integers(0, T, 60)])
+    n = 777
+    got = api.router_bwd(x.to(gpu), torch.from_numpy(ids).to(gpu), torch.from_numpy(dg).to(gpu),
+                         counts=torch.from_numpy(counts).to(gpu),
+                         n_tokens=torch.tensor([n], dtype=torch.int32, device=gpu), balance_coef=0.5)
+    l = x.double().numpy()[rows]
+    want = S.router_backward(l, ids[rows], dg[rows], counts=counts, n_tokens=n, balance_coef=0.5)
+    size = np.abs(dg).max() + 0.5 * E / n
+    base._check("dlogits", got[torch.from_numpy(rows).to(gpu)], want, 8 * base._rel(l, E) * size)
+    assert torch.all(got.double().sum(1).abs() < 1e-5)  # every row: a softmax's gradients sum to 0
