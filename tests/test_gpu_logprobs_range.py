@@ -85,3 +85,34 @@ def test_gradients_of_rows_far_from_zero_are_bounded(gpu, dtype, temperature):
     most = (2 * a.abs() + b.abs() * (0.5 + r.entropy)) / temperature
     assert torch.isfinite(d).all()
     assert torch.all(d.abs() <= 1.01 * most[:, None])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("N", [70001, (1 << 22) + 1003])
+def test_more_rows_than_a_launch_takes(gpu, dtype, N):
+    """Short rows past the backward's 65535 and the forward's 2^22: rows from
+    the start, around every end of a launch and from the end."""
+    from paper_2606_11867_amd import api
+    print(f"\n[case] logprobs rows N={N}", flush=True)
+    V = 9
+    gen = torch.Generator(device=gpu).manual_seed(N)
+    x = (torch.randn(N, V, generator=gen, device=gpu) * 3).to(dtype)
+    t = torch.randint(-1, V, (N,), generator=gen, device=gpu).to(torch.int32)
+    a, b = torch.randn(N, generator=gen, device=gpu), torch.randn(N, generator=gen, device=gpu)
+    r = api.token_logprobs(x, t, n_top=2, ws=api.logprobs_workspace(gpu))
+    d = api.token_logprobs_bwd(x, t, r.lse, a, entropy=r.entropy, dentropy=b)
+    ends = [0, N] + list(range(65535, N, 65535))[:3] + list(range(65535, N, 65535))[-3:] + [1 << 22]
+    rows = np.unique(np.concatenate([np.arange(e - 20, e + 20) for e in ends]))
+    rows = rows[(rows >= 0) & (rows < N)]
+    pick = torch.from_numpy(rows).to(gpu)
+    l, tt, an, bn = x[pick].double().cpu().numpy(), t[pick].cpu().numpy(), a[pick].cpu().numpy(), b[pick].cpu().numpy()
+    ref = S.token_logprobs(l, tt, n_top=2)
+    tol = U * (16 * np.abs(l).max() + V / 256 + 128)
+    base._close("logp", r.logp[pick], ref["logp"], tol)
+    base._close("entropy", r.entropy[pick], ref["entropy"], tol * (2 + ref["entropy"]))
+    assert np.array_equal(r.top_ids[pick].cpu().numpy(), ref["top_ids"])
+    want = S.token_logprobs_backward(l, tt, an, bn)
+    size = (np.abs(an) + np.abs(bn) * (2 + ref["entropy"]) * 2)[:, None]
+    base._close("dlogits", d[pick], want, 4 * tol * size)
+    # every row: the gradients of a softmax sum to 0, each within 2^-8 of itself at worst
+    assert torch.all(d.float().sum(1).abs() <= 2.0 ** -8 * (2 * a.abs() + 2 * b.abs() * r.entropy.abs()) + 1e-4)
