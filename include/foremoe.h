@@ -628,8 +628,11 @@ int foremoe_plan_rank_slots(const int32_t* copy_rank, int32_t E, int32_t C_max, 
  *   counts[e] picks of expert e, n_tokens[0] tokens, prob_mean[e] the mean
  *   of pi_e (0 without tokens), and with f_e = counts[e] / sum(counts)
  *   balance_loss[0] = E * sum_e f_e * prob_mean[e], 1 for an even load.
- *   A NaN or +inf logit makes pi NaN, and the gates that it enters; ids
- *   stay in range.
+ *   A NaN logit makes pi NaN, and the gates that it enters; so does +inf with
+ *   softmax scores (a sigmoid's is 1). Ids stay in range.
+ *   A gate is as exact as the fp32 difference of its logit from the largest
+ *   one, ratios of sigmoid scores that are themselves too small for fp32
+ *   included; with a bias the picks compare fp32 scores.
  * logits [T, E] of dtype; bias [E] fp32 or NULL; mask [T] bytes or NULL;
  * ids [T, K] out (may be ids_in); gates [T, K] fp32 out. 1 <= E <=
  * FOREMOE_MAX_EXPERTS, 1 <= K <= min(E, FOREMOE_MAX_TOPK), T*K < 2^31.
@@ -736,6 +739,8 @@ int foremoe_token_logprobs_bwd(const void* logits, foremoe_dtype dtype, int64_t 
  *   shows it at the next step. Zero-filled states are the start.
  * tensors: HOST array, read during the call only; pointers aligned to their
  * types. n = 0: skipped. One launch for every FOREMOE_ADAMW_LAUNCH tensors.
+ * The launches carry the tensors, the rates and the step number: a captured
+ * call repeats that step, with what grad_scale then holds.
  */
 #define FOREMOE_ADAMW_BLOCK 256
 #define FOREMOE_ADAMW_LAUNCH 48

@@ -127,7 +127,9 @@ __device__ __forceinline__ void unpack(u32x4 v, float* x) {
 // cancels. m starts at the lowest finite number, so an x of -inf adds nothing
 // to s. Where m c is so large that its rounding is no small part of a y (a row
 // that a mask fills with -1e9, or the type's ends), x - m is taken first and
-// then scaled: m c itself is the reference.
+// then scaled: m c itself is the reference. Powers and logarithms are the
+// hardware's, within a unit in the last place; a y is within |y| 2^-24 of its
+// value, as a scaled logit is in fp32.
 __device__ __forceinline__ bool huge(float mc) { return !(fabsf(mc) < 0x1p24f); }
 
 // Either kind of reference, exactly.

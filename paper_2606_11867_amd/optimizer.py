@@ -152,7 +152,8 @@ class AdamW:
     def step(self, lr: Optional[float] = None, grad_scale: Optional[torch.Tensor] = None) -> None:
         """One step on the current stream. lr: from now on. grad_scale: a
         device fp32 scalar that every gradient is multiplied by (clipping,
-        loss scaling)."""
+        loss scaling). Captured in a graph, a replay is this step again, with
+        this step's number, lr and tensors."""
         if lr is not None:
             self.lr = lr
         # a tensor was given other memory, or a weight decay was changed

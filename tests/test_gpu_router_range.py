@@ -197,3 +197,33 @@ def test_backward_past_the_first_pass(gpu, T, E, K, most):
     size = np.abs(dg).max() + 0.5 * E / n
     base._check("dlogits", got[torch.from_numpy(rows).to(gpu)], want, 8 * base._rel(l, E) * size)
     assert torch.all(got.double().sum(1).abs() < 1e-5)  # every row: a softmax's gradients sum to 0
+
+
+@pytest.mark.parametrize("E", [12, 128, 700])
+def test_sigmoid_of_nan_and_infinity(gpu, E):
+    """A NaN makes the shares NaN and a gate only where it enters; the score
+    of +inf is 1, that of -inf is out of service."""
+    from paper_2606_11867_amd import api
+    K = 4
+    x, _ = base._logits(6, E, torch.float32, seed=E)
+    x[1, 3] = float("nan")
+    x[2, 5] = float("inf")
+    x[3, 1::2] = -float("inf")
+    l = x.double().numpy()
+    for renorm in (True, False):
+        r = api.router_fwd(x.to(gpu), K, score="sigmoid", renorm=renorm)
+        ids, g = r.ids.cpu().numpy(), r.gates.double().cpu().numpy()
+        assert 3 not in ids[1] and ids[2, 0] == 5 and np.all(ids[3] % 2 == 0) and ids.min() >= 0 and ids.max() < E
+        assert torch.isnan(r.prob_mean).all()
+        rows = [0, 2, 3, 4, 5]
+        ref = S.router_forward(l[rows], K, score="sigmoid", renorm=renorm)
+        assert np.array_equal(ids[rows], ref["ids"])
+        assert np.all(np.abs(g[rows] / ref["gates"] - 1) <= 24 * U)
+        assert np.isfinite(g[1]).all()  # the NaN was not picked
+        clean = api.router_fwd(x[rows].to(gpu), K, score="sigmoid", renorm=renorm)
+        base._check("prob_mean", clean.prob_mean, ref["prob_mean"], (base._rel(l, E) + 65 * U) * ref["prob_mean"])
+        d = api.router_bwd(x.to(gpu), r.ids, torch.ones(6, K, device=gpu), score="sigmoid", renorm=renorm).cpu()
+        assert torch.isfinite(d[rows]).all()
+        replay = torch.zeros(6, K, dtype=torch.int32, device=gpu) + torch.tensor([3, 0, 2, 4], device=gpu)
+        q = api.router_fwd(x.to(gpu), K, score="sigmoid", renorm=renorm, ids=replay.int(), stats=False).gates.cpu()
+        assert torch.isnan(q[1, 0]) and torch.isfinite(q[[0, 2, 4, 5]]).all()
