@@ -5,10 +5,10 @@
 // cleared fp32 gradients, 16 with 8-bit moments and bf16 gradients. There the
 // vector units come near as well: about 60 instruction slots an element for
 // decoding, an exact square root, two maxima and encoding. Measured on MI355X:
-//   75.5 M elements, 32 bits, masters, cleared gradients  392-448 us, 5.7-6.5 TB/s
-//   the same with 8-bit states                            235-250 us, 6.7-7.1 TB/s
-//   68.9 M in 60 tensors, 8 bits, bf16 gradients          202-207 us, 5.4 TB/s
-//   40 tensors of 64 to 40000 elements                    4.8 us, one launch
+//   75.5 M elements, 32 bits, masters, cleared gradients  450-466 us, 5.5-5.7 TB/s
+//   the same with 8-bit states                            255-261 us, 6.4-6.5 TB/s
+//   68.9 M in 60 tensors, 8 bits, bf16 gradients          173-185 us, 6.0-6.4 TB/s, two launches
+//   40 tensors of 64 to 40000 elements                    4.9 us, one launch
 // Records travel in the kernel's arguments (4 KiB hold 48), so a step needs
 // no table in device memory; a workgroup finds its record by bisection.
 #include <limits.h>

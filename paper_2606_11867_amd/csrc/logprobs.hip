@@ -9,9 +9,9 @@
 // instruction slots an element (4 of them the exponential) against 13 that
 // fit in the time of 2 bytes. Measured on MI355X:
 //   8192 x 131072 bf16, a fifth ignored   258-270 us, 6.4-6.6 TB/s
-//   2045 x 32003 fp32                     51 us, 5.2 TB/s
-//   8192 x 131072 bf16, 20 alternatives   415 us, 5.2 TB/s
-//   1 x 131072 bf16: 6.1 us, with 20 alternatives 14.1 us: latency (pieces, their
+//   2045 x 32003 fp32                     47 us, 5.1 TB/s
+//   8192 x 131072 bf16, 20 alternatives   420 us, 5.1 TB/s
+//   1 x 131072 bf16: 7.2 us, with 20 alternatives 15.2 us: latency (pieces, their
 //   join and two rankings)
 // A row of few is cut into pieces; each leaves its sums and its sorted top
 // places in the workspace, and the last to finish, by a ticket, joins them in
@@ -19,7 +19,7 @@
 //
 // Backward: every gradient from its logit and four numbers of the row, one
 // read and one write: HBM-bound, forward and backward of 4096 x 131072 bf16
-// 467 us (2.8 GB, 6.0 TB/s).
+// 456-467 us (2.8 GB, 6.0-6.1 TB/s).
 #include <limits.h>
 #include <math.h>
 
@@ -63,7 +63,8 @@ constexpr int kMaxPieces = 16;
 constexpr int kFewRows = 256;    // fewer rows than this are cut into pieces
 // and into about so many of all rows (us at 256, 512, 1024: 64 x 131072 bf16
 // 10.5, 10.8, 13.4, with 20 places 23.0, 22.1, 22.1; 130 x 70001 fp32 with 20
-// places 32.2, 27.9, 30.9; 200 x 131072 16.5, 18.5, 22.1)
+// places 32.2, 27.9, 30.9; 200 x 131072 16.5, 18.5, 22.1): the rows with places
+// decide, those without would like fewer
 constexpr int kSplit = 512;
 constexpr int kMaxSplit = kSplit + kFewRows;
 static_assert(kMaxSplit >= kMaxPieces * (kFewRows / kMaxPieces));

@@ -9,10 +9,10 @@
 // thousand tokens a launch's round trips to memory. The picked logits are
 // read again by id, from cache, so that replayed and picked ids take one path.
 // Kernels' times on MI355X (us):
-//   24 x 128 bf16, 8 picks 3.5; 16384 x 128 fp32: 8.4 picked, 3.8 replayed
-//   32768 x 256 bf16: 12.5, with sigmoid scores and bias 22; fp32 replay 6.4
-//   statistics: 2 to 5 more in the kernel and one of 5.3 behind it
-//   backward: 16384 x 128 fp32 7.1, 32768 x 256 bf16 13.5-14.4
+//   24 x 128 bf16, 8 picks 3.5; 16384 x 128 fp32: 7.8 picked, 3.3-3.7 replayed
+//   32768 x 256 bf16: 12.1, with sigmoid scores and bias 22; replayed 4.7
+//   statistics: 2 to 5 more in the kernel and one of 5.4-5.7 behind it
+//   backward: 16384 x 128 fp32 6.4-7.3, 32768 x 256 bf16 13.0-14.1
 // Statistics: a workgroup sums its tokens' distributions in registers (fp32) and
 // counts picks in LDS, leaves them in the workspace, and router_stats_kernel
 // adds the workgroups' parts in a fixed order: no floating-point atomics. At
@@ -351,9 +351,9 @@ __device__ __forceinline__ void pick_keys(float (&key)[V], int K, int lane, int 
 // for a key that is never picked. All of a token's integers differ, so the
 // next one below the last pick is last + max(p - last) modulo 2^32 (what is
 // not below wraps round to less): a subtraction and half a maximum for each,
-// and nothing to take out. (32768 x 256: 19.7 -> 15.3 us. With the leading 24
-// bits of fp32 keys, and pick_keys where those do not decide, the kernel's
-// registers spilled: 8.1 -> 12.8 us for a replay.)
+// and nothing to take out. (32768 x 256: 19.7 -> 15.3 us. The leading 24 bits
+// of fp32 keys, with pick_keys where those do not decide, were tried while one
+// kernel found ids in every way, and its registers spilled; not since.)
 template <int L, int V, int C>
 __device__ __forceinline__ void pick_packed(const float (&key)[V], int K, int lane, int (&id)[C]) {
   constexpr uint32_t kIds = L == 16 ? 0xff : 0x3ff;
