@@ -21,7 +21,11 @@
  *
  *   plus the operators around the layer in a policy-update step:
  *   foremoe_router_* (ids, gates, balance loss), foremoe_token_logprobs*
- *   and foremoe_adamw_*.
+ *   and foremoe_adamw_*;
+ *
+ *   and those that take the weights from an update to the rollout:
+ *   foremoe_muon_step, foremoe_mxfp4_*, foremoe_grouped_ffn_mxfp4_fwd and
+ *   foremoe_few_tokens_ffn*.
  *
  * Conventions (all entry points):
  *  - Every pointer argument is a DEVICE pointer unless stated otherwise; the
@@ -767,6 +771,156 @@ int foremoe_adamw_step(const foremoe_adamw_tensor* tensors, int32_t n_tensors,
 int foremoe_adamw_state_values(const uint8_t* m, const float* m_scale, const uint8_t* v,
                                const float* v_scale, int64_t n, float* m_out, float* v_out,
                                void* stream);
+
+/*
+ * From an update to the rollout: the Muon step that updates the experts'
+ * matrices, their quantisation to microscaled 4-bit floats, the expert FFN in
+ * those for prompts, and the whole expert layer for the few tokens of a
+ * decoding step.
+ *
+ * Microscaled 4-bit floats (MXFP4). FOREMOE_MX_BLOCK consecutive elements of
+ * a row share a scale 2^e, and an element is a sign and one of 0, 0.5, 1, 1.5,
+ * 2, 3, 4, 6 (the low three bits of its code, the sign above them) times the
+ * scale. e is the least exponent at which the block's largest magnitude is
+ * below 7 * 2^e, so that it rounds to 6 * 2^e at most, within [-127, 125];
+ * elements are rounded to nearest, ties to the even code, and what exceeds
+ * 7 * 2^125 is held as 6 * 2^125. A scale is the byte e + 127; 255 makes its
+ * block NaN, as a NaN or infinite element does.
+ * A matrix [rows, cols] is codes [rows, 16 * ceil(cols / 32)] bytes, element j
+ * of a row in byte j / 2 (the even one in the low half), and scales [rows,
+ * ceil(cols / 32)] bytes. A row's last block may be short: its other codes
+ * are 0.
+ */
+#define FOREMOE_MX_BLOCK 32
+/*
+ * Quantise x [rows, cols] of dtype, rows ld elements apart (any alignment that
+ * the type has). codes 16-byte aligned, scales any. n_rows NULL, or a device
+ * int32: only the rows below it are read and written (slot_offset + S of a
+ * gathered buffer whose rows end there). 0 <= rows < 2^31, 1 <= cols < 2^31.
+ */
+int foremoe_mxfp4_quantize(const void* x, foremoe_dtype dtype, int64_t ld, int64_t rows,
+                           int64_t cols, const int32_t* n_rows, uint8_t* codes, uint8_t* scales,
+                           void* stream);
+/* The values that codes and scales stand for, out [rows, cols] of dtype, rows
+ * ld elements apart. Exact in either type, down to 2^-128 (half the least
+ * scale). */
+int foremoe_mxfp4_values(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t cols,
+                         void* out, foremoe_dtype dtype, int64_t ld, void* stream);
+
+/*
+ * Step 4, forward, with operands in 4 bits. For the rows of each slot j, with
+ * w = slot_widx[j] as in foremoe_grouped_ffn_fwd (a w outside [0, W): rows
+ * left as they were):
+ *   A = X Wg[w]^T, U = X Wu[w]^T,  H = silu(A) * U in fp32,
+ *   Y = Q(H) Wd[w]^T, Q quantising rows to MXFP4; fp32 accumulation.
+ * x_codes [n_cap, d / 2], x_scales [n_cap, d / 32]: the gathered rows, from
+ * foremoe_mxfp4_quantize. gate_up_codes [W, 2F, d / 2] with scales
+ * [W, 2F, d / 32], down_codes [W, d, F / 2] with scales [W, d, F / 32]: the
+ * weights' matrices quantised. y_perm [n_cap, d] bf16. Rows outside every
+ * slot are left as they were.
+ * d % 128 == 0, F % 128 == 0, 2 * d * F < 2^32 (else FOREMOE_EUNSUPPORTED).
+ * n_cap * max(d, F) < 2^38. Codes and y 16-byte aligned, scales 4-byte.
+ * ws: foremoe_ffn_mxfp4_workspace_size(n_cap, F) bytes, 256-byte aligned, for
+ * Q(H); needs no initialisation. Calls that share one must not overlap in
+ * time. Forward only: gradients go through the unquantised weights.
+ */
+size_t foremoe_ffn_mxfp4_workspace_size(int64_t n_cap, int32_t F);
+int foremoe_grouped_ffn_mxfp4_fwd(const uint8_t* x_codes, const uint8_t* x_scales, int32_t d,
+                                  int32_t F, int32_t S, const int32_t* slot_offset,
+                                  const int32_t* slot_widx, int32_t W, const uint8_t* gate_up_codes,
+                                  const uint8_t* gate_up_scales, const uint8_t* down_codes,
+                                  const uint8_t* down_scales, int64_t n_cap, void* y_perm, void* ws,
+                                  size_t ws_bytes, void* stream);
+
+/*
+ * The whole expert layer for a few tokens, from the router's ids and gates to
+ * the layer's output, in two launches that read each picked expert's weights
+ * once (steps 1-5 in one call; no permute, no plan):
+ *   y[t, :] = sum_{k ascending} gates[t, k] * Wd[w] (silu(Wg[w] x_t) * (Wu[w] x_t)),
+ *   w = expert_widx[ids[t, k]]
+ * over the places k whose id is in [0, E) and whose w is in [0, W) (the
+ * others count as 0 whatever their gate holds: padding, experts of other
+ * ranks); a token without any gets a zero row. Two places of a token may name
+ * one expert. The sums and the hidden rows are held in fp32.
+ * x [T, d] of dtype, rows ld elements apart; ids, gates [T, K]; expert_widx
+ * [E] int32 or NULL (the identity; then E <= W); w_gate_up [W, 2F, d] and
+ * w_down [W, d, F] as in foremoe_grouped_ffn_fwd, contiguous, of dtype, or of
+ * the _mxfp4 call in 4 bits (codes and scales as above), with bf16 x; y [T, d]
+ * of out_dtype. 0 <= T <= FOREMOE_FEW_TOKENS, 1 <= K <= FOREMOE_MAX_TOPK,
+ * T * K <= FOREMOE_FEW_PAIRS, 1 <= E <= FOREMOE_MAX_EXPERTS, 1 <= W <=
+ * FOREMOE_MAX_SLOTS. bf16 and fp32: any d, F >= 1 (rows of weights whose
+ * bytes are a multiple of 16 are read 16 bytes at a time, others element by
+ * element); _mxfp4: d and F multiples of 32.  2 * d * F < 2^31.
+ * Pointers aligned to their types, w_* and codes to 16 bytes.
+ * ws: foremoe_few_workspace_size(T, K, F) bytes for the hidden rows (one of
+ * the largest T, K and F serves smaller calls), 256-byte aligned; needs no
+ * initialisation. Calls that share one must not overlap in time.
+ */
+#define FOREMOE_FEW_TOKENS 128
+#define FOREMOE_FEW_PAIRS 2048
+size_t foremoe_few_workspace_size(int64_t T, int32_t K, int32_t F);
+int foremoe_few_tokens_ffn(const void* x, foremoe_dtype dtype, int64_t ld, int64_t T, int32_t d,
+                           int32_t F, const int32_t* ids, const float* gates, int32_t K, int32_t E,
+                           const int32_t* expert_widx, int32_t W, const void* w_gate_up,
+                           const void* w_down, void* y, foremoe_dtype out_dtype, void* ws,
+                           size_t ws_bytes, void* stream);
+int foremoe_few_tokens_ffn_mxfp4(const void* x, int64_t ld, int64_t T, int32_t d, int32_t F,
+                                 const int32_t* ids, const float* gates, int32_t K, int32_t E,
+                                 const int32_t* expert_widx, int32_t W,
+                                 const uint8_t* gate_up_codes, const uint8_t* gate_up_scales,
+                                 const uint8_t* down_codes, const uint8_t* down_scales, void* y,
+                                 foremoe_dtype out_dtype, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * One Muon step over many tensors, each a batch of matrices [rows, cols]:
+ *   g = grad * grad_scale[0]  (grad_scale NULL: 1)
+ *   m = momentum m + g,  u = g + momentum m (nesterov) or m
+ *   X = u / max(|u|, eps), |u| the Frobenius norm of the matrix (no move
+ *       where that is 0)
+ *   ns_steps times X = a X + (b G + c G G) X with G = X X^T, in the
+ *       transposed form where rows > cols; coef = {a, b, c}
+ *   p = p (1 - lr weight_decay) - lr scale X
+ * p is master where the record has one (param, of bf16, then gets its rounded
+ * copy), else param itself. zero_grads != 0: grad is zero afterwards.
+ * m, norms, X and all sums are fp32 (norms' sums fp64). The products' factors
+ * are X, G and b G + c G G rounded to fp16 (2^-11 of an element, or 2^-33
+ * where that is more); a X is of the unrounded X, so that directions that u
+ * does not have stay as small as fp32 holds them. X of the step is within
+ * about 2^-9 of its norm of the exact one. Coefficients that let singular
+ * values pass 100 overflow.
+ * A matrix with a NaN or infinite element, or whose u has one, becomes NaN;
+ * the others do not.
+ * tensors: HOST array, read during the call only; pointers aligned to their
+ * types; param, grad, master and m hold [batch, rows, cols] contiguous. batch
+ * = 0: skipped. batch <= 2^30, 1 <= rows, cols <= FOREMOE_MUON_SIDE,
+ * min(rows, cols) <= FOREMOE_MUON_RANK, and with both sides rounded up to 128
+ * at most 2^35 elements. 0 <= ns_steps <= 16.
+ * coef: HOST array of 3.
+ * ws: foremoe_muon_workspace_size(tensors, n_tensors) bytes, 256-byte aligned,
+ * needs no initialisation; calls that share one must not overlap in time.
+ * Captured in a graph, a replay repeats the call with the tensors and rates
+ * that it was captured with, and with what grad_scale then holds.
+ */
+#define FOREMOE_MUON_LAUNCH 24
+#define FOREMOE_MUON_SIDE (1 << 20)
+#define FOREMOE_MUON_RANK 16384
+typedef struct foremoe_muon_tensor {
+  void* param;   /* [batch, rows, cols] of param_dtype          */
+  void* grad;    /* [batch, rows, cols] of grad_dtype           */
+  float* master; /* the same, fp32, or NULL; bf16 parameters only */
+  float* m;      /* the same, fp32                              */
+  int64_t batch;
+  int32_t rows;
+  int32_t cols;
+  double weight_decay;
+  double scale;
+} foremoe_muon_tensor;
+size_t foremoe_muon_workspace_size(const foremoe_muon_tensor* tensors, int32_t n_tensors);
+int foremoe_muon_step(const foremoe_muon_tensor* tensors, int32_t n_tensors,
+                      foremoe_dtype param_dtype, foremoe_dtype grad_dtype, double lr,
+                      double momentum, int32_t nesterov, int32_t ns_steps, const double* coef,
+                      double eps, const float* grad_scale, int32_t zero_grads, void* ws,
+                      size_t ws_bytes, void* stream);
 
 /*
  * Timed forms of the four row-GEMM calls (a measurement aid, not an

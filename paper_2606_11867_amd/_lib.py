@@ -31,6 +31,9 @@ SOFTMAX = 0
 SIGMOID = 1
 MAX_TOP = 32
 ADAMW_BLOCK = 256
+MX_BLOCK = 32
+FEW_TOKENS = 128
+FEW_PAIRS = 2048
 
 c_i32, c_i64, c_sz, c_p = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_void_p
 c_f32, c_f64 = ctypes.c_float, ctypes.c_double
@@ -68,6 +71,14 @@ class AdamWTensor(ctypes.Structure):
 
 
 PAdamWTensor = ctypes.POINTER(AdamWTensor)
+
+
+class MuonTensor(ctypes.Structure):
+    _fields_ = [("param", c_p), ("grad", c_p), ("master", c_p), ("m", c_p), ("batch", c_i64), ("rows", c_i32),
+                ("cols", c_i32), ("weight_decay", c_f64), ("scale", c_f64)]
+
+
+PMuonTensor = ctypes.POINTER(MuonTensor)
 
 # name -> (restype, argtypes)
 SIGNATURES = {
@@ -132,6 +143,19 @@ SIGNATURES = {
     "foremoe_adamw_step": (ctypes.c_int, [PAdamWTensor, c_i32, c_i32, c_i32, c_i32, c_f64, c_f64, c_f64, c_f64, c_i64,
                                           c_p, c_i32, c_p]),
     "foremoe_adamw_state_values": (ctypes.c_int, [c_p, c_p, c_p, c_p, c_i64, c_p, c_p, c_p]),
+    "foremoe_mxfp4_quantize": (ctypes.c_int, [c_p, c_i32, c_i64, c_i64, c_i64, c_p, c_p, c_p, c_p]),
+    "foremoe_mxfp4_values": (ctypes.c_int, [c_p, c_p, c_i64, c_i64, c_p, c_i32, c_i64, c_p]),
+    "foremoe_ffn_mxfp4_workspace_size": (c_sz, [c_i64, c_i32]),
+    "foremoe_grouped_ffn_mxfp4_fwd": (ctypes.c_int, [c_p, c_p, c_i32, c_i32, c_i32, c_p, c_p, c_i32, c_p, c_p, c_p, c_p,
+                                                     c_i64, c_p, c_p, c_sz, c_p]),
+    "foremoe_few_workspace_size": (c_sz, [c_i64, c_i32, c_i32]),
+    "foremoe_few_tokens_ffn": (ctypes.c_int, [c_p, c_i32, c_i64, c_i64, c_i32, c_i32, c_p, c_p, c_i32, c_i32, c_p,
+                                              c_i32, c_p, c_p, c_p, c_i32, c_p, c_sz, c_p]),
+    "foremoe_few_tokens_ffn_mxfp4": (ctypes.c_int, [c_p, c_i64, c_i64, c_i32, c_i32, c_p, c_p, c_i32, c_i32, c_p,
+                                                    c_i32, c_p, c_p, c_p, c_p, c_p, c_i32, c_p, c_sz, c_p]),
+    "foremoe_muon_workspace_size": (c_sz, [PMuonTensor, c_i32]),
+    "foremoe_muon_step": (ctypes.c_int, [PMuonTensor, c_i32, c_i32, c_i32, c_f64, c_f64, c_i32, c_i32,
+                                         ctypes.POINTER(c_f64), c_f64, c_p, c_i32, c_p, c_sz, c_p]),
     "foremoe_ffn_gate_up_fwd_timed": (ctypes.c_int, [c_p, c_i32, c_i32, c_i32, c_i32, c_p, c_p, c_i32, c_p,
                                                      c_i64, c_p, c_p, c_p, c_sz, c_p, c_p, c_p]),
     "foremoe_ffn_down_fwd_timed": (ctypes.c_int, [c_p, c_i32, c_i32, c_i32, c_i32, c_p, c_p, c_i32, c_p, c_i64,

@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes
 from dataclasses import dataclass
-from typing import NamedTuple, Optional, Tuple
+from typing import NamedTuple, Optional, Tuple, Union
 
 import numpy as np
 import torch
@@ -374,7 +374,7 @@ def _rows(t: torch.Tensor, name: str) -> int:
         raise ValueError(f"{name}: expected [rows, columns]")
     rows, cols = t.shape
     by_row, by_col = t.stride()
-    if by_col != 1 and cols > 1:
+    if by_col != 1 and cols > 1 and rows > 0:
         raise ValueError(f"{name}: rows must be contiguous")
     if rows <= 1:
         return max(cols, 1)
@@ -564,6 +564,184 @@ def adamw_state_values(m: torch.Tensor, m_scale: torch.Tensor, v: torch.Tensor, 
         _vec(v, n, torch.uint8, "v", dev), _vec(v_scale, blocks, torch.float32, "v_scale", dev), n, m_out.data_ptr(),
         v_out.data_ptr(), _stream(dev)), "foremoe_adamw_state_values")
     return m_out, v_out
+
+
+# ---------------------------------------------------------------------------
+# Microscaled 4-bit floats, the expert FFN in them, and the layer for a few
+# tokens (see include/foremoe.h)
+# ---------------------------------------------------------------------------
+def _launch(device: torch.device, call, where: str) -> None:
+    """call() with the device current, as a launch on its stream needs it."""
+    if torch._C._cuda_getDevice() == device.index:
+        check(call(), where)
+    else:
+        with torch.cuda.device(device):
+            check(call(), where)
+
+
+class MXFP4(NamedTuple):
+    """A tensor [..., n] in 4 bits: codes [..., 16 * ceil(n / 32)] and scales
+    [..., ceil(n / 32)], uint8, both contiguous."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+
+
+def _mx_shape(n: int) -> Tuple[int, int]:
+    blocks = -(-n // _lib.MX_BLOCK)
+    return blocks * (_lib.MX_BLOCK // 2), blocks
+
+
+def _mx(q: MXFP4, lead: tuple, n: int, name: str, device: torch.device) -> Tuple[int, int]:
+    """The addresses of q's codes and scales, q checked to be of [*lead, n]."""
+    out = []
+    for t, cols, part in zip(q, _mx_shape(n), ("codes", "scales")):
+        if t.dtype != torch.uint8:
+            raise TypeError(f"{name}.{part} must be uint8")
+        if t.shape != (*lead, cols):
+            raise ValueError(f"{name}.{part}: {tuple(t.shape)}, {(*lead, cols)} expected")
+        if t.device != device:
+            raise ValueError(f"{name}.{part} is on {t.device}, not {device}")
+        out.append(_ptr(t))
+    return out[0], out[1]
+
+
+def _as_rows(t: torch.Tensor, name: str):
+    """(rows, columns, elements between rows) of [..., columns]: a matrix whose
+    rows may be apart, or a contiguous tensor."""
+    if t.dim() == 2:
+        return t.shape[0], t.shape[1], _rows(t, name)
+    if t.dim() < 1:
+        raise ValueError(f"{name}: expected [..., columns]")
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous device tensor, or [rows, columns]")
+    return (t.numel() // t.shape[-1] if t.shape[-1] else 0), t.shape[-1], t.shape[-1]
+
+
+def mxfp4_quantize(x: torch.Tensor, *, n_rows: Optional[torch.Tensor] = None, out: Optional[MXFP4] = None) -> MXFP4:
+    """x [..., n] (fp32 or bf16) in 4 bits, blocks of 32 along the last
+    dimension. n_rows: a device int32; only the rows below it are quantised, the
+    others' codes and scales keep what they held (slot_offset[-1:] of gathered
+    rows). out: where it goes."""
+    rows, cols, ld = _as_rows(x, "x")
+    dev = x.device
+    if out is None:
+        c, b = _mx_shape(cols)
+        out = MXFP4(torch.empty(*x.shape[:-1], c, dtype=torch.uint8, device=dev),
+                    torch.empty(*x.shape[:-1], b, dtype=torch.uint8, device=dev))
+        codes, scales = out.codes.data_ptr(), out.scales.data_ptr()
+    else:
+        codes, scales = _mx(out, tuple(x.shape[:-1]), cols, "out", dev)
+    n = _vec(n_rows, 1, torch.int32, "n_rows", dev)
+    _launch(dev, lambda: _lib.load().foremoe_mxfp4_quantize(x.data_ptr(), _dt(x), ld, rows, cols, n, codes, scales,
+                                                            _stream(dev)), "foremoe_mxfp4_quantize")
+    return out
+
+
+def mxfp4_values(q: MXFP4, n: Optional[int] = None, *, dtype: torch.dtype = torch.float32,
+                 out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The values that q stands for, [..., n] (n: by default whole blocks).
+    out: where they go (fp32 or bf16; the rows of a matrix may be apart)."""
+    dev = q.codes.device
+    lead = tuple(q.codes.shape[:-1])
+    n = q.scales.shape[-1] * _lib.MX_BLOCK if n is None else n
+    if out is None:
+        out = torch.empty(*lead, n, dtype=dtype, device=dev)
+    elif out.shape != (*lead, n) or out.device != dev:
+        raise ValueError("out must be [..., n] beside q")
+    codes, scales = _mx(q, lead, n, "q", dev)
+    rows, _, ld = _as_rows(out, "out")
+    _launch(dev, lambda: _lib.load().foremoe_mxfp4_values(codes, scales, rows, n, out.data_ptr(), _dt(out), ld,
+                                                          _stream(dev)), "foremoe_mxfp4_values")
+    return out
+
+
+def ffn_mxfp4_workspace(n_cap: int, F: int, device) -> torch.Tensor:
+    """Scratch of grouped_ffn_mxfp4_fwd, for the hidden rows in 4 bits."""
+    n = _lib.load().foremoe_ffn_mxfp4_workspace_size(n_cap, F)
+    if n == 0:
+        raise ValueError("invalid sizes (F must be a multiple of 128)")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def grouped_ffn_mxfp4_fwd(x_perm: MXFP4, slot_offset: torch.Tensor, slot_widx: torch.Tensor, w_gate_up: MXFP4,
+                          w_down: MXFP4, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """grouped_ffn_fwd's y_perm (bf16) with operands in 4 bits: gathered rows
+    [n_cap, d] and weights [W, 2F, d], [W, d, F], each from mxfp4_quantize; the
+    hidden rows are quantised on the way. ws: from ffn_mxfp4_workspace (one is
+    made when missing)."""
+    dev = x_perm.codes.device
+    if x_perm.codes.dim() != 2 or w_gate_up.codes.dim() != 3 or w_down.codes.dim() != 3:
+        raise ValueError("x_perm [n_cap, d], w_gate_up [W, 2F, d] and w_down [W, d, F] expected")
+    n_cap, W = x_perm.codes.shape[0], w_gate_up.codes.shape[0]
+    d, F = x_perm.scales.shape[1] * _lib.MX_BLOCK, w_gate_up.codes.shape[1] // 2
+    S = slot_widx.shape[0]
+    xc, xs = _mx(x_perm, (n_cap,), d, "x_perm", dev)
+    gc, gs = _mx(w_gate_up, (W, 2 * F), d, "w_gate_up", dev)
+    dc, ds = _mx(w_down, (W, d), F, "w_down", dev)
+    y = torch.empty(n_cap, d, dtype=torch.bfloat16, device=dev)
+    if ws is None and n_cap and F % 128 == 0:
+        ws = ffn_mxfp4_workspace(n_cap, F, dev)
+    _launch(dev, lambda: _lib.load().foremoe_grouped_ffn_mxfp4_fwd(
+        xc, xs, d, F, S, _vec(slot_offset, S + 1, torch.int32, "slot_offset", dev),
+        _vec(slot_widx, S, torch.int32, "slot_widx", dev), W, gc, gs, dc, ds, n_cap, y.data_ptr(), *_ws(ws, dev),
+        _stream(dev)), "foremoe_grouped_ffn_mxfp4_fwd")
+    return y
+
+
+def few_tokens_workspace(T: int, K: int, d: int, F: int, device) -> torch.Tensor:
+    """Scratch of few_tokens_ffn, for the hidden rows; one of the largest T, K
+    and F serves smaller calls too."""
+    n = _lib.load().foremoe_few_workspace_size(T, K, F)
+    if n == 0:
+        raise ValueError(f"invalid sizes: at most {_lib.FEW_TOKENS} tokens and {_lib.FEW_PAIRS} pairs")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def few_tokens_ffn(x: torch.Tensor, ids: torch.Tensor, gates: torch.Tensor,
+                   w_gate_up: Union[torch.Tensor, MXFP4], w_down: Union[torch.Tensor, MXFP4], *,
+                   expert_widx: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None,
+                   ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The expert layer for the few tokens of a decoding step: y [T, d] from x
+    [T, d] (rows may be apart), the router's ids and gates [T, K], and weights
+    [W, 2F, d], [W, d, F] of x's type or in 4 bits (then x is bf16). expert_widx
+    [E] int32: which weights an expert has here, -1: none (its part of the sum
+    is another rank's); without it expert e has weights e. out_dtype: by default
+    x's. ws: from few_tokens_workspace (one is made when missing)."""
+    ld = _rows(x, "x")
+    T, d = x.shape
+    dev = x.device
+    if ids.dim() != 2 or ids.shape[0] != T:
+        raise ValueError("ids must be [T, K]")
+    K = ids.shape[1]
+    mx = isinstance(w_gate_up, MXFP4)
+    if mx != isinstance(w_down, MXFP4):
+        raise TypeError("w_gate_up and w_down: both in 4 bits or neither")
+    gu = w_gate_up.codes if mx else w_gate_up
+    if gu.dim() != 3:
+        raise ValueError("w_gate_up must be [W, 2F, d]")
+    W, F = gu.shape[0], gu.shape[1] // 2
+    if mx:
+        if x.dtype != torch.bfloat16:
+            raise TypeError("weights in 4 bits go with bf16 x")
+        weights = (*_mx(w_gate_up, (W, 2 * F), d, "w_gate_up", dev), *_mx(w_down, (W, d), F, "w_down", dev))
+    else:
+        for t, shape, name in ((w_gate_up, (W, 2 * F, d), "w_gate_up"), (w_down, (W, d, F), "w_down")):
+            if t.shape != shape:
+                raise ValueError(f"{name}: {tuple(t.shape)}, {shape} expected")
+        weights = tuple(_vec(t, t.numel(), x.dtype, name, dev)
+                        for t, name in ((w_gate_up, "w_gate_up"), (w_down, "w_down")))
+    E = W if expert_widx is None else expert_widx.numel()
+    out_dtype = x.dtype if out_dtype is None else out_dtype
+    y = torch.empty(T, d, dtype=out_dtype, device=dev)
+    if ws is None:
+        ws = few_tokens_workspace(T, K, d, F, dev)
+    head = (x.data_ptr(),) + (() if mx else (_dt(x),)) + (ld, T, d, F)
+    args = (*head, _vec(ids, T * K, torch.int32, "ids", dev), _vec(gates, T * K, torch.float32, "gates", dev), K, E,
+            _vec(expert_widx, E, torch.int32, "expert_widx", dev), W, *weights, y.data_ptr(), _dt(y), *_ws(ws, dev),
+            _stream(dev))
+    name = "foremoe_few_tokens_ffn_mxfp4" if mx else "foremoe_few_tokens_ffn"
+    _launch(dev, lambda: getattr(_lib.load(), name)(*args), name)
+    return y
 
 
 # ---------------------------------------------------------------------------

@@ -1,0 +1,219 @@
+"""The Muon step on the GPU against the oracle.
+
+m: a product and a sum, within 4 u of their magnitudes (u = 2^-24). X: the
+oracle also runs the iteration with the products' factors rounded to fp16 as the
+format has them; how far that is from the exact iteration is what the format
+costs. Sums in another order, and fp32 ones, flip some of those roundings, each
+by as much again: X may be off by three times that distance, in the Frobenius
+norm. The update itself is fp32: 4 u of p and of the move, and half a step of
+bf16 (2^-8) where p is stored so.
+"""
+import numpy as np
+import pytest
+import torch
+
+import oracle.foremoe_rollout as R
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+COEF = (3.4445, -4.7750, 2.0315)
+BF16, F32 = torch.bfloat16, torch.float32
+DT = {"bf16": BF16, "f32": F32}
+
+
+def _np(t):
+    return t.detach().double().cpu().numpy()
+
+
+def _matrix(rng, shape, rank=None):
+    r = min(shape[-2:]) if rank is None else rank
+    return rng.standard_normal((*shape[:-1], r)) @ rng.standard_normal((*shape[:-2], r, shape[-1])) * 1e-3
+
+
+def _x_close(got, u, eps=1e-7, steps=5):
+    """X of one matrix against the oracle's, from u."""
+    n = max(np.linalg.norm(u), eps)
+    exact, held = R.newton_schulz(u / n, COEF, steps), R.newton_schulz_fp16(u / n, COEF, steps)
+    lim = 3 * np.linalg.norm(held - exact) + 1e-6 * np.linalg.norm(exact) + 1e-30
+    assert np.linalg.norm(got - exact) <= lim, (np.linalg.norm(got - exact), lim)
+    return exact
+
+
+SHAPES = [(1, 1), (1, 5), (7, 1), (3, 4), (31, 64), (64, 31), (128, 128), (129, 200), (300, 130), (2, 40, 70),
+          (3, 2, 90, 33), (256, 513), (5, 128, 16)]
+
+
+@pytest.mark.parametrize("nesterov", [False, True])
+@pytest.mark.parametrize("param,masters,grad", [("f32", False, "f32"), ("bf16", True, "f32"), ("bf16", False, "bf16")])
+def test_muon(gpu, param, masters, grad, nesterov):
+    from paper_2606_11867_amd.optimizer import Muon
+    print(f"\n[case] muon {param} masters={masters} grad={grad} nesterov={nesterov}", flush=True)
+    rng = np.random.default_rng(21)
+    to = lambda a, dt: torch.from_numpy(a.astype(np.float32)).to(gpu).to(DT[dt])  # noqa: E731
+    ps = [to(rng.standard_normal(s) * 0.1, param) for s in SHAPES]
+    gs = [to(_matrix(rng, s), grad) for s in SHAPES]
+    scale = [0.5 + 0.1 * i for i in range(len(SHAPES))]
+    opt = Muon(ps, gs, lr=0.05, momentum=0.9, nesterov=nesterov, weight_decay=0.1, scale=scale, masters=masters,
+               zero_grads=True)
+    clip = torch.full((1,), 0.7, device=gpu)
+    for step in range(3):
+        if step:
+            for g, s in zip(gs, SHAPES):
+                g.copy_(to(_matrix(rng, s), "f32"))
+        fp = [_np(t) for t in (opt.masters or ps)]
+        fm, fg = [_np(t) for t in opt.states], [_np(t) for t in gs]
+        opt.step(grad_scale=clip if step else None)
+        k = float(np.float32(0.7)) if step else 1.0
+        for i, s in enumerate(SHAPES):
+            m = _np(opt.states[i])
+            assert np.all(np.abs(m - (0.9 * fm[i] + k * fg[i])) <= 4 * U * (np.abs(fm[i]) + np.abs(fg[i])) + 1e-44)
+            u = k * fg[i] + 0.9 * m if nesterov else m
+            got = _np((opt.masters or ps)[i])
+            move = (fp[i] * (1 - 0.05 * 0.1) - got) / (0.05 * scale[i])
+            # the step's own roundings, over lr * scale
+            slack = 8 * U * (np.abs(fp[i]) + np.abs(got)) + (2.0 ** -8 * np.abs(got) if param == "bf16" and not masters else 0)
+            for j, (mv, uu, sl) in enumerate(zip(move.reshape(-1, *s[-2:]), u.reshape(-1, *s[-2:]),
+                                                 (slack / (0.05 * scale[i])).reshape(-1, *s[-2:]))):
+                n = np.linalg.norm(uu)
+                exact, held = R.newton_schulz(uu / n, COEF, 5), R.newton_schulz_fp16(uu / n, COEF, 5)
+                lim = 3 * np.linalg.norm(held - exact) + 1e-5 * np.linalg.norm(exact) + np.linalg.norm(sl)
+                assert np.linalg.norm(mv - exact) <= lim, (s, j, np.linalg.norm(mv - exact), lim)
+            if param == "bf16" and masters:
+                assert torch.equal(ps[i], opt.masters[i].to(BF16))
+            assert not gs[i].any()
+
+
+@pytest.mark.parametrize("rank", [1, 5, 40])
+@pytest.mark.parametrize("shape", [(130, 300), (300, 130), (256, 256)])
+def test_low_rank_and_sizes(gpu, shape, rank):
+    """Directions that u does not have stay empty; from the least to the
+    largest numbers, X does not go by the size of u."""
+    from paper_2606_11867_amd.optimizer import Muon
+    print(f"\n[case] muon rank {rank} of {shape}", flush=True)
+    rng = np.random.default_rng(rank)
+    base = _matrix(rng, shape, rank)
+    for factor in (1.0, 1e-30, 1e30):
+        g = torch.from_numpy((base * factor).astype(np.float32)).to(gpu)
+        p = torch.zeros(shape, device=gpu)
+        Muon([p], [g], lr=1.0, momentum=0.0, nesterov=False, scale=-1.0, eps=0.0).step()
+        _x_close(_np(p), _np(g), eps=0.0)
+
+
+def test_nothing_and_not_finite(gpu):
+    """A matrix of zeros does not move; one with a NaN or an infinity becomes
+    NaN; its neighbours in the batch are what they would be without it."""
+    from paper_2606_11867_amd.optimizer import Muon
+    rng = np.random.default_rng(5)
+    g = torch.from_numpy(_matrix(rng, (5, 40, 50)).astype(np.float32)).to(gpu)
+    run = lambda t, eps: (lambda p: (Muon([p], [t.clone()], lr=1.0, momentum=0.0, scale=1.0, eps=eps).step(), p)[1])(  # noqa: E731
+        torch.ones(5, 40, 50, device=gpu))
+    good = run(g, 1e-7)
+    g[1], g[2, 3, 4], g[3, 0, 0] = 0.0, float("nan"), float("inf")
+    for eps in (1e-7, 0.0):
+        p = run(g, eps)
+        assert bool((p[1] == 1.0).all())
+        assert bool(torch.isnan(p[2]).all()) and bool(torch.isnan(p[3]).all())
+        assert torch.equal(p[0], good[0]) and torch.equal(p[4], good[4])
+    # eps above the norm: X of a small u is small
+    small = torch.full((1, 6, 6), 1e-3, device=gpu)
+    p = torch.zeros(1, 6, 6, device=gpu)
+    Muon([p], [small], lr=1.0, momentum=0.0, nesterov=False, scale=-1.0, eps=1.0).step()
+    _x_close(_np(p)[0], _np(small)[0], eps=1.0)
+
+
+def test_steps_and_coefficients(gpu):
+    from paper_2606_11867_amd.optimizer import Muon
+    rng = np.random.default_rng(6)
+    g = torch.from_numpy(_matrix(rng, (48, 80)).astype(np.float32)).to(gpu)
+    for steps in (0, 1, 2, 16):
+        for coef in (COEF, (1.5, -0.5, 0.0)):
+            p = torch.zeros(48, 80, device=gpu)
+            Muon([p], [g], lr=1.0, momentum=0.0, nesterov=False, scale=-1.0, steps=steps, coefficients=coef).step()
+            u = _np(g) / np.linalg.norm(_np(g))
+            exact, held = R.newton_schulz(u, coef, steps), R.newton_schulz_fp16(u, coef, steps)
+            # without steps X is held in two fp16 numbers, 2^-11 of 2^-11
+            lim = 3 * np.linalg.norm(held - exact) + 2.0 ** -21 * np.linalg.norm(exact)
+            assert np.linalg.norm(_np(p) - exact) <= lim, (steps, coef)
+
+
+def test_parts_are_matrices_of_their_own(gpu):
+    """gate_up [E, 2F, d] with two parts is [2E, F, d]; more tensors than one
+    launch takes; odd addresses."""
+    from paper_2606_11867_amd.optimizer import Muon
+    rng = np.random.default_rng(7)
+    base = _matrix(rng, (3, 2 * 20, 30)).astype(np.float32)
+    out = []
+    for shape, parts in (((3, 40, 30), 2), ((6, 20, 30), 1)):
+        p, g = torch.zeros(shape, device=gpu), torch.from_numpy(base.reshape(shape)).to(gpu)
+        Muon([p], [g], lr=1.0, parts=parts).step()
+        out.append(p.view(6, 20, 30))
+    assert torch.equal(*out)
+    ps, gs = [], []
+    for i in range(55):
+        buf = torch.zeros(9 * 12 + 3, device=gpu)
+        ps.append(buf[1 + i % 3:][:108].view(9, 12))
+        gs.append(torch.from_numpy(base[0, :9, :12] * (1 + i)).to(gpu))
+    opt = Muon(ps, gs, lr=1.0, scale=1.0)
+    opt.step()
+    for p in ps[1:]:
+        np.testing.assert_allclose(_np(p), _np(ps[0]), atol=2.0 ** -9)
+
+
+def test_captured_and_repeated(gpu):
+    """A replay is the step again, on what the gradients then hold."""
+    from paper_2606_11867_amd.optimizer import Muon
+    rng = np.random.default_rng(8)
+    shapes = [(2, 40, 100), (130, 20)]
+    new = lambda: [torch.from_numpy(_matrix(rng, s).astype(np.float32)).to(gpu) for s in shapes]  # noqa: E731
+    start = [torch.randn(s, device=gpu) for s in shapes]
+
+    def make():
+        ps = [t.clone() for t in start]
+        gs = [torch.zeros_like(t) for t in ps]
+        return ps, gs, Muon(ps, gs, lr=0.01, zero_grads=True)
+
+    (pa, ga, a), (pb, gb, b) = make(), make()
+    side = torch.cuda.Stream(gpu)
+    side.wait_stream(torch.cuda.current_stream(gpu))
+    with torch.cuda.stream(side):
+        a.step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        a.step()
+    for t, s in zip(pa, start):
+        t.copy_(s)
+    for t in a.states:
+        t.zero_()
+    for _ in range(4):
+        grads = new()
+        for g, h, v in zip(ga, gb, grads):
+            g.copy_(v)
+            h.copy_(v)
+        graph.replay()
+        torch.cuda.synchronize()
+        b.step()
+        for x, y in zip((*pa, *a.states, *ga), (*pb, *b.states, *gb)):
+            assert torch.equal(x, y)
+
+
+def test_tensors_given_other_memory(gpu):
+    from paper_2606_11867_amd.optimizer import Muon
+    p, g = torch.zeros(8, 8, device=gpu), torch.randn(8, 8, device=gpu)
+    opt = Muon([p], [g], lr=1.0, momentum=0.0, nesterov=False, weight_decay=0.0)
+    opt.step()
+    first = p.clone()
+    old, p.data = p.data, torch.zeros(8, 8, device=gpu)
+    opt.step()
+    assert torch.equal(p, first) and torch.equal(old, first)
+    g.data = torch.zeros(8, 8, dtype=BF16, device=gpu)
+    with pytest.raises(TypeError):
+        opt.step()
+    with pytest.raises(ValueError):
+        opt.scale = [1.0, 2.0]
+    for bad in (dict(params=[p], grads=[]), dict(params=[], grads=[]), dict(params=[p.view(-1)], grads=[p]),
+                dict(params=[p], grads=[p], parts=3), dict(params=[p], grads=[p], ws=torch.empty(4, device=gpu)),
+                dict(params=[p], grads=[p], masters=[p])):
+        with pytest.raises(ValueError):
+            Muon(**bad)
