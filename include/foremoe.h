@@ -893,7 +893,7 @@ int foremoe_few_tokens_ffn_mxfp4(const void* x, int64_t ld, int64_t T, int32_t d
  * tensors: HOST array, read during the call only; pointers aligned to their
  * types; param, grad, master and m hold [batch, rows, cols] contiguous. batch
  * = 0: skipped. batch <= 2^30, 1 <= rows, cols <= FOREMOE_MUON_SIDE,
- * min(rows, cols) <= FOREMOE_MUON_RANK, and with both sides rounded up to 128
+ * min(rows, cols) <= FOREMOE_MUON_RANK, and with both sides rounded up to 256
  * at most 2^35 elements. 0 <= ns_steps <= 16.
  * coef: HOST array of 3.
  * ws: foremoe_muon_workspace_size(tensors, n_tensors) bytes, 256-byte aligned,

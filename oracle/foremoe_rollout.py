@@ -112,14 +112,15 @@ def newton_schulz(x, coef, steps):
 
 def newton_schulz_fp16(x, coef, steps):
     """The same with the products' factors rounded to fp16 as the step's format
-    has them: X in two numbers, of which the products take the first."""
+    has them: X in two numbers, of which the products take the first, and the
+    last step does without the second (unless it is the first too)."""
     a, b, c = coef
     half = lambda v: v.astype(np.float16).astype(np.float64)  # noqa: E731
     tall = x.shape[0] > x.shape[1]
     x = (x.T if tall else x) * 256
-    for _ in range(steps):
+    for i in range(steps):
         hi = half(x)
-        x = hi + half((x - hi) * 1024) / 1024
+        x = hi + half((x - hi) * 1024) / 1024 if i == 0 or i + 1 < steps else hi
         g = half(hi @ hi.T / 256)
         p = half(b * g + c * (g @ g) / 256)
         x = a * x + p @ hi / 256

@@ -33,15 +33,8 @@ struct FewArgs {
   char* h;                           // bf16: planes [2][pairs][Fp]; fp32: [pairs][Fp]
   void* y;
   int y_f32;
+  int width, tiles;  // of the second product: output columns of a tile, tiles of a workgroup
 };
-
-// The weights that pair p goes to, or -1.
-__device__ __forceinline__ int pair_weights(const FewArgs& a, int p) {
-  const int id = a.ids[p];
-  if (id < 0 || id >= a.E) return -1;
-  const int w = a.widx ? a.widx[id] : id;
-  return w >= 0 && w < a.W ? w : -1;
-}
 
 // A chunk is 64 bytes of a row of weights: 16 bytes for each of four lanes.
 template <int WT>
@@ -54,21 +47,37 @@ struct Chunk {
 
 struct WeightFrag {
   uint4 v;
-  float scale;
+  uint32_t scale;  // 4 bits: the block's scale byte
 };
+
+// The scale bytes of chunks c and c + 1 of a row of nb blocks, those past its
+// end aside: eight bytes in one load (a load a byte took 17 of 101 us of 24
+// tokens in 4 bits). Rows shorter than that go byte by byte.
+__device__ __forceinline__ uint64_t load_scales(const uint8_t* scales, int nb, int c) {
+  const int at = 4 * c;
+  if (nb >= 8) {
+    const int from = at + 8 <= nb ? at : nb - 8, skip = at - from;
+    uint64_t v;
+    __builtin_memcpy(&v, scales + from, 8);
+    return skip < 8 ? v >> (8 * skip) : 0;
+  }
+  uint64_t v = 0;
+  for (int i = 0; i < 8; ++i)
+    if (at + i < nb) v |= (uint64_t)scales[at + i] << (8 * i);
+  return v;
+}
 
 // This lane's part of chunk c of a row (zeros past its end). VEC: the row
 // starts on 16 bytes and its length is a multiple of them.
 template <int WT, bool VEC>
-__device__ __forceinline__ WeightFrag load_weights(const char* row, const uint8_t* scales, int n, int c, int g) {
+__device__ __forceinline__ WeightFrag load_weights(const char* row, int n, int c, int g) {
   using C = Chunk<WT>;
   WeightFrag f;
-  f.v = uint4{0, 0, 0, 0}, f.scale = 0.0f;
+  f.v = uint4{0, 0, 0, 0}, f.scale = 0;
   const int k = c * C::K + g * C::PER_LANE;
   if (k >= n) return f;
   if constexpr (VEC) {
     f.v = *(const uint4*)(row + (size_t)c * 64 + g * 16);
-    if constexpr (WT == kFp4) f.scale = mx_scale_operand(scales[k / kMxBlock]);
   } else if constexpr (WT == kBf16) {
     const uint16_t* p = (const uint16_t*)row + k;
     uint32_t w[4] = {0, 0, 0, 0};
@@ -104,303 +113,430 @@ __device__ __forceinline__ TokenFrag<WT> load_token(const char* row, int n, int 
 #pragma unroll
     for (int i = 0; i < C::OPERANDS; ++i) f.v[i] = *(const uint4*)(row + (size_t)k * C::ES + 16 * i);
   } else {
-    f.v[0] = load_weights<WT == kFp4 ? kBf16 : WT, false>(row, nullptr, n, c, g).v;
+    f.v[0] = load_weights<WT == kFp4 ? kBf16 : WT, false>(row, n, c, g).v;
   }
   return f;
 }
 
-// acc[row of weights][token] += weights x tokens; PLANES of the tokens add up.
-template <int WT, int PLANES>
-__device__ __forceinline__ f32x4 multiply(const WeightFrag& w, const TokenFrag<WT>* t, f32x4 acc) {
+// acc[row of weights][token] += weights x tokens.
+template <int WT>
+__device__ __forceinline__ f32x4 multiply(const WeightFrag& w, const TokenFrag<WT>& t, f32x4 acc) {
   if constexpr (WT == kF32) {
     const float a[4] = {__uint_as_float(w.v.x), __uint_as_float(w.v.y), __uint_as_float(w.v.z), __uint_as_float(w.v.w)};
-    const uint4 u = t[0].v[0];
+    const uint4 u = t.v[0];
     const float b[4] = {__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w)};
 #pragma unroll
     for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], acc, 0, 0, 0);
   } else if constexpr (WT == kBf16) {
-#pragma unroll
-    for (int p = 0; p < PLANES; ++p)
-      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w.v),
-                                                    __builtin_bit_cast(bf16x8, t[p].v[0]), acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w.v), __builtin_bit_cast(bf16x8, t.v[0]),
+                                                  acc, 0, 0, 0);
   } else {
     const uint32_t q[4] = {w.v.x, w.v.y, w.v.z, w.v.w};
+    const float s = mx_scale_operand(w.scale);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const uint4 a = {mx_get2_bf16<0>(q[i], w.scale), mx_get2_bf16<1>(q[i], w.scale), mx_get2_bf16<2>(q[i], w.scale),
-                       mx_get2_bf16<3>(q[i], w.scale)};
-#pragma unroll
-      for (int p = 0; p < PLANES; ++p)
-        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
-                                                      __builtin_bit_cast(bf16x8, t[p].v[i]), acc, 0, 0, 0);
+      const uint4 a = {mx_get2_bf16<0>(q[i], s), mx_get2_bf16<1>(q[i], s), mx_get2_bf16<2>(q[i], s),
+                       mx_get2_bf16<3>(q[i], s)};
+      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, t.v[i]),
+                                                    acc, 0, 0, 0);
     }
   }
   return acc;
 }
 
 // ---------------------------------------------------------------------------
-// gate/up. Grid: (tiles of 8 hidden columns, candidates): with more pairs than
-// matrices a candidate is a matrix, else a pair, the first of those that share
-// its matrix.
+// The pairs of a call by the matrix that they go to, in LDS: every workgroup
+// finds them by itself.
 // ---------------------------------------------------------------------------
-constexpr int kUpThreads = 256, kUpWaves = kUpThreads / 64;
+struct Groups {
+  uint16_t list[FOREMOE_FEW_PAIRS];      // pairs, matrix by matrix
+  int16_t place[FOREMOE_FEW_PAIRS];      // of a pair in the list, or -1
+  uint16_t used[FOREMOE_MAX_SLOTS];      // the matrices that have pairs
+  uint16_t begin_used[FOREMOE_MAX_SLOTS + 1];  // their first places, and the end
+  int begin[FOREMOE_MAX_SLOTS];          // (while grouping) pairs of a matrix, then its first place
+  int waves[32];
+  int n_used, most;                      // most: pairs of a matrix
+};
 
-template <int WT, bool VEC, int NG>
-__device__ __forceinline__ void up_groups(const FewArgs& a, const uint16_t* list, int first, int count, const char* row,
-                                          const uint8_t* scales, float (*red)[4][16][16]) {
-  using C = Chunk<WT>;
-  constexpr int U = 4;
-  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int g = lane >> 4, col = lane & 15;
-  const char* tok[NG];
-  bool there[NG];
-#pragma unroll
-  for (int i = 0; i < NG; ++i) {
-    const int q = first + 16 * i + col;
-    there[i] = q < count;
-    tok[i] = (const char*)a.x + (there[i] ? (int64_t)(list[q] / a.K) * a.ld * C::ES : 0);
-  }
-  f32x4 acc[NG];
-#pragma unroll
-  for (int i = 0; i < NG; ++i) acc[i] = f32x4{0, 0, 0, 0};
-  const int nc = (a.d + C::K - 1) / C::K;
-  for (int c0 = wave; c0 < nc; c0 += U * kUpWaves) {
-    WeightFrag w[U];
-    TokenFrag<WT> t[U][NG];
-#pragma unroll
-    for (int u = 0; u < U; ++u) w[u] = load_weights<WT, VEC>(row, scales, a.d, c0 + u * kUpWaves, g);
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int i = 0; i < NG; ++i) t[u][i] = load_token<WT, VEC>(tok[i], a.d, c0 + u * kUpWaves, g, there[i]);
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int i = 0; i < NG; ++i) acc[i] = multiply<WT, 1>(w[u], &t[u][i], acc[i]);
-  }
-#pragma unroll
-  for (int i = 0; i < NG; ++i)
-#pragma unroll
-    for (int q = 0; q < 4; ++q) red[wave][i][4 * g + q][col] = acc[i][q];
-}
-
-template <int WT, bool VEC>
-__global__ __launch_bounds__(kUpThreads) void few_up_kernel(FewArgs a) {
-  __shared__ uint16_t list[FOREMOE_FEW_PAIRS];
-  __shared__ int s_count, s_earlier;
-  __shared__ float red[kUpWaves][4][16][16];
-  const int pairs = a.T * a.K, tid = threadIdx.x;
-  const bool by_pair = pairs <= a.W;
-  const int w = by_pair ? pair_weights(a, blockIdx.y) : (int)blockIdx.y;
-  if (w < 0) return;
-  if (tid == 0) s_count = 0, s_earlier = 0;
-  __syncthreads();
-  // the order of the list does not matter: a token's column is its own
-  for (int p = tid; p < pairs; p += kUpThreads) {
-    if (pair_weights(a, p) == w) {
-      if (by_pair && p < (int)blockIdx.y) s_earlier = 1;
-      list[atomicAdd(&s_count, 1)] = (uint16_t)p;
-    }
-  }
-  __syncthreads();
-  const int count = s_count;
-  if (count == 0 || s_earlier) return;
-
-  using C = Chunk<WT>;
-  const int f0 = blockIdx.x * 8, r = lane_id() & 15;
-  // rows 0-7: Wg, 8-15: Wu; those past F repeat the last and are not used
-  const int f = f0 + (r & 7) < a.F ? f0 + (r & 7) : a.F - 1;
-  const int64_t row = (int64_t)w * 2 * a.F + (r < 8 ? f : a.F + f);
-  const char* rp = a.gu + (WT == kFp4 ? row * (a.d / 2) : row * a.d * C::ES);
-  const uint8_t* sp = WT == kFp4 ? a.gu_scales + row * (a.d / kMxBlock) : nullptr;
-  const int64_t plane = (int64_t)pairs * a.Fp;
-  for (int first = 0; first < count; first += 64) {
-    const int left = count - first;
-    if (left <= 16) up_groups<WT, VEC, 1>(a, list, first, count, rp, sp, red);
-    else if (left <= 32) up_groups<WT, VEC, 2>(a, list, first, count, rp, sp, red);
-    else up_groups<WT, VEC, 4>(a, list, first, count, rp, sp, red);
-    __syncthreads();
-    const int n = left < 64 ? left : 64;
-    for (int o = tid; o < n * 8; o += kUpThreads) {
-      const int j = o & 7, q = o >> 3;
-      float ga = 0, up = 0;
-#pragma unroll
-      for (int v = 0; v < kUpWaves; ++v) ga += red[v][q >> 4][j][q & 15], up += red[v][q >> 4][j + 8][q & 15];
-      if (f0 + j < a.F) {
-        const float h = ga / (1.0f + expf(-ga)) * up;
-        const int64_t at = (int64_t)list[first + q] * a.Fp + f0 + j;
-        if constexpr (WT == kF32) {
-          ((float*)a.h)[at] = h;
-        } else {
-          const uint32_t hi = pack_bf2(h, 0.0f) & 0xffffu;
-          ((uint16_t*)a.h)[at] = (uint16_t)hi;
-          // (an infinite h leaves NaN: nothing)
-          const float rest = h - bf2f(hi);
-          ((uint16_t*)a.h)[plane + at] = rest == rest ? (uint16_t)pack_bf2(rest, 0.0f) : (uint16_t)0;
-        }
+// The order of the pairs within a matrix is whatever the atomics make it; no
+// result depends on it, as a token's column of a product is its own.
+template <int THREADS>
+__device__ __forceinline__ void group_pairs(const FewArgs& a, Groups& G) {
+  if (a.T * a.K <= 64) {
+    // one wavefront, a lane to a pair, without a scan over all matrices
+    // (one token of 128 experts: both kernels together 26 -> 21 us)
+    if (threadIdx.x < 64) {
+      const int pairs = a.T * a.K, lane = lane_id();
+      int w = lane < pairs ? a.ids[lane] : -1;
+      if ((unsigned)w >= (unsigned)a.E) w = -1;
+      if (w >= 0 && a.widx) w = a.widx[w];
+      if ((unsigned)w >= (unsigned)a.W) w = -1;
+      uint64_t left = __ballot(w >= 0);
+      int at = 0, n = 0, most = 0;
+      while (left) {
+        const int p = __builtin_ctzll(left), v = __builtin_amdgcn_readlane(w, p);
+        const uint64_t same = __ballot(w == v);
+        const int m = __popcll(same);
+        if (lane == 0) G.used[n] = (uint16_t)v, G.begin_used[n] = (uint16_t)at;
+        if (w == v) G.list[at + lanes_below(same)] = (uint16_t)lane, G.place[lane] = (int16_t)(at + lanes_below(same));
+        at += m, ++n, most = m > most ? m : most;
+        left &= ~same;
       }
-    }
-    // the last tile also clears what the rows are longer than F
-    if (blockIdx.x == gridDim.x - 1) {
-      const int extra = a.Fp - a.F;
-      for (int o = tid; o < n * extra; o += kUpThreads) {
-        const int64_t at = (int64_t)list[first + o / extra] * a.Fp + a.F + o % extra;
-        if constexpr (WT == kF32) ((float*)a.h)[at] = 0.0f;
-        else ((uint16_t*)a.h)[at] = 0, ((uint16_t*)a.h)[plane + at] = 0;
-      }
+      if (lane < pairs && w < 0) G.place[lane] = -1;
+      if (lane == 0) G.n_used = n, G.most = most, G.begin_used[n] = (uint16_t)at;
     }
     __syncthreads();
+    return;
   }
-}
-
-// ---------------------------------------------------------------------------
-// down and the sum over a token's experts. The 16 rows of an instruction are 8
-// output columns at two chunks of the k axis, and its 16 columns 8 tokens at
-// the same two: the two diagonal quarters are the products.
-// ---------------------------------------------------------------------------
-constexpr int kDownThreads = 1024, kDownWaves = kDownThreads / 64;
-
-template <int WT, bool VEC, int NG>
-__device__ __forceinline__ void down_groups(const FewArgs& a, const uint16_t* list, int first, int count,
-                                            const char* row, const uint8_t* scales, int part, int parts, float* yp) {
-  using C = Chunk<WT>;
-  constexpr int U = NG == 1 ? 4 : 2, PLANES = WT == kF32 ? 1 : 2;
-  const int lane = lane_id(), g = lane >> 4, r = lane & 15, odd = r >> 3;
-  const int64_t plane = (int64_t)a.T * a.K * a.Fp * C::ES;
-  const char* tok[NG];
-  bool there[NG];
-#pragma unroll
-  for (int i = 0; i < NG; ++i) {
-    const int q = first + 8 * i + (r & 7);
-    there[i] = q < count;
-    tok[i] = a.h + (there[i] ? (int64_t)list[q] * a.Fp * C::ES : 0);
-  }
-  f32x4 acc[NG];
-#pragma unroll
-  for (int i = 0; i < NG; ++i) acc[i] = f32x4{0, 0, 0, 0};
-  const int nc = (a.F + 2 * C::K - 1) / (2 * C::K);  // pairs of chunks
-  for (int c0 = part; c0 < nc; c0 += U * parts) {
-    WeightFrag w[U];
-    TokenFrag<WT> t[U][NG][PLANES];
-#pragma unroll
-    for (int u = 0; u < U; ++u) w[u] = load_weights<WT, VEC>(row, scales, a.F, 2 * (c0 + u * parts) + odd, g);
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int i = 0; i < NG; ++i)
-#pragma unroll
-        for (int p = 0; p < PLANES; ++p)
-          t[u][i][p] = load_token<WT, true>(tok[i] + p * plane, a.Fp, 2 * (c0 + u * parts) + odd, g, there[i]);
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int i = 0; i < NG; ++i) acc[i] = multiply<WT, PLANES>(w[u], t[u][i], acc[i]);
-  }
-#pragma unroll
-  for (int i = 0; i < NG; ++i)
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      // row 4 g + q and column r of the even chunks, row + 8 and column + 8 of the odd
-      const float v = acc[i][q] + __shfl(acc[i][q], (lane + 40) & 63, 64);
-      const int at = first + 8 * i + r;
-      if (r < 8 && g < 2 && at < count) yp[((size_t)part * a.T * a.K + list[at]) * 8 + 4 * g + q] = v;
-    }
-}
-
-template <int WT, bool VEC, int CAP>
-__global__ __launch_bounds__(kDownThreads) void few_down_kernel(FewArgs a) {
-  __shared__ float yp[CAP * 8];              // [parts][pairs][8]
-  __shared__ uint16_t list[FOREMOE_FEW_PAIRS];  // pairs by matrix
-  __shared__ int16_t of_pair[FOREMOE_FEW_PAIRS];
-  __shared__ int begin[FOREMOE_MAX_SLOTS + 1];
-  __shared__ uint16_t used[FOREMOE_MAX_SLOTS];
-  __shared__ int wave_pairs[kDownWaves], wave_used[kDownWaves];
+  constexpr int WAVES = THREADS / 64, PER = FOREMOE_FEW_PAIRS / THREADS, WPER = FOREMOE_MAX_SLOTS / THREADS;
   const int pairs = a.T * a.K, tid = threadIdx.x, lane = lane_id();
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-
-  // group the pairs by matrix; the order within a group does not matter
-  begin[tid] = 0;
-  __syncthreads();
-  int w_of[2], rank[2];
+  int w[PER], rank[PER];
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int p = tid + i * kDownThreads;
-    w_of[i] = p < pairs ? pair_weights(a, p) : -1;
-    if (p < pairs) of_pair[p] = (int16_t)w_of[i];
-    if (w_of[i] >= 0) rank[i] = atomicAdd(&begin[w_of[i]], 1);
+  for (int i = 0; i < PER; ++i) {
+    const int p = tid + i * THREADS;
+    w[i] = p < pairs ? a.ids[p] : -1;
+    if ((unsigned)w[i] >= (unsigned)a.E) w[i] = -1;
   }
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    if (w[i] >= 0 && a.widx) w[i] = a.widx[w[i]];
+    if ((unsigned)w[i] >= (unsigned)a.W) w[i] = -1;
+  }
+#pragma unroll
+  for (int i = 0; i < WPER; ++i) G.begin[tid + i * THREADS] = 0;
+  if (tid == 0) G.most = 16;  // (or less)
   __syncthreads();
-  const int mine = begin[tid];
-  int upto = mine;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) rank[i] = w[i] >= 0 ? atomicAdd(&G.begin[w[i]], 1) : 0;
+  __syncthreads();
+  // a thread's matrices are neighbours: tid * WPER ..
+  int mine[WPER], sum = 0, some = 0;
+#pragma unroll
+  for (int i = 0; i < WPER; ++i) {
+    mine[i] = G.begin[tid * WPER + i], sum += mine[i], some += mine[i] > 0;
+    if (mine[i] > 16) atomicMax(&G.most, mine[i]);
+  }
+  int upto = sum | some << 16;  // at most 2048 pairs, 1024 matrices
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
     const int v = __shfl_up(upto, o, 64);
     if (lane >= o) upto += v;
   }
-  const uint64_t any = __ballot(mine > 0);
-  if (lane == 63) wave_pairs[wave] = upto;
-  if (lane == 0) wave_used[wave] = __popcll(any);
+  if (lane == 63) G.waves[wave] = upto;
   __syncthreads();
-  int base = 0, ubase = 0, n_used = 0;
-  for (int v = 0; v < kDownWaves; ++v) {
-    if (v < wave) base += wave_pairs[v], ubase += wave_used[v];
-    n_used += wave_used[v];
+  int before = upto - (sum | some << 16), all = 0;
+#pragma unroll
+  for (int v = 0; v < WAVES; ++v) {
+    const int x = G.waves[v];
+    if (v < wave) before += x;
+    all += x;
   }
-  begin[tid] = base + upto - mine;
-  if (tid == kDownThreads - 1) begin[FOREMOE_MAX_SLOTS] = base + upto;
-  if (mine > 0) used[ubase + lanes_below(any)] = (uint16_t)tid;
+  int at = before & 0xffff, u = before >> 16;
+#pragma unroll
+  for (int i = 0; i < WPER; ++i) {
+    G.begin[tid * WPER + i] = at;
+    if (mine[i] > 0) G.begin_used[u] = (uint16_t)at, G.used[u++] = (uint16_t)(tid * WPER + i);
+    at += mine[i];
+  }
+  if (tid == 0) G.n_used = all >> 16, G.begin_used[all >> 16] = (uint16_t)(all & 0xffff);
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
-    if (w_of[i] >= 0) list[begin[w_of[i]] + rank[i]] = (uint16_t)(tid + i * kDownThreads);
-  __syncthreads();
-
-  // parts of the k axis where experts are fewer than wavefronts
-  int parts = 1;
-  while (n_used > 0 && 2 * parts * n_used <= kDownWaves && 2 * parts * pairs <= CAP) parts *= 2;
-
-  using C = Chunk<WT>;
-  const int c0 = blockIdx.x * 8, r = lane & 15;
-  const int out = c0 + (r & 7) < a.d ? c0 + (r & 7) : a.d - 1;
-  for (int u = wave; u < n_used * parts; u += kDownWaves) {
-    const int w = __builtin_amdgcn_readfirstlane(used[u / parts]), part = u % parts;
-    const int first = __builtin_amdgcn_readfirstlane(begin[w]), count = __builtin_amdgcn_readfirstlane(begin[w + 1]);
-    const int64_t row = (int64_t)w * a.d + out;
-    const char* rp = a.dn + (WT == kFp4 ? row * (a.F / 2) : row * a.F * C::ES);
-    const uint8_t* sp = WT == kFp4 ? a.dn_scales + row * (a.F / kMxBlock) : nullptr;
-    for (int at = first; at < count; at += 32) {
-      const int left = count - at;
-      if (left <= 8) down_groups<WT, VEC, 1>(a, list, at, count, rp, sp, part, parts, yp);
-      else if (left <= 16) down_groups<WT, VEC, 2>(a, list, at, count, rp, sp, part, parts, yp);
-      else down_groups<WT, VEC, 4>(a, list, at, count, rp, sp, part, parts, yp);
-    }
+  for (int i = 0; i < PER; ++i) {
+    const int p = tid + i * THREADS, to = w[i] >= 0 ? G.begin[w[i]] + rank[i] : -1;
+    if (p < pairs) G.place[p] = (int16_t)to;
+    if (to >= 0) G.list[to] = (uint16_t)p;
   }
   __syncthreads();
-  for (int o = tid; o < a.T * 8; o += kDownThreads) {
-    const int t = o >> 3, j = o & 7;
-    if (c0 + j >= a.d) continue;
-    float s = 0.0f;
-    for (int k = 0; k < a.K; ++k) {
-      const int p = t * a.K + k;
-      if (of_pair[p] < 0) continue;
-      float v = 0.0f;
-      for (int q = 0; q < parts; ++q) v += yp[((size_t)q * pairs + p) * 8 + j];
-      s += a.gates[p] * v;
+}
+
+// Parts that the k axis (nc steps) of each of n units is cut into for 16
+// wavefronts, with `each` of `slots` partial sums for a part of all units: the
+// shortest time, a unit or part costing four steps besides its own.
+__device__ __forceinline__ int parts_for(int n, int nc, int each, int slots) {
+  int best = 1, cost = (n + 15) / 16 * (nc + 4);
+  for (int p = 2; p <= 16 && p <= nc && p * each <= slots; p *= 2) {
+    const int c = (n * p + 15) / 16 * ((nc + p - 1) / p + 4);
+    if (c < cost) cost = c, best = p;
+  }
+  return best;
+}
+
+// ---------------------------------------------------------------------------
+// gate/up. A unit is 8 hidden columns of a matrix in use; a workgroup to a CU
+// takes its even share of them, a wavefront a unit or a part of its k axis.
+// ---------------------------------------------------------------------------
+constexpr int kFewThreads = 1024, kFewWaves = 16, kUpSlots = 1024;
+// Steps of weights in flight behind those that are multiplied: as many as the
+// registers of 16 wavefronts a CU hold beside NG groups of tokens.
+template <int WT, int NG>
+constexpr int kAhead = WT == kFp4 ? (NG == 1 ? 2 : 1) : (NG == 4 ? 2 : 4);
+// Groups of tokens that a step of weights is multiplied with, at most.
+template <int WT>
+constexpr int kGroups = WT == kFp4 ? 2 : 4;
+
+// sums[i] += rows of weights x the tokens at tok[i], over chunks [c0, c1) of
+// the k axis, in steps of S chunks (lane: chunk c + odd where S is 2). The
+// weights of the next U steps are on their way while these are multiplied.
+template <int WT, bool WVEC, bool TVEC, int NG, int U, int S>
+__device__ __forceinline__ void stream_rows(const char* row, const uint8_t* scales, int n, const char* const* tok,
+                                            const bool* there, int nt, int c0, int c1, int odd, int g, f32x4* sums) {
+#pragma unroll
+  for (int i = 0; i < NG; ++i) sums[i] = f32x4{0, 0, 0, 0};
+  using C = Chunk<WT>;
+  // elements past the last chunk count as zeros
+  const int wn = min(n, c1 * C::K), tn = min(nt, c1 * C::K);
+  WeightFrag next[U];
+  // lanes of the even and the odd chunks of a pair have the same two scale words
+  constexpr int SW = (U * S + 1) / 2;
+  uint64_t ns[SW];
+  auto load = [&](int c) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) next[u] = load_weights<WT, WVEC>(row, wn, c + u * S + odd, g);
+    if constexpr (WT == kFp4) {
+#pragma unroll
+      for (int i = 0; i < SW; ++i) ns[i] = load_scales(scales, n / kMxBlock, c + 2 * i);
     }
-    const int64_t at = (int64_t)t * a.d + c0 + j;
-    if (a.y_f32) ((float*)a.y)[at] = s;
-    else ((uint16_t*)a.y)[at] = (uint16_t)pack_bf2(s, 0.0f);
+  };
+  load(c0);
+  for (int c = c0; c < c1; c += U * S) {
+    WeightFrag w[U];
+    TokenFrag<WT> t[U][NG];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      w[u] = next[u];
+      if constexpr (WT == kFp4) {
+        const int by = u * S + (S == 2 ? odd : 0);
+        w[u].scale = (uint32_t)(ns[u * S / 2] >> (8 * (4 * (by & 1) + g))) & 0xffu;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int i = 0; i < NG; ++i) t[u][i] = load_token<WT, TVEC>(tok[i], tn, c + u * S + odd, g, there[i]);
+    load(c + U * S);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int i = 0; i < NG; ++i) sums[i] = multiply<WT>(w[u], t[u][i], sums[i]);
+  }
+}
+
+// Both products of up to 16 NG pairs from place `first` on, over chunks [c0, c1).
+template <int WT, bool VEC, int NG>
+__device__ __forceinline__ void up_groups(const FewArgs& a, const Groups& G, int first, int end, const char* row,
+                                          const uint8_t* scales, int c0, int c1, f32x4* sums) {
+  using C = Chunk<WT>;
+  const int lane = lane_id(), g = lane >> 4, col = lane & 15;
+  const char* tok[NG];
+  bool there[NG];
+#pragma unroll
+  for (int i = 0; i < NG; ++i) {
+    const int q = first + 16 * i + col;
+    there[i] = q < end;
+    tok[i] = (const char*)a.x + (there[i] ? (int64_t)(G.list[q] / a.K) * a.ld * C::ES : 0);
+  }
+  stream_rows<WT, VEC, VEC, NG, kAhead<WT, NG>, 1>(row, scales, a.d, tok, there, a.d, c0, c1, 0, g, sums);
+}
+
+template <int WT>
+__device__ __forceinline__ void put_h(const FewArgs& a, int pair, int f, float gate, float up) {
+  const float h = f < a.F ? gate / (1.0f + expf(-gate)) * up : 0.0f;
+  const int64_t at = (int64_t)pair * a.Fp + f;
+  if constexpr (WT == kF32) {
+    ((float*)a.h)[at] = h;
+  } else {
+    const uint32_t hi = pack_bf2(h, 0.0f) & 0xffffu;
+    const float rest = h - bf2f(hi);  // (an infinite h leaves NaN: nothing)
+    ((uint16_t*)a.h)[at] = (uint16_t)hi;
+    ((uint16_t*)a.h)[(int64_t)a.T * a.K * a.Fp + at] = rest == rest ? (uint16_t)pack_bf2(rest, 0.0f) : (uint16_t)0;
+  }
+}
+
+template <int WT, bool VEC>
+__global__ __launch_bounds__(kFewThreads) void few_up_kernel(FewArgs a) {
+  __shared__ Groups G;
+  __shared__ float partial[kUpSlots][16];  // [unit][part][pair][row]
+  group_pairs<kFewThreads>(a, G);
+  using C = Chunk<WT>;
+  const int lane = lane_id(), g = lane >> 4, r = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // units are numbered matrix by matrix, so that a workgroup's are neighbours
+  // in memory and have the same tokens
+  const int n_used = G.n_used, tiles = (a.F + 7) / 8;
+  const int64_t units = (int64_t)tiles * n_used;
+  const int64_t u0 = units * blockIdx.x / gridDim.x;
+  const int n = (int)(units * (blockIdx.x + 1) / gridDim.x - u0);
+  if (n == 0) return;
+  const int nc = (a.d + C::K - 1) / C::K;
+  const int parts = G.most <= 16 ? parts_for(n, nc, n * 16, kUpSlots) : 1;
+  for (int i = wave; i < n * parts; i += kFewWaves) {
+    const int unit = i / parts, part = i % parts;
+    const int c = __builtin_amdgcn_readfirstlane((int)((u0 + unit) / tiles));
+    const int tile = __builtin_amdgcn_readfirstlane((int)((u0 + unit) % tiles));
+    const int k0 = nc * part / parts, k1 = nc * (part + 1) / parts;
+    const int w = __builtin_amdgcn_readfirstlane(G.used[c]);
+    const int first = __builtin_amdgcn_readfirstlane(G.begin_used[c]), end = __builtin_amdgcn_readfirstlane(G.begin_used[c + 1]);
+    // rows 0-7: Wg, 8-15: Wu; those past F repeat the last and are not used
+    const int f0 = tile * 8, f = f0 + (r & 7) < a.F ? f0 + (r & 7) : a.F - 1;
+    const int64_t row = (int64_t)w * 2 * a.F + (r < 8 ? f : a.F + f);
+    const char* rp = a.gu + (WT == kFp4 ? row * (a.d / 2) : row * a.d * C::ES);
+    const uint8_t* sp = WT == kFp4 ? a.gu_scales + row * (a.d / kMxBlock) : nullptr;
+    auto done = [&](f32x4 sums, int at) {
+      // this lane: rows 4 g .. of column r; the up's are 8 rows below the gate's
+      const int q = at + r;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float v = sums[e], up = __shfl_xor(v, 32, 64);
+        if (q >= end) continue;
+        if (parts > 1) partial[(unit * parts + part) * 16 + r][4 * g + e] = v;
+        else if (g < 2) put_h<WT>(a, G.list[q], f0 + 4 * g + e, v, up);
+      }
+    };
+    for (int at = first; at < end; at += 16 * kGroups<WT>) {
+      f32x4 sums[4];
+      if (end - at <= 16) {
+        up_groups<WT, VEC, 1>(a, G, at, end, rp, sp, k0, k1, sums);
+        done(sums[0], at);
+      } else if (kGroups<WT> == 2 || end - at <= 32) {
+        up_groups<WT, VEC, 2>(a, G, at, end, rp, sp, k0, k1, sums);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) done(sums[k], at + 16 * k);
+      } else {
+        up_groups<WT, VEC, kGroups<WT>>(a, G, at, end, rp, sp, k0, k1, sums);
+#pragma unroll
+        for (int k = 0; k < kGroups<WT>; ++k) done(sums[k], at + 16 * k);
+      }
+    }
+  }
+  if (parts > 1) {
+    __syncthreads();
+    for (int o = threadIdx.x; o < n * 128; o += kFewThreads) {
+      const int unit = o >> 7, q = (o >> 3) & 15, j = o & 7;
+      const int c = (int)((u0 + unit) / tiles), first = G.begin_used[c];
+      if (first + q >= G.begin_used[c + 1]) continue;
+      float gate = 0, up = 0;
+      for (int p = 0; p < parts; ++p) {
+        const float* v = partial[(unit * parts + p) * 16 + q];
+        gate += v[j], up += v[j + 8];
+      }
+      put_h<WT>(a, G.list[first + q], (int)((u0 + unit) % tiles) * 8 + j, gate, up);
+    }
+  }
+  // what the rows of h are longer than F's whole tiles is cleared by the
+  // workgroup of a matrix's last unit
+  const int past = tiles * 8, extra = a.Fp - past;
+  for (int c = (int)((u0 + tiles) / tiles - 1); (int64_t)(c + 1) * tiles <= u0 + n; ++c) {
+    const int first = G.begin_used[c], m = G.begin_used[c + 1] - first;
+    for (int o = threadIdx.x; o < m * extra; o += kFewThreads)
+      put_h<WT>(a, G.list[first + o / extra], past + o % extra, 0.0f, 0.0f);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// down and the sum over a token's experts. The 16 rows of an instruction are 8
+// output columns at two chunks of the k axis. Its 16 columns are 4 pairs at
+// the same two, both planes of each (fp32: 8 pairs): of its products one row
+// half by one column half each is wanted.
+// ---------------------------------------------------------------------------
+template <int WT, bool VEC, int NG>
+__device__ __forceinline__ void down_groups(const FewArgs& a, const Groups& G, int first, int end, const char* row,
+                                            const uint8_t* scales, int c0, int c1, float* yp) {
+  using C = Chunk<WT>;
+  constexpr int P = WT == kF32 ? 8 : 4;  // pairs of a group
+  const int lane = lane_id(), g = lane >> 4, r = lane & 15;
+  const int64_t plane = WT != kF32 && (r & 4) ? (int64_t)a.T * a.K * a.Fp * C::ES : 0;
+  const char* tok[NG];
+  bool there[NG];
+#pragma unroll
+  for (int i = 0; i < NG; ++i) {
+    const int q = first + P * i + (r & (P - 1));
+    there[i] = q < end;
+    tok[i] = a.h + (there[i] ? (int64_t)G.list[q] * a.Fp * C::ES + plane : 0);
+  }
+  f32x4 acc[NG];
+  stream_rows<WT, VEC, true, NG, kAhead<WT, NG>, 2>(row, scales, a.F, tok, there, a.Fp, c0, c1, r >> 3, g, acc);
+#pragma unroll
+  for (int i = 0; i < NG; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      // row 4 g + e and column r of the even chunks, row + 8 and column + 8 of the odd
+      float v = acc[i][e];
+      v += __shfl(v, (lane + 40) & 63, 64);
+      if constexpr (WT != kF32) v += __shfl(v, (lane + 4) & 63, 64);  // the second plane
+      const int q = first + P * i + r;
+      if (r < P && g < 2 && q < end) yp[q * 8 + 4 * g + e] = v;
+    }
+}
+
+template <int WT, bool VEC, int CAP>
+__global__ __launch_bounds__(kFewThreads) void few_down_kernel(FewArgs a) {
+  __shared__ Groups G;
+  __shared__ float yp[CAP * 8];  // [tile][part][place][8]
+  group_pairs<kFewThreads>(a, G);
+  const int tid = threadIdx.x, lane = lane_id();
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n_used = G.n_used, count = G.begin_used[n_used];
+  using C = Chunk<WT>;
+  constexpr int P = WT == kF32 ? 8 : 4;
+  const int r = lane & 15, nc = (a.F + 2 * C::K - 1) / (2 * C::K);  // pairs of chunks
+  // this workgroup's tiles of a.width columns, as many at a time as their
+  // sums have room
+  const int t0 = a.tiles * (int)blockIdx.x, t1 = min(t0 + a.tiles, (a.d + a.width - 1) / a.width);
+  const int room = count > 0 ? CAP / count : t1 - t0;
+  for (int tile0 = t0; tile0 < t1; tile0 += room) {
+    const int nt = min(room, t1 - tile0);
+    const int parts = parts_for(n_used * nt, nc, count * nt, CAP);
+    for (int u = wave; u < n_used * nt * parts; u += kFewWaves) {
+      const int part = u % parts, tile = u / parts % nt, c = u / parts / nt;
+      const int w = __builtin_amdgcn_readfirstlane(G.used[c]);
+      const int first = __builtin_amdgcn_readfirstlane(G.begin_used[c]), end = __builtin_amdgcn_readfirstlane(G.begin_used[c + 1]);
+      const int col = (tile0 + tile) * a.width, cols = min(a.width, a.d - col);
+      const int64_t row = (int64_t)w * a.d + col + min(r & 7, cols - 1);
+      const char* rp = a.dn + (WT == kFp4 ? row * (a.F / 2) : row * a.F * C::ES);
+      const uint8_t* sp = WT == kFp4 ? a.dn_scales + row * (a.F / kMxBlock) : nullptr;
+      const int k0 = nc * part / parts * 2, k1 = nc * (part + 1) / parts * 2;
+      float* to = yp + (size_t)(tile * parts + part) * count * 8;
+      for (int at = first; at < end; at += kGroups<WT> * P) {
+        if (end - at <= P) down_groups<WT, VEC, 1>(a, G, at, end, rp, sp, k0, k1, to);
+        else if (kGroups<WT> == 2 || end - at <= 2 * P) down_groups<WT, VEC, 2>(a, G, at, end, rp, sp, k0, k1, to);
+        else down_groups<WT, VEC, kGroups<WT>>(a, G, at, end, rp, sp, k0, k1, to);
+      }
+    }
+    __syncthreads();
+    const int c0 = tile0 * a.width, cols = min(nt * a.width, a.d - c0);
+    for (int o = tid; o < a.T * cols; o += kFewThreads) {
+      const int t = o / cols, j = o % cols;
+      const float* from = yp + (size_t)(j / a.width * parts) * count * 8 + j % a.width;
+      float s = 0.0f;
+      for (int k = 0; k < a.K; ++k) {
+        const int q = G.place[t * a.K + k];
+        if (q < 0) continue;
+        float v = 0.0f;
+        for (int p = 0; p < parts; ++p) v += from[((size_t)p * count + q) * 8];
+        s = fmaf(a.gates[t * a.K + k], v, s);
+      }
+      const int64_t at = (int64_t)t * a.d + c0 + j;
+      if (a.y_f32) ((float*)a.y)[at] = s;
+      else ((uint16_t*)a.y)[at] = (uint16_t)pack_bf2(s, 0.0f);
+    }
+    if (tile0 + room < t1) __syncthreads();
   }
 }
 
 template <int WT, bool UP_VEC, bool DOWN_VEC>
-void launch_few(const FewArgs& a, hipStream_t st) {
-  const int pairs = a.T * a.K;
-  hipLaunchKernelGGL((few_up_kernel<WT, UP_VEC>), dim3((a.F + 7) / 8, pairs < a.W ? pairs : a.W), dim3(kUpThreads), 0,
-                     st, a);
-  const dim3 grid((a.d + 7) / 8);
-  if (pairs <= 512) hipLaunchKernelGGL((few_down_kernel<WT, DOWN_VEC, 512>), grid, dim3(kDownThreads), 0, st, a);
-  else hipLaunchKernelGGL((few_down_kernel<WT, DOWN_VEC, 2048>), grid, dim3(kDownThreads), 0, st, a);
+void launch_few(FewArgs a, hipStream_t st) {
+  const int pairs = a.T * a.K, cus = num_cus();
+  const int64_t units = (int64_t)((a.F + 7) / 8) * (pairs < a.W ? pairs : a.W);
+  hipLaunchKernelGGL((few_up_kernel<WT, UP_VEC>), dim3((unsigned)(units < cus ? units : cus)), dim3(kFewThreads), 0, st,
+                     a);
+  // an even share of the columns to every CU, in tiles of 8 at most
+  const int share = (a.d + cus - 1) / cus;
+  a.tiles = (share + 7) / 8;
+  a.width = (share + a.tiles - 1) / a.tiles;
+  const dim3 grid((a.d + a.tiles * a.width - 1) / (a.tiles * a.width));
+  if (pairs <= 512) hipLaunchKernelGGL((few_down_kernel<WT, DOWN_VEC, 512>), grid, dim3(kFewThreads), 0, st, a);
+  else hipLaunchKernelGGL((few_down_kernel<WT, DOWN_VEC, 2048>), grid, dim3(kFewThreads), 0, st, a);
 }
 
 }  // namespace

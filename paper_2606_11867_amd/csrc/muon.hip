@@ -10,7 +10,8 @@
 // leaves; the products take the first, a X takes both. So a product's factors
 // are rounded to 2^-12 of themselves, and directions that u does not have stay
 // at the size that fp32 leaves there: P X alone would fill them with the
-// rounding of X, which each of the first steps multiplies by a.
+// rounding of X, which each of the first steps multiplies by a. (The last step
+// does without the second numbers: that is one factor a.)
 // X, G and P are held 2^8 times as large, which keeps entries of large, even
 // matrices (1/sqrt(m n) and less) above fp16's subnormal numbers.
 #include <math.h>
@@ -21,7 +22,7 @@
 namespace foremoe {
 namespace {
 
-constexpr int kMuonTile = 128, kMuonBK = 64, kMuonNS = 2, kMuonWaves = 4;
+constexpr int kMuonBK = 64, kMuonNS = 2;
 constexpr int kMomentThreads = 256, kMomentChunk = 16384;  // elements of a matrix per workgroup
 constexpr float kHeld = 256.0f, kRest = 1024.0f;
 
@@ -38,6 +39,7 @@ struct MuonRec {
   uint16_t *x[2], *rest[2];  // [batch, mm, nn]
   uint16_t *gram, *poly;     // [batch, mm, mm]
   double* squares;           // [batch, chunks]
+  int32_t wide;              // the tensors' rows start on 16 bytes: read and written so
   // first workgroup of the record in each kind of launch
   uint32_t at_moment, at_scale, at_sym, at_full;
 };
@@ -45,6 +47,8 @@ struct MuonRec {
 struct MuonArgs {
   MuonRec rec[FOREMOE_MUON_LAUNCH];
   int n_rec, nesterov, zero_grads, from;  // from: which X the launch reads
+  int has_rest, put_rest;  // whether that X has its second numbers, and the written one
+  uint32_t n_sym, n_full;                 // workgroups with work in the products' launches
   float momentum, a, b, c;
   double eps;
   const float* grad_scale;
@@ -54,36 +58,97 @@ static_assert(sizeof(MuonArgs) <= 4096, "kernel arguments");
 __device__ __forceinline__ uint16_t half_bits(float v) { return __builtin_bit_cast(uint16_t, (_Float16)v); }
 __device__ __forceinline__ float half_value(uint32_t b) { return (float)__builtin_bit_cast(_Float16, (uint16_t)b); }
 
+// Two values as the fp16 numbers next to them, and 2^10 times what those leave.
+__device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t& rest) {
+  const uint32_t ha = half_bits(a), hb = half_bits(b);
+  hi = ha | hb << 16;
+  rest = (uint32_t)half_bits((a - half_value(ha)) * kRest) | (uint32_t)half_bits((b - half_value(hb)) * kRest) << 16;
+}
+__device__ __forceinline__ float join(uint32_t hi, uint32_t rest, int second) {
+  return half_value(hi >> (16 * second) & 0xffffu) + half_value(rest >> (16 * second) & 0xffffu) * (1.0f / kRest);
+}
+
 template <class At>
-__device__ __forceinline__ int find_rec(const MuonArgs& a, At at) {
+__device__ __forceinline__ int find_rec(const MuonArgs& a, uint32_t b, At at) {
   int r = 0;
   for (int i = 1; i < a.n_rec; ++i)
-    if (at(a.rec[i]) <= blockIdx.x) r = i;
+    if (at(a.rec[i]) <= b) r = i;
   return r;
 }
 
-template <bool BF16_IN>
-__device__ __forceinline__ float element(const void* p, int64_t i) {
-  if constexpr (BF16_IN) return bf2f(((const uint16_t*)p)[i]);
-  else return ((const float*)p)[i];
+// Four neighbours of a tensor, from element i on: at once (wide), or those
+// of them that are below n.
+template <bool BF16_T>
+__device__ __forceinline__ void get4(const void* p, int64_t i, int64_t left, bool wide, float* v) {
+  if constexpr (BF16_T) {
+    const uint16_t* q = (const uint16_t*)p + i;
+    if (wide && left >= 4) {
+      const uint2 w = *(const uint2*)q;
+      v[0] = bf2f(w.x & 0xffffu), v[1] = __uint_as_float(w.x & 0xffff0000u);
+      v[2] = bf2f(w.y & 0xffffu), v[3] = __uint_as_float(w.y & 0xffff0000u);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = e < left ? bf2f(q[e]) : 0.0f;
+    }
+  } else {
+    const float* q = (const float*)p + i;
+    if (wide && left >= 4) {
+      const float4 w = *(const float4*)q;
+      v[0] = w.x, v[1] = w.y, v[2] = w.z, v[3] = w.w;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = e < left ? q[e] : 0.0f;
+    }
+  }
+}
+template <bool BF16_T>
+__device__ __forceinline__ void put4(void* p, int64_t i, int64_t left, bool wide, const float* v) {
+  if constexpr (BF16_T) {
+    uint16_t* q = (uint16_t*)p + i;
+    const uint2 w = {pack_bf2(v[0], v[1]), pack_bf2(v[2], v[3])};
+    if (wide && left >= 4) {
+      *(uint2*)q = w;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (e < left) q[e] = (uint16_t)((e < 2 ? w.x : w.y) >> (16 * (e & 1)));
+    }
+  } else {
+    float* q = (float*)p + i;
+    if (wide && left >= 4) {
+      *(float4*)q = float4{v[0], v[1], v[2], v[3]};
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (e < left) q[e] = v[e];
+    }
+  }
 }
 
 // m and the squares of u, a workgroup to a chunk of a matrix.
 template <bool GBF16>
 __global__ __launch_bounds__(kMomentThreads) void muon_moment_kernel(MuonArgs a) {
-  const MuonRec& r = a.rec[find_rec(a, [](const MuonRec& q) { return q.at_moment; })];
+  const MuonRec& r = a.rec[find_rec(a, blockIdx.x, [](const MuonRec& q) { return q.at_moment; })];
   const uint32_t b = blockIdx.x - r.at_moment;
   const int64_t matrix = b / r.chunks, chunk = b % r.chunks;
   const int64_t n = (int64_t)r.rows * r.cols, base = matrix * n;
   const int64_t lo = chunk * kMomentChunk, hi = lo + kMomentChunk < n ? lo + kMomentChunk : n;
   const float gs = a.grad_scale ? *a.grad_scale : 1.0f;
+  const bool wide = r.wide;
   double s = 0;
-  for (int64_t i = lo + threadIdx.x; i < hi; i += kMomentThreads) {
-    const float g = element<GBF16>(r.grad, base + i) * gs;
-    const float m = fmaf(a.momentum, r.m[base + i], g);
-    r.m[base + i] = m;
-    const float u = a.nesterov ? fmaf(a.momentum, m, g) : m;
-    s += (double)u * u;
+#pragma unroll 4
+  for (int64_t i = lo + threadIdx.x * 4; i < hi; i += kMomentThreads * 4) {
+    float g[4], m[4];
+    get4<GBF16>(r.grad, base + i, hi - i, wide, g);
+    get4<false>(r.m, base + i, hi - i, wide, m);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      g[e] *= gs;
+      m[e] = fmaf(a.momentum, m[e], g[e]);
+      const float u = a.nesterov ? fmaf(a.momentum, m[e], g[e]) : m[e];
+      s += (double)u * u;
+    }
+    put4<false>(r.m, base + i, hi - i, wide, m);
   }
   __shared__ double part[kMomentThreads / 64];
 #pragma unroll
@@ -100,25 +165,20 @@ __global__ __launch_bounds__(kMomentThreads) void muon_moment_kernel(MuonArgs a)
 // X = u / max(|u|, eps), 64 x 64 of the padded matrix to a workgroup.
 template <bool GBF16>
 __global__ __launch_bounds__(256) void muon_scale_kernel(MuonArgs a) {
-  const MuonRec& r = a.rec[find_rec(a, [](const MuonRec& q) { return q.at_scale; })];
+  const MuonRec& r = a.rec[find_rec(a, blockIdx.x, [](const MuonRec& q) { return q.at_scale; })];
   const uint32_t b = blockIdx.x - r.at_scale;
   const uint32_t tn = r.nn / 64, tiles = (uint32_t)(r.mm / 64) * tn;
   const int64_t matrix = b / tiles;
   const int i0 = (int)(b % tiles / tn) * 64, j0 = (int)(b % tiles % tn) * 64;
-  const bool tall = r.rows > r.cols;
+  const bool tall = r.rows > r.cols, wide = r.wide;
   const int tid = threadIdx.x;
-  // the matrix's norm, summed in the same order by every workgroup
-  __shared__ double part[256];
   __shared__ float tile[64][65];
+  // the matrix's norm, summed in the same order by every wavefront
   double s = 0;
-  for (uint32_t i = tid; i < r.chunks; i += 256) s += r.squares[matrix * r.chunks + i];
-  part[tid] = s;
-  __syncthreads();
-  for (int o = 128; o; o >>= 1) {
-    if (tid < o) part[tid] += part[tid + o];
-    __syncthreads();
-  }
-  const double norm = sqrt(part[0]);
+  for (uint32_t i = tid & 63; i < r.chunks; i += 64) s += r.squares[matrix * r.chunks + i];
+#pragma unroll
+  for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o, 64);
+  const double norm = sqrt(s);
   const double den = !(norm <= a.eps) ? norm : a.eps;
   // nothing in it: no move; not finite: NaN everywhere
   const double inv = den == 0 ? 0.0 : (isinf(den) ? (double)NAN : 1.0 / den);
@@ -126,47 +186,85 @@ __global__ __launch_bounds__(256) void muon_scale_kernel(MuonArgs a) {
   const int64_t base = matrix * (int64_t)r.rows * r.cols;
   // read along the source's rows
   const int r0 = tall ? j0 : i0, c0 = tall ? i0 : j0;
-  for (int e = tid; e < 4096; e += 256) {
-    const int rr = r0 + (e >> 6), cc = c0 + (e & 63);
-    float v = 0.0f;
-    if (rr < r.rows && cc < r.cols) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int tr = k * 16 + (tid >> 4), tc = (tid & 15) * 4;
+    const int rr = r0 + tr, cc = c0 + tc, left = r.cols - cc;
+    float u[4] = {0, 0, 0, 0};
+    if (rr < r.rows && left > 0) {
       const int64_t i = base + (int64_t)rr * r.cols + cc;
-      float u = r.m[i];
-      if (a.nesterov) u = fmaf(a.momentum, u, element<GBF16>(r.grad, i) * gs);
-      if (a.zero_grads) {
-        if constexpr (GBF16) ((uint16_t*)r.grad)[i] = 0;
-        else ((float*)r.grad)[i] = 0.0f;
+      get4<false>(r.m, i, left, wide, u);
+      if (a.nesterov) {
+        float g[4];
+        get4<GBF16>(r.grad, i, left, wide, g);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) u[e] = fmaf(a.momentum, u[e], g[e] * gs);
       }
-      v = (float)((double)u * inv) * kHeld;
+      if (a.zero_grads) {
+        const float z[4] = {0, 0, 0, 0};
+        put4<GBF16>(r.grad, i, left, wide, z);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) u[e] = e < left ? (float)((double)u[e] * inv) * kHeld : 0.0f;
     }
-    tile[e >> 6][e & 63] = v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) tile[tr][tc + e] = u[e];
   }
   __syncthreads();
   const int64_t at = matrix * (int64_t)r.mm * r.nn;
-  for (int e = tid; e < 4096; e += 256) {
-    const int i = e >> 6, j = e & 63;
-    const float v = tall ? tile[j][i] : tile[i][j];
-    const uint16_t h = half_bits(v);
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int i = k * 32 + (tid >> 3), j = (tid & 7) * 8;
+    uint32_t h[4], l[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float v0 = tall ? tile[j + 2 * e][i] : tile[i][j + 2 * e];
+      const float v1 = tall ? tile[j + 2 * e + 1][i] : tile[i][j + 2 * e + 1];
+      split2(v0, v1, h[e], l[e]);
+    }
     const int64_t o = at + (int64_t)(i0 + i) * r.nn + j0 + j;
-    r.x[0][o] = h;
-    r.rest[0][o] = half_bits((v - half_value(h)) * kRest);
+    *(uint4*)(r.x[0] + o) = uint4{h[0], h[1], h[2], h[3]};
+    *(uint4*)(r.rest[0] + o) = uint4{l[0], l[1], l[2], l[3]};
   }
 }
 
-enum Product { kGram = 0, kPoly = 1, kApply = 2 };
+enum Product { kGram = 0, kPoly = 1, kApply = 2, kUpdate = 3 };
 
-// One 128 x 128 tile of one matrix's product.
-template <Product P>
-__global__ __launch_bounds__(64 * kMuonWaves) void muon_product_kernel(MuonArgs a) {
-  constexpr int T = kMuonTile, BK = kMuonBK, NS = kMuonNS, NW = kMuonWaves;
-  constexpr bool SYM = P != kApply;
-  using CoreT = Core<T, T, 2, 2, false, Fp16>;
+// p = p (1 - lr weight_decay) - lr scale X for four neighbours, x = 2^8 X.
+template <bool PBF16>
+__device__ __forceinline__ void update4(const MuonRec& r, int64_t i, int left, const float* x) {
+  float p[4];
+  const bool wide = r.wide;
+  if (PBF16 && !r.master) get4<true>(r.param, i, left, wide, p);
+  else get4<false>(PBF16 ? r.master : r.param, i, left, wide, p);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) p[e] = fmaf(-r.move, x[e] * (1.0f / kHeld), p[e] * r.decay);
+  if (r.master) put4<false>(r.master, i, left, wide, p);
+  put4<PBF16>(r.param, i, left, wide, p);
+}
+
+// One T x T tile of one matrix's product, by wavefronts of 64 x 64 (T = 128) or
+// 64 x 128 (T = 256). The workgroups of an XCD have neighbouring tiles, whose
+// operands its L2 then holds once (48 matrices of 768 x 2048, G: 135 -> 92 us).
+// The sums go through LDS, so that memory is read and written in whole lines
+// (X of the same: 412 -> 242 us). kUpdate is the last step's kApply: its X
+// goes into the parameters at once.
+template <int P, bool PBF16, int T>
+__global__ __launch_bounds__(T * 2) void muon_product_kernel(MuonArgs a) {
+  constexpr int BK = kMuonBK, NS = kMuonNS, NW = T / 32, NT = 64 * NW, WN = T / 2;
+  constexpr bool SYM = P == kGram || P == kPoly;
+  using CoreT = Core<T, T, T / 64, 2, false, Fp16>;
   using AT = KTile<T, BK, NW>;
   using BT = typename std::conditional<SYM, KTile<T, BK, NW>, MTile<T, BK, NW>>::type;
   constexpr int STAGE = AT::BYTES + BT::BYTES;
-  __shared__ __attribute__((aligned(1024))) char lds[NS * STAGE];
-  const MuonRec& r = a.rec[find_rec(a, [](const MuonRec& q) { return SYM ? q.at_sym : q.at_full; })];
-  const uint32_t b = blockIdx.x - (SYM ? r.at_sym : r.at_full);
+  constexpr int LD = T + 4;  // floats of a row of sums: rows 4 banks apart
+  constexpr int H = 64;      // the sums go through LDS by the rows of a wavefront
+  constexpr int LDS_BYTES = NS * STAGE > H * LD * 4 ? NS * STAGE : H * LD * 4;
+  __shared__ __attribute__((aligned(1024))) char lds[LDS_BYTES];
+  const uint32_t bid = (uint32_t)xcd_virtual_id();
+  if (bid >= (SYM ? a.n_sym : a.n_full)) return;
+  const MuonRec& r = a.rec[find_rec(a, bid, [](const MuonRec& q) { return SYM ? q.at_sym : q.at_full; })];
+  const uint32_t b = bid - (SYM ? r.at_sym : r.at_full);
   const uint32_t tm = (uint32_t)r.mm / T, tn = (uint32_t)r.nn / T;
   const uint32_t tiles = SYM ? tm * (tm + 1) / 2 : tm * tn;
   const int64_t matrix = b / tiles;
@@ -180,13 +278,14 @@ __global__ __launch_bounds__(64 * kMuonWaves) void muon_product_kernel(MuonArgs 
   }
   const int i0 = __builtin_amdgcn_readfirstlane((int)ti) * T, j0 = __builtin_amdgcn_readfirstlane((int)tj) * T;
   const int lane = lane64(), wave = wave_id(), wm = wave / 2, wn = wave % 2;
-  const uint16_t* X = r.x[a.from] + matrix * (int64_t)r.mm * r.nn;
-  const uint16_t* G = r.gram + matrix * (int64_t)r.mm * r.mm;
+  const int64_t xat = matrix * (int64_t)r.mm * r.nn;
+  const uint16_t* X = r.x[a.from] + xat;
+  uint16_t* G = r.gram + matrix * (int64_t)r.mm * r.mm;
   uint16_t* Q = r.poly + matrix * (int64_t)r.mm * r.mm;
   const int lda = P == kGram ? r.nn : r.mm, ldb = P == kPoly ? r.mm : r.nn;
   const int KT = (P == kGram ? r.nn : r.mm) / BK;
   const uint16_t* abase = (P == kGram ? X : P == kPoly ? G : Q) + (int64_t)i0 * lda;
-  const uint16_t* bbase = P == kApply ? X + j0 : (P == kGram ? X : G) + (int64_t)j0 * ldb;
+  const uint16_t* bbase = SYM ? (P == kGram ? X : G) + (int64_t)j0 * ldb : X + j0;
   const uint32_t lda2 = (uint32_t)lda * 2, ldb2 = (uint32_t)ldb * 2;
   const uint32_t lds0 = lds_addr(lds);
   auto off_a = [&](int q) -> uint32_t { return (uint32_t)q * lda2; };
@@ -214,62 +313,102 @@ __global__ __launch_bounds__(64 * kMuonWaves) void muon_product_kernel(MuonArgs 
   CoreT core;
   const typename CoreT::template Offsets<AT, BT, BK> offs(lane, wm, wn);
   core.zero();
-  pipelined_k_loop<CoreT, AT, BT, BK, NS, 1>(core, lds, KT, offs, issue, false, [] {});
-
-  const int64_t xat = matrix * (int64_t)r.mm * r.nn;
+  pipelined_k_loop<CoreT, AT, BT, BK, NS, T == 256 ? 2 : 1>(core, lds, KT, offs, issue, false, [] {});
+  float(*sum)[LD] = (float(*)[LD])lds;
+  const int tid = threadIdx.x;
+  const bool tall = r.rows > r.cols;
+#pragma unroll 1
+  for (int part = 0; part < T / H; ++part) {
+    __syncthreads();  // every wavefront has read its last fragments, or the sums before
+    if (wm == part) {
 #pragma unroll
-  for (int i = 0; i < CoreT::MB; ++i)
+      for (int i = 0; i < CoreT::MB; ++i)
 #pragma unroll
-    for (int j = 0; j < CoreT::NB; ++j) {
-      const int row = i0 + wm * 64 + 32 * i + (lane & 31);
+        for (int j = 0; j < CoreT::NB; ++j)
 #pragma unroll
-      for (int q4 = 0; q4 < 4; ++q4) {
-        const int col = j0 + wn * 64 + 32 * j + 8 * q4 + 4 * (lane >> 5);
-        float v[4];
+          for (int q = 0; q < 4; ++q) {
+            float v[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = core.acc[i][j][4 * q4 + e] * (1.0f / kHeld);
+            for (int e = 0; e < 4; ++e) v[e] = core.acc[i][j][4 * q + e] * (1.0f / kHeld);
+            *(float4*)&sum[32 * i + (lane & 31)][wn * WN + 32 * j + 8 * q + 4 * (lane >> 5)] =
+                float4{v[0], v[1], v[2], v[3]};
+          }
+    }
+    __syncthreads();
+    const int ih = i0 + part * H;  // their first row
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int i = k * 16 + tid / (T / 8), j = tid % (T / 8) * 8;
+      float v[8];
+      *(float4*)v = *(const float4*)&sum[i][j];
+      *(float4*)(v + 4) = *(const float4*)&sum[i][j + 4];
+      if constexpr (P == kApply || P == kUpdate) {
+        const int64_t o = xat + (int64_t)(ih + i) * r.nn + j0 + j;
+        const uint4 h4 = *(const uint4*)(r.x[a.from] + o);
+        const uint4 l4 = a.has_rest ? *(const uint4*)(r.rest[a.from] + o) : uint4{0, 0, 0, 0};
+        const uint32_t h[4] = {h4.x, h4.y, h4.z, h4.w}, l[4] = {l4.x, l4.y, l4.z, l4.w};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = fmaf(a.a, join(h[e / 2], l[e / 2], e & 1), v[e]);
         if constexpr (P == kApply) {
-          const int64_t o = xat + (int64_t)row * r.nn + col;
-          const uint2 h = *(const uint2*)(r.x[a.from] + o), l = *(const uint2*)(r.rest[a.from] + o);
-          const uint32_t hw[2] = {h.x, h.y}, lw[2] = {l.x, l.y};
-          uint32_t nh[2] = {0, 0}, nl[2] = {0, 0};
+          uint32_t nh[4], nl[4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int s = 16 * (e & 1);
-            const float old = half_value(hw[e / 2] >> s & 0xffffu) + half_value(lw[e / 2] >> s & 0xffffu) * (1.0f / kRest);
-            const float x = fmaf(a.a, old, v[e]);
-            const uint32_t hb = half_bits(x);
-            nh[e / 2] |= hb << s;
-            nl[e / 2] |= (uint32_t)half_bits((x - half_value(hb)) * kRest) << s;
-          }
-          *(uint2*)(r.x[a.from ^ 1] + o) = uint2{nh[0], nh[1]};
-          *(uint2*)(r.rest[a.from ^ 1] + o) = uint2{nl[0], nl[1]};
+          for (int e = 0; e < 4; ++e) split2(v[2 * e], v[2 * e + 1], nh[e], nl[e]);
+          *(uint4*)(r.x[a.from ^ 1] + o) = uint4{nh[0], nh[1], nh[2], nh[3]};
+          if (a.put_rest) *(uint4*)(r.rest[a.from ^ 1] + o) = uint4{nl[0], nl[1], nl[2], nl[3]};
         } else {
-          uint16_t* out = P == kGram ? (uint16_t*)G : Q;
-          if constexpr (P == kPoly) {
-            const uint2 h = *(const uint2*)(G + (int64_t)row * r.mm + col);
-            const uint32_t hw[2] = {h.x, h.y};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = fmaf(a.c, v[e], a.b * half_value(hw[e / 2] >> (16 * (e & 1)) & 0xffffu));
-          }
-          uint16_t hb[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) hb[e] = half_bits(v[e]);
-          *(uint2*)(out + (int64_t)row * r.mm + col) =
-              uint2{(uint32_t)hb[0] | (uint32_t)hb[1] << 16, (uint32_t)hb[2] | (uint32_t)hb[3] << 16};
-          if (ti != tj) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) out[(int64_t)(col + e) * r.mm + row] = hb[e];
-          }
+          *(float4*)&sum[i][j] = *(const float4*)v;
+          *(float4*)&sum[i][j + 4] = *(const float4*)(v + 4);
         }
+      } else {
+        const int64_t o = (int64_t)(ih + i) * r.mm + j0 + j;
+        if constexpr (P == kPoly) {
+          const uint4 g4 = *(const uint4*)(G + o);
+          const uint32_t g[4] = {g4.x, g4.y, g4.z, g4.w};
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = fmaf(a.c, v[e], a.b * half_value(g[e / 2] >> (16 * (e & 1)) & 0xffffu));
+          *(float4*)&sum[i][j] = *(const float4*)v;
+          *(float4*)&sum[i][j + 4] = *(const float4*)(v + 4);
+        }
+        uint32_t h[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) h[e] = (uint32_t)half_bits(v[2 * e]) | (uint32_t)half_bits(v[2 * e + 1]) << 16;
+        *(uint4*)((P == kGram ? G : Q) + o) = uint4{h[0], h[1], h[2], h[3]};
       }
     }
+    if (P == kApply || (SYM && ti == tj)) continue;
+    __syncthreads();
+    if constexpr (SYM) {  // the same on the other side of the diagonal
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int j = k * (NT / 8) + (tid >> 3), i = (tid & 7) * 8;
+        uint32_t h[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          h[e] = (uint32_t)half_bits(sum[i + 2 * e][j]) | (uint32_t)half_bits(sum[i + 2 * e + 1][j]) << 16;
+        *(uint4*)((P == kGram ? G : Q) + (int64_t)(j0 + j) * r.mm + ih + i) = uint4{h[0], h[1], h[2], h[3]};
+      }
+    } else {
+      // H rows of X by T columns: of the parameters too, or T rows by H columns
+      const int r0 = tall ? j0 : ih, c0 = tall ? ih : j0;
+      const int64_t base = matrix * (int64_t)r.rows * r.cols;
+#pragma unroll 4
+      for (int k = 0; k < 8; ++k) {
+        const int i = tall ? k * (NT / 16) + tid / 16 : k * 8 + tid / (T / 4), j = (tall ? tid % 16 : tid % (T / 4)) * 4;
+        const int left = r.cols - (c0 + j);
+        if (r0 + i >= r.rows || left <= 0) continue;
+        float x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = tall ? sum[j + e][i] : sum[i][j + e];
+        update4<PBF16>(r, base + (int64_t)(r0 + i) * r.cols + c0 + j, left, x);
+      }
+    }
+  }
 }
 
-// p = p (1 - lr weight_decay) - lr scale X, 64 x 64 of X to a workgroup.
+// The update without any step of the iteration: 64 x 64 of X to a workgroup.
 template <bool PBF16>
 __global__ __launch_bounds__(256) void muon_update_kernel(MuonArgs a) {
-  const MuonRec& r = a.rec[find_rec(a, [](const MuonRec& q) { return q.at_scale; })];
+  const MuonRec& r = a.rec[find_rec(a, blockIdx.x, [](const MuonRec& q) { return q.at_scale; })];
   const uint32_t b = blockIdx.x - r.at_scale;
   const uint32_t tn = r.nn / 64, tiles = (uint32_t)(r.mm / 64) * tn;
   const int64_t matrix = b / tiles;
@@ -281,32 +420,25 @@ __global__ __launch_bounds__(256) void muon_update_kernel(MuonArgs a) {
   for (int e = tid; e < 4096; e += 256) {
     const int i = e >> 6, j = e & 63;
     const int64_t o = at + (int64_t)(i0 + i) * r.nn + j0 + j;
-    const float x = (half_value(r.x[a.from][o]) + half_value(r.rest[a.from][o]) * (1.0f / kRest)) * (1.0f / kHeld);
+    const float x = join(r.x[0][o], r.rest[0][o], 0);
     if (tall) tile[j][i] = x;
     else tile[i][j] = x;
   }
   __syncthreads();
   const int r0 = tall ? j0 : i0, c0 = tall ? i0 : j0;
   const int64_t base = matrix * (int64_t)r.rows * r.cols;
-  for (int e = tid; e < 4096; e += 256) {
-    const int rr = r0 + (e >> 6), cc = c0 + (e & 63);
-    if (rr >= r.rows || cc >= r.cols) continue;
-    const int64_t o = base + (int64_t)rr * r.cols + cc;
-    const float old = PBF16 && !r.master ? bf2f(((const uint16_t*)r.param)[o])
-                                         : (r.master ? r.master[o] : ((const float*)r.param)[o]);
-    const float p = fmaf(-r.move, tile[e >> 6][e & 63], old * r.decay);
-    if (r.master) r.master[o] = p;
-    if constexpr (PBF16) ((uint16_t*)r.param)[o] = (uint16_t)pack_bf2(p, 0.0f);
-    else ((float*)r.param)[o] = p;
+  for (int k = 0; k < 4; ++k) {
+    const int i = k * 16 + (tid >> 4), j = (tid & 15) * 4, left = r.cols - (c0 + j);
+    if (r0 + i < r.rows && left > 0) update4<PBF16>(r, base + (int64_t)(r0 + i) * r.cols + c0 + j, left, &tile[i][j]);
   }
 }
 
-int64_t pad_side(int64_t n) { return (n + kMuonTile - 1) / kMuonTile * kMuonTile; }
+int64_t pad_side(int64_t n, int tile) { return (n + tile - 1) / tile * tile; }
 
 // Lays a tensor's part of the workspace out from `at` (bytes); returns its end.
-size_t lay_out(const foremoe_muon_tensor& t, size_t at, char* ws, MuonRec* r) {
+size_t lay_out(const foremoe_muon_tensor& t, int tile, size_t at, char* ws, MuonRec* r) {
   const int64_t s = t.rows < t.cols ? t.rows : t.cols, l = t.rows < t.cols ? t.cols : t.rows;
-  const int64_t mm = pad_side(s), nn = pad_side(l);
+  const int64_t mm = pad_side(s, tile), nn = pad_side(l, tile);
   const int64_t chunks = (s * l + kMomentChunk - 1) / kMomentChunk;
   auto take = [&](size_t bytes) {
     char* p = ws + at;
@@ -326,10 +458,56 @@ size_t lay_out(const foremoe_muon_tensor& t, size_t at, char* ws, MuonRec* r) {
   return at;
 }
 
-// 64 x 64 tiles of a tensor: no launch over it has more workgroups.
+// 64 x 64 tiles of a tensor padded to 256: no launch over it has more workgroups.
 constexpr int64_t kMuonMostTiles = (int64_t)1 << 23;
 int64_t scale_tiles(const foremoe_muon_tensor& t) {
-  return t.batch * (pad_side(t.rows) / 64) * (pad_side(t.cols) / 64);
+  return t.batch * (pad_side(t.rows, 256) / 64) * (pad_side(t.cols, 256) / 64);
+}
+
+// Tiles of the products' launches over the tensors [i, end): of the symmetric
+// ones, and of X. A k step of a 256-wide tile takes a CU about as long as one
+// of two 128-wide ones, four times the work against two; one 128-wide tile
+// alone about half of that. So the wide ones are faster where whole rounds of
+// them fill the CUs and the padding does not take it back (us, 128 / 256: 48
+// matrices of 768 x 2048, G 92 / 118, X 242 / 215; 6 of 2048 x 7168, G 229 /
+// 194, X 488 / 455).
+struct Tiles {
+  int pad, sym, full;
+};
+Tiles choose_tiles(const foremoe_muon_tensor* tensors, int i, int end) {
+  // rounds x k steps of a launch of `tile` over matrices padded to `pad`
+  auto cost = [&](int tile, int pad, bool of_x) {
+    double tiles = 0, steps = 0;
+    for (int j = i; j < end; ++j) {
+      const foremoe_muon_tensor& t = tensors[j];
+      if (t.batch == 0) continue;
+      const double m = (double)pad_side(t.rows < t.cols ? t.rows : t.cols, pad);
+      const double n = (double)pad_side(t.rows < t.cols ? t.cols : t.rows, pad);
+      const double tm = m / tile, count = t.batch * (of_x ? tm * (n / tile) : tm * (tm + 1) / 2);
+      tiles += count, steps += count * (of_x ? m : n + m);
+    }
+    if (tiles == 0) return 0.0;
+    const bool wide = tile == 256;
+    return ceil(tiles / (wide ? 256 : 512)) * (steps / tiles) * (wide || tiles > 256 ? 1.0 : 0.5);
+  };
+  const double sym = cost(128, 256, false), full = cost(128, 256, true);
+  const double wide_sym = cost(256, 256, false), wide_full = cost(256, 256, true);
+  const double narrow = cost(128, 128, false) + cost(128, 128, true);
+  if (narrow <= fmin(sym, wide_sym) + fmin(full, wide_full)) return {128, 128, 128};
+  return {256, wide_sym < sym ? 256 : 128, wide_full < full ? 256 : 128};
+}
+
+// The end of the launches' group of tensors that starts at i.
+int group_end(const foremoe_muon_tensor* tensors, int i, int n) {
+  int count = 0;
+  int64_t tiles = 0;
+  for (; i < n; ++i) {
+    if (tensors[i].batch == 0) continue;
+    tiles += scale_tiles(tensors[i]);
+    if (count == FOREMOE_MUON_LAUNCH || (count > 0 && tiles > kMuonMostTiles)) break;
+    ++count;
+  }
+  return i;
 }
 
 int check_tensor(const foremoe_muon_tensor& t, int i) {
@@ -345,15 +523,25 @@ int check_tensor(const foremoe_muon_tensor& t, int i) {
   return FOREMOE_OK;
 }
 
-// Whether a tensor starts another launch behind n others of `tiles` tiles.
-bool starts_launch(const foremoe_muon_tensor& t, int n, int64_t tiles) {
-  return n == FOREMOE_MUON_LAUNCH || (n > 0 && tiles + scale_tiles(t) > kMuonMostTiles);
-}
-
 }  // namespace
 }  // namespace foremoe
 
 using namespace foremoe;
+
+// (grids of a multiple of the XCDs: see xcd_virtual_id)
+template <int T>
+static void launch_symmetric(const MuonArgs& a, hipStream_t st) {
+  const dim3 grid((a.n_sym + 7) / 8 * 8), threads(T * 2);
+  hipLaunchKernelGGL((muon_product_kernel<kGram, false, T>), grid, threads, 0, st, a);
+  hipLaunchKernelGGL((muon_product_kernel<kPoly, false, T>), grid, threads, 0, st, a);
+}
+template <int T>
+static void launch_x(const MuonArgs& a, int product, bool param_bf16, hipStream_t st) {
+  const dim3 grid((a.n_full + 7) / 8 * 8), threads(T * 2);
+  if (product == kApply) hipLaunchKernelGGL((muon_product_kernel<kApply, false, T>), grid, threads, 0, st, a);
+  else if (param_bf16) hipLaunchKernelGGL((muon_product_kernel<kUpdate, true, T>), grid, threads, 0, st, a);
+  else hipLaunchKernelGGL((muon_product_kernel<kUpdate, false, T>), grid, threads, 0, st, a);
+}
 
 #define REQUIRE(cond, ...)                                      \
   do {                                                          \
@@ -366,17 +554,16 @@ extern "C" {
 
 size_t foremoe_muon_workspace_size(const foremoe_muon_tensor* tensors, int32_t n_tensors) {
   if (n_tensors < 0 || (n_tensors > 0 && !tensors)) return 0;
-  size_t most = 256, at = 0;
-  int64_t tiles = 0;
-  int n = 0;
-  for (int i = 0; i < n_tensors; ++i) {
+  for (int i = 0; i < n_tensors; ++i)
     if (check_tensor(tensors[i], i) != FOREMOE_OK) return 0;
-    if (tensors[i].batch == 0) continue;
-    if (starts_launch(tensors[i], n, tiles)) n = 0, at = 0, tiles = 0;
-    at = lay_out(tensors[i], at, nullptr, nullptr);
+  size_t most = 256;
+  for (int i = 0, end; i < n_tensors; i = end) {
+    end = group_end(tensors, i, n_tensors);
+    const int pad = choose_tiles(tensors, i, end).pad;
+    size_t at = 0;
+    for (int j = i; j < end; ++j)
+      if (tensors[j].batch) at = lay_out(tensors[j], pad, at, nullptr, nullptr);
     most = at > most ? at : most;
-    tiles += scale_tiles(tensors[i]);
-    ++n;
   }
   return most;
 }
@@ -419,46 +606,57 @@ int foremoe_muon_step(const foremoe_muon_tensor* tensors, int32_t n_tensors, for
   a.nesterov = nesterov != 0, a.zero_grads = zero_grads != 0, a.grad_scale = grad_scale;
   a.momentum = (float)momentum, a.a = (float)coef[0], a.b = (float)coef[1], a.c = (float)coef[2], a.eps = eps;
   hipStream_t st = (hipStream_t)stream;
-  uint64_t moment = 0, scale = 0, sym = 0, full = 0;
-  size_t at = 0;
   int rc = FOREMOE_OK;
-  auto flush = [&] {
-    if (!a.n_rec || rc != FOREMOE_OK) return;
-    a.from = 0;
-    const dim3 gm((unsigned)moment), gsc((unsigned)scale), gsy((unsigned)sym), gf((unsigned)full), pt(64 * kMuonWaves);
+  for (int i = 0, end; i < n_tensors && rc == FOREMOE_OK; i = end) {
+    end = group_end(tensors, i, n_tensors);
+    const Tiles tiles = choose_tiles(tensors, i, end);
+    uint64_t moment = 0, scale = 0, sym = 0, full = 0;
+    size_t at = 0;
+    a.n_rec = 0;
+    for (int j = i; j < end; ++j) {
+      const foremoe_muon_tensor& t = tensors[j];
+      if (t.batch == 0) continue;
+      MuonRec& r = a.rec[a.n_rec++];
+      at = lay_out(t, tiles.pad, at, (char*)ws, &r);
+      r.param = t.param, r.grad = t.grad, r.master = t.master, r.m = t.m;
+      r.batch = t.batch, r.rows = t.rows, r.cols = t.cols;
+      r.wide = t.cols % 4 == 0 && !misaligned(t.param, 16) && !misaligned(t.grad, 16) && !misaligned(t.master, 16) &&
+               !misaligned(t.m, 16);
+      r.decay = (float)(1 - lr * t.weight_decay), r.move = (float)(lr * t.scale);
+      const uint64_t ts = r.mm / tiles.sym;
+      r.at_moment = (uint32_t)moment, r.at_scale = (uint32_t)scale;
+      r.at_sym = (uint32_t)sym, r.at_full = (uint32_t)full;
+      moment += (uint64_t)t.batch * r.chunks, scale += (uint64_t)t.batch * (r.mm / 64) * (r.nn / 64);
+      sym += (uint64_t)t.batch * (ts * (ts + 1) / 2);
+      full += (uint64_t)t.batch * (r.mm / tiles.full) * (r.nn / tiles.full);
+    }
+    if (a.n_rec == 0) continue;
+    a.n_sym = (uint32_t)sym, a.n_full = (uint32_t)full, a.from = 0;
+    const dim3 gm((unsigned)moment), gs((unsigned)scale);
     if (grad_dtype == FOREMOE_BF16) {
       hipLaunchKernelGGL((muon_moment_kernel<true>), gm, dim3(kMomentThreads), 0, st, a);
-      hipLaunchKernelGGL((muon_scale_kernel<true>), gsc, dim3(256), 0, st, a);
+      hipLaunchKernelGGL((muon_scale_kernel<true>), gs, dim3(256), 0, st, a);
     } else {
       hipLaunchKernelGGL((muon_moment_kernel<false>), gm, dim3(kMomentThreads), 0, st, a);
-      hipLaunchKernelGGL((muon_scale_kernel<false>), gsc, dim3(256), 0, st, a);
+      hipLaunchKernelGGL((muon_scale_kernel<false>), gs, dim3(256), 0, st, a);
     }
-    for (int i = 0; i < ns_steps; ++i) {
-      hipLaunchKernelGGL((muon_product_kernel<kGram>), gsy, pt, 0, st, a);
-      hipLaunchKernelGGL((muon_product_kernel<kPoly>), gsy, pt, 0, st, a);
-      hipLaunchKernelGGL((muon_product_kernel<kApply>), gf, pt, 0, st, a);
+    if (ns_steps == 0) {
+      if (param_dtype == FOREMOE_BF16) hipLaunchKernelGGL((muon_update_kernel<true>), gs, dim3(256), 0, st, a);
+      else hipLaunchKernelGGL((muon_update_kernel<false>), gs, dim3(256), 0, st, a);
+    }
+    for (int step = 0; step < ns_steps; ++step) {
+      // the X before the last step has no second numbers: one more step
+      // multiplies what that leaves out by a at most
+      a.has_rest = step == 0 || step + 1 < ns_steps, a.put_rest = step + 2 < ns_steps;
+      const int apply = step + 1 < ns_steps ? kApply : kUpdate;
+      if (tiles.sym == 256) launch_symmetric<256>(a, st);
+      else launch_symmetric<128>(a, st);
+      if (tiles.full == 256) launch_x<256>(a, apply, param_dtype == FOREMOE_BF16, st);
+      else launch_x<128>(a, apply, param_dtype == FOREMOE_BF16, st);
       a.from ^= 1;
     }
-    if (param_dtype == FOREMOE_BF16) hipLaunchKernelGGL((muon_update_kernel<true>), gsc, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((muon_update_kernel<false>), gsc, dim3(256), 0, st, a);
     rc = check_launch("muon_step");
-    a.n_rec = 0, at = 0, moment = scale = sym = full = 0;
-  };
-  for (int i = 0; i < n_tensors; ++i) {
-    const foremoe_muon_tensor& t = tensors[i];
-    if (t.batch == 0) continue;
-    if (starts_launch(t, a.n_rec, (int64_t)scale)) flush();
-    MuonRec& r = a.rec[a.n_rec++];
-    at = lay_out(t, at, (char*)ws, &r);
-    r.param = t.param, r.grad = t.grad, r.master = t.master, r.m = t.m;
-    r.batch = t.batch, r.rows = t.rows, r.cols = t.cols;
-    r.decay = (float)(1 - lr * t.weight_decay), r.move = (float)(lr * t.scale);
-    const uint64_t tm = r.mm / kMuonTile, tn = r.nn / kMuonTile;
-    r.at_moment = (uint32_t)moment, r.at_scale = (uint32_t)scale, r.at_sym = (uint32_t)sym, r.at_full = (uint32_t)full;
-    moment += (uint64_t)t.batch * r.chunks, scale += (uint64_t)t.batch * tm * tn * 4;
-    sym += (uint64_t)t.batch * (tm * (tm + 1) / 2), full += (uint64_t)t.batch * tm * tn;
   }
-  flush();
   return rc;
 }
 

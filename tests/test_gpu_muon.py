@@ -217,3 +217,21 @@ def test_tensors_given_other_memory(gpu):
                 dict(params=[p], grads=[p], masters=[p])):
         with pytest.raises(ValueError):
             Muon(**bad)
+
+
+@pytest.mark.parametrize("shape", [(64, 500, 700), (90, 515, 300), (150, 256, 256)])
+def test_many_large_matrices(gpu, shape):
+    """Enough of them for the wide tiles; some are looked at."""
+    from paper_2606_11867_amd.optimizer import Muon
+    print(f"\n[case] muon {shape}", flush=True)
+    rng = np.random.default_rng(9)
+    g = torch.randn(shape, device=gpu) * 1e-3
+    look = [0, 1, shape[0] // 2, shape[0] - 1]
+    g[look[1]] = torch.from_numpy(_matrix(rng, shape[1:], 20).astype(np.float32)).to(gpu)
+    p = torch.zeros(shape, device=gpu)
+    Muon([p], [g], lr=1.0, momentum=0.0, nesterov=False, scale=-1.0).step()
+    for i in look:
+        _x_close(_np(p[i]), _np(g[i]))
+    q = torch.zeros_like(p)
+    Muon([q], [g], lr=1.0, momentum=0.0, nesterov=False, scale=-1.0).step()
+    assert torch.equal(p, q)
