@@ -110,14 +110,27 @@ def newton_schulz(x, coef, steps):
     return x.T if tall else x
 
 
-def newton_schulz_fp16(x, coef, steps):
-    """The same with the products' factors rounded to fp16 as the step's format
-    has them: X in two numbers, of which the products take the first, and the
-    last step does without the second (unless it is the first too)."""
+def newton_schulz_held(x, coef, steps):
+    """The same with the roundings that the step's format has. A side of at most
+    64: G and the product of all M = a I + b G + c G G in fp32, X = Q X0. Else
+    the products' factors in fp16, of X the first of two numbers; the last step
+    does without the second (unless it is the first too)."""
+    tall = x.shape[0] > x.shape[1]
+    x = x.T if tall else x
+    if min(x.shape) <= 64:
+        f = np.float32
+        a, b, c = (f(v) for v in coef)
+        g = x.astype(f) @ x.astype(f).T
+        q = np.eye(len(x), dtype=f)
+        for _ in range(steps):
+            m = a * np.eye(len(x), dtype=f) + b * g + c * (g @ g)
+            q = m @ q
+            g = m @ g @ m
+        x = (q @ x.astype(f)).astype(np.float64)
+        return x.T if tall else x
     a, b, c = coef
     half = lambda v: v.astype(np.float16).astype(np.float64)  # noqa: E731
-    tall = x.shape[0] > x.shape[1]
-    x = (x.T if tall else x) * 256
+    x = x * 256
     for i in range(steps):
         hi = half(x)
         x = hi + half((x - hi) * 1024) / 1024 if i == 0 or i + 1 < steps else hi

@@ -22,7 +22,7 @@
 namespace foremoe {
 namespace {
 
-constexpr int kMuonBK = 64, kMuonNS = 2;
+constexpr int kMuonBK = 64;
 constexpr int kMomentThreads = 256, kMomentChunk = 16384;  // elements of a matrix per workgroup
 constexpr float kHeld = 256.0f, kRest = 1024.0f;
 
@@ -36,19 +36,34 @@ struct MuonRec {
   int32_t mm, nn;          // padded sides, mm the smaller one's
   uint32_t chunks;         // of a matrix, in the momentum pass
   float decay, move;       // 1 - lr weight_decay, lr scale
-  uint16_t *x[2], *rest[2];  // [batch, mm, nn]
-  uint16_t *gram, *poly;     // [batch, mm, mm]
-  double* squares;           // [batch, chunks]
   int32_t wide;              // the tensors' rows start on 16 bytes: read and written so
-  // first workgroup of the record in each kind of launch
-  uint32_t at_moment, at_scale, at_sym, at_full;
+  union {
+    struct {
+      uint16_t *x[2], *rest[2];  // [batch, mm, nn]
+      uint16_t *gram, *poly;     // [batch, mm, mm]
+      double* squares;           // [batch, chunks]
+    };
+    struct {  // small matrices (m <= 64)
+      float* part;      // [batch, chunks, 64, 64]: of each chunk of columns u u^T over 2^(2 e)
+      int32_t* part_e;  // [batch, chunks]: e + 127
+      float* q;         // [batch, 64, 64]: Q
+      double* inverse;  // [batch]: 1 / max(|u|, eps)
+    };
+  };
+};
+
+// First workgroup of every record in a launch.
+struct Firsts {
+  uint32_t at[FOREMOE_MUON_LAUNCH];
 };
 
 struct MuonArgs {
+  Firsts first;  // of this launch
   MuonRec rec[FOREMOE_MUON_LAUNCH];
   int n_rec, nesterov, zero_grads, from;  // from: which X the launch reads
   int has_rest, put_rest;  // whether that X has its second numbers, and the written one
-  uint32_t n_sym, n_full;                 // workgroups with work in the products' launches
+  uint32_t n_work;         // workgroups with work in a product's launch
+  int steps;
   float momentum, a, b, c;
   double eps;
   const float* grad_scale;
@@ -68,11 +83,10 @@ __device__ __forceinline__ float join(uint32_t hi, uint32_t rest, int second) {
   return half_value(hi >> (16 * second) & 0xffffu) + half_value(rest >> (16 * second) & 0xffffu) * (1.0f / kRest);
 }
 
-template <class At>
-__device__ __forceinline__ int find_rec(const MuonArgs& a, uint32_t b, At at) {
+__device__ __forceinline__ int find_rec(const MuonArgs& a, uint32_t b) {
   int r = 0;
-  for (int i = 1; i < a.n_rec; ++i)
-    if (at(a.rec[i]) <= b) r = i;
+#pragma unroll
+  for (int i = 1; i < FOREMOE_MUON_LAUNCH; ++i) r += i < a.n_rec && a.first.at[i] <= b;
   return r;
 }
 
@@ -128,8 +142,9 @@ __device__ __forceinline__ void put4(void* p, int64_t i, int64_t left, bool wide
 // m and the squares of u, a workgroup to a chunk of a matrix.
 template <bool GBF16>
 __global__ __launch_bounds__(kMomentThreads) void muon_moment_kernel(MuonArgs a) {
-  const MuonRec& r = a.rec[find_rec(a, blockIdx.x, [](const MuonRec& q) { return q.at_moment; })];
-  const uint32_t b = blockIdx.x - r.at_moment;
+  const int ri = find_rec(a, blockIdx.x);
+  const MuonRec& r = a.rec[ri];
+  const uint32_t b = blockIdx.x - a.first.at[ri];
   const int64_t matrix = b / r.chunks, chunk = b % r.chunks;
   const int64_t n = (int64_t)r.rows * r.cols, base = matrix * n;
   const int64_t lo = chunk * kMomentChunk, hi = lo + kMomentChunk < n ? lo + kMomentChunk : n;
@@ -165,8 +180,9 @@ __global__ __launch_bounds__(kMomentThreads) void muon_moment_kernel(MuonArgs a)
 // X = u / max(|u|, eps), 64 x 64 of the padded matrix to a workgroup.
 template <bool GBF16>
 __global__ __launch_bounds__(256) void muon_scale_kernel(MuonArgs a) {
-  const MuonRec& r = a.rec[find_rec(a, blockIdx.x, [](const MuonRec& q) { return q.at_scale; })];
-  const uint32_t b = blockIdx.x - r.at_scale;
+  const int ri = find_rec(a, blockIdx.x);
+  const MuonRec& r = a.rec[ri];
+  const uint32_t b = blockIdx.x - a.first.at[ri];
   const uint32_t tn = r.nn / 64, tiles = (uint32_t)(r.mm / 64) * tn;
   const int64_t matrix = b / tiles;
   const int i0 = (int)(b % tiles / tn) * 64, j0 = (int)(b % tiles % tn) * 64;
@@ -230,17 +246,36 @@ __global__ __launch_bounds__(256) void muon_scale_kernel(MuonArgs a) {
 
 enum Product { kGram = 0, kPoly = 1, kApply = 2, kUpdate = 3 };
 
-// p = p (1 - lr weight_decay) - lr scale X for four neighbours, x = 2^8 X.
-template <bool PBF16>
-__device__ __forceinline__ void update4(const MuonRec& r, int64_t i, int left, const float* x) {
-  float p[4];
+// p = p (1 - lr weight_decay) - lr scale X at N places of four neighbours:
+// place(k, i, left) gives the element and how many of its row are left there
+// (none: not a place), x(k, v) the values of 2^8 X. All reads come first, as
+// the compiler cannot move one past a store.
+template <bool PBF16, int N, class Place, class X>
+__device__ __forceinline__ void update_n(const MuonRec& r, Place place, X x) {
+  float p[N][4];
   const bool wide = r.wide;
-  if (PBF16 && !r.master) get4<true>(r.param, i, left, wide, p);
-  else get4<false>(PBF16 ? r.master : r.param, i, left, wide, p);
 #pragma unroll
-  for (int e = 0; e < 4; ++e) p[e] = fmaf(-r.move, x[e] * (1.0f / kHeld), p[e] * r.decay);
-  if (r.master) put4<false>(r.master, i, left, wide, p);
-  put4<PBF16>(r.param, i, left, wide, p);
+  for (int k = 0; k < N; ++k) {
+    int64_t i;
+    int left;
+    place(k, i, left);
+    if (left <= 0) continue;
+    if (PBF16 && !r.master) get4<true>(r.param, i, left, wide, p[k]);
+    else get4<false>(PBF16 ? r.master : r.param, i, left, wide, p[k]);
+  }
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    int64_t i;
+    int left;
+    place(k, i, left);
+    if (left <= 0) continue;
+    float v[4];
+    x(k, v);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) p[k][e] = fmaf(-r.move, v[e] * (1.0f / kHeld), p[k][e] * r.decay);
+    if (r.master) put4<false>(r.master, i, left, wide, p[k]);
+    put4<PBF16>(r.param, i, left, wide, p[k]);
+  }
 }
 
 // One T x T tile of one matrix's product, by wavefronts of 64 x 64 (T = 128) or
@@ -248,10 +283,11 @@ __device__ __forceinline__ void update4(const MuonRec& r, int64_t i, int left, c
 // operands its L2 then holds once (48 matrices of 768 x 2048, G: 135 -> 92 us).
 // The sums go through LDS, so that memory is read and written in whole lines
 // (X of the same: 412 -> 242 us). kUpdate is the last step's kApply: its X
-// goes into the parameters at once.
-template <int P, bool PBF16, int T>
+// goes into the parameters at once. NS stages of 64 of the k axis: two, or
+// four where a CU has one small tile alone and nothing else hides the loads.
+template <int P, bool PBF16, int T, int NS>
 __global__ __launch_bounds__(T * 2) void muon_product_kernel(MuonArgs a) {
-  constexpr int BK = kMuonBK, NS = kMuonNS, NW = T / 32, NT = 64 * NW, WN = T / 2;
+  constexpr int BK = kMuonBK, NW = T / 32, NT = 64 * NW, WN = T / 2;
   constexpr bool SYM = P == kGram || P == kPoly;
   using CoreT = Core<T, T, T / 64, 2, false, Fp16>;
   using AT = KTile<T, BK, NW>;
@@ -262,9 +298,10 @@ __global__ __launch_bounds__(T * 2) void muon_product_kernel(MuonArgs a) {
   constexpr int LDS_BYTES = NS * STAGE > H * LD * 4 ? NS * STAGE : H * LD * 4;
   __shared__ __attribute__((aligned(1024))) char lds[LDS_BYTES];
   const uint32_t bid = (uint32_t)xcd_virtual_id();
-  if (bid >= (SYM ? a.n_sym : a.n_full)) return;
-  const MuonRec& r = a.rec[find_rec(a, bid, [](const MuonRec& q) { return SYM ? q.at_sym : q.at_full; })];
-  const uint32_t b = bid - (SYM ? r.at_sym : r.at_full);
+  if (bid >= a.n_work) return;
+  const int ri = find_rec(a, bid);
+  const MuonRec& r = a.rec[ri];
+  const uint32_t b = bid - a.first.at[ri];
   const uint32_t tm = (uint32_t)r.mm / T, tn = (uint32_t)r.nn / T;
   const uint32_t tiles = SYM ? tm * (tm + 1) / 2 : tm * tn;
   const int64_t matrix = b / tiles;
@@ -310,15 +347,35 @@ __global__ __launch_bounds__(T * 2) void muon_product_kernel(MuonArgs a) {
                   sb[p - AT::PER_WAVE], p - AT::PER_WAVE);
     }
   };
+  // What the epilogue reads of X or G, 16 bytes at a time, is on its way a
+  // part ahead, the first under the k loop where the registers hold it.
+  const int tid = threadIdx.x, ei = tid / (T / 8), ej = tid % (T / 8) * 8;  // row (+ 16 k) and column
+  constexpr bool OF_X = P == kApply || P == kUpdate;
+  uint4 old[2][4], rest[2][4];
+  auto fetch = [&](int part) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int row = i0 + part * H + k * 16 + ei;
+      if constexpr (OF_X) {
+        const int64_t o = xat + (int64_t)row * r.nn + j0 + ej;
+        old[part & 1][k] = *(const uint4*)(r.x[a.from] + o);
+        if (a.has_rest) rest[part & 1][k] = *(const uint4*)(r.rest[a.from] + o);
+      } else if constexpr (P == kPoly) {
+        old[part & 1][k] = *(const uint4*)(G + (int64_t)row * r.mm + j0 + ej);
+      }
+    }
+  };
+  if constexpr (T == 128) fetch(0);
   CoreT core;
   const typename CoreT::template Offsets<AT, BT, BK> offs(lane, wm, wn);
   core.zero();
   pipelined_k_loop<CoreT, AT, BT, BK, NS, T == 256 ? 2 : 1>(core, lds, KT, offs, issue, false, [] {});
+  if constexpr (T != 128) fetch(0);
+
   float(*sum)[LD] = (float(*)[LD])lds;
-  const int tid = threadIdx.x;
   const bool tall = r.rows > r.cols;
-#pragma unroll 1
-  for (int part = 0; part < T / H; ++part) {
+  static_for<0, T / H>([&](auto partc) {
+    constexpr int part = decltype(partc)::value;
     __syncthreads();  // every wavefront has read its last fragments, or the sums before
     if (wm == part) {
 #pragma unroll
@@ -335,18 +392,20 @@ __global__ __launch_bounds__(T * 2) void muon_product_kernel(MuonArgs a) {
           }
     }
     __syncthreads();
+    if constexpr (part + 1 < T / H) fetch(part + 1);
     const int ih = i0 + part * H;  // their first row
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const int i = k * 16 + tid / (T / 8), j = tid % (T / 8) * 8;
+      const int i = k * 16 + ei, j = ej;
       float v[8];
       *(float4*)v = *(const float4*)&sum[i][j];
       *(float4*)(v + 4) = *(const float4*)&sum[i][j + 4];
-      if constexpr (P == kApply || P == kUpdate) {
+      const uint4 h4 = old[part & 1][k];
+      const uint32_t h[4] = {h4.x, h4.y, h4.z, h4.w};
+      if constexpr (OF_X) {
         const int64_t o = xat + (int64_t)(ih + i) * r.nn + j0 + j;
-        const uint4 h4 = *(const uint4*)(r.x[a.from] + o);
-        const uint4 l4 = a.has_rest ? *(const uint4*)(r.rest[a.from] + o) : uint4{0, 0, 0, 0};
-        const uint32_t h[4] = {h4.x, h4.y, h4.z, h4.w}, l[4] = {l4.x, l4.y, l4.z, l4.w};
+        const uint4 l4 = a.has_rest ? rest[part & 1][k] : uint4{0, 0, 0, 0};
+        const uint32_t l[4] = {l4.x, l4.y, l4.z, l4.w};
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = fmaf(a.a, join(h[e / 2], l[e / 2], e & 1), v[e]);
         if constexpr (P == kApply) {
@@ -362,54 +421,56 @@ __global__ __launch_bounds__(T * 2) void muon_product_kernel(MuonArgs a) {
       } else {
         const int64_t o = (int64_t)(ih + i) * r.mm + j0 + j;
         if constexpr (P == kPoly) {
-          const uint4 g4 = *(const uint4*)(G + o);
-          const uint32_t g[4] = {g4.x, g4.y, g4.z, g4.w};
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = fmaf(a.c, v[e], a.b * half_value(g[e / 2] >> (16 * (e & 1)) & 0xffffu));
+          for (int e = 0; e < 8; ++e) v[e] = fmaf(a.c, v[e], a.b * half_value(h[e / 2] >> (16 * (e & 1)) & 0xffffu));
           *(float4*)&sum[i][j] = *(const float4*)v;
           *(float4*)&sum[i][j + 4] = *(const float4*)(v + 4);
         }
-        uint32_t h[4];
+        uint32_t w[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) h[e] = (uint32_t)half_bits(v[2 * e]) | (uint32_t)half_bits(v[2 * e + 1]) << 16;
-        *(uint4*)((P == kGram ? G : Q) + o) = uint4{h[0], h[1], h[2], h[3]};
+        for (int e = 0; e < 4; ++e) w[e] = (uint32_t)half_bits(v[2 * e]) | (uint32_t)half_bits(v[2 * e + 1]) << 16;
+        *(uint4*)((P == kGram ? G : Q) + o) = uint4{w[0], w[1], w[2], w[3]};
       }
     }
-    if (P == kApply || (SYM && ti == tj)) continue;
-    __syncthreads();
-    if constexpr (SYM) {  // the same on the other side of the diagonal
+    if (P != kApply && !(SYM && ti == tj)) {
+      __syncthreads();
+      if constexpr (SYM) {  // the same on the other side of the diagonal
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int j = k * (NT / 8) + (tid >> 3), i = (tid & 7) * 8;
-        uint32_t h[4];
+        for (int k = 0; k < 4; ++k) {
+          const int j = k * (NT / 8) + (tid >> 3), i = (tid & 7) * 8;
+          uint32_t w[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          h[e] = (uint32_t)half_bits(sum[i + 2 * e][j]) | (uint32_t)half_bits(sum[i + 2 * e + 1][j]) << 16;
-        *(uint4*)((P == kGram ? G : Q) + (int64_t)(j0 + j) * r.mm + ih + i) = uint4{h[0], h[1], h[2], h[3]};
-      }
-    } else {
-      // H rows of X by T columns: of the parameters too, or T rows by H columns
-      const int r0 = tall ? j0 : ih, c0 = tall ? ih : j0;
-      const int64_t base = matrix * (int64_t)r.rows * r.cols;
-#pragma unroll 4
-      for (int k = 0; k < 8; ++k) {
-        const int i = tall ? k * (NT / 16) + tid / 16 : k * 8 + tid / (T / 4), j = (tall ? tid % 16 : tid % (T / 4)) * 4;
-        const int left = r.cols - (c0 + j);
-        if (r0 + i >= r.rows || left <= 0) continue;
-        float x[4];
+          for (int e = 0; e < 4; ++e)
+            w[e] = (uint32_t)half_bits(sum[i + 2 * e][j]) | (uint32_t)half_bits(sum[i + 2 * e + 1][j]) << 16;
+          *(uint4*)((P == kGram ? G : Q) + (int64_t)(j0 + j) * r.mm + ih + i) = uint4{w[0], w[1], w[2], w[3]};
+        }
+      } else {
+        // H rows of X by T columns: of the parameters too, or T rows by H columns
+        const int r0 = tall ? j0 : ih, c0 = tall ? ih : j0;
+        const int pi = tall ? tid / 16 : tid / (T / 4), pk = tall ? NT / 16 : 8, pj = (tall ? tid % 16 : tid % (T / 4)) * 4;
+        const int64_t base = matrix * (int64_t)r.rows * r.cols;
+        update_n<PBF16, 8>(
+            r,
+            [&](int k, int64_t& o, int& left) {
+              const int row = r0 + pi + pk * k;
+              o = base + (int64_t)row * r.cols + c0 + pj, left = row < r.rows ? r.cols - (c0 + pj) : 0;
+            },
+            [&](int k, float* v) {
+              const int i = pi + pk * k;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = tall ? sum[j + e][i] : sum[i][j + e];
-        update4<PBF16>(r, base + (int64_t)(r0 + i) * r.cols + c0 + j, left, x);
+              for (int e = 0; e < 4; ++e) v[e] = tall ? sum[pj + e][i] : sum[i][pj + e];
+            });
       }
     }
-  }
+  });
 }
 
 // The update without any step of the iteration: 64 x 64 of X to a workgroup.
 template <bool PBF16>
 __global__ __launch_bounds__(256) void muon_update_kernel(MuonArgs a) {
-  const MuonRec& r = a.rec[find_rec(a, blockIdx.x, [](const MuonRec& q) { return q.at_scale; })];
-  const uint32_t b = blockIdx.x - r.at_scale;
+  const int ri = find_rec(a, blockIdx.x);
+  const MuonRec& r = a.rec[ri];
+  const uint32_t b = blockIdx.x - a.first.at[ri];
   const uint32_t tn = r.nn / 64, tiles = (uint32_t)(r.mm / 64) * tn;
   const int64_t matrix = b / tiles;
   const int i0 = (int)(b % tiles / tn) * 64, j0 = (int)(b % tiles % tn) * 64;
@@ -425,15 +486,265 @@ __global__ __launch_bounds__(256) void muon_update_kernel(MuonArgs a) {
     else tile[i][j] = x;
   }
   __syncthreads();
-  const int r0 = tall ? j0 : i0, c0 = tall ? i0 : j0;
+  const int r0 = tall ? j0 : i0, c0 = tall ? i0 : j0, j = (tid & 15) * 4;
   const int64_t base = matrix * (int64_t)r.rows * r.cols;
+  update_n<PBF16, 4>(
+      r,
+      [&](int k, int64_t& o, int& left) {
+        const int row = r0 + (tid >> 4) + 16 * k;
+        o = base + (int64_t)row * r.cols + c0 + j, left = row < r.rows ? r.cols - (c0 + j) : 0;
+      },
+      [&](int k, float* v) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = tile[(tid >> 4) + 16 * k][j + e];
+      });
+}
+
+// ---------------------------------------------------------------------------
+// Matrices with a side of at most 64: three launches for all steps, in fp32.
+// With M = a I + b G + c G G, all of G, M and Q are polynomials of the first G
+// and commute: X = Q X0 with Q = M .. M, and the next G is M G M. So X is read
+// twice, for the first G and for Q X0, and the rest happens in the LDS of one
+// workgroup a matrix. (fp16 factors would move X of a matrix with a side below
+// 16 by up to 2^-6 of its norm, as one singular value's error does not average
+// out; fp32 ones move it by 2^-20, or 2^-11 where u is next to singular, whose
+// small directions G holds squared.)
+// ---------------------------------------------------------------------------
+constexpr int kSmall = 64, kSmallLD = 65, kSmallChunks = 64;
+
+// u of the 64 x 64 tile of the matrix whose first long index is l0, the small
+// side as rows, times `inv`, into LDS; zeros past the ends.
+template <bool GBF16, bool STORE_M>
+__device__ __forceinline__ void small_u(const MuonArgs& a, const MuonRec& r, int64_t base, int l0, double inv,
+                                        float (*u)[kSmallLD]) {
+  const bool tall = r.rows > r.cols;
+  const float gs = a.grad_scale ? *a.grad_scale : 1.0f;
+  const int r0 = tall ? l0 : 0, c0 = tall ? 0 : l0;
+#pragma unroll
   for (int k = 0; k < 4; ++k) {
-    const int i = k * 16 + (tid >> 4), j = (tid & 15) * 4, left = r.cols - (c0 + j);
-    if (r0 + i < r.rows && left > 0) update4<PBF16>(r, base + (int64_t)(r0 + i) * r.cols + c0 + j, left, &tile[i][j]);
+    const int tr = k * 16 + (threadIdx.x >> 4), tc = (threadIdx.x & 15) * 4;
+    const int rr = r0 + tr, cc = c0 + tc, left = r.cols - cc;
+    float v[4] = {0, 0, 0, 0};
+    if (rr < r.rows && left > 0) {
+      const int64_t i = base + (int64_t)rr * r.cols + cc;
+      float g[4] = {0, 0, 0, 0};
+      get4<false>(r.m, i, left, r.wide, v);
+      if (STORE_M || a.nesterov) {
+        get4<GBF16>(r.grad, i, left, r.wide, g);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) g[e] *= gs;
+      }
+      if constexpr (STORE_M) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = fmaf(a.momentum, v[e], g[e]);
+        put4<false>(r.m, i, left, r.wide, v);
+      } else if (a.zero_grads) {
+        const float z[4] = {0, 0, 0, 0};
+        put4<GBF16>(r.grad, i, left, r.wide, z);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (a.nesterov) v[e] = fmaf(a.momentum, v[e], g[e]);
+        v[e] = e >= left ? 0.0f : (STORE_M ? v[e] : (float)((double)v[e] * inv));
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (tall) u[tc + e][tr] = v[e];
+      else u[tr][tc + e] = v[e];
+    }
   }
 }
 
+// A 32 x 32 quarter of A B (TRANS: A B^T) of LDS matrices, k below n: block
+// (wave / 2, wave % 2) of the wavefront, the sums as the matrix instruction
+// leaves them (row 8 (q / 4) + 4 (lane / 32) + q % 4, column lane % 32).
+template <bool TRANS>
+__device__ __forceinline__ f32x16 small_product(const float (*A)[kSmallLD], const float (*B)[kSmallLD], int n) {
+  const int lane = lane64(), wave = wave_id(), l = lane & 31, h = lane >> 5;
+  const int i = 32 * (wave >> 1) + l, j = 32 * (wave & 1) + l;
+  f32x16 acc;
+#pragma unroll
+  for (int q = 0; q < 16; ++q) acc[q] = 0.0f;
+#pragma unroll 8
+  for (int k = 0; k < n; k += 2)
+    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(A[i][k + h], TRANS ? B[j][k + h] : B[k + h][j], acc, 0, 0, 0);
+  return acc;
+}
+template <class F>
+__device__ __forceinline__ void small_each(F&& f) {  // f(q, row, column)
+  const int lane = lane64(), wave = wave_id();
+#pragma unroll
+  for (int q = 0; q < 16; ++q)
+    f(q, 32 * (wave >> 1) + 8 * (q / 4) + 4 * (lane >> 5) + q % 4, 32 * (wave & 1) + (lane & 31));
+}
+
+// m, and a chunk's part of u u^T. The sums are of u over a power of two that
+// the chunk's largest element gives, so that no square leaves the range of fp32.
+template <bool GBF16>
+__global__ __launch_bounds__(256) void muon_small_gram_kernel(MuonArgs a) {
+  const int ri = find_rec(a, blockIdx.x);
+  const MuonRec& r = a.rec[ri];
+  const uint32_t b = blockIdx.x - a.first.at[ri];
+  const int64_t matrix = b / r.chunks, chunk = b % r.chunks;
+  const int n = r.rows > r.cols ? r.rows : r.cols;  // the long side, in tiles of 64
+  const int tiles = (n + 63) / 64, t0 = (int)(tiles * chunk / r.chunks), t1 = (int)(tiles * (chunk + 1) / r.chunks);
+  const int64_t base = matrix * (int64_t)r.rows * r.cols;
+  __shared__ float u[kSmall][kSmallLD];
+  __shared__ uint32_t most[4];
+  f32x16 acc;
+#pragma unroll
+  for (int q = 0; q < 16; ++q) acc[q] = 0.0f;
+  int e = 0;  // biased exponent that the sums are over
+  for (int t = t0; t < t1; ++t) {
+    __syncthreads();
+    small_u<GBF16, true>(a, r, base, t * 64, 1.0, u);
+    __syncthreads();
+    uint32_t top = 0;
+    for (int i = threadIdx.x; i < 4096; i += 256) {
+      const uint32_t v = __float_as_uint(u[i >> 6][i & 63]) & 0x7fffffffu;
+      top = v > top ? v : top;
+    }
+#pragma unroll
+    for (int o = 32; o; o >>= 1) {
+      const uint32_t v = __shfl_xor(top, o, 64);
+      top = v > top ? v : top;
+    }
+    if (lane64() == 0) most[wave_id()] = top;
+    __syncthreads();
+    top = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) top = most[w] > top ? most[w] : top;
+    const int et = (int)(top >> 23);
+    if (et > e) {
+      const float down = ldexpf(1.0f, 2 * (e - et));
+#pragma unroll
+      for (int q = 0; q < 16; ++q) acc[q] *= down;
+      e = et;
+    }
+    for (int i = threadIdx.x; i < 4096; i += 256) u[i >> 6][i & 63] = ldexpf(u[i >> 6][i & 63], 127 - e);
+    __syncthreads();
+    const f32x16 s = small_product<true>(u, u, kSmall);
+#pragma unroll
+    for (int q = 0; q < 16; ++q) acc[q] += s[q];
+  }
+  float* to = r.part + (matrix * r.chunks + chunk) * (kSmall * kSmall);
+  small_each([&](int q, int i, int j) { to[i * kSmall + j] = acc[q]; });
+  if (threadIdx.x == 0) r.part_e[matrix * r.chunks + chunk] = e;
+}
+
+// Q and 1 / max(|u|, eps) of a matrix.
+__global__ __launch_bounds__(256) void muon_small_steps_kernel(MuonArgs a) {
+  const int ri = find_rec(a, blockIdx.x);
+  const MuonRec& r = a.rec[ri];
+  const int64_t matrix = blockIdx.x - a.first.at[ri];
+  const int m = r.rows < r.cols ? r.rows : r.cols, n = (m + 1) & ~1, tid = threadIdx.x;
+  __shared__ float G[kSmall][kSmallLD], M[kSmall][kSmallLD], S[kSmall][kSmallLD], Q[kSmall][kSmallLD];
+  const float* part = r.part + matrix * r.chunks * (kSmall * kSmall);
+  const int32_t* part_e = r.part_e + matrix * r.chunks;
+  const int lane = lane64();
+  const int mine = lane < (int)r.chunks ? part_e[lane] : 0;  // (at most 64 chunks)
+  int e = mine;
+#pragma unroll
+  for (int o = 32; o; o >>= 1) {
+    const int other = __shfl_xor(e, o, 64);
+    e = other > e ? other : e;
+  }
+  const float scale = ldexpf(1.0f, 2 * (mine - e));
+  float s[16];
+#pragma unroll
+  for (int k = 0; k < 16; ++k) s[k] = 0.0f;
+#pragma unroll 4
+  for (int c = 0; c < (int)r.chunks; ++c) {
+    const float by = __shfl(scale, c, 64);
+#pragma unroll
+    for (int k = 0; k < 16; ++k) s[k] = fmaf(part[c * (kSmall * kSmall) + tid + 256 * k], by, s[k]);
+  }
+#pragma unroll
+  for (int k = 0; k < 16; ++k) G[(tid + 256 * k) >> 6][(tid + 256 * k) & 63] = s[k];
+  __syncthreads();
+  // |u|^2 over 2^(2 (e - 127)), summed in the same order by every thread
+  double trace = 0;
+  for (int i = 0; i < m; ++i) trace += G[i][i];
+  const double norm = e == 255 ? (double)NAN : ldexp(sqrt(trace), e - 127);
+  const double den = !(norm <= a.eps) ? norm : a.eps;
+  // nothing in it: no move; not finite: NaN everywhere
+  const double inv = den == 0 ? 0.0 : 1.0 / den;
+  const double by = ldexp(inv, e - 127);
+  __syncthreads();
+  for (int i = tid; i < kSmall * kSmall; i += 256) {
+    const int x = i >> 6, y = i & 63;
+    G[x][y] = (float)(G[x][y] * by * by);
+    Q[x][y] = x == y ? 1.0f : 0.0f;
+  }
+  __syncthreads();
+  const bool idle = 32 * (wave_id() >> 1) >= m || 32 * (wave_id() & 1) >= m;
+  for (int t = 0; t < a.steps; ++t) {
+    if (!idle) {
+      const f32x16 s = small_product<false>(G, G, n);
+      small_each([&](int q, int i, int j) {
+        M[i][j] = (i == j ? a.a : 0.0f) + fmaf(a.b, G[i][j], a.c * s[q]);
+      });
+    }
+    __syncthreads();
+    f32x16 nq, mg;
+    if (!idle) {
+      nq = small_product<false>(M, Q, n);
+      if (t + 1 < a.steps) {
+        mg = small_product<false>(M, G, n);
+        small_each([&](int q, int i, int j) { S[i][j] = mg[q]; });
+      }
+    }
+    __syncthreads();
+    if (!idle) {
+      small_each([&](int q, int i, int j) { Q[i][j] = nq[q]; });
+      if (t + 1 < a.steps) {
+        mg = small_product<false>(S, M, n);
+        small_each([&](int q, int i, int j) { G[i][j] = mg[q]; });
+      }
+    }
+    __syncthreads();
+  }
+  for (int i = tid; i < kSmall * kSmall; i += 256) r.q[matrix * (kSmall * kSmall) + i] = Q[i >> 6][i & 63];
+  if (tid == 0) r.inverse[matrix] = inv;
+}
+
+// X = Q X0 for 64 of the long side, and the parameters.
+template <bool GBF16, bool PBF16>
+__global__ __launch_bounds__(256) void muon_small_update_kernel(MuonArgs a) {
+  const int ri = find_rec(a, blockIdx.x);
+  const MuonRec& r = a.rec[ri];
+  const uint32_t b = blockIdx.x - a.first.at[ri];
+  const bool tall = r.rows > r.cols;
+  const int tiles = ((tall ? r.rows : r.cols) + 63) / 64, tid = threadIdx.x;
+  const int64_t matrix = b / tiles;
+  const int l0 = (int)(b % tiles) * 64, m = tall ? r.cols : r.rows, n = (m + 1) & ~1;
+  const int64_t base = matrix * (int64_t)r.rows * r.cols;
+  __shared__ float u[kSmall][kSmallLD], Q[kSmall][kSmallLD];
+  for (int i = tid; i < kSmall * kSmall; i += 256) Q[i >> 6][i & 63] = r.q[matrix * (kSmall * kSmall) + i];
+  small_u<GBF16, false>(a, r, base, l0, r.inverse[matrix], u);
+  __syncthreads();
+  const f32x16 x = small_product<false>(Q, u, n);
+  __syncthreads();
+  small_each([&](int q, int i, int j) { u[i][j] = x[q] * kHeld; });
+  __syncthreads();
+  const int r0 = tall ? l0 : 0, c0 = tall ? 0 : l0, i0 = tid >> 4, j = (tid & 15) * 4;
+  update_n<PBF16, 4>(
+      r,
+      [&](int k, int64_t& at, int& left) {
+        const int row = r0 + i0 + 16 * k;
+        at = base + (int64_t)row * r.cols + c0 + j, left = row < r.rows ? r.cols - (c0 + j) : 0;
+      },
+      [&](int k, float* v) {
+        const int i = i0 + 16 * k;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = tall ? u[j + e][i] : u[i][j + e];
+      });
+}
+
 int64_t pad_side(int64_t n, int tile) { return (n + tile - 1) / tile * tile; }
+
+bool is_small(const foremoe_muon_tensor& t) { return t.rows <= kSmall || t.cols <= kSmall; }
 
 // Lays a tensor's part of the workspace out from `at` (bytes); returns its end.
 size_t lay_out(const foremoe_muon_tensor& t, int tile, size_t at, char* ws, MuonRec* r) {
@@ -446,6 +757,18 @@ size_t lay_out(const foremoe_muon_tensor& t, int tile, size_t at, char* ws, Muon
     return p;
   };
   MuonRec q{};
+  if (s <= kSmall) {
+    const int64_t tiles = (l + 63) / 64;
+    // parts of u u^T to be joined by one workgroup: 16, more for the longest
+    const int64_t most = tiles < 256 ? 16 : kSmallChunks;
+    q.chunks = (uint32_t)(tiles < most ? tiles : most);
+    q.part = (float*)take((size_t)t.batch * q.chunks * kSmall * kSmall * 4);
+    q.part_e = (int32_t*)take((size_t)t.batch * q.chunks * 4);
+    q.q = (float*)take((size_t)t.batch * kSmall * kSmall * 4);
+    q.inverse = (double*)take((size_t)t.batch * 8);
+    if (r) *r = q;
+    return at;
+  }
   for (int i = 0; i < 2; ++i) {
     q.x[i] = (uint16_t*)take((size_t)t.batch * mm * nn * 2);
     q.rest[i] = (uint16_t*)take((size_t)t.batch * mm * nn * 2);
@@ -480,7 +803,7 @@ Tiles choose_tiles(const foremoe_muon_tensor* tensors, int i, int end) {
     double tiles = 0, steps = 0;
     for (int j = i; j < end; ++j) {
       const foremoe_muon_tensor& t = tensors[j];
-      if (t.batch == 0) continue;
+      if (t.batch == 0 || is_small(t)) continue;
       const double m = (double)pad_side(t.rows < t.cols ? t.rows : t.cols, pad);
       const double n = (double)pad_side(t.rows < t.cols ? t.cols : t.rows, pad);
       const double tm = m / tile, count = t.batch * (of_x ? tm * (n / tile) : tm * (tm + 1) / 2);
@@ -528,19 +851,68 @@ int check_tensor(const foremoe_muon_tensor& t, int i) {
 
 using namespace foremoe;
 
-// (grids of a multiple of the XCDs: see xcd_virtual_id)
-template <int T>
-static void launch_symmetric(const MuonArgs& a, hipStream_t st) {
-  const dim3 grid((a.n_sym + 7) / 8 * 8), threads(T * 2);
-  hipLaunchKernelGGL((muon_product_kernel<kGram, false, T>), grid, threads, 0, st, a);
-  hipLaunchKernelGGL((muon_product_kernel<kPoly, false, T>), grid, threads, 0, st, a);
+// The grid of a launch with count(record) workgroups to a matrix.
+template <class Count>
+static unsigned grid_of(MuonArgs& a, Count count) {
+  uint64_t n = 0;
+  for (int i = 0; i < a.n_rec; ++i) {
+    a.first.at[i] = (uint32_t)n;
+    n += (uint64_t)a.rec[i].batch * count(a.rec[i]);
+  }
+  a.n_work = (uint32_t)n;
+  return (unsigned)n;
 }
-template <int T>
-static void launch_x(const MuonArgs& a, int product, bool param_bf16, hipStream_t st) {
-  const dim3 grid((a.n_full + 7) / 8 * 8), threads(T * 2);
-  if (product == kApply) hipLaunchKernelGGL((muon_product_kernel<kApply, false, T>), grid, threads, 0, st, a);
-  else if (param_bf16) hipLaunchKernelGGL((muon_product_kernel<kUpdate, true, T>), grid, threads, 0, st, a);
-  else hipLaunchKernelGGL((muon_product_kernel<kUpdate, false, T>), grid, threads, 0, st, a);
+
+static void launch_small(MuonArgs& a, bool pb16, bool gb16, hipStream_t st) {
+  unsigned n = grid_of(a, [](const MuonRec& r) { return (uint64_t)r.chunks; });
+  if (gb16) hipLaunchKernelGGL((muon_small_gram_kernel<true>), dim3(n), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((muon_small_gram_kernel<false>), dim3(n), dim3(256), 0, st, a);
+  n = grid_of(a, [](const MuonRec&) { return (uint64_t)1; });
+  hipLaunchKernelGGL(muon_small_steps_kernel, dim3(n), dim3(256), 0, st, a);
+  n = grid_of(a, [](const MuonRec& r) { return (uint64_t)((r.rows > r.cols ? r.rows : r.cols) + 63) / 64; });
+  if (gb16 && pb16) hipLaunchKernelGGL((muon_small_update_kernel<true, true>), dim3(n), dim3(256), 0, st, a);
+  else if (gb16) hipLaunchKernelGGL((muon_small_update_kernel<true, false>), dim3(n), dim3(256), 0, st, a);
+  else if (pb16) hipLaunchKernelGGL((muon_small_update_kernel<false, true>), dim3(n), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((muon_small_update_kernel<false, false>), dim3(n), dim3(256), 0, st, a);
+}
+
+// (a grid of a multiple of the XCDs: see xcd_virtual_id)
+template <int P, bool PBF16>
+static void launch_product(MuonArgs& a, int tile, hipStream_t st) {
+  const uint64_t T = tile;
+  const unsigned n = grid_of(a, [T](const MuonRec& r) {
+    const uint64_t tm = r.mm / T;
+    return P == kGram || P == kPoly ? tm * (tm + 1) / 2 : tm * (r.nn / T);
+  });
+  const dim3 grid((n + 7) / 8 * 8), threads(tile * 2);
+  if (tile == 256) hipLaunchKernelGGL((muon_product_kernel<P, PBF16, 256, 2>), grid, threads, 0, st, a);
+  else if (n > 256) hipLaunchKernelGGL((muon_product_kernel<P, PBF16, 128, 2>), grid, threads, 0, st, a);
+  else hipLaunchKernelGGL((muon_product_kernel<P, PBF16, 128, 4>), grid, threads, 0, st, a);
+}
+
+static void launch_large(MuonArgs& a, const Tiles& tiles, bool pb16, bool gb16, hipStream_t st) {
+  unsigned n = grid_of(a, [](const MuonRec& r) { return (uint64_t)r.chunks; });
+  if (gb16) hipLaunchKernelGGL((muon_moment_kernel<true>), dim3(n), dim3(kMomentThreads), 0, st, a);
+  else hipLaunchKernelGGL((muon_moment_kernel<false>), dim3(n), dim3(kMomentThreads), 0, st, a);
+  n = grid_of(a, [](const MuonRec& r) { return (uint64_t)(r.mm / 64) * (r.nn / 64); });
+  if (gb16) hipLaunchKernelGGL((muon_scale_kernel<true>), dim3(n), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((muon_scale_kernel<false>), dim3(n), dim3(256), 0, st, a);
+  if (a.steps == 0) {
+    if (pb16) hipLaunchKernelGGL((muon_update_kernel<true>), dim3(n), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((muon_update_kernel<false>), dim3(n), dim3(256), 0, st, a);
+  }
+  a.from = 0;
+  for (int step = 0; step < a.steps; ++step) {
+    // the X before the last step has no second numbers: one more step
+    // multiplies what that leaves out by a at most
+    a.has_rest = step == 0 || step + 1 < a.steps, a.put_rest = step + 2 < a.steps;
+    launch_product<kGram, false>(a, tiles.sym, st);
+    launch_product<kPoly, false>(a, tiles.sym, st);
+    if (step + 1 < a.steps) launch_product<kApply, false>(a, tiles.full, st);
+    else if (pb16) launch_product<kUpdate, true>(a, tiles.full, st);
+    else launch_product<kUpdate, false>(a, tiles.full, st);
+    a.from ^= 1;
+  }
 }
 
 #define REQUIRE(cond, ...)                                      \
@@ -603,59 +975,34 @@ int foremoe_muon_step(const foremoe_muon_tensor* tensors, int32_t n_tensors, for
   REQUIRE(!misaligned(ws, 256), "muon_step: workspace misaligned");
 
   MuonArgs a{};
-  a.nesterov = nesterov != 0, a.zero_grads = zero_grads != 0, a.grad_scale = grad_scale;
+  a.nesterov = nesterov != 0, a.zero_grads = zero_grads != 0, a.grad_scale = grad_scale, a.steps = ns_steps;
   a.momentum = (float)momentum, a.a = (float)coef[0], a.b = (float)coef[1], a.c = (float)coef[2], a.eps = eps;
+  const bool pb16 = param_dtype == FOREMOE_BF16, gb16 = grad_dtype == FOREMOE_BF16;
   hipStream_t st = (hipStream_t)stream;
   int rc = FOREMOE_OK;
   for (int i = 0, end; i < n_tensors && rc == FOREMOE_OK; i = end) {
     end = group_end(tensors, i, n_tensors);
     const Tiles tiles = choose_tiles(tensors, i, end);
-    uint64_t moment = 0, scale = 0, sym = 0, full = 0;
     size_t at = 0;
-    a.n_rec = 0;
-    for (int j = i; j < end; ++j) {
-      const foremoe_muon_tensor& t = tensors[j];
-      if (t.batch == 0) continue;
-      MuonRec& r = a.rec[a.n_rec++];
-      at = lay_out(t, tiles.pad, at, (char*)ws, &r);
-      r.param = t.param, r.grad = t.grad, r.master = t.master, r.m = t.m;
-      r.batch = t.batch, r.rows = t.rows, r.cols = t.cols;
-      r.wide = t.cols % 4 == 0 && !misaligned(t.param, 16) && !misaligned(t.grad, 16) && !misaligned(t.master, 16) &&
-               !misaligned(t.m, 16);
-      r.decay = (float)(1 - lr * t.weight_decay), r.move = (float)(lr * t.scale);
-      const uint64_t ts = r.mm / tiles.sym;
-      r.at_moment = (uint32_t)moment, r.at_scale = (uint32_t)scale;
-      r.at_sym = (uint32_t)sym, r.at_full = (uint32_t)full;
-      moment += (uint64_t)t.batch * r.chunks, scale += (uint64_t)t.batch * (r.mm / 64) * (r.nn / 64);
-      sym += (uint64_t)t.batch * (ts * (ts + 1) / 2);
-      full += (uint64_t)t.batch * (r.mm / tiles.full) * (r.nn / tiles.full);
+    for (int small = 1; small >= 0; --small) {
+      a.n_rec = 0;
+      for (int j = i; j < end; ++j) {
+        const foremoe_muon_tensor& t = tensors[j];
+        if (t.batch == 0 || is_small(t) != (small != 0)) continue;
+        MuonRec& r = a.rec[a.n_rec++];
+        at = lay_out(t, tiles.pad, at, (char*)ws, &r);
+        r.param = t.param, r.grad = t.grad, r.master = t.master, r.m = t.m;
+        r.batch = t.batch, r.rows = t.rows, r.cols = t.cols;
+        r.wide = t.cols % 4 == 0 && !misaligned(t.param, 16) && !misaligned(t.grad, 16) && !misaligned(t.master, 16) &&
+                 !misaligned(t.m, 16);
+        r.decay = (float)(1 - lr * t.weight_decay), r.move = (float)(lr * t.scale);
+      }
+      if (a.n_rec == 0) continue;
+      if (small) launch_small(a, pb16, gb16, st);
+      else launch_large(a, tiles, pb16, gb16, st);
+      rc = check_launch("muon_step");
+      if (rc != FOREMOE_OK) break;
     }
-    if (a.n_rec == 0) continue;
-    a.n_sym = (uint32_t)sym, a.n_full = (uint32_t)full, a.from = 0;
-    const dim3 gm((unsigned)moment), gs((unsigned)scale);
-    if (grad_dtype == FOREMOE_BF16) {
-      hipLaunchKernelGGL((muon_moment_kernel<true>), gm, dim3(kMomentThreads), 0, st, a);
-      hipLaunchKernelGGL((muon_scale_kernel<true>), gs, dim3(256), 0, st, a);
-    } else {
-      hipLaunchKernelGGL((muon_moment_kernel<false>), gm, dim3(kMomentThreads), 0, st, a);
-      hipLaunchKernelGGL((muon_scale_kernel<false>), gs, dim3(256), 0, st, a);
-    }
-    if (ns_steps == 0) {
-      if (param_dtype == FOREMOE_BF16) hipLaunchKernelGGL((muon_update_kernel<true>), gs, dim3(256), 0, st, a);
-      else hipLaunchKernelGGL((muon_update_kernel<false>), gs, dim3(256), 0, st, a);
-    }
-    for (int step = 0; step < ns_steps; ++step) {
-      // the X before the last step has no second numbers: one more step
-      // multiplies what that leaves out by a at most
-      a.has_rest = step == 0 || step + 1 < ns_steps, a.put_rest = step + 2 < ns_steps;
-      const int apply = step + 1 < ns_steps ? kApply : kUpdate;
-      if (tiles.sym == 256) launch_symmetric<256>(a, st);
-      else launch_symmetric<128>(a, st);
-      if (tiles.full == 256) launch_x<256>(a, apply, param_dtype == FOREMOE_BF16, st);
-      else launch_x<128>(a, apply, param_dtype == FOREMOE_BF16, st);
-      a.from ^= 1;
-    }
-    rc = check_launch("muon_step");
   }
   return rc;
 }

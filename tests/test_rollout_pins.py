@@ -78,14 +78,15 @@ def test_newton_schulz_maps_singular_values():
 @pytest.mark.parametrize("shape", [(24, 40), (130, 70), (128, 128)])
 def test_the_formats_rounding_is_small(shape):
     """Factors rounded to fp16 move X by a few 2^-11 of its norm, also where
-    u has few directions: the others stay empty."""
+    u has few directions: the others stay empty. Small matrices are in fp32,
+    whose rounding of G shows where u is next to singular."""
     rng = np.random.default_rng(3)
     coef = (3.4445, -4.7750, 2.0315)
     for rank in (min(shape), 4):
         x = rng.standard_normal((shape[0], rank)) @ rng.standard_normal((rank, shape[1]))
         x /= np.linalg.norm(x)
-        a, b = R.newton_schulz(x, coef, 5), R.newton_schulz_fp16(x, coef, 5)
-        assert 0 < np.linalg.norm(a - b) < 2.0 ** -8 * np.linalg.norm(a)
+        a, b = R.newton_schulz(x, coef, 5), R.newton_schulz_held(x, coef, 5)
+        assert 0 < np.linalg.norm(a - b) < (2.0 ** -8 if min(shape) > 64 else 2.0 ** -11) * np.linalg.norm(a)
 
 
 def test_muon_without_a_gradient_does_not_move():
