@@ -819,7 +819,8 @@ int foremoe_mxfp4_values(const uint8_t* codes, const uint8_t* scales, int64_t ro
  * weights' matrices quantised. y_perm [n_cap, d] bf16. Rows outside every
  * slot are left as they were.
  * d % 128 == 0, F % 128 == 0, 2 * d * F < 2^32 (else FOREMOE_EUNSUPPORTED).
- * n_cap * max(d, F) < 2^38. Codes and y 16-byte aligned, scales 4-byte.
+ * (n_cap / 128 + S + 1) * max(d, F) / 128 < 2^23. Codes and y 16-byte aligned,
+ * scales 4-byte.
  * ws: foremoe_ffn_mxfp4_workspace_size(n_cap, F) bytes, 256-byte aligned, for
  * Q(H); needs no initialisation. Calls that share one must not overlap in
  * time. Forward only: gradients go through the unquantised weights.

@@ -139,37 +139,57 @@ struct SlotTile {
   int w;
 };
 
-// The slot and rows of row tile t (tiles numbered slot by slot), found by
-// every wavefront alone. False past the last.
+// Row tiles of the slot that this lane has of those from j0 on, its rows, and
+// the row tiles up to and with it.
 template <int BM>
-__device__ __forceinline__ bool find_row_tile(const Ffn4Args& a, int t, SlotTile& r) {
-  const int lane = lane64();
-  for (int j0 = 0; j0 < a.S; j0 += 64) {
-    const int j = j0 + lane;
-    int64_t beg = 0, end = 0;
-    if (j < a.S) {
-      beg = a.slot_offset[j], end = a.slot_offset[j + 1];
-      beg = beg < 0 ? 0 : (beg > a.n_cap ? a.n_cap : beg);
-      end = end > a.n_cap ? a.n_cap : end;
-    }
-    const int mine = end > beg ? (int)((end - beg + BM - 1) / BM) : 0;
-    int upto = mine;
+__device__ __forceinline__ int slot_tiles_of(const Ffn4Args& a, int j0, int64_t& beg, int64_t& end, int& upto) {
+  const int lane = lane64(), j = j0 + lane;
+  beg = end = 0;
+  if (j < a.S) {
+    beg = a.slot_offset[j], end = a.slot_offset[j + 1];
+    beg = beg < 0 ? 0 : (beg > a.n_cap ? a.n_cap : beg);
+    end = end > a.n_cap ? a.n_cap : end;
+  }
+  const int mine = end > beg ? (int)((end - beg + BM - 1) / BM) : 0;
+  upto = mine;
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int v = __shfl_up(upto, o, 64);
-      if (lane >= o) upto += v;
-    }
-    const uint64_t hit = __ballot(upto > t);
+  for (int o = 1; o < 64; o <<= 1) {
+    const int v = __shfl_up(upto, o, 64);
+    if (lane >= o) upto += v;
+  }
+  return mine;
+}
+
+// The tile of workgroup b, found by every wavefront alone: row tiles are
+// numbered slot by slot, tiles along N within them, and each of the 8 XCDs has
+// an even share of neighbours, which have their rows and weights in its L2
+// once. False where there is none.
+template <int BM>
+__device__ __forceinline__ bool find_tile(const Ffn4Args& a, unsigned b, SlotTile& r, int& nt) {
+  int64_t beg, end;
+  int upto, all = 0;
+  for (int j0 = 0; j0 < a.S; j0 += 64) {
+    slot_tiles_of<BM>(a, j0, beg, end, upto);
+    all += __shfl(upto, 63, 64);
+  }
+  const int64_t tiles = (int64_t)all * a.n_tiles, share = (tiles + 7) / 8, at = b / 8, t = (b % 8) * share + at;
+  if (at >= share || t >= tiles) return false;
+  int m = (int)(t / a.n_tiles);
+  nt = (int)(t % a.n_tiles);
+  for (int j0 = 0; j0 < a.S; j0 += 64) {
+    const int mine = slot_tiles_of<BM>(a, j0, beg, end, upto);
+    const uint64_t hit = __ballot(upto > m);
     if (hit) {
       const int who = __builtin_ctzll(hit);
       const int before = __shfl(upto - mine, who, 64);
-      const int b = __shfl((int)beg, who, 64), e = __shfl((int)end, who, 64);
-      r.row0 = __builtin_amdgcn_readfirstlane(b + (t - before) * BM);
+      const int first = __shfl((int)beg, who, 64), e = __shfl((int)end, who, 64);
+      r.row0 = __builtin_amdgcn_readfirstlane(first + (m - before) * BM);
       r.end = __builtin_amdgcn_readfirstlane(e);
       r.w = __builtin_amdgcn_readfirstlane(a.slot_widx[j0 + who]);
+      nt = __builtin_amdgcn_readfirstlane(nt);
       return true;
     }
-    t -= __shfl(upto, 63, 64);
+    m -= __shfl(upto, 63, 64);
   }
   return false;
 }
@@ -180,29 +200,42 @@ __device__ __forceinline__ void dma4(i32x4 rs, uint32_t lds_wave_base, uint32_t 
   asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(m0v), "v"(voff), "s"(rs) : "memory");
 }
 
-constexpr int kMxM = 128, kMxN = 256, kMxStages = 3, kMxWaves = 4;
+constexpr int kMxWaves = 4;
+// Large tiles, two workgroups a CU; small ones with loads further ahead, for
+// calls with too few rows to give every CU a large one.
+constexpr int kMxM = 128, kMxN = 256, kMxStages = 3, kMxSmallM = 64, kMxSmallN = 128, kMxSmallStages = 6;
 
-template <bool GATE_UP>
+// Four scale words of a lane's rows, one for each of four stages.
+struct ScaleWords {
+  uint32_t w[4];
+};
+
+template <bool GATE_UP, int BM, int BN, int NS>
 __global__ __launch_bounds__(64 * kMxWaves, 2) void ffn4_kernel(Ffn4Args a) {
-  constexpr int BM = kMxM, BN = kMxN, NS = kMxStages, NW = kMxWaves;
+  constexpr int NW = kMxWaves;
   // 128 codes are 64 bytes: the geometry of a tile of 32 16-bit elements
   using AT = KTile<BM, 32, NW>;
   using BT = KTile<BN, 32, NW>;
-  constexpr int SCALES = (BM + BN) * 4;  // a word (four blocks) per row
-  constexpr int STAGE = AT::BYTES + BT::BYTES + SCALES;
-  constexpr int NSC = (BM + BN) / 64;    // wavefront loads of scales
-  constexpr int SC_PER_WAVE = (NSC + NW - 1) / NW;
-  constexpr int PER = AT::PER_WAVE + BT::PER_WAVE + SC_PER_WAVE;
-  constexpr int WM = 64, WN = 128, MB = WM / 32, NB = WN / 32;
-  __shared__ __attribute__((aligned(1024))) char lds[NS * STAGE + 256];  // the last 256: loads of nothing
+  constexpr int STAGE = AT::BYTES + BT::BYTES, ROWS = BM + BN;
+  constexpr int PER = AT::PER_WAVE + BT::PER_WAVE;
+  // Scales come for four stages at once, 16 bytes of a row, into one buffer
+  // that is free again when all have read theirs (a word of a row for every
+  // stage: 8200 x 7168 x 4096 245 us, this 180).
+  constexpr int SC_LOADS = ROWS / 64, SC_PER = (SC_LOADS + NW - 1) / NW, SCALES = ROWS * 16;
+  constexpr int WM = BM / 2, WN = BN / 2, MB = WM / 32, NB = WN / 32;
+  constexpr int YLD = BN * 2 + 16;  // bytes of a row of y in LDS
+  static_assert(ROWS % 64 == 0 && SC_PER <= 2 && (NS - 2) * PER + 2 < 64, "loads of scales, and in flight");
+  static_assert(NS * STAGE >= BM * YLD, "the output's tile takes the stages' place");
+  __shared__ __attribute__((aligned(1024))) char lds[NS * STAGE + SCALES];
 
   SlotTile r;
-  if (!find_row_tile<BM>(a, (int)(blockIdx.x / (unsigned)a.n_tiles), r)) return;
+  int nt;
+  if (!find_tile<BM>(a, blockIdx.x, r, nt)) return;
   if (r.w < 0 || r.w >= a.W) return;
-  const int nt = blockIdx.x % (unsigned)a.n_tiles;
   const int lane = lane64(), wave = wave_id(), half = lane >> 5;
   const int wm = wave >> 1, wn = wave & 1;
   const uint32_t lds0 = lds_addr(lds);
+  char* const sc = lds + NS * STAGE;
   const uint32_t kb = (uint32_t)a.K / 2, ks = (uint32_t)a.K / 32;  // bytes of a row of codes, of scales
   const int KT = a.K / 128;
 
@@ -218,32 +251,50 @@ __global__ __launch_bounds__(64 * kMxWaves, 2) void ffn4_kernel(Ffn4Args a) {
   auto wrow = [&](int i) -> uint32_t {
     return (uint32_t)(GATE_UP ? (i < BN / 2 ? n0 + i : a.F + n0 + i - BN / 2) : n0 + i);
   };
-  uint32_t va[AT::PER_WAVE], vb[BT::PER_WAVE], vs[SC_PER_WAVE];
+  uint32_t va[AT::PER_WAVE], vb[BT::PER_WAVE], vs[SC_PER];
 #pragma unroll
   for (int i = 0; i < AT::PER_WAVE; ++i) va[i] = AT::voff(lane, [&](int q) { return (uint32_t)q * kb; }, i);
 #pragma unroll
   for (int i = 0; i < BT::PER_WAVE; ++i) vb[i] = BT::voff(lane, [&](int q) { return wrow(q) * kb; }, i);
 #pragma unroll
-  for (int i = 0; i < SC_PER_WAVE; ++i) {
+  for (int i = 0; i < SC_PER; ++i) {
     const int q = (wave + NW * i) * 64 + lane;  // row of the A tile, then of the B tile
     vs[i] = q < BM ? (uint32_t)q * ks : wrow(q - BM) * ks;
   }
-  auto issue = [&](int kt) {
+  auto issue = [&](int kt) {  // stages past the last load nothing
     const bool live = kt < KT;
     const uint32_t at = lds0 + (uint32_t)((kt % NS) * STAGE);
-    const uint32_t kc = live ? (uint32_t)kt * 64u : 0u, kw = live ? (uint32_t)kt * 4u : 0u;
+    const uint32_t kc = live ? (uint32_t)kt * 64u : 0u;
     const i32x4 ra = buf_rsrc(abase + kc, live ? abytes - kc : 0u), rb = buf_rsrc(bbase + kc, live ? bbytes - kc : 0u);
 #pragma unroll
     for (int i = 0; i < AT::PER_WAVE; ++i) AT::issue(ra, at, va[i], i);
 #pragma unroll
     for (int i = 0; i < BT::PER_WAVE; ++i) BT::issue(rb, at + AT::BYTES, vb[i], i);
+  };
+  // The 16 bytes from o on of every row: those of stages 4 g .. 4 g + 3, or
+  // the row's last 16, so that no load reaches past a row. Where a row has
+  // fewer (K < 512), word by word.
+  const bool by_word = ks < 16;
+  auto first_of = [&](int g) -> uint32_t { return (uint32_t)g * 16u + 16u <= ks ? (uint32_t)g * 16u : ks - 16u; };
+  auto scales_of = [&](int i, uint32_t o, bool live) {  // the resource of wavefront load i
+    const int q = wave + NW * i;
+    const bool some = live && q < SC_LOADS, is_a = q * 64 < BM;
+    return buf_rsrc((is_a ? asbase : bsbase) + (some ? o : 0u), some ? (is_a ? asbytes : bsbytes) - o : 0u);
+  };
+  auto issue_scales = [&](int g) {
+    const bool live = g * 4 < KT;
+    const uint32_t o = live ? first_of(g) : 0u;
 #pragma unroll
-    for (int i = 0; i < SC_PER_WAVE; ++i) {
-      const int q = wave + NW * i;
-      const bool some = live && q < NSC, is_a = q * 64 < BM;
-      dma4(buf_rsrc((is_a ? asbase : bsbase) + kw, some ? (is_a ? asbytes : bsbytes) - kw : 0u),
-           q < NSC ? at + AT::BYTES + BT::BYTES + q * 256 : lds0 + NS * STAGE, vs[i]);
-    }
+    for (int i = 0; i < SC_PER; ++i)
+      if (wave + NW * i < SC_LOADS)
+        dma16(scales_of(i, o, live), lds0 + NS * STAGE + (wave + NW * i) * 1024, vs[i]);
+  };
+  auto issue_words = [&] {
+    for (int k = 0; k < KT; ++k)
+#pragma unroll
+      for (int i = 0; i < SC_PER; ++i)
+        if (wave + NW * i < SC_LOADS)
+          dma4(scales_of(i, (uint32_t)k * 4u, true), lds0 + NS * STAGE + k * ROWS * 4 + (wave + NW * i) * 256, vs[i]);
   };
 
   f32x16 acc[MB][NB];
@@ -267,45 +318,93 @@ __global__ __launch_bounds__(64 * kMxWaves, 2) void ffn4_kernel(Ffn4Args a) {
 #pragma unroll
   for (int kk = 0; kk < 2; ++kk) ka[kk] = AT::kstep_off(lane, kk);
 
+  ScaleWords sa[MB], sb[NB];
+  // this lane's blocks of a stage are 2 kk + half: their bytes 2 kk after the shift
+  auto read_scales = [&](int g) {
+    const uint32_t skip = by_word ? 0u : ((uint32_t)g * 16u - first_of(g)) / 4u;  // words of the stages before
+    auto read = [&](int row, ScaleWords& s) {
+      if (by_word) {
+#pragma unroll
+        for (int k = 0; k < 3; ++k) s.w[k] = k < KT ? ((const uint32_t*)sc)[k * ROWS + row] : 0u;
+        s.w[3] = 0;
+      } else {
+        const uint4 v = ((const uint4*)sc)[row];
+        s.w[0] = v.x, s.w[1] = v.y, s.w[2] = v.z, s.w[3] = v.w;
+        if (skip == 1) s.w[0] = s.w[1], s.w[1] = s.w[2], s.w[2] = s.w[3];
+        if (skip == 2) s.w[0] = s.w[2], s.w[1] = s.w[3];
+        if (skip == 3) s.w[0] = s.w[3];
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) s.w[k] >>= 8 * half;
+    };
+#pragma unroll
+    for (int i = 0; i < MB; ++i) read(wm * WM + i * 32 + (lane & 31), sa[i]);
+#pragma unroll
+    for (int j = 0; j < NB; ++j) read(BM + bcol(j) + (lane & 31), sb[j]);
+  };
+
+  if (by_word) issue_words();
+  else issue_scales(0);
 #pragma unroll
   for (int s = 0; s < NS - 1; ++s) issue(s);
-  for (int kt = 0; kt < KT; ++kt) {
-    wait_vm<(NS - 2) * PER>();  // stage kt has landed
-    __syncthreads();            // for every wavefront, and stage kt - 1 has been read
-    issue(kt + NS - 1);
-    const char* st = lds + (kt % NS) * STAGE;
-    const uint32_t* sc = (const uint32_t*)(st + AT::BYTES + BT::BYTES);
-    uint32_t sa[MB], sb[NB];  // this lane's blocks are 2 kk + half: their bytes 2 kk after the shift
+  for (int k0 = 0; k0 < KT; k0 += 4) {
+    static_for<0, 4>([&](auto pc) {
+      constexpr int ph = decltype(pc)::value;
+      const int kt = k0 + ph;
+      if (kt >= KT) return;
+      // Stage kt has landed: what may be in flight are the codes of the NS - 2
+      // stages after it (with scales among them, one load or two fewer). Before
+      // scales are read, which were asked for behind the codes of three
+      // iterations ago, the codes of two. With NS = 3, in the iteration after
+      // they were asked for, they may be in flight too.
+      if constexpr (ph == 0 && NS > 4) {
+        if (k0 > 0) wait_vm<2 * PER>();
+        else wait_vm<(NS - 2) * PER>();
+      } else if constexpr (ph == 2 && NS == 3) {
+        if (by_word || wave >= SC_LOADS) wait_vm<(NS - 2) * PER>();  // (words came first)
+        else if (wave + NW < SC_LOADS) wait_vm<(NS - 2) * PER + 2>();
+        else wait_vm<(NS - 2) * PER + 1>();
+      } else {
+        wait_vm<(NS - 2) * PER>();
+      }
+      __syncthreads();  // for every wavefront, and stage kt - 1 has been read
+      issue(kt + NS - 1);
+      if constexpr (ph == 0) read_scales(k0 / 4);
+      if constexpr (ph == 1) {
+        if (!by_word) issue_scales(k0 / 4 + 1);
+      }
+      const char* st = lds + (kt % NS) * STAGE;
+      static_for<0, 2>([&](auto kkc) {
+        constexpr int kk = decltype(kkc)::value;
+        i32x4 fa[MB], fb[NB];
 #pragma unroll
-    for (int i = 0; i < MB; ++i) sa[i] = sc[wm * WM + i * 32 + (lane & 31)] >> (8 * half);
+        for (int i = 0; i < MB; ++i) fa[i] = *(const i32x4*)(st + oa[i] + ka[kk]);
 #pragma unroll
-    for (int j = 0; j < NB; ++j) sb[j] = sc[BM + bcol(j) + (lane & 31)] >> (8 * half);
-    static_for<0, 2>([&](auto kkc) {
-      constexpr int kk = decltype(kkc)::value;
-      i32x4 fa[MB], fb[NB];
+        for (int j = 0; j < NB; ++j) fb[j] = *(const i32x4*)(st + ob[j] + ka[kk]);
 #pragma unroll
-      for (int i = 0; i < MB; ++i) fa[i] = *(const i32x4*)(st + oa[i] + ka[kk]);
+        for (int i = 0; i < MB; ++i)
 #pragma unroll
-      for (int j = 0; j < NB; ++j) fb[j] = *(const i32x4*)(st + ob[j] + ka[kk]);
-#pragma unroll
-      for (int i = 0; i < MB; ++i)
-#pragma unroll
-        for (int j = 0; j < NB; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
-              __builtin_shufflevector(fb[j], fb[j], 0, 1, 2, 3, -1, -1, -1, -1),
-              __builtin_shufflevector(fa[i], fa[i], 0, 1, 2, 3, -1, -1, -1, -1), acc[i][j], 4, 4, 2 * kk, sb[j], 2 * kk,
-              sa[i]);
+          for (int j = 0; j < NB; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+                __builtin_shufflevector(fb[j], fb[j], 0, 1, 2, 3, -1, -1, -1, -1),
+                __builtin_shufflevector(fa[i], fa[i], 0, 1, 2, 3, -1, -1, -1, -1), acc[i][j], 4, 4, 2 * kk,
+                (int)sb[j].w[ph], 2 * kk, (int)sa[i].w[ph]);
+      });
     });
   }
-  wait_vm<0>();  // the loads of nothing, before the workgroup's LDS is another's
+  wait_vm<0>();     // the loads of nothing have landed too
+  __syncthreads();  // and every wavefront has read its last stage: the output takes its place
 
   // block (i, j), register q: row 32 i + lane % 32, column 32 j + 8 (q / 4) + 4 half + q % 4
+  const int tid = threadIdx.x;
+  if constexpr (GATE_UP) {
+    // a tile of BN / 2 columns of h: BN / 4 bytes of codes and BN / 64 of scales a row
+    constexpr int HLD = BN / 4 + 16, PARTS = BN / 64;
+    typedef typename std::conditional<PARTS == 4, uint32_t, uint16_t>::type Scales;
+    char* const hs = lds + BM * HLD;
 #pragma unroll
-  for (int i = 0; i < MB; ++i) {
-    const int64_t row = r.row0 + wm * WM + i * 32 + (lane & 31);
-    const bool there = row < r.end;
-    if constexpr (GATE_UP) {
-      const int64_t hrow = row * (a.F / 32);
+    for (int i = 0; i < MB; ++i) {
+      const int row = wm * WM + i * 32 + (lane & 31);
 #pragma unroll
       for (int j = 0; j < NB / 2; ++j) {
         float g[16], h[16];
@@ -327,33 +426,45 @@ __global__ __launch_bounds__(64 * kMxWaves, 2) void ffn4_kernel(Ffn4Args a) {
         for (int q = 0; q < 16; ++q) h[q] *= inv;
         // codes of the four columns of each group of eight that this lane
         // has; the other half's lane has the other four
-        uint32_t c[4];
+        const int col = wn * (WN / 2) + j * 32;
+        char* const to = lds + row * HLD + col / 2 + 2 * half;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) c[q] = mx_put2<1>(mx_put2<0>(0u, h[4 * q], h[4 * q + 1]), h[4 * q + 2], h[4 * q + 3]);
-        const int f = n0 + wn * (WN / 2) + j * 32;
-        uint32_t word[2];  // of groups 0, 1 in the lower half's lanes, of 2, 3 in the upper's
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          const uint32_t give = half ? c[q] : c[q + 2], keep = half ? c[q + 2] : c[q];
-          const uint32_t got = __shfl_xor(give, 32, 64);
-          word[q] = half ? (got & 0xffffu) | keep << 16 : (keep & 0xffffu) | got << 16;
+        for (int q = 0; q < 4; ++q) {
+          const uint32_t c = mx_put2<1>(mx_put2<0>(0u, h[4 * q], h[4 * q + 1]), h[4 * q + 2], h[4 * q + 3]);
+          *(uint16_t*)(to + 4 * q) = s == 255 ? (uint16_t)0 : (uint16_t)c;
         }
-        if (there) {
-          if (s == 255) word[0] = word[1] = 0;
-          *(uint2*)(a.h_codes + row * (a.F / 2) + f / 2 + 8 * half) = uint2{word[0], word[1]};
-          if (half == 0) a.h_scales[hrow + f / 32] = (uint8_t)s;
-        }
+        if (half == 0) hs[row * PARTS + col / 32] = (char)s;
       }
-    } else {
+    }
+    __syncthreads();
 #pragma unroll
-      for (int j = 0; j < NB; ++j) {
-        const int c = n0 + wn * WN + j * 32 + 4 * half;
-        if (there && c < a.N) {  // N is a multiple of 128: a block is in or out
+    for (int o = tid; o < BM * PARTS; o += 64 * NW) {
+      const int row = o / PARTS, part = o % PARTS;
+      if (row < rows)
+        *(uint4*)(a.h_codes + (r.row0 + row) * (a.F / 2) + n0 / 2 + 16 * part) = *(const uint4*)(lds + row * HLD + 16 * part);
+    }
+    if (tid < rows)
+      *(Scales*)(a.h_scales + (r.row0 + tid) * (a.F / 32) + n0 / 32) = *(const Scales*)(hs + PARTS * tid);
+  } else {
 #pragma unroll
-          for (int q = 0; q < 4; ++q)
-            *(uint2*)(a.y + row * a.N + c + 8 * q) = uint2{pack_bf2(acc[i][j][4 * q], acc[i][j][4 * q + 1]),
-                                                           pack_bf2(acc[i][j][4 * q + 2], acc[i][j][4 * q + 3])};
-        }
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          *(uint2*)(lds + (wm * WM + i * 32 + (lane & 31)) * YLD + (wn * WN + j * 32 + 4 * half + 8 * q) * 2) =
+              uint2{pack_bf2(acc[i][j][4 * q], acc[i][j][4 * q + 1]), pack_bf2(acc[i][j][4 * q + 2], acc[i][j][4 * q + 3])};
+    __syncthreads();
+    // whole lines: 512 bytes of a row by 32 lanes (8 bytes of a row at a time
+    // from the registers: 16278 x 768 x 2048 50 us, this 30)
+    constexpr int LANES = BN / 8, AT_ONCE = 64 * NW / LANES;
+    const int part = tid % LANES;
+    if (n0 + part * 8 < a.N) {
+#pragma unroll 4
+      for (int k = 0; k < BM / AT_ONCE; ++k) {
+        const int row = k * AT_ONCE + tid / LANES;
+        if (row < rows)
+          *(uint4*)(a.y + (r.row0 + row) * a.N + n0 + part * 8) = *(const uint4*)(lds + row * YLD + 16 * part);
       }
     }
   }
@@ -370,6 +481,25 @@ using namespace foremoe;
   } while (0)
 
 static bool misaligned(const void* p, uintptr_t bytes) { return ((uintptr_t)p & (bytes - 1)) != 0; }
+
+// One product. Every slot has at most one tile that is not full; tiles are
+// large unless even the most that there can be leave CUs without one.
+template <bool GATE_UP>
+static void launch_ffn4(Ffn4Args a, hipStream_t st) {
+  auto grid = [&](int bm, int bn) {
+    a.n_tiles = (a.N + bn - 1) / bn;
+    return (a.n_cap + bm - 1) / bm * a.n_tiles + (int64_t)a.S * a.n_tiles;
+  };
+  auto rounded = [](int64_t n) { return dim3((unsigned)((n + 7) / 8 * 8)); };  // one share for each XCD: see find_tile
+  int64_t n = grid(kMxM, kMxN);
+  if (n > num_cus()) {
+    hipLaunchKernelGGL((ffn4_kernel<GATE_UP, kMxM, kMxN, kMxStages>), rounded(n), dim3(64 * kMxWaves), 0, st, a);
+  } else {
+    n = grid(kMxSmallM, kMxSmallN);
+    hipLaunchKernelGGL((ffn4_kernel<GATE_UP, kMxSmallM, kMxSmallN, kMxSmallStages>), rounded(n), dim3(64 * kMxWaves), 0,
+                       st, a);
+  }
+}
 
 static unsigned quant_blocks(int64_t units) {
   const int64_t nb = (units + kQuantThreads - 1) / kQuantThreads;
@@ -469,20 +599,18 @@ int foremoe_grouped_ffn_mxfp4_fwd(const uint8_t* x_codes, const uint8_t* x_scale
   uint8_t* h_codes = (uint8_t*)ws;
   uint8_t* h_scales = h_codes + align_up((size_t)n_cap * (F / 2), 256);
   hipStream_t st = (hipStream_t)stream;
-  // every slot has at most one tile that is not full
-  const int64_t row_tiles = (n_cap + kMxM - 1) / kMxM + S;
   Ffn4Args a{};
   a.slot_offset = slot_offset, a.slot_widx = slot_widx, a.S = S, a.W = W, a.n_cap = n_cap, a.F = F;
   a.h_codes = h_codes, a.h_scales = h_scales, a.y = (uint16_t*)y_perm;
+  REQUIRE((n_cap / 128 + S + 1) * ((d > F ? d : F) / 128) < (int64_t)1 << 23, "grouped_ffn_mxfp4_fwd: too many tiles");
   a.a_codes = x_codes, a.a_scales = x_scales, a.b_codes = gate_up_codes, a.b_scales = gate_up_scales;
-  a.K = d, a.N = 2 * F, a.n_tiles = F / (kMxN / 2);
-  REQUIRE(row_tiles * ((d > F ? d : F) / 128) < (int64_t)1 << 31, "grouped_ffn_mxfp4_fwd: too many tiles");
-  hipLaunchKernelGGL((ffn4_kernel<true>), dim3((unsigned)(row_tiles * a.n_tiles)), dim3(64 * kMxWaves), 0, st, a);
-  int rc = check_launch("grouped_ffn_mxfp4_fwd (gate/up)");
+  a.K = d, a.N = 2 * F;
+  launch_ffn4<true>(a, st);
+  const int rc = check_launch("grouped_ffn_mxfp4_fwd (gate/up)");
   if (rc != FOREMOE_OK) return rc;
   a.a_codes = h_codes, a.a_scales = h_scales, a.b_codes = down_codes, a.b_scales = down_scales;
-  a.K = F, a.N = d, a.n_tiles = (d + kMxN - 1) / kMxN;
-  hipLaunchKernelGGL((ffn4_kernel<false>), dim3((unsigned)(row_tiles * a.n_tiles)), dim3(64 * kMxWaves), 0, st, a);
+  a.K = F, a.N = d;
+  launch_ffn4<false>(a, st);
   return check_launch("grouped_ffn_mxfp4_fwd (down)");
 }
 
