@@ -842,7 +842,9 @@ int foremoe_grouped_ffn_mxfp4_fwd(const uint8_t* x_codes, const uint8_t* x_scale
  * over the places k whose id is in [0, E) and whose w is in [0, W) (the
  * others count as 0 whatever their gate holds: padding, experts of other
  * ranks); a token without any gets a zero row. Two places of a token may name
- * one expert. The sums and the hidden rows are held in fp32.
+ * one expert. Sums are fp32; so are the hidden rows, or they are held as two
+ * bf16 numbers each (their rounding, and that of what it leaves: 2^-16), three
+ * where y is fp32 (2^-24).
  * x [T, d] of dtype, rows ld elements apart; ids, gates [T, K]; expert_widx
  * [E] int32 or NULL (the identity; then E <= W); w_gate_up [W, 2F, d] and
  * w_down [W, d, F] as in foremoe_grouped_ffn_fwd, contiguous, of dtype, or of

@@ -4,12 +4,12 @@
 // weights by up to 16 tokens); nothing else is worth counting.
 //
 //   gate/up: a workgroup takes 8 hidden columns (8 rows of Wg, 8 of Wu) of one
-//     expert, its wavefronts the k axis; H in fp32, as two bf16 planes (its
-//     rounding, and what that leaves) where the weights are bf16 or 4 bits.
 //   down: a workgroup takes 8 output columns of every expert, its wavefronts
 //     the experts, or parts of their k axis where experts are few. So it holds
 //     a token's sum over its experts alone: no partial sums in memory, no
 //     counters, a fixed order.
+#include <type_traits>
+
 #include "common.h"
 #include "mx.h"
 
@@ -18,6 +18,8 @@ namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
 
 enum Weights { kBf16 = 0, kF32 = 1, kFp4 = 2 };
 
@@ -30,9 +32,10 @@ struct FewArgs {
   const int32_t* widx;
   const char *gu, *dn;               // weights or codes
   const uint8_t *gu_scales, *dn_scales;
-  char* h;                           // bf16: planes [2][pairs][Fp]; fp32: [pairs][Fp]
+  char* h;                           // bf16: planes [2 or 3][pairs][Fp]; fp32: [pairs][Fp]
   void* y;
   int y_f32;
+  int planes;        // of the hidden rows
   int width, tiles;  // of the second product: output columns of a tile, tiles of a workgroup
 };
 
@@ -50,49 +53,54 @@ struct WeightFrag {
   uint32_t scale;  // 4 bits: the block's scale byte
 };
 
-// The scale bytes of chunks c and c + 1 of a row of nb blocks, those past its
-// end aside: eight bytes in one load (a load a byte took 17 of 101 us of 24
-// tokens in 4 bits). Rows shorter than that go byte by byte.
+// The scale bytes of CHUNKS chunks from c on of a row of nb blocks, in one
+// load (a load a byte took 17 of 101 us of 24 tokens in 4 bits). CHECKED: some
+// may be past the row's end.
+template <int CHUNKS, bool CHECKED>
 __device__ __forceinline__ uint64_t load_scales(const uint8_t* scales, int nb, int c) {
+  typedef typename std::conditional<CHUNKS == 2, uint64_t, uint32_t>::type Word;
+  constexpr int N = 4 * CHUNKS;
   const int at = 4 * c;
-  if (nb >= 8) {
-    const int from = at + 8 <= nb ? at : nb - 8, skip = at - from;
-    uint64_t v;
-    __builtin_memcpy(&v, scales + from, 8);
-    return skip < 8 ? v >> (8 * skip) : 0;
+  Word v = 0;
+  if constexpr (CHECKED) {
+    if (nb >= N) {  // the row's last ones, moved down
+      const int from = at + N <= nb ? at : nb - N;
+      __builtin_memcpy(&v, scales + from, N);
+      v = at < nb ? v >> (8 * (at - from)) : 0;
+    } else {
+      for (int i = 0; i < N; ++i)
+        if (at + i < nb) v |= (Word)scales[at + i] << (8 * i);
+    }
+  } else {
+    __builtin_memcpy(&v, scales + at, N);
   }
-  uint64_t v = 0;
-  for (int i = 0; i < 8; ++i)
-    if (at + i < nb) v |= (uint64_t)scales[at + i] << (8 * i);
   return v;
 }
 
-// This lane's part of chunk c of a row (zeros past its end). VEC: the row
-// starts on 16 bytes and its length is a multiple of them.
-template <int WT, bool VEC>
-__device__ __forceinline__ WeightFrag load_weights(const char* row, int n, int c, int g) {
+// This lane's part of chunk c of a row of n elements. CHECKED: zeros past its
+// end. VEC: the row starts on 16 bytes and its length is a multiple of them.
+template <int WT, bool VEC, bool CHECKED>
+__device__ __forceinline__ uint4 load_weights(const char* row, int n, int c, int g) {
   using C = Chunk<WT>;
-  WeightFrag f;
-  f.v = uint4{0, 0, 0, 0}, f.scale = 0;
   const int k = c * C::K + g * C::PER_LANE;
-  if (k >= n) return f;
   if constexpr (VEC) {
-    f.v = *(const uint4*)(row + (size_t)c * 64 + g * 16);
+    if (CHECKED && k >= n) return uint4{0, 0, 0, 0};
+    return *(const uint4*)(row + (size_t)c * 64 + g * 16);
   } else if constexpr (WT == kBf16) {
     const uint16_t* p = (const uint16_t*)row + k;
     uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (k + i < n) w[i / 2] |= (uint32_t)p[i] << (16 * (i & 1));
-    f.v = uint4{w[0], w[1], w[2], w[3]};
+      if (!CHECKED || k + i < n) w[i / 2] |= (uint32_t)p[i] << (16 * (i & 1));
+    return uint4{w[0], w[1], w[2], w[3]};
   } else {
     const uint32_t* p = (const uint32_t*)row + k;
-    f.v.x = p[0];
-    if (k + 1 < n) f.v.y = p[1];
-    if (k + 2 < n) f.v.z = p[2];
-    if (k + 3 < n) f.v.w = p[3];
+    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (!CHECKED || k + i < n) w[i] = p[i];
+    return uint4{w[0], w[1], w[2], w[3]};
   }
-  return f;
 }
 
 template <int WT>
@@ -100,20 +108,40 @@ struct TokenFrag {
   uint4 v[Chunk<WT>::OPERANDS];
 };
 
-// The same k of a token's row (of n elements, readable in 16 bytes if VEC).
-template <int WT, bool VEC>
-__device__ __forceinline__ TokenFrag<WT> load_token(const char* row, int n, int c, int g, bool there) {
+// Tokens (or hidden rows) of a matrix, one to a column of a product. VEC: read
+// through a range-checked buffer, in which a column without a token lies
+// outside: it reads zeros, without a branch and without touching memory (lanes
+// that read another's address again took a third of the gate/up product of 24
+// tokens in 4 bits).
+struct Tokens {
+  __amdgpu_buffer_rsrc_t buffer;
+  const char* base;  // (in LDS where they are staged)
+};
+constexpr uint32_t kOutside = 0xF0000000u;  // more than a buffer has, and room to count up
+
+__device__ __forceinline__ Tokens tokens_at(const void* base, uint32_t bytes) {
+  return Tokens{__builtin_amdgcn_make_buffer_rsrc((void*)base, 0, bytes, 0x00020000), (const char*)base};
+}
+
+// The same k of the token at offset `at`. STAGED: in LDS, whole chunks long.
+template <int WT, bool VEC, bool STAGED, bool HIDDEN, bool CHECKED>
+__device__ __forceinline__ TokenFrag<WT> load_token(const Tokens& tokens, uint32_t at, int n, int c, int g) {
   using C = Chunk<WT>;
   TokenFrag<WT> f;
-#pragma unroll
-  for (int i = 0; i < C::OPERANDS; ++i) f.v[i] = uint4{0, 0, 0, 0};
   const int k = c * C::K + g * C::PER_LANE;
-  if (!there || k >= n) return f;
-  if constexpr (VEC) {
+  if constexpr (STAGED) {
 #pragma unroll
-    for (int i = 0; i < C::OPERANDS; ++i) f.v[i] = *(const uint4*)(row + (size_t)k * C::ES + 16 * i);
+    for (int i = 0; i < C::OPERANDS; ++i)
+      f.v[i] = __builtin_bit_cast(uint4, *(const lds_u32x4*)(uintptr_t)(at + (uint32_t)(k * C::ES + 16 * i)));
+  } else if constexpr (VEC) {
+    constexpr bool APART = HIDDEN && WT == kFp4;  // see h_place
+    const uint32_t o = CHECKED && k >= n ? kOutside : at + (uint32_t)((APART ? c * C::K + g * 8 : k) * C::ES);
+#pragma unroll
+    for (int i = 0; i < C::OPERANDS; ++i)
+      f.v[i] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(tokens.buffer, o, (APART ? 64 : 16) * i, 0));
   } else {
-    f.v[0] = load_weights<WT == kFp4 ? kBf16 : WT, false>(row, n, c, g).v;
+    f.v[0] = uint4{0, 0, 0, 0};
+    if (at < kOutside) f.v[0] = load_weights<WT == kFp4 ? kBf16 : WT, false, CHECKED>(tokens.base + at, n, c, g);
   }
   return f;
 }
@@ -266,90 +294,148 @@ __device__ __forceinline__ int parts_for(int n, int nc, int each, int slots) {
 // gate/up. A unit is 8 hidden columns of a matrix in use; a workgroup to a CU
 // takes its even share of them, a wavefront a unit or a part of its k axis.
 // ---------------------------------------------------------------------------
-constexpr int kFewThreads = 1024, kFewWaves = 16, kUpSlots = 1024;
+constexpr int kFewThreads = 1024, kFewWaves = 16, kUpSlots = 1024, kUpStage = 72 << 10;
 // Steps of weights in flight behind those that are multiplied: as many as the
 // registers of 16 wavefronts a CU hold beside NG groups of tokens.
 template <int WT, int NG>
-constexpr int kAhead = WT == kFp4 ? (NG == 1 ? 2 : 1) : (NG == 4 ? 2 : 4);
+constexpr int kAhead = WT == kFp4 ? 1 : (NG == 4 ? 2 : 4);
+template <int WT, int NG>
+constexpr int kAheadStaged = 4;
+template <int WT, int NG>
+constexpr int kAheadDown = WT == kFp4 ? (NG == 1 ? 3 : 1) : (NG == 4 ? 2 : 4);
 // Groups of tokens that a step of weights is multiplied with, at most.
 template <int WT>
 constexpr int kGroups = WT == kFp4 ? 2 : 4;
 
-// sums[i] += rows of weights x the tokens at tok[i], over chunks [c0, c1) of
-// the k axis, in steps of S chunks (lane: chunk c + odd where S is 2). The
-// weights of the next U steps are on their way while these are multiplied.
-template <int WT, bool WVEC, bool TVEC, int NG, int U, int S>
-__device__ __forceinline__ void stream_rows(const char* row, const uint8_t* scales, int n, const char* const* tok,
-                                            const bool* there, int nt, int c0, int c1, int odd, int g, f32x4* sums) {
+// sums[i] = rows of weights x the tokens at offsets tok[i], over chunks [c0, c1) of
+// the k axis, in steps of S chunks (lane: chunk c + odd where S is 2). U steps
+// at a time without a branch, the weights of the next on their way while these
+// are multiplied; then the steps that are left, one of which may end in the
+// row's last, short chunk.
+template <int WT, bool WVEC, bool TVEC, bool STAGED, bool HIDDEN, int NG, int U, int S>
+__device__ __forceinline__ void stream_rows(const char* row, const uint8_t* scales, int n,
+                                            const Tokens& tokens, const uint32_t* tok, int nt, int c0, int c1, int odd, int g, f32x4* sums) {
+  using C = Chunk<WT>;
 #pragma unroll
   for (int i = 0; i < NG; ++i) sums[i] = f32x4{0, 0, 0, 0};
-  using C = Chunk<WT>;
-  // elements past the last chunk count as zeros
-  const int wn = min(n, c1 * C::K), tn = min(nt, c1 * C::K);
-  WeightFrag next[U];
-  // lanes of the even and the odd chunks of a pair have the same two scale words
-  constexpr int SW = (U * S + 1) / 2;
-  uint64_t ns[SW];
-  auto load = [&](int c) {
+  const int by = 8 * g + (S == 2 ? 32 * odd : 0);  // bit of this lane's scale
+  const int blocks = (min(c1, n / (C::K * S) * S) - c0) / (U * S);
+  if (blocks > 0) {
+    WeightFrag next[U];
+    uint64_t ns[U];
+    auto load = [&](int c) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) next[u] = load_weights<WT, WVEC>(row, wn, c + u * S + odd, g);
-    if constexpr (WT == kFp4) {
-#pragma unroll
-      for (int i = 0; i < SW; ++i) ns[i] = load_scales(scales, n / kMxBlock, c + 2 * i);
-    }
-  };
-  load(c0);
-  for (int c = c0; c < c1; c += U * S) {
-    WeightFrag w[U];
-    TokenFrag<WT> t[U][NG];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      w[u] = next[u];
+      for (int u = 0; u < U; ++u) next[u].v = load_weights<WT, WVEC, false>(row, n, c + u * S + odd, g);
       if constexpr (WT == kFp4) {
-        const int by = u * S + (S == 2 ? odd : 0);
-        w[u].scale = (uint32_t)(ns[u * S / 2] >> (8 * (4 * (by & 1) + g))) & 0xffu;
+#pragma unroll
+        for (int u = 0; u < U; ++u) ns[u] = load_scales<S, false>(scales, 0, c + u * S);
+      }
+    };
+    load(c0);
+    for (int b = 0; b < blocks; ++b) {
+      const int c = c0 + b * U * S;
+      WeightFrag w[U];
+      TokenFrag<WT> t[STAGED ? 1 : U][NG];  // (from LDS a step at a time)
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        w[u] = next[u];
+        if constexpr (WT == kFp4) w[u].scale = (uint32_t)(ns[u] >> by) & 0xffu;
+      }
+      auto load_t = [&](int to, int u) {
+#pragma unroll
+        for (int i = 0; i < NG; ++i)
+          t[to][i] = load_token<WT, TVEC, STAGED, HIDDEN, false>(tokens, tok[i], nt, c + u * S + odd, g);
+      };
+      if constexpr (!STAGED) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) load_t(u, u);
+      }
+      load(b + 1 < blocks ? c + U * S : c);  // (the last again: no branch)
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if constexpr (STAGED) load_t(0, u);
+#pragma unroll
+        for (int i = 0; i < NG; ++i) sums[i] = multiply<WT>(w[u], t[STAGED ? 0 : u][i], sums[i]);
       }
     }
+  }
+  for (int c = c0 + (blocks > 0 ? blocks : 0) * U * S; c < c1; c += S) {
+    WeightFrag w;
+    w.v = load_weights<WT, WVEC, true>(row, n, c + odd, g);
+    w.scale = WT == kFp4 ? (uint32_t)(load_scales<S, true>(scales, n / kMxBlock, c) >> by) & 0xffu : 0;
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int i = 0; i < NG; ++i) t[u][i] = load_token<WT, TVEC>(tok[i], tn, c + u * S + odd, g, there[i]);
-    load(c + U * S);
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int i = 0; i < NG; ++i) sums[i] = multiply<WT>(w[u], t[u][i], sums[i]);
+    for (int i = 0; i < NG; ++i)
+      sums[i] = multiply<WT>(w, load_token<WT, TVEC, STAGED, HIDDEN, true>(tokens, tok[i], nt, c + odd, g), sums[i]);
   }
 }
 
-// Both products of up to 16 NG pairs from place `first` on, over chunks [c0, c1).
-template <int WT, bool VEC, int NG>
-__device__ __forceinline__ void up_groups(const FewArgs& a, const Groups& G, int first, int end, const char* row,
-                                          const uint8_t* scales, int c0, int c1, f32x4* sums) {
+// Both products of up to 16 NG pairs from place `first` on, over chunks [c0,
+// c1). STAGED: the token of place q is at stage + (q - q0) * stride in LDS.
+template <int WT, bool VEC, bool STAGED, int NG>
+__device__ __forceinline__ void up_groups(const FewArgs& a, const Groups& G, uint32_t stage, int stride, int q0,
+                                          int first, int end, const char* row, const uint8_t* scales, int c0, int c1,
+                                          f32x4* sums) {
   using C = Chunk<WT>;
   const int lane = lane_id(), g = lane >> 4, col = lane & 15;
-  const char* tok[NG];
-  bool there[NG];
+  uint32_t tok[NG];
 #pragma unroll
   for (int i = 0; i < NG; ++i) {
     const int q = first + 16 * i + col;
-    there[i] = q < end;
-    tok[i] = (const char*)a.x + (there[i] ? (int64_t)(G.list[q] / a.K) * a.ld * C::ES : 0);
+    // (staged, a column without a token reads another's: no product of it is used)
+    if constexpr (STAGED) tok[i] = stage + (uint32_t)(((q < end ? q : first) - q0) * stride);
+    else tok[i] = q < end ? (uint32_t)(G.list[q] / a.K * a.ld * C::ES) : kOutside;
   }
-  stream_rows<WT, VEC, VEC, NG, kAhead<WT, NG>, 1>(row, scales, a.d, tok, there, a.d, c0, c1, 0, g, sums);
+  const Tokens x = tokens_at(a.x, (uint32_t)(((a.T - 1) * a.ld + a.d) * C::ES));
+  constexpr int U = STAGED ? kAheadStaged<WT, NG> : kAhead<WT, NG>;
+  stream_rows<WT, VEC, VEC, STAGED, false, NG, U, 1>(row, scales, a.d, x, tok, a.d, c0, c1, 0, g, sums);
 }
 
+// The same of all pairs of one matrix, up to 16 kGroups at a time; done(sums,
+// q) takes those of the 16 from place q on.
+template <int WT, bool VEC, bool STAGED, class Done>
+__device__ __forceinline__ void up_unit(const FewArgs& a, const Groups& G, uint32_t stage, int stride, int q0, int first,
+                                        int end, const char* row, const uint8_t* scales, int c0, int c1, Done&& done) {
+  for (int at = first; at < end; at += 16 * kGroups<WT>) {
+    f32x4 sums[4];
+    if (end - at <= 16) {
+      up_groups<WT, VEC, STAGED, 1>(a, G, stage, stride, q0, at, end, row, scales, c0, c1, sums);
+      done(sums[0], at);
+    } else if (kGroups<WT> == 2 || end - at <= 32) {
+      up_groups<WT, VEC, STAGED, 2>(a, G, stage, stride, q0, at, end, row, scales, c0, c1, sums);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) done(sums[k], at + 16 * k);
+    } else {
+      up_groups<WT, VEC, STAGED, kGroups<WT>>(a, G, stage, stride, q0, at, end, row, scales, c0, c1, sums);
+#pragma unroll
+      for (int k = 0; k < kGroups<WT>; ++k) done(sums[k], at + 16 * k);
+    }
+  }
+}
+
+// Where element f of a hidden row lies. With 4-bit weights a lane takes 32
+// neighbours of a chunk, eight at a time: the eights that the four lanes take
+// together lie together.
+template <int WT>
+__device__ __forceinline__ int h_place(int f) {
+  return WT == kFp4 ? (f & ~127) | (f >> 3 & 3) << 5 | (f >> 5 & 3) << 3 | (f & 7) : f;
+}
+
+// An element of the hidden rows: fp32, or a bf16 plane for its rounding and one
+// or two for what the planes before leave.
 template <int WT>
 __device__ __forceinline__ void put_h(const FewArgs& a, int pair, int f, float gate, float up) {
   const float h = f < a.F ? gate / (1.0f + expf(-gate)) * up : 0.0f;
-  const int64_t at = (int64_t)pair * a.Fp + f;
+  const int64_t at = (int64_t)pair * a.Fp + h_place<WT>(f), plane = (int64_t)a.T * a.K * a.Fp;
   if constexpr (WT == kF32) {
     ((float*)a.h)[at] = h;
   } else {
-    const uint32_t hi = pack_bf2(h, 0.0f) & 0xffffu;
-    const float rest = h - bf2f(hi);  // (an infinite h leaves NaN: nothing)
-    ((uint16_t*)a.h)[at] = (uint16_t)hi;
-    ((uint16_t*)a.h)[(int64_t)a.T * a.K * a.Fp + at] = rest == rest ? (uint16_t)pack_bf2(rest, 0.0f) : (uint16_t)0;
+    float left = h;
+    for (int p = 0; p < a.planes; ++p) {
+      const uint32_t b = pack_bf2(left, 0.0f) & 0xffffu;
+      ((uint16_t*)a.h)[p * plane + at] = (uint16_t)b;
+      left -= bf2f(b);
+      if (!(fabsf(left) < INFINITY)) left = 0.0f;  // an infinite h leaves NaN: nothing
+    }
   }
 }
 
@@ -357,6 +443,7 @@ template <int WT, bool VEC>
 __global__ __launch_bounds__(kFewThreads) void few_up_kernel(FewArgs a) {
   __shared__ Groups G;
   __shared__ float partial[kUpSlots][16];  // [unit][part][pair][row]
+  __shared__ __attribute__((aligned(16))) char stage[WT == kFp4 ? kUpStage : 16];
   group_pairs<kFewThreads>(a, G);
   using C = Chunk<WT>;
   const int lane = lane_id(), g = lane >> 4, r = lane & 15;
@@ -369,6 +456,24 @@ __global__ __launch_bounds__(kFewThreads) void few_up_kernel(FewArgs a) {
   const int n = (int)(units * (blockIdx.x + 1) / gridDim.x - u0);
   if (n == 0) return;
   const int nc = (a.d + C::K - 1) / C::K;
+  // In 4 bits the tokens of this workgroup's matrices are staged where they fit:
+  // from memory they take four times as many loads as the weights (24 tokens:
+  // 68 -> 57 us; with 16-bit weights, where they take as many, the wait for the
+  // staging costs more than it saves, 298 -> 352).
+  const int m0 = (int)(u0 / tiles), m1 = (int)((u0 + n - 1) / tiles);
+  const int q0 = G.begin_used[m0], staged_pairs = G.begin_used[m1 + 1] - q0;
+  const int stride = nc * C::K * C::ES + 16;  // rows 4 banks apart
+  const bool staged = WT == kFp4 && staged_pairs * (int64_t)stride <= kUpStage;
+  const uint32_t stage0 = (uint32_t)(uintptr_t)stage;
+  if (staged) {
+    const int per_row = nc * C::K * C::ES / 16, have = a.d * C::ES / 16;  // 16-byte pieces, and those before the end
+    for (int o = threadIdx.x; o < staged_pairs * per_row; o += kFewThreads) {
+      const int q = o / per_row, j = o % per_row;
+      const char* from = (const char*)a.x + (int64_t)(G.list[q0 + q] / a.K) * a.ld * C::ES;
+      *(uint4*)(stage + q * stride + 16 * j) = j < have ? ((const uint4*)from)[j] : uint4{0, 0, 0, 0};
+    }
+    __syncthreads();
+  }
   const int parts = G.most <= 16 ? parts_for(n, nc, n * 16, kUpSlots) : 1;
   for (int i = wave; i < n * parts; i += kFewWaves) {
     const int unit = i / parts, part = i % parts;
@@ -393,21 +498,8 @@ __global__ __launch_bounds__(kFewThreads) void few_up_kernel(FewArgs a) {
         else if (g < 2) put_h<WT>(a, G.list[q], f0 + 4 * g + e, v, up);
       }
     };
-    for (int at = first; at < end; at += 16 * kGroups<WT>) {
-      f32x4 sums[4];
-      if (end - at <= 16) {
-        up_groups<WT, VEC, 1>(a, G, at, end, rp, sp, k0, k1, sums);
-        done(sums[0], at);
-      } else if (kGroups<WT> == 2 || end - at <= 32) {
-        up_groups<WT, VEC, 2>(a, G, at, end, rp, sp, k0, k1, sums);
-#pragma unroll
-        for (int k = 0; k < 2; ++k) done(sums[k], at + 16 * k);
-      } else {
-        up_groups<WT, VEC, kGroups<WT>>(a, G, at, end, rp, sp, k0, k1, sums);
-#pragma unroll
-        for (int k = 0; k < kGroups<WT>; ++k) done(sums[k], at + 16 * k);
-      }
-    }
+    if (WT == kFp4 && staged) up_unit<WT, VEC, WT == kFp4>(a, G, stage0, stride, q0, first, end, rp, sp, k0, k1, done);
+    else up_unit<WT, VEC, false>(a, G, 0, 0, 0, first, end, rp, sp, k0, k1, done);
   }
   if (parts > 1) {
     __syncthreads();
@@ -435,27 +527,28 @@ __global__ __launch_bounds__(kFewThreads) void few_up_kernel(FewArgs a) {
 
 // ---------------------------------------------------------------------------
 // down and the sum over a token's experts. The 16 rows of an instruction are 8
-// output columns at two chunks of the k axis. Its 16 columns are 4 pairs at
-// the same two, both planes of each (fp32: 8 pairs): of its products one row
-// half by one column half each is wanted.
+// output columns at two chunks of the k axis. Its 16 columns are the same two
+// chunks of PL planes of 8 / PL pairs (fp32 one plane; bf16 two, or for an fp32
+// output three and an empty one): of its products one row half by one column
+// half each is wanted.
 // ---------------------------------------------------------------------------
-template <int WT, bool VEC, int NG>
+template <int WT, bool VEC, int PL, int NG>
 __device__ __forceinline__ void down_groups(const FewArgs& a, const Groups& G, int first, int end, const char* row,
                                             const uint8_t* scales, int c0, int c1, float* yp) {
   using C = Chunk<WT>;
-  constexpr int P = WT == kF32 ? 8 : 4;  // pairs of a group
+  constexpr int P = 8 / PL;  // pairs of a group
   const int lane = lane_id(), g = lane >> 4, r = lane & 15;
-  const int64_t plane = WT != kF32 && (r & 4) ? (int64_t)a.T * a.K * a.Fp * C::ES : 0;
-  const char* tok[NG];
-  bool there[NG];
+  const int plane = (r & 7) / P;
+  const uint32_t plane_bytes = (uint32_t)(a.T * a.K * a.Fp * C::ES);
+  uint32_t tok[NG];
 #pragma unroll
   for (int i = 0; i < NG; ++i) {
     const int q = first + P * i + (r & (P - 1));
-    there[i] = q < end;
-    tok[i] = a.h + (there[i] ? (int64_t)G.list[q] * a.Fp * C::ES + plane : 0);
+    tok[i] = q < end && plane < 3 ? (uint32_t)(G.list[q] * a.Fp * C::ES) + plane * plane_bytes : kOutside;
   }
+  const Tokens h = tokens_at(a.h, plane_bytes * (WT == kF32 ? 1 : a.planes));
   f32x4 acc[NG];
-  stream_rows<WT, VEC, true, NG, kAhead<WT, NG>, 2>(row, scales, a.F, tok, there, a.Fp, c0, c1, r >> 3, g, acc);
+  stream_rows<WT, VEC, true, false, true, NG, kAheadDown<WT, NG>, 2>(row, scales, a.F, h, tok, a.Fp, c0, c1, r >> 3, g, acc);
 #pragma unroll
   for (int i = 0; i < NG; ++i)
 #pragma unroll
@@ -463,13 +556,14 @@ __device__ __forceinline__ void down_groups(const FewArgs& a, const Groups& G, i
       // row 4 g + e and column r of the even chunks, row + 8 and column + 8 of the odd
       float v = acc[i][e];
       v += __shfl(v, (lane + 40) & 63, 64);
-      if constexpr (WT != kF32) v += __shfl(v, (lane + 4) & 63, 64);  // the second plane
+      if constexpr (PL >= 2) v += __shfl(v, (lane + 4) & 63, 64);  // the other planes
+      if constexpr (PL == 4) v += __shfl(v, (lane + 2) & 63, 64);
       const int q = first + P * i + r;
       if (r < P && g < 2 && q < end) yp[q * 8 + 4 * g + e] = v;
     }
 }
 
-template <int WT, bool VEC, int CAP>
+template <int WT, bool VEC, int PL, int CAP>
 __global__ __launch_bounds__(kFewThreads) void few_down_kernel(FewArgs a) {
   __shared__ Groups G;
   __shared__ float yp[CAP * 8];  // [tile][part][place][8]
@@ -478,7 +572,7 @@ __global__ __launch_bounds__(kFewThreads) void few_down_kernel(FewArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n_used = G.n_used, count = G.begin_used[n_used];
   using C = Chunk<WT>;
-  constexpr int P = WT == kF32 ? 8 : 4;
+  constexpr int P = 8 / PL;
   const int r = lane & 15, nc = (a.F + 2 * C::K - 1) / (2 * C::K);  // pairs of chunks
   // this workgroup's tiles of a.width columns, as many at a time as their
   // sums have room
@@ -498,9 +592,9 @@ __global__ __launch_bounds__(kFewThreads) void few_down_kernel(FewArgs a) {
       const int k0 = nc * part / parts * 2, k1 = nc * (part + 1) / parts * 2;
       float* to = yp + (size_t)(tile * parts + part) * count * 8;
       for (int at = first; at < end; at += kGroups<WT> * P) {
-        if (end - at <= P) down_groups<WT, VEC, 1>(a, G, at, end, rp, sp, k0, k1, to);
-        else if (kGroups<WT> == 2 || end - at <= 2 * P) down_groups<WT, VEC, 2>(a, G, at, end, rp, sp, k0, k1, to);
-        else down_groups<WT, VEC, kGroups<WT>>(a, G, at, end, rp, sp, k0, k1, to);
+        if (end - at <= P) down_groups<WT, VEC, PL, 1>(a, G, at, end, rp, sp, k0, k1, to);
+        else if (kGroups<WT> == 2 || end - at <= 2 * P) down_groups<WT, VEC, PL, 2>(a, G, at, end, rp, sp, k0, k1, to);
+        else down_groups<WT, VEC, PL, kGroups<WT>>(a, G, at, end, rp, sp, k0, k1, to);
       }
     }
     __syncthreads();
@@ -535,8 +629,18 @@ void launch_few(FewArgs a, hipStream_t st) {
   a.tiles = (share + 7) / 8;
   a.width = (share + a.tiles - 1) / a.tiles;
   const dim3 grid((a.d + a.tiles * a.width - 1) / (a.tiles * a.width));
-  if (pairs <= 512) hipLaunchKernelGGL((few_down_kernel<WT, DOWN_VEC, 512>), grid, dim3(kFewThreads), 0, st, a);
-  else hipLaunchKernelGGL((few_down_kernel<WT, DOWN_VEC, 2048>), grid, dim3(kFewThreads), 0, st, a);
+#define DOWN(PL, CAP) hipLaunchKernelGGL((few_down_kernel<WT, DOWN_VEC, PL, CAP>), grid, dim3(kFewThreads), 0, st, a)
+  if constexpr (WT == kF32) {
+    if (pairs <= 512) DOWN(1, 512);
+    else DOWN(1, 2048);
+  } else if (a.planes == 2) {
+    if (pairs <= 512) DOWN(2, 512);
+    else DOWN(2, 2048);
+  } else {
+    if (pairs <= 512) DOWN(4, 512);
+    else DOWN(4, 2048);
+  }
+#undef DOWN
 }
 
 }  // namespace
@@ -566,6 +670,8 @@ static int few_check(const char* name, const FewArgs& a, int64_t T, int64_t x_by
   REQUIRE(a.d >= 1 && a.F >= 1 && 2 * (int64_t)a.d * a.F < (int64_t)1 << 31, "%s: d=%d, F=%d: 2 d F outside [1, 2^31)",
           name, a.d, a.F);
   REQUIRE(a.ld >= a.d && a.ld <= (int64_t)1 << 40, "%s: ld=%lld below d or above 2^40", name, (long long)a.ld);
+  if ((T * a.ld + a.d) * 4 >= kOutside || T * a.K * few_row(a.F) * 8 >= kOutside)
+    return set_error(FOREMOE_EUNSUPPORTED, "%s: x, or the hidden rows, past 3.7 GB", name);
   if (T == 0) return FOREMOE_OK;
   REQUIRE(a.x && a.ids && a.gates && a.gu && a.dn && a.y && ws, "%s: NULL pointer", name);
   REQUIRE(!misaligned(a.x, x_bytes) && !misaligned(a.ids, 4) && !misaligned(a.gates, 4) && !misaligned(a.widx, 4) &&
@@ -581,7 +687,7 @@ extern "C" {
 
 size_t foremoe_few_workspace_size(int64_t T, int32_t K, int32_t F) {
   if (T < 0 || T > FOREMOE_FEW_TOKENS || K < 1 || K > FOREMOE_MAX_TOPK || T * K > FOREMOE_FEW_PAIRS || F < 1) return 0;
-  const size_t n = (size_t)(T * K) * (size_t)few_row(F) * 4;
+  const size_t n = (size_t)(T * K) * (size_t)few_row(F) * 6;  // three bf16 planes, or fp32
   return n < 256 ? 256 : n;
 }
 
@@ -593,7 +699,7 @@ int foremoe_few_tokens_ffn(const void* x, foremoe_dtype dtype, int64_t ld, int64
   FewArgs a{};
   a.x = x, a.ld = ld, a.T = (int)T, a.K = K, a.E = E, a.W = W, a.d = d, a.F = F, a.Fp = (int)few_row(F);
   a.ids = ids, a.gates = gates, a.widx = expert_widx, a.gu = (const char*)w_gate_up, a.dn = (const char*)w_down;
-  a.h = (char*)ws, a.y = y, a.y_f32 = out_dtype == FOREMOE_F32;
+  a.h = (char*)ws, a.y = y, a.y_f32 = out_dtype == FOREMOE_F32, a.planes = a.y_f32 ? 3 : 2;
   const int64_t b = dtype == FOREMOE_BF16 ? 2 : 4;
   const int rc = few_check("few_tokens_ffn", a, T, b, out_dtype, ws, ws_bytes);
   if (rc != FOREMOE_OK || T == 0) return rc;
@@ -621,7 +727,7 @@ int foremoe_few_tokens_ffn_mxfp4(const void* x, int64_t ld, int64_t T, int32_t d
   a.x = x, a.ld = ld, a.T = (int)T, a.K = K, a.E = E, a.W = W, a.d = d, a.F = F, a.Fp = (int)few_row(F);
   a.ids = ids, a.gates = gates, a.widx = expert_widx, a.gu = (const char*)gate_up_codes, a.dn = (const char*)down_codes;
   a.gu_scales = gate_up_scales, a.dn_scales = down_scales;
-  a.h = (char*)ws, a.y = y, a.y_f32 = out_dtype == FOREMOE_F32;
+  a.h = (char*)ws, a.y = y, a.y_f32 = out_dtype == FOREMOE_F32, a.planes = a.y_f32 ? 3 : 2;
   const int rc = few_check("few_tokens_ffn_mxfp4", a, T, 2, out_dtype, ws, ws_bytes);
   if (rc != FOREMOE_OK) return rc;
   if (d % kMxBlock || F % kMxBlock)

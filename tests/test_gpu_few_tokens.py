@@ -2,9 +2,9 @@
 
 Tolerances: a sum of n products in fp32 is within n u of the sum of their
 magnitudes (u = 2^-24), whatever its order; bf16 weights and values of 4-bit
-ones are exact factors. The hidden rows are kept in fp32, or as two bf16 each
-(the second a rounding, half a step of 2^-8, of what the first's left, which is
-2^-8 of the value): 2^-16. bf16 outputs: half a step of 2^-8.
+ones are exact factors. The hidden rows are kept in fp32, or as two or three
+bf16 each, every one half a step of 2^-8 of what those before leave: 2^-16, and
+2^-24 where the output is fp32. bf16 outputs: half a step of 2^-8.
 """
 import numpy as np
 import pytest
@@ -48,7 +48,7 @@ def _limit(x, ids, gates, gu, dn, widx, ref, out):
             a, u = au[:F], au[F:]
             err = d * U * (np.abs(gu[w]) @ np.abs(x[t]))
             h = R.silu(a) * u
-            eh = 1.1 * err[:F] * (np.abs(u) + err[F:]) + np.abs(a) * err[F:] + (16 * U + 2.0 ** -16) * np.abs(h)
+            eh = 1.1 * err[:F] * (np.abs(u) + err[F:]) + np.abs(a) * err[F:] + (16 * U + (2.0 ** -16 if out == "bf16" else U)) * np.abs(h)
             mag = np.abs(dn[w]) @ (np.abs(h) + eh)
             lim[t] += abs(gates[t, k]) * (np.abs(dn[w]) @ eh + (2 * F + ids.shape[1] + 2) * U * mag)
     if out == "bf16":
