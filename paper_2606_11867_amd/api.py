@@ -570,13 +570,23 @@ def adamw_state_values(m: torch.Tensor, m_scale: torch.Tensor, v: torch.Tensor, 
 # Microscaled 4-bit floats, the expert FFN in them, and the layer for a few
 # tokens (see include/foremoe.h)
 # ---------------------------------------------------------------------------
-def _launch(device: torch.device, call, where: str) -> None:
-    """call() with the device current, as a launch on its stream needs it."""
+def _call(device: torch.device, fn, args: tuple, where: str) -> None:
+    """fn(*args, stream) with the device current, as a launch on its stream needs it."""
     if torch._C._cuda_getDevice() == device.index:
-        check(call(), where)
+        status = fn(*args, torch._C._cuda_getCurrentRawStream(device.index))
     else:
         with torch.cuda.device(device):
-            check(call(), where)
+            status = fn(*args, torch._C._cuda_getCurrentRawStream(device.index))
+    if status:
+        check(status, where)
+
+
+def _at(t: torch.Tensor, n: int, dtype: torch.dtype, name: str, device: torch.device) -> int:
+    """_vec's address; a tensor that is right is found to be so in one line,
+    as half of a small call's time is the host's."""
+    if t.dtype is dtype and t.numel() == n and t.device == device and t.is_cuda and t.is_contiguous():
+        return t.data_ptr()
+    return _vec(t, n, dtype, name, device)
 
 
 class MXFP4(NamedTuple):
@@ -586,30 +596,26 @@ class MXFP4(NamedTuple):
     scales: torch.Tensor
 
 
-def _mx_shape(n: int) -> Tuple[int, int]:
-    blocks = -(-n // _lib.MX_BLOCK)
-    return blocks * (_lib.MX_BLOCK // 2), blocks
+_U8 = torch.uint8
 
 
 def _mx(q: MXFP4, lead: tuple, n: int, name: str, device: torch.device) -> Tuple[int, int]:
     """The addresses of q's codes and scales, q checked to be of [*lead, n]."""
-    out = []
-    for t, cols, part in zip(q, _mx_shape(n), ("codes", "scales")):
-        if t.dtype != torch.uint8:
-            raise TypeError(f"{name}.{part} must be uint8")
-        if t.shape != (*lead, cols):
-            raise ValueError(f"{name}.{part}: {tuple(t.shape)}, {(*lead, cols)} expected")
-        if t.device != device:
-            raise ValueError(f"{name}.{part} is on {t.device}, not {device}")
-        out.append(_ptr(t))
-    return out[0], out[1]
+    codes, scales = q
+    blocks = -(-n // _lib.MX_BLOCK)
+    for t, shape, part in ((codes, (*lead, 16 * blocks), "codes"), (scales, (*lead, blocks), "scales")):
+        if t.shape != shape:
+            raise ValueError(f"{name}.{part}: {tuple(t.shape)}, {shape} expected")
+    return (_at(codes, codes.numel(), _U8, f"{name}.codes", device),
+            _at(scales, scales.numel(), _U8, f"{name}.scales", device))
 
 
 def _as_rows(t: torch.Tensor, name: str):
     """(rows, columns, elements between rows) of [..., columns]: a matrix whose
     rows may be apart, or a contiguous tensor."""
     if t.dim() == 2:
-        return t.shape[0], t.shape[1], _rows(t, name)
+        rows, cols = t.shape
+        return rows, cols, _rows(t, name)
     if t.dim() < 1:
         raise ValueError(f"{name}: expected [..., columns]")
     if not t.is_cuda or not t.is_contiguous():
@@ -625,15 +631,14 @@ def mxfp4_quantize(x: torch.Tensor, *, n_rows: Optional[torch.Tensor] = None, ou
     rows, cols, ld = _as_rows(x, "x")
     dev = x.device
     if out is None:
-        c, b = _mx_shape(cols)
-        out = MXFP4(torch.empty(*x.shape[:-1], c, dtype=torch.uint8, device=dev),
-                    torch.empty(*x.shape[:-1], b, dtype=torch.uint8, device=dev))
+        lead, blocks = x.shape[:-1], -(-cols // _lib.MX_BLOCK)
+        out = MXFP4(torch.empty(*lead, 16 * blocks, dtype=_U8, device=dev), torch.empty(*lead, blocks, dtype=_U8, device=dev))
         codes, scales = out.codes.data_ptr(), out.scales.data_ptr()
     else:
         codes, scales = _mx(out, tuple(x.shape[:-1]), cols, "out", dev)
-    n = _vec(n_rows, 1, torch.int32, "n_rows", dev)
-    _launch(dev, lambda: _lib.load().foremoe_mxfp4_quantize(x.data_ptr(), _dt(x), ld, rows, cols, n, codes, scales,
-                                                            _stream(dev)), "foremoe_mxfp4_quantize")
+    n = None if n_rows is None else _at(n_rows, 1, torch.int32, "n_rows", dev)
+    _call(dev, _lib.load().foremoe_mxfp4_quantize, (x.data_ptr(), _dt(x), ld, rows, cols, n, codes, scales),
+          "foremoe_mxfp4_quantize")
     return out
 
 
@@ -650,8 +655,8 @@ def mxfp4_values(q: MXFP4, n: Optional[int] = None, *, dtype: torch.dtype = torc
         raise ValueError("out must be [..., n] beside q")
     codes, scales = _mx(q, lead, n, "q", dev)
     rows, _, ld = _as_rows(out, "out")
-    _launch(dev, lambda: _lib.load().foremoe_mxfp4_values(codes, scales, rows, n, out.data_ptr(), _dt(out), ld,
-                                                          _stream(dev)), "foremoe_mxfp4_values")
+    _call(dev, _lib.load().foremoe_mxfp4_values, (codes, scales, rows, n, out.data_ptr(), _dt(out), ld),
+          "foremoe_mxfp4_values")
     return out
 
 
@@ -667,24 +672,24 @@ def grouped_ffn_mxfp4_fwd(x_perm: MXFP4, slot_offset: torch.Tensor, slot_widx: t
                           w_down: MXFP4, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
     """grouped_ffn_fwd's y_perm (bf16) with operands in 4 bits: gathered rows
     [n_cap, d] and weights [W, 2F, d], [W, d, F], each from mxfp4_quantize; the
-    hidden rows are quantised on the way. ws: from ffn_mxfp4_workspace (one is
-    made when missing)."""
+    hidden rows are quantised on the way. Rows outside every slot are not
+    written. ws: from ffn_mxfp4_workspace (one is made when missing)."""
     dev = x_perm.codes.device
     if x_perm.codes.dim() != 2 or w_gate_up.codes.dim() != 3 or w_down.codes.dim() != 3:
         raise ValueError("x_perm [n_cap, d], w_gate_up [W, 2F, d] and w_down [W, d, F] expected")
-    n_cap, W = x_perm.codes.shape[0], w_gate_up.codes.shape[0]
-    d, F = x_perm.scales.shape[1] * _lib.MX_BLOCK, w_gate_up.codes.shape[1] // 2
-    S = slot_widx.shape[0]
+    n_cap = x_perm.codes.shape[0]
+    W, F2, _ = w_gate_up.codes.shape
+    d, F, S = x_perm.scales.shape[1] * _lib.MX_BLOCK, F2 // 2, slot_widx.shape[0]
     xc, xs = _mx(x_perm, (n_cap,), d, "x_perm", dev)
     gc, gs = _mx(w_gate_up, (W, 2 * F), d, "w_gate_up", dev)
     dc, ds = _mx(w_down, (W, d), F, "w_down", dev)
     y = torch.empty(n_cap, d, dtype=torch.bfloat16, device=dev)
     if ws is None and n_cap and F % 128 == 0:
         ws = ffn_mxfp4_workspace(n_cap, F, dev)
-    _launch(dev, lambda: _lib.load().foremoe_grouped_ffn_mxfp4_fwd(
-        xc, xs, d, F, S, _vec(slot_offset, S + 1, torch.int32, "slot_offset", dev),
-        _vec(slot_widx, S, torch.int32, "slot_widx", dev), W, gc, gs, dc, ds, n_cap, y.data_ptr(), *_ws(ws, dev),
-        _stream(dev)), "foremoe_grouped_ffn_mxfp4_fwd")
+    _call(dev, _lib.load().foremoe_grouped_ffn_mxfp4_fwd,
+          (xc, xs, d, F, S, _at(slot_offset, S + 1, torch.int32, "slot_offset", dev),
+           _at(slot_widx, S, torch.int32, "slot_widx", dev), W, gc, gs, dc, ds, n_cap, y.data_ptr(), *_ws(ws, dev)),
+          "foremoe_grouped_ffn_mxfp4_fwd")
     return y
 
 
@@ -709,38 +714,39 @@ def few_tokens_ffn(x: torch.Tensor, ids: torch.Tensor, gates: torch.Tensor,
     x's. ws: from few_tokens_workspace (one is made when missing)."""
     ld = _rows(x, "x")
     T, d = x.shape
-    dev = x.device
+    dev, dtype = x.device, x.dtype
     if ids.dim() != 2 or ids.shape[0] != T:
         raise ValueError("ids must be [T, K]")
     K = ids.shape[1]
     mx = isinstance(w_gate_up, MXFP4)
     if mx != isinstance(w_down, MXFP4):
         raise TypeError("w_gate_up and w_down: both in 4 bits or neither")
-    gu = w_gate_up.codes if mx else w_gate_up
-    if gu.dim() != 3:
+    shape = (w_gate_up.codes if mx else w_gate_up).shape
+    if len(shape) != 3:
         raise ValueError("w_gate_up must be [W, 2F, d]")
-    W, F = gu.shape[0], gu.shape[1] // 2
+    W, F = shape[0], shape[1] // 2
+    lib = _lib.load()
     if mx:
-        if x.dtype != torch.bfloat16:
+        if dtype is not torch.bfloat16:
             raise TypeError("weights in 4 bits go with bf16 x")
         weights = (*_mx(w_gate_up, (W, 2 * F), d, "w_gate_up", dev), *_mx(w_down, (W, d), F, "w_down", dev))
+        fn, name, head = lib.foremoe_few_tokens_ffn_mxfp4, "foremoe_few_tokens_ffn_mxfp4", (x.data_ptr(), ld)
     else:
-        for t, shape, name in ((w_gate_up, (W, 2 * F, d), "w_gate_up"), (w_down, (W, d, F), "w_down")):
-            if t.shape != shape:
-                raise ValueError(f"{name}: {tuple(t.shape)}, {shape} expected")
-        weights = tuple(_vec(t, t.numel(), x.dtype, name, dev)
-                        for t, name in ((w_gate_up, "w_gate_up"), (w_down, "w_down")))
-    E = W if expert_widx is None else expert_widx.numel()
-    out_dtype = x.dtype if out_dtype is None else out_dtype
-    y = torch.empty(T, d, dtype=out_dtype, device=dev)
+        if shape != (W, 2 * F, d):
+            raise ValueError(f"w_gate_up: {tuple(shape)}, {(W, 2 * F, d)} expected")
+        if w_down.shape != (W, d, F):
+            raise ValueError(f"w_down: {tuple(w_down.shape)}, {(W, d, F)} expected")
+        weights = (_at(w_gate_up, W * 2 * F * d, dtype, "w_gate_up", dev), _at(w_down, W * d * F, dtype, "w_down", dev))
+        fn, name, head = lib.foremoe_few_tokens_ffn, "foremoe_few_tokens_ffn", (x.data_ptr(), _dt(x), ld)
+    E, widx = W, None
+    if expert_widx is not None:
+        E = expert_widx.numel()
+        widx = _at(expert_widx, E, torch.int32, "expert_widx", dev)
+    y = torch.empty(T, d, dtype=dtype if out_dtype is None else out_dtype, device=dev)
     if ws is None:
         ws = few_tokens_workspace(T, K, d, F, dev)
-    head = (x.data_ptr(),) + (() if mx else (_dt(x),)) + (ld, T, d, F)
-    args = (*head, _vec(ids, T * K, torch.int32, "ids", dev), _vec(gates, T * K, torch.float32, "gates", dev), K, E,
-            _vec(expert_widx, E, torch.int32, "expert_widx", dev), W, *weights, y.data_ptr(), _dt(y), *_ws(ws, dev),
-            _stream(dev))
-    name = "foremoe_few_tokens_ffn_mxfp4" if mx else "foremoe_few_tokens_ffn"
-    _launch(dev, lambda: getattr(_lib.load(), name)(*args), name)
+    _call(dev, fn, (*head, T, d, F, _at(ids, T * K, torch.int32, "ids", dev), _at(gates, T * K, torch.float32, "gates", dev),
+                    K, E, widx, W, *weights, y.data_ptr(), _dt(y), *_ws(ws, dev)), name)
     return y
 
 

@@ -13,7 +13,7 @@ from typing import List, Optional, Sequence, Tuple, Union
 import torch
 
 from . import _lib
-from .api import _dt, _launch, _stream, _vec
+from .api import _call, _dt, _stream, _vec
 
 F32 = torch.float32
 
@@ -313,7 +313,7 @@ class Muon:
             self._fill()
         coef = (ctypes.c_double * 3)(*self.coefficients)
         scale = _vec(grad_scale, 1, F32, "grad_scale", self.device)
-        _launch(self.device, lambda: self.lib.foremoe_muon_step(
+        _call(self.device, self.lib.foremoe_muon_step, (
             self._records, len(self._params), self._pdt, self._gdt, self.lr, self.momentum, self.nesterov, self.steps,
-            coef, self.eps, scale, self.zero_grads, self.ws.data_ptr(), self.ws.numel() * self.ws.element_size(),
-            _stream(self.device)), "foremoe_muon_step")
+            coef, self.eps, scale, self.zero_grads, self.ws.data_ptr(), self.ws.numel() * self.ws.element_size()),
+            "foremoe_muon_step")
