@@ -22,8 +22,12 @@
 namespace foremoe {
 namespace {
 
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
 constexpr int kMuonBK = 64;
-constexpr int kMomentThreads = 256, kMomentChunk = 16384;  // elements of a matrix per workgroup
+// Elements of a matrix to a workgroup of the momentum pass: 4096, more where
+// that would leave over 1024 sums to add up.
+constexpr int kMomentThreads = 256, kMomentChunk = 4096, kMomentMost = 1024;
 constexpr float kHeld = 256.0f, kRest = 1024.0f;
 
 struct MuonRec {
@@ -35,6 +39,7 @@ struct MuonRec {
   int32_t rows, cols;
   int32_t mm, nn;          // padded sides, mm the smaller one's
   uint32_t chunks;         // of a matrix, in the momentum pass
+  int32_t chunk;           // elements of one
   float decay, move;       // 1 - lr weight_decay, lr scale
   int32_t wide;              // the tensors' rows start on 16 bytes: read and written so
   union {
@@ -147,7 +152,7 @@ __global__ __launch_bounds__(kMomentThreads) void muon_moment_kernel(MuonArgs a)
   const uint32_t b = blockIdx.x - a.first.at[ri];
   const int64_t matrix = b / r.chunks, chunk = b % r.chunks;
   const int64_t n = (int64_t)r.rows * r.cols, base = matrix * n;
-  const int64_t lo = chunk * kMomentChunk, hi = lo + kMomentChunk < n ? lo + kMomentChunk : n;
+  const int64_t lo = chunk * r.chunk, hi = lo + r.chunk < n ? lo + r.chunk : n;
   const float gs = a.grad_scale ? *a.grad_scale : 1.0f;
   const bool wide = r.wide;
   double s = 0;
@@ -250,19 +255,20 @@ enum Product { kGram = 0, kPoly = 1, kApply = 2, kUpdate = 3 };
 // place(k, i, left) gives the element and how many of its row are left there
 // (none: not a place), x(k, v) the values of 2^8 X. All reads come first, as
 // the compiler cannot move one past a store.
-template <bool PBF16, int N, class Place, class X>
-__device__ __forceinline__ void update_n(const MuonRec& r, Place place, X x) {
-  float p[N][4];
-  const bool wide = r.wide;
+template <bool PBF16, int N, class Place>
+__device__ __forceinline__ void update_read(const MuonRec& r, Place place, float (*p)[4]) {
 #pragma unroll
   for (int k = 0; k < N; ++k) {
     int64_t i;
     int left;
     place(k, i, left);
     if (left <= 0) continue;
-    if (PBF16 && !r.master) get4<true>(r.param, i, left, wide, p[k]);
-    else get4<false>(PBF16 ? r.master : r.param, i, left, wide, p[k]);
+    if (PBF16 && !r.master) get4<true>(r.param, i, left, r.wide, p[k]);
+    else get4<false>(PBF16 ? r.master : r.param, i, left, r.wide, p[k]);
   }
+}
+template <bool PBF16, int N, class Place, class X>
+__device__ __forceinline__ void update_write(const MuonRec& r, Place place, X x, float (*p)[4]) {
 #pragma unroll
   for (int k = 0; k < N; ++k) {
     int64_t i;
@@ -273,9 +279,15 @@ __device__ __forceinline__ void update_n(const MuonRec& r, Place place, X x) {
     x(k, v);
 #pragma unroll
     for (int e = 0; e < 4; ++e) p[k][e] = fmaf(-r.move, v[e] * (1.0f / kHeld), p[k][e] * r.decay);
-    if (r.master) put4<false>(r.master, i, left, wide, p[k]);
-    put4<PBF16>(r.param, i, left, wide, p[k]);
+    if (r.master) put4<false>(r.master, i, left, r.wide, p[k]);
+    put4<PBF16>(r.param, i, left, r.wide, p[k]);
   }
+}
+template <bool PBF16, int N, class Place, class X>
+__device__ __forceinline__ void update_n(const MuonRec& r, Place place, X x) {
+  float p[N][4];
+  update_read<PBF16, N>(r, place, p);
+  update_write<PBF16, N>(r, place, x, p);
 }
 
 // One T x T tile of one matrix's product, by wavefronts of 64 x 64 (T = 128) or
@@ -374,6 +386,7 @@ __global__ __launch_bounds__(T * 2) void muon_product_kernel(MuonArgs a) {
 
   float(*sum)[LD] = (float(*)[LD])lds;
   const bool tall = r.rows > r.cols;
+  const int64_t base = matrix * (int64_t)r.rows * r.cols;
   static_for<0, T / H>([&](auto partc) {
     constexpr int part = decltype(partc)::value;
     __syncthreads();  // every wavefront has read its last fragments, or the sums before
@@ -391,9 +404,19 @@ __global__ __launch_bounds__(T * 2) void muon_product_kernel(MuonArgs a) {
                 float4{v[0], v[1], v[2], v[3]};
           }
     }
+    const int ih = i0 + part * H;  // their first row
+    // kUpdate: H rows of X by T columns are so many of the parameters, or T
+    // rows by H columns; of a small tile they are read here already
+    const int r0 = tall ? j0 : ih, c0 = tall ? ih : j0;
+    const int pi = tall ? tid / 16 : tid / (T / 4), pk = tall ? NT / 16 : 8, pj = (tall ? tid % 16 : tid % (T / 4)) * 4;
+    auto place = [&](int k, int64_t& o, int& left) {
+      const int row = r0 + pi + pk * k;
+      o = base + (int64_t)row * r.cols + c0 + pj, left = row < r.rows ? r.cols - (c0 + pj) : 0;
+    };
+    float param[P == kUpdate ? 8 : 1][4];
+    if constexpr (P == kUpdate && T == 128) update_read<PBF16, 8>(r, place, param);
     __syncthreads();
     if constexpr (part + 1 < T / H) fetch(part + 1);
-    const int ih = i0 + part * H;  // their first row
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const int i = k * 16 + ei, j = ej;
@@ -445,21 +468,15 @@ __global__ __launch_bounds__(T * 2) void muon_product_kernel(MuonArgs a) {
           *(uint4*)((P == kGram ? G : Q) + (int64_t)(j0 + j) * r.mm + ih + i) = uint4{w[0], w[1], w[2], w[3]};
         }
       } else {
-        // H rows of X by T columns: of the parameters too, or T rows by H columns
-        const int r0 = tall ? j0 : ih, c0 = tall ? ih : j0;
-        const int pi = tall ? tid / 16 : tid / (T / 4), pk = tall ? NT / 16 : 8, pj = (tall ? tid % 16 : tid % (T / 4)) * 4;
-        const int64_t base = matrix * (int64_t)r.rows * r.cols;
-        update_n<PBF16, 8>(
-            r,
-            [&](int k, int64_t& o, int& left) {
-              const int row = r0 + pi + pk * k;
-              o = base + (int64_t)row * r.cols + c0 + pj, left = row < r.rows ? r.cols - (c0 + pj) : 0;
-            },
+        if constexpr (T != 128) update_read<PBF16, 8>(r, place, param);
+        update_write<PBF16, 8>(
+            r, place,
             [&](int k, float* v) {
               const int i = pi + pk * k;
 #pragma unroll
               for (int e = 0; e < 4; ++e) v[e] = tall ? sum[pj + e][i] : sum[i][pj + e];
-            });
+            },
+            param);
       }
     }
   });
@@ -579,6 +596,22 @@ __device__ __forceinline__ void small_each(F&& f) {  // f(q, row, column)
     f(q, 32 * (wave >> 1) + 8 * (q / 4) + 4 * (lane >> 5) + q % 4, 32 * (wave & 1) + (lane & 31));
 }
 
+// The same by wavefronts of 16 x 16, for matrices with a side of at most 32.
+__device__ __forceinline__ f32x4 small_product16(const float (*A)[kSmallLD], const float (*B)[kSmallLD], int n) {
+  const int lane = lane64(), wave = wave_id(), l = lane & 15, h = lane >> 4;
+  const int i = 16 * (wave >> 1) + l, j = 16 * (wave & 1) + l;
+  f32x4 acc = {0, 0, 0, 0};
+#pragma unroll 4
+  for (int k = 0; k < n; k += 4) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(A[i][k + h], B[k + h][j], acc, 0, 0, 0);
+  return acc;
+}
+template <class F>
+__device__ __forceinline__ void small_each16(F&& f) {
+  const int lane = lane64(), wave = wave_id();
+#pragma unroll
+  for (int q = 0; q < 4; ++q) f(q, 16 * (wave >> 1) + 4 * (lane >> 4) + q, 16 * (wave & 1) + (lane & 15));
+}
+
 // m, and a chunk's part of u u^T. The sums are of u over a power of two that
 // the chunk's largest element gives, so that no square leaves the range of fp32.
 template <bool GBF16>
@@ -633,12 +666,36 @@ __global__ __launch_bounds__(256) void muon_small_gram_kernel(MuonArgs a) {
   if (threadIdx.x == 0) r.part_e[matrix * r.chunks + chunk] = e;
 }
 
+// All steps of a matrix in LDS. product(A, B) gives this wavefront's part of A
+// B, each(f) its elements.
+template <class Product, class Each>
+__device__ __forceinline__ void small_steps(const MuonArgs& a, float (*G)[kSmallLD], float (*M)[kSmallLD],
+                                            float (*S)[kSmallLD], float (*Q)[kSmallLD], Product product, Each each) {
+  for (int t = 0; t < a.steps; ++t) {
+    const auto s = product(G, G);
+    each([&](int q, int i, int j) { M[i][j] = (i == j ? a.a : 0.0f) + fmaf(a.b, G[i][j], a.c * s[q]); });
+    __syncthreads();
+    const auto nq = product(M, Q);
+    if (t + 1 < a.steps) {
+      const auto mg = product(M, G);
+      each([&](int q, int i, int j) { S[i][j] = mg[q]; });
+    }
+    __syncthreads();
+    each([&](int q, int i, int j) { Q[i][j] = nq[q]; });
+    if (t + 1 < a.steps) {
+      const auto ng = product(S, M);
+      each([&](int q, int i, int j) { G[i][j] = ng[q]; });
+    }
+    __syncthreads();
+  }
+}
+
 // Q and 1 / max(|u|, eps) of a matrix.
 __global__ __launch_bounds__(256) void muon_small_steps_kernel(MuonArgs a) {
   const int ri = find_rec(a, blockIdx.x);
   const MuonRec& r = a.rec[ri];
   const int64_t matrix = blockIdx.x - a.first.at[ri];
-  const int m = r.rows < r.cols ? r.rows : r.cols, n = (m + 1) & ~1, tid = threadIdx.x;
+  const int m = r.rows < r.cols ? r.rows : r.cols, n = (m + 3) & ~3, tid = threadIdx.x;
   __shared__ float G[kSmall][kSmallLD], M[kSmall][kSmallLD], S[kSmall][kSmallLD], Q[kSmall][kSmallLD];
   const float* part = r.part + matrix * r.chunks * (kSmall * kSmall);
   const int32_t* part_e = r.part_e + matrix * r.chunks;
@@ -651,6 +708,8 @@ __global__ __launch_bounds__(256) void muon_small_steps_kernel(MuonArgs a) {
     e = other > e ? other : e;
   }
   const float scale = ldexpf(1.0f, 2 * (mine - e));
+  // this thread's elements: column tid % 64, rows tid / 64 + 4 k
+  const int col = tid & 63;
   float s[16];
 #pragma unroll
   for (int k = 0; k < 16; ++k) s[k] = 0.0f;
@@ -661,7 +720,7 @@ __global__ __launch_bounds__(256) void muon_small_steps_kernel(MuonArgs a) {
     for (int k = 0; k < 16; ++k) s[k] = fmaf(part[c * (kSmall * kSmall) + tid + 256 * k], by, s[k]);
   }
 #pragma unroll
-  for (int k = 0; k < 16; ++k) G[(tid + 256 * k) >> 6][(tid + 256 * k) & 63] = s[k];
+  for (int k = 0; k < 16; ++k) G[(tid >> 6) + 4 * k][col] = s[k];
   __syncthreads();
   // |u|^2 over 2^(2 (e - 127)), summed in the same order by every thread
   double trace = 0;
@@ -672,38 +731,20 @@ __global__ __launch_bounds__(256) void muon_small_steps_kernel(MuonArgs a) {
   const double inv = den == 0 ? 0.0 : 1.0 / den;
   const double by = ldexp(inv, e - 127);
   __syncthreads();
-  for (int i = tid; i < kSmall * kSmall; i += 256) {
-    const int x = i >> 6, y = i & 63;
-    G[x][y] = (float)(G[x][y] * by * by);
-    Q[x][y] = x == y ? 1.0f : 0.0f;
+#pragma unroll
+  for (int k = 0; k < 16; ++k) {
+    const int row = (tid >> 6) + 4 * k;
+    G[row][col] = (float)(s[k] * by * by);
+    Q[row][col] = row == col ? 1.0f : 0.0f;
   }
   __syncthreads();
-  const bool idle = 32 * (wave_id() >> 1) >= m || 32 * (wave_id() & 1) >= m;
-  for (int t = 0; t < a.steps; ++t) {
-    if (!idle) {
-      const f32x16 s = small_product<false>(G, G, n);
-      small_each([&](int q, int i, int j) {
-        M[i][j] = (i == j ? a.a : 0.0f) + fmaf(a.b, G[i][j], a.c * s[q]);
-      });
-    }
-    __syncthreads();
-    f32x16 nq, mg;
-    if (!idle) {
-      nq = small_product<false>(M, Q, n);
-      if (t + 1 < a.steps) {
-        mg = small_product<false>(M, G, n);
-        small_each([&](int q, int i, int j) { S[i][j] = mg[q]; });
-      }
-    }
-    __syncthreads();
-    if (!idle) {
-      small_each([&](int q, int i, int j) { Q[i][j] = nq[q]; });
-      if (t + 1 < a.steps) {
-        mg = small_product<false>(S, M, n);
-        small_each([&](int q, int i, int j) { G[i][j] = mg[q]; });
-      }
-    }
-    __syncthreads();
+  if (m <= 32) {
+    // (elements past the matrix: zeros, but for the diagonal of M and Q)
+    small_steps(
+        a, G, M, S, Q, [&](auto A, auto B) { return small_product16(A, B, n); }, [&](auto f) { small_each16(f); });
+  } else {
+    small_steps(
+        a, G, M, S, Q, [&](auto A, auto B) { return small_product<false>(A, B, n); }, [&](auto f) { small_each(f); });
   }
   for (int i = tid; i < kSmall * kSmall; i += 256) r.q[matrix * (kSmall * kSmall) + i] = Q[i >> 6][i & 63];
   if (tid == 0) r.inverse[matrix] = inv;
@@ -750,7 +791,8 @@ bool is_small(const foremoe_muon_tensor& t) { return t.rows <= kSmall || t.cols 
 size_t lay_out(const foremoe_muon_tensor& t, int tile, size_t at, char* ws, MuonRec* r) {
   const int64_t s = t.rows < t.cols ? t.rows : t.cols, l = t.rows < t.cols ? t.cols : t.rows;
   const int64_t mm = pad_side(s, tile), nn = pad_side(l, tile);
-  const int64_t chunks = (s * l + kMomentChunk - 1) / kMomentChunk;
+  const int64_t even = ((s * l + kMomentMost - 1) / kMomentMost + 1023) / 1024 * 1024;
+  const int64_t chunk = even > kMomentChunk ? even : kMomentChunk, chunks = (s * l + chunk - 1) / chunk;
   auto take = [&](size_t bytes) {
     char* p = ws + at;
     at = align_up(at + bytes, 256);
@@ -776,7 +818,7 @@ size_t lay_out(const foremoe_muon_tensor& t, int tile, size_t at, char* ws, Muon
   q.gram = (uint16_t*)take((size_t)t.batch * mm * mm * 2);
   q.poly = (uint16_t*)take((size_t)t.batch * mm * mm * 2);
   q.squares = (double*)take((size_t)t.batch * chunks * 8);
-  q.mm = (int)mm, q.nn = (int)nn, q.chunks = (uint32_t)chunks;
+  q.mm = (int)mm, q.nn = (int)nn, q.chunks = (uint32_t)chunks, q.chunk = (int32_t)chunk;
   if (r) *r = q;
   return at;
 }
