@@ -139,59 +139,49 @@ struct SlotTile {
   int w;
 };
 
-// Row tiles of the slot that this lane has of those from j0 on, its rows, and
-// the row tiles up to and with it.
-template <int BM>
-__device__ __forceinline__ int slot_tiles_of(const Ffn4Args& a, int j0, int64_t& beg, int64_t& end, int& upto) {
-  const int lane = lane64(), j = j0 + lane;
-  beg = end = 0;
-  if (j < a.S) {
-    beg = a.slot_offset[j], end = a.slot_offset[j + 1];
-    beg = beg < 0 ? 0 : (beg > a.n_cap ? a.n_cap : beg);
-    end = end > a.n_cap ? a.n_cap : end;
-  }
-  const int mine = end > beg ? (int)((end - beg + BM - 1) / BM) : 0;
-  upto = mine;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int v = __shfl_up(upto, o, 64);
-    if (lane >= o) upto += v;
-  }
-  return mine;
+// Inclusive sum over the lanes.
+__device__ __forceinline__ int lanes_up_to(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);  // row_shr:1, 2, 4, 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, true);  // row_bcast:15, 31
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, true);
+  return v;
 }
 
-// The tile of workgroup b, found by every wavefront alone: row tiles are
-// numbered slot by slot, tiles along N within them, and each of the 8 XCDs has
-// an even share of neighbours, which have their rows and weights in its L2
-// once. False where there is none.
+// The tile of workgroup b, found by every wavefront alone, a lane to neighbouring
+// slots: row tiles are numbered slot by slot, tiles along N within them, and each
+// of the 8 XCDs has an even share of neighbours, which have their rows and
+// weights in its L2 once. False where there is none.
 template <int BM>
 __device__ __forceinline__ bool find_tile(const Ffn4Args& a, unsigned b, SlotTile& r, int& nt) {
-  int64_t beg, end;
-  int upto, all = 0;
-  for (int j0 = 0; j0 < a.S; j0 += 64) {
-    slot_tiles_of<BM>(a, j0, beg, end, upto);
-    all += __shfl(upto, 63, 64);
-  }
-  const int64_t tiles = (int64_t)all * a.n_tiles, share = (tiles + 7) / 8, at = b / 8, t = (b % 8) * share + at;
+  const int per = (a.S + 63) / 64, j0 = lane64() * per, n_cap = (int)a.n_cap;
+  int beg, end, w;
+  auto tiles_of = [&](int j) -> int {  // of slot j, with its rows and matrix
+    beg = end = 0, w = -1;
+    if (j < a.S) beg = a.slot_offset[j], end = a.slot_offset[j + 1], w = a.slot_widx[j];
+    beg = min(max(beg, 0), n_cap), end = min(end, n_cap);
+    return end > beg ? (int)(((unsigned)(end - beg) + BM - 1) / BM) : 0;
+  };
+  int mine = 0;
+  for (int i = per - 1; i >= 0; --i) mine += tiles_of(j0 + i);
+  const int upto = lanes_up_to(mine), all = __builtin_amdgcn_readlane(upto, 63);
+  const unsigned tiles = (unsigned)all * a.n_tiles, share = (tiles + 7) / 8, at = b / 8, t = (b % 8) * share + at;
   if (at >= share || t >= tiles) return false;
-  int m = (int)(t / a.n_tiles);
+  const int m = (int)(t / a.n_tiles);
   nt = (int)(t % a.n_tiles);
-  for (int j0 = 0; j0 < a.S; j0 += 64) {
-    const int mine = slot_tiles_of<BM>(a, j0, beg, end, upto);
-    const uint64_t hit = __ballot(upto > m);
-    if (hit) {
-      const int who = __builtin_ctzll(hit);
-      const int before = __shfl(upto - mine, who, 64);
-      const int first = __shfl((int)beg, who, 64), e = __shfl((int)end, who, 64);
-      r.row0 = __builtin_amdgcn_readfirstlane(first + (m - before) * BM);
-      r.end = __builtin_amdgcn_readfirstlane(e);
-      r.w = __builtin_amdgcn_readfirstlane(a.slot_widx[j0 + who]);
-      nt = __builtin_amdgcn_readfirstlane(nt);
-      return true;
-    }
-    m -= __shfl(upto, 63, 64);
+  const int who = __builtin_ctzll(__ballot(upto > m));
+  int first = m - (upto - mine);  // of this lane's slots
+  for (int i = 0, n; i < per; ++i) {
+    n = i == 0 ? (per == 1 ? mine : tiles_of(j0)) : tiles_of(j0 + i);
+    if (first < n) break;
+    first -= n;
   }
-  return false;
+  r.row0 = __builtin_amdgcn_readlane(beg + first * BM, who);
+  r.end = __builtin_amdgcn_readlane(end, who);
+  r.w = __builtin_amdgcn_readlane(w, who);
+  return true;
 }
 
 // One wavefront moves 64 x 4 bytes: lane l's word lands at lds_wave_base + 4 l.
