@@ -131,6 +131,7 @@ struct Ffn4Args {
   const int32_t* slot_offset;
   const int32_t* slot_widx;
   int S, W, n_tiles;   // n_tiles: tiles along N
+  int group;           // row tiles of a slot that are taken together, see find_tile
   int64_t n_cap;
 };
 
@@ -151,9 +152,13 @@ __device__ __forceinline__ int lanes_up_to(int v) {
 }
 
 // The tile of workgroup b, found by every wavefront alone, a lane to neighbouring
-// slots: row tiles are numbered slot by slot, tiles along N within them, and each
-// of the 8 XCDs has an even share of neighbours, which have their rows and
-// weights in its L2 once. False where there is none.
+// slots. Tiles are numbered slot by slot, and each of the 8 XCDs has an even share
+// of neighbours, which have their rows and weights in its L2 once. Within a slot
+// a.group row tiles go along N together: one where a matrix fits an L2 (4 MB)
+// beside the rows, and eight where it does not and its columns would be read
+// again for every row tile (us, one / eight: gate/up 8 x 512 rows, 4096 x 14336,
+// 460 / 357; down of the same 247 / 222; but down 2048 x 768 of 16278 rows
+// 33.6 / 38). False where there is none.
 template <int BM>
 __device__ __forceinline__ bool find_tile(const Ffn4Args& a, unsigned b, SlotTile& r, int& nt) {
   const int per = (a.S + 63) / 64, j0 = lane64() * per, n_cap = (int)a.n_cap;
@@ -170,15 +175,19 @@ __device__ __forceinline__ bool find_tile(const Ffn4Args& a, unsigned b, SlotTil
   const unsigned tiles = (unsigned)all * a.n_tiles, share = (tiles + 7) / 8, at = b / 8, t = (b % 8) * share + at;
   if (at >= share || t >= tiles) return false;
   const int m = (int)(t / a.n_tiles);
-  nt = (int)(t % a.n_tiles);
   const int who = __builtin_ctzll(__ballot(upto > m));
   int first = m - (upto - mine);  // of this lane's slots
-  for (int i = 0, n; i < per; ++i) {
+  int n = 0;  // of the tile's slot
+  for (int i = 0; i < per; ++i) {
     n = i == 0 ? (per == 1 ? mine : tiles_of(j0)) : tiles_of(j0 + i);
     if (first < n) break;
     first -= n;
   }
-  r.row0 = __builtin_amdgcn_readlane(beg + first * BM, who);
+  const int in_slot = __builtin_amdgcn_readlane(first, who), group = in_slot / a.group * a.group;
+  const int high = min(a.group, __builtin_amdgcn_readlane(n, who) - group);
+  const unsigned u = (unsigned)(in_slot - group) * a.n_tiles + t % a.n_tiles;
+  nt = (int)(u / high);
+  r.row0 = __builtin_amdgcn_readlane(beg, who) + (group + (int)(u % high)) * BM;
   r.end = __builtin_amdgcn_readlane(end, who);
   r.w = __builtin_amdgcn_readlane(w, who);
   return true;
@@ -210,7 +219,7 @@ __global__ __launch_bounds__(64 * kMxWaves, 2) void ffn4_kernel(Ffn4Args a) {
   constexpr int PER = AT::PER_WAVE + BT::PER_WAVE;
   // Scales come for four stages at once, 16 bytes of a row, into one buffer
   // that is free again when all have read theirs (a word of a row for every
-  // stage: 8200 x 7168 x 4096 245 us, this 180).
+  // stage: 8200 x 7168 x 4096 245 us, this 200).
   constexpr int SC_LOADS = ROWS / 64, SC_PER = (SC_LOADS + NW - 1) / NW, SCALES = ROWS * 16;
   constexpr int WM = BM / 2, WN = BN / 2, MB = WM / 32, NB = WN / 32;
   constexpr int YLD = BN * 2 + 16;  // bytes of a row of y in LDS
@@ -446,7 +455,7 @@ __global__ __launch_bounds__(64 * kMxWaves, 2) void ffn4_kernel(Ffn4Args a) {
               uint2{pack_bf2(acc[i][j][4 * q], acc[i][j][4 * q + 1]), pack_bf2(acc[i][j][4 * q + 2], acc[i][j][4 * q + 3])};
     __syncthreads();
     // whole lines: 512 bytes of a row by 32 lanes (8 bytes of a row at a time
-    // from the registers: 16278 x 768 x 2048 50 us, this 30)
+    // from the registers: 16278 x 768 x 2048 50 us, this 35)
     constexpr int LANES = BN / 8, AT_ONCE = 64 * NW / LANES;
     const int part = tid % LANES;
     if (n0 + part * 8 < a.N) {
@@ -482,6 +491,7 @@ static void launch_ffn4(Ffn4Args a, hipStream_t st) {
   };
   auto rounded = [](int64_t n) { return dim3((unsigned)((n + 7) / 8 * 8)); };  // one share for each XCD: see find_tile
   int64_t n = grid(kMxM, kMxN);
+  a.group = (int64_t)a.N * a.K / 2 <= 2 << 20 ? 1 : 8;
   if (n > num_cus()) {
     hipLaunchKernelGGL((ffn4_kernel<GATE_UP, kMxM, kMxN, kMxStages>), rounded(n), dim3(64 * kMxWaves), 0, st, a);
   } else {
