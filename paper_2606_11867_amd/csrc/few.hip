@@ -3,11 +3,19 @@
 // into registers as the first operand of the matrix instructions (16 rows of
 // weights by up to 16 tokens); nothing else is worth counting.
 //
-//   gate/up: a workgroup takes 8 hidden columns (8 rows of Wg, 8 of Wu) of one
-//   down: a workgroup takes 8 output columns of every expert, its wavefronts
-//     the experts, or parts of their k axis where experts are few. So it holds
-//     a token's sum over its experts alone: no partial sums in memory, no
-//     counters, a fixed order.
+//   gate/up: a unit is 8 hidden columns (8 rows of Wg, 8 of Wu) of one matrix in
+//     use; a workgroup to a CU takes its even share of all units, a wavefront a
+//     unit or, where they are few, a part of its k axis.
+//   down: a workgroup takes its even share of the output columns, of every
+//     matrix in use, a wavefront up to 8 columns of one, or a part of their k
+//     axis. So it holds a token's sum over its experts alone: no partial sums in
+//     memory, no counters, a fixed order.
+//
+// Bound by memory where many experts are picked: 64 tokens over 32 experts of
+// 7168 x 2048 in bf16, whose weights are 2.8 GB, take 302 and 208 us (6.2 and 4.5
+// TB/s). One token of 8 experts of 2048 x 768 takes 16 and 12 us, of which 12
+// would be its 75 MB: there the latency of a launch, of the ids and of the first
+// weights counts.
 #include <type_traits>
 
 #include "common.h"
@@ -117,7 +125,8 @@ struct Tokens {
   __amdgpu_buffer_rsrc_t buffer;
   const char* base;  // (in LDS where they are staged)
 };
-constexpr uint32_t kOutside = 0xF0000000u;  // more than a buffer has, and room to count up
+constexpr uint32_t kOutside = 0xF0000000u;  // more than a buffer has, and room for a row behind it
+constexpr int kFewSide = 1 << 25;           // longest row: 2^27 bytes
 
 __device__ __forceinline__ Tokens tokens_at(const void* base, uint32_t bytes) {
   return Tokens{__builtin_amdgcn_make_buffer_rsrc((void*)base, 0, bytes, 0x00020000), (const char*)base};
@@ -191,8 +200,8 @@ struct Groups {
 template <int THREADS>
 __device__ __forceinline__ void group_pairs(const FewArgs& a, Groups& G) {
   if (a.T * a.K <= 64) {
-    // one wavefront, a lane to a pair, without a scan over all matrices
-    // (one token of 128 experts: both kernels together 26 -> 21 us)
+    // one wavefront, a lane to a pair, without the tables and the scan over all
+    // matrices that more pairs need
     if (threadIdx.x < 64) {
       const int pairs = a.T * a.K, lane = lane_id();
       int w = lane < pairs ? a.ids[lane] : -1;
@@ -458,7 +467,7 @@ __global__ __launch_bounds__(kFewThreads) void few_up_kernel(FewArgs a) {
   const int nc = (a.d + C::K - 1) / C::K;
   // In 4 bits the tokens of this workgroup's matrices are staged where they fit:
   // from memory they take four times as many loads as the weights (24 tokens:
-  // 68 -> 57 us; with 16-bit weights, where they take as many, the wait for the
+  // 68 -> 57 us, 51 since its loads have no branches; with 16-bit weights, where they take as many, the wait for the
   // staging costs more than it saves, 298 -> 352).
   const int m0 = (int)(u0 / tiles), m1 = (int)((u0 + n - 1) / tiles);
   const int q0 = G.begin_used[m0], staged_pairs = G.begin_used[m1 + 1] - q0;
@@ -670,8 +679,9 @@ static int few_check(const char* name, const FewArgs& a, int64_t T, int64_t x_by
   REQUIRE(a.d >= 1 && a.F >= 1 && 2 * (int64_t)a.d * a.F < (int64_t)1 << 31, "%s: d=%d, F=%d: 2 d F outside [1, 2^31)",
           name, a.d, a.F);
   REQUIRE(a.ld >= a.d && a.ld <= (int64_t)1 << 40, "%s: ld=%lld below d or above 2^40", name, (long long)a.ld);
-  if ((T * a.ld + a.d) * 4 >= kOutside || T * a.K * few_row(a.F) * 8 >= kOutside)
-    return set_error(FOREMOE_EUNSUPPORTED, "%s: x, or the hidden rows, past 3.7 GB", name);
+  if (a.d >= kFewSide || a.F >= kFewSide || (T * a.ld + a.d) * 4 >= kOutside || T * a.K * few_row(a.F) * 8 >= kOutside)
+    return set_error(FOREMOE_EUNSUPPORTED, "%s: d=%d or F=%d not below 2^25, or x or the hidden rows past 3.7 GB", name, a.d,
+                     a.F);
   if (T == 0) return FOREMOE_OK;
   REQUIRE(a.x && a.ids && a.gates && a.gu && a.dn && a.y && ws, "%s: NULL pointer", name);
   REQUIRE(!misaligned(a.x, x_bytes) && !misaligned(a.ids, 4) && !misaligned(a.gates, 4) && !misaligned(a.widx, 4) &&

@@ -95,6 +95,8 @@ SIZES = {
     "crowded": dict(T=128, d=160, F=64, E=3, W=3, K=2, widx=False),  # more than 64 tokens an expert
     "wide": dict(T=3, d=1056, F=1120, E=5, W=5, K=5),
     "pairs": dict(T=128, d=64, F=32, E=40, W=40, K=16),  # 2048 pairs
+    "long-rows": dict(T=12, d=8192, F=64, E=3, W=3, K=2),  # past what the LDS holds
+    "long-and-crowded": dict(T=40, d=2048, F=72 * 32, E=2, W=2, K=2, dead=0.1),
     "many-experts": dict(T=5, d=64, F=64, E=1024, W=1024, K=3, widx=False),
 }
 

@@ -194,6 +194,33 @@ def test_grouped_ffn(gpu, d, F, rows, widx):
     assert torch.equal(api.grouped_ffn_mxfp4_fwd(xq, off_t, widx_t, gu, dn, ws=ws)[:n], y[:n])
 
 
+@pytest.mark.parametrize("d,F,rows,extra", [
+    (384, 128, [i % 4 for i in range(260)], 0),  # scales word by word, every tile short
+    (1152, 640, [(7 * i) % 131 for i in range(90)], 0),
+    (512, 256, [130, 0, 257, 128], 20000),  # a padded batch
+    (4096, 640, [1300, 5, 129], 7000),  # a matrix past an L2: row tiles by eights
+])
+def test_large_tiles(gpu, d, F, rows, extra):
+    """Where rows and slots may need more tiles than the GPU has CUs."""
+    from paper_2606_11867_amd import api
+    print(f"\n[case] ffn4 large tiles d={d} F={F} slots={len(rows)}", flush=True)
+    rng = np.random.default_rng(d * 3 + F)
+    W, n = 2, sum(rows)
+    gu, gu_v = _weights(rng, gpu, W, 2 * F, d)
+    dn, dn_v = _weights(rng, gpu, W, d, F)
+    x = torch.zeros(n + extra, d, dtype=BF16, device=gpu)
+    x[:n] = torch.from_numpy(rng.standard_normal((n, d)).astype(np.float32)).to(gpu)
+    off = np.concatenate([[0], np.cumsum(rows)]).astype(np.int32)
+    widx = np.arange(len(rows), dtype=np.int32) % W
+    off_t = torch.from_numpy(off).to(gpu)
+    xq = api.mxfp4_quantize(x, n_rows=off_t[-1:])
+    y = api.grouped_ffn_mxfp4_fwd(xq, off_t, torch.from_numpy(widx).to(gpu), gu, dn)
+    xv = R.mxfp4_values(xq.codes[:n].cpu().numpy(), xq.scales[:n].cpu().numpy())
+    for w in range(W):  # all rows of a matrix at once
+        at = np.concatenate([np.arange(off[j], off[j + 1]) for j in range(len(rows)) if widx[j] == w])
+        _check_slot(xv[at], gu_v[w], dn_v[w], _np(y[torch.from_numpy(at).to(gpu)]))
+
+
 def test_rows_outside_slots_are_left(gpu):
     """Through the C call, on a y that holds something."""
     from paper_2606_11867_amd import _lib, api

@@ -87,6 +87,9 @@ def test_few_tokens_refuses(lib, mx):
                dict(ws=None), dict(ws_bytes=n - 1), dict(ws=FAKE + 64), dict(x=FAKE + 1), dict(gu=FAKE + 8),
                dict(out=0, y=FAKE + 2)):
         assert call(**kw) == -1, kw
+    n = lib.foremoe_few_workspace_size(8, 4, 1 << 25)
+    for kw in (dict(d=1 << 25, F=1, ld=1 << 25), dict(d=1, F=1 << 25), dict(ld=1 << 30)):
+        assert call(ws_bytes=n, **kw) == -2, kw
     if mx:
         assert call(d=48, ld=64) == -2 and call(F=80) == -2
         assert call(x=FAKE + 2) == -1 and call(ld=65) == -1 and call(gus=None) == -1
