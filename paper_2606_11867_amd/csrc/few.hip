@@ -12,8 +12,10 @@
 //     memory, no counters, a fixed order.
 //
 // Bound by memory where many experts are picked: 64 tokens over 32 experts of
-// 7168 x 2048 in bf16, whose weights are 2.8 GB, take 302 and 208 us (6.2 and 4.5
-// TB/s). One token of 8 experts of 2048 x 768 takes 16 and 12 us, of which 12
+// 7168 x 2048 in bf16 pick 28 of them, 2.45 GB, and take 313 and 208 us (5.2 and
+// 3.9 TB/s); 24 tokens of 8 of 128 experts of 2048 x 768 in 4 bits, 0.25 GB, 37 and
+// 34 us, of which a good part is each wavefront's wait for a unit's first weights.
+// One token of 8 experts of 2048 x 768 takes 16 and 12 us, of which 12
 // would be its 75 MB: there the latency of a launch, of the ids and of the first
 // weights counts.
 #include <type_traits>
@@ -309,46 +311,58 @@ constexpr int kFewThreads = 1024, kFewWaves = 16, kUpSlots = 1024, kUpStage = 72
 template <int WT, int NG>
 constexpr int kAhead = WT == kFp4 ? 1 : (NG == 4 ? 2 : 4);
 template <int WT, int NG>
-constexpr int kAheadStaged = 4;
+constexpr int kAheadStaged = NG == 1 ? 4 : 2;  // (4 for both spills registers: 51 us of 24 tokens in 4 bits, 37 so)
 template <int WT, int NG>
 constexpr int kAheadDown = WT == kFp4 ? (NG == 1 ? 3 : 1) : (NG == 4 ? 2 : 4);
 // Groups of tokens that a step of weights is multiplied with, at most.
 template <int WT>
 constexpr int kGroups = WT == kFp4 ? 2 : 4;
 
-// sums[i] = rows of weights x the tokens at offsets tok[i], over chunks [c0, c1) of
-// the k axis, in steps of S chunks (lane: chunk c + odd where S is 2). U steps
-// at a time without a branch, the weights of the next on their way while these
-// are multiplied; then the steps that are left, one of which may end in the
-// row's last, short chunk.
+// Rows of a unit, chunks [c0, c1) of them.
+struct Stretch {
+  const char* row;
+  const uint8_t* scales;
+  int c0, c1;
+};
+// U steps of weights on their way.
+template <int WT, int U, int S>
+struct Ahead {
+  uint4 v[U];
+  typename std::conditional<S == 2, uint64_t, uint32_t>::type scales[WT == kFp4 ? U : 1];
+};
+template <int WT, bool WVEC, int U, int S>
+__device__ __forceinline__ void load_ahead(Ahead<WT, U, S>& to, const Stretch& s, int n, int c, int odd, int g) {
+#pragma unroll
+  for (int u = 0; u < U; ++u) to.v[u] = load_weights<WT, WVEC, false>(s.row, n, c + u * S + odd, g);
+  if constexpr (WT == kFp4) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) to.scales[u] = load_scales<S, false>(s.scales, 0, c + u * S);
+  }
+}
+
+// sums[i] = rows of weights x the tokens at offsets tok[i] over a stretch, in
+// steps of S chunks (lane: chunk c + odd where S is 2). U steps at a time
+// without a branch, the weights of the next on their way while these are
+// multiplied; then the steps that are left, one of which may end in the row's
+// last, short chunk.
 template <int WT, bool WVEC, bool TVEC, bool STAGED, bool HIDDEN, int NG, int U, int S>
-__device__ __forceinline__ void stream_rows(const char* row, const uint8_t* scales, int n,
-                                            const Tokens& tokens, const uint32_t* tok, int nt, int c0, int c1, int odd, int g, f32x4* sums) {
-  using C = Chunk<WT>;
+__device__ __forceinline__ void stream_rows(const Stretch& s, int n, const Tokens& tokens, const uint32_t* tok, int nt,
+                                            int odd, int g, f32x4* sums) {
 #pragma unroll
   for (int i = 0; i < NG; ++i) sums[i] = f32x4{0, 0, 0, 0};
   const int by = 8 * g + (S == 2 ? 32 * odd : 0);  // bit of this lane's scale
-  const int blocks = (min(c1, n / (C::K * S) * S) - c0) / (U * S);
+  const int whole = min(s.c1, n / (Chunk<WT>::K * S) * S) - s.c0, blocks = whole > 0 ? whole / (U * S) : 0;
   if (blocks > 0) {
-    WeightFrag next[U];
-    uint64_t ns[U];
-    auto load = [&](int c) {
-#pragma unroll
-      for (int u = 0; u < U; ++u) next[u].v = load_weights<WT, WVEC, false>(row, n, c + u * S + odd, g);
-      if constexpr (WT == kFp4) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) ns[u] = load_scales<S, false>(scales, 0, c + u * S);
-      }
-    };
-    load(c0);
+    Ahead<WT, U, S> next;
+    load_ahead<WT, WVEC, U, S>(next, s, n, s.c0, odd, g);
     for (int b = 0; b < blocks; ++b) {
-      const int c = c0 + b * U * S;
+      const int c = s.c0 + b * U * S;
       WeightFrag w[U];
       TokenFrag<WT> t[STAGED ? 1 : U][NG];  // (from LDS a step at a time)
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        w[u] = next[u];
-        if constexpr (WT == kFp4) w[u].scale = (uint32_t)(ns[u] >> by) & 0xffu;
+        w[u].v = next.v[u];
+        if constexpr (WT == kFp4) w[u].scale = (uint32_t)(next.scales[u] >> by) & 0xffu;
       }
       auto load_t = [&](int to, int u) {
 #pragma unroll
@@ -359,7 +373,7 @@ __device__ __forceinline__ void stream_rows(const char* row, const uint8_t* scal
 #pragma unroll
         for (int u = 0; u < U; ++u) load_t(u, u);
       }
-      load(b + 1 < blocks ? c + U * S : c);  // (the last again: no branch)
+      load_ahead<WT, WVEC, U, S>(next, s, n, b + 1 < blocks ? c + U * S : c, odd, g);  // (the last again: no branch)
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         if constexpr (STAGED) load_t(0, u);
@@ -368,22 +382,21 @@ __device__ __forceinline__ void stream_rows(const char* row, const uint8_t* scal
       }
     }
   }
-  for (int c = c0 + (blocks > 0 ? blocks : 0) * U * S; c < c1; c += S) {
+  for (int c = s.c0 + blocks * U * S; c < s.c1; c += S) {
     WeightFrag w;
-    w.v = load_weights<WT, WVEC, true>(row, n, c + odd, g);
-    w.scale = WT == kFp4 ? (uint32_t)(load_scales<S, true>(scales, n / kMxBlock, c) >> by) & 0xffu : 0;
+    w.v = load_weights<WT, WVEC, true>(s.row, n, c + odd, g);
+    w.scale = WT == kFp4 ? (uint32_t)(load_scales<S, true>(s.scales, n / kMxBlock, c) >> by) & 0xffu : 0;
 #pragma unroll
     for (int i = 0; i < NG; ++i)
       sums[i] = multiply<WT>(w, load_token<WT, TVEC, STAGED, HIDDEN, true>(tokens, tok[i], nt, c + odd, g), sums[i]);
   }
 }
 
-// Both products of up to 16 NG pairs from place `first` on, over chunks [c0,
-// c1). STAGED: the token of place q is at stage + (q - q0) * stride in LDS.
+// Both products of up to 16 NG pairs from place `first` on, over a stretch.
+// STAGED: the token of place q is at stage + (q - q0) * stride in LDS.
 template <int WT, bool VEC, bool STAGED, int NG>
 __device__ __forceinline__ void up_groups(const FewArgs& a, const Groups& G, uint32_t stage, int stride, int q0,
-                                          int first, int end, const char* row, const uint8_t* scales, int c0, int c1,
-                                          f32x4* sums) {
+                                          int first, int end, const Stretch& s, f32x4* sums) {
   using C = Chunk<WT>;
   const int lane = lane_id(), g = lane >> 4, col = lane & 15;
   uint32_t tok[NG];
@@ -396,25 +409,25 @@ __device__ __forceinline__ void up_groups(const FewArgs& a, const Groups& G, uin
   }
   const Tokens x = tokens_at(a.x, (uint32_t)(((a.T - 1) * a.ld + a.d) * C::ES));
   constexpr int U = STAGED ? kAheadStaged<WT, NG> : kAhead<WT, NG>;
-  stream_rows<WT, VEC, VEC, STAGED, false, NG, U, 1>(row, scales, a.d, x, tok, a.d, c0, c1, 0, g, sums);
+  stream_rows<WT, VEC, VEC, STAGED, false, NG, U, 1>(s, a.d, x, tok, a.d, 0, g, sums);
 }
 
 // The same of all pairs of one matrix, up to 16 kGroups at a time; done(sums,
 // q) takes those of the 16 from place q on.
 template <int WT, bool VEC, bool STAGED, class Done>
 __device__ __forceinline__ void up_unit(const FewArgs& a, const Groups& G, uint32_t stage, int stride, int q0, int first,
-                                        int end, const char* row, const uint8_t* scales, int c0, int c1, Done&& done) {
+                                        int end, const Stretch& s, Done&& done) {
   for (int at = first; at < end; at += 16 * kGroups<WT>) {
     f32x4 sums[4];
     if (end - at <= 16) {
-      up_groups<WT, VEC, STAGED, 1>(a, G, stage, stride, q0, at, end, row, scales, c0, c1, sums);
+      up_groups<WT, VEC, STAGED, 1>(a, G, stage, stride, q0, at, end, s, sums);
       done(sums[0], at);
     } else if (kGroups<WT> == 2 || end - at <= 32) {
-      up_groups<WT, VEC, STAGED, 2>(a, G, stage, stride, q0, at, end, row, scales, c0, c1, sums);
+      up_groups<WT, VEC, STAGED, 2>(a, G, stage, stride, q0, at, end, s, sums);
 #pragma unroll
       for (int k = 0; k < 2; ++k) done(sums[k], at + 16 * k);
     } else {
-      up_groups<WT, VEC, STAGED, kGroups<WT>>(a, G, stage, stride, q0, at, end, row, scales, c0, c1, sums);
+      up_groups<WT, VEC, STAGED, kGroups<WT>>(a, G, stage, stride, q0, at, end, s, sums);
 #pragma unroll
       for (int k = 0; k < kGroups<WT>; ++k) done(sums[k], at + 16 * k);
     }
@@ -467,7 +480,7 @@ __global__ __launch_bounds__(kFewThreads) void few_up_kernel(FewArgs a) {
   const int nc = (a.d + C::K - 1) / C::K;
   // In 4 bits the tokens of this workgroup's matrices are staged where they fit:
   // from memory they take four times as many loads as the weights (24 tokens:
-  // 68 -> 57 us, 51 since its loads have no branches; with 16-bit weights, where they take as many, the wait for the
+  // 68 -> 57 us, 37 with what came after; with 16-bit weights, where they take as many, the wait for the
   // staging costs more than it saves, 298 -> 352).
   const int m0 = (int)(u0 / tiles), m1 = (int)((u0 + n - 1) / tiles);
   const int q0 = G.begin_used[m0], staged_pairs = G.begin_used[m1 + 1] - q0;
@@ -507,8 +520,8 @@ __global__ __launch_bounds__(kFewThreads) void few_up_kernel(FewArgs a) {
         else if (g < 2) put_h<WT>(a, G.list[q], f0 + 4 * g + e, v, up);
       }
     };
-    if (WT == kFp4 && staged) up_unit<WT, VEC, WT == kFp4>(a, G, stage0, stride, q0, first, end, rp, sp, k0, k1, done);
-    else up_unit<WT, VEC, false>(a, G, 0, 0, 0, first, end, rp, sp, k0, k1, done);
+    if (WT == kFp4 && staged) up_unit<WT, VEC, WT == kFp4>(a, G, stage0, stride, q0, first, end, Stretch{rp, sp, k0, k1}, done);
+    else up_unit<WT, VEC, false>(a, G, 0, 0, 0, first, end, Stretch{rp, sp, k0, k1}, done);
   }
   if (parts > 1) {
     __syncthreads();
@@ -542,8 +555,8 @@ __global__ __launch_bounds__(kFewThreads) void few_up_kernel(FewArgs a) {
 // half each is wanted.
 // ---------------------------------------------------------------------------
 template <int WT, bool VEC, int PL, int NG>
-__device__ __forceinline__ void down_groups(const FewArgs& a, const Groups& G, int first, int end, const char* row,
-                                            const uint8_t* scales, int c0, int c1, float* yp) {
+__device__ __forceinline__ void down_groups(const FewArgs& a, const Groups& G, int first, int end, const Stretch& s,
+                                            float* yp) {
   using C = Chunk<WT>;
   constexpr int P = 8 / PL;  // pairs of a group
   const int lane = lane_id(), g = lane >> 4, r = lane & 15;
@@ -557,7 +570,7 @@ __device__ __forceinline__ void down_groups(const FewArgs& a, const Groups& G, i
   }
   const Tokens h = tokens_at(a.h, plane_bytes * (WT == kF32 ? 1 : a.planes));
   f32x4 acc[NG];
-  stream_rows<WT, VEC, true, false, true, NG, kAheadDown<WT, NG>, 2>(row, scales, a.F, h, tok, a.Fp, c0, c1, r >> 3, g, acc);
+  stream_rows<WT, VEC, true, false, true, NG, kAheadDown<WT, NG>, 2>(s, a.F, h, tok, a.Fp, r >> 3, g, acc);
 #pragma unroll
   for (int i = 0; i < NG; ++i)
 #pragma unroll
@@ -598,12 +611,12 @@ __global__ __launch_bounds__(kFewThreads) void few_down_kernel(FewArgs a) {
       const int64_t row = (int64_t)w * a.d + col + min(r & 7, cols - 1);
       const char* rp = a.dn + (WT == kFp4 ? row * (a.F / 2) : row * a.F * C::ES);
       const uint8_t* sp = WT == kFp4 ? a.dn_scales + row * (a.F / kMxBlock) : nullptr;
-      const int k0 = nc * part / parts * 2, k1 = nc * (part + 1) / parts * 2;
+      const Stretch s{rp, sp, nc * part / parts * 2, nc * (part + 1) / parts * 2};
       float* to = yp + (size_t)(tile * parts + part) * count * 8;
       for (int at = first; at < end; at += kGroups<WT> * P) {
-        if (end - at <= P) down_groups<WT, VEC, PL, 1>(a, G, at, end, rp, sp, k0, k1, to);
-        else if (kGroups<WT> == 2 || end - at <= 2 * P) down_groups<WT, VEC, PL, 2>(a, G, at, end, rp, sp, k0, k1, to);
-        else down_groups<WT, VEC, PL, kGroups<WT>>(a, G, at, end, rp, sp, k0, k1, to);
+        if (end - at <= P) down_groups<WT, VEC, PL, 1>(a, G, at, end, s, to);
+        else if (kGroups<WT> == 2 || end - at <= 2 * P) down_groups<WT, VEC, PL, 2>(a, G, at, end, s, to);
+        else down_groups<WT, VEC, PL, kGroups<WT>>(a, G, at, end, s, to);
       }
     }
     __syncthreads();
