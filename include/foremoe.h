@@ -853,8 +853,14 @@ int foremoe_grouped_ffn_mxfp4_fwd(const uint8_t* x_codes, const uint8_t* x_scale
  * T * K <= FOREMOE_FEW_PAIRS, 1 <= E <= FOREMOE_MAX_EXPERTS, 1 <= W <=
  * FOREMOE_MAX_SLOTS. bf16 and fp32: any d, F >= 1 (rows of weights whose
  * bytes are a multiple of 16 are read 16 bytes at a time, others element by
- * element); _mxfp4: d and F multiples of 32.  2 * d * F < 2^31.
- * Pointers aligned to their types, w_* and codes to 16 bytes.
+ * element); _mxfp4: d and F multiples of 32.  2 * d * F < 2^31. d, F < 2^25,
+ * and x and the hidden rows below 3.7 GB (else FOREMOE_EUNSUPPORTED).
+ * Pointers aligned to their types, w_* and codes to 16 bytes; _mxfp4: x's rows
+ * to 16 bytes (ld a multiple of 8).
+ * The same call gives the same bits. How the sums over d and F are cut depends
+ * on T, K and which experts are picked, so a token's may differ with the others
+ * beside it by fp32 roundings. A NaN stays with the tokens that meet it; an
+ * infinite element of Wd may give NaN where the sum would be infinite.
  * ws: foremoe_few_workspace_size(T, K, F) bytes for the hidden rows (one of
  * the largest T, K and F serves smaller calls), 256-byte aligned; needs no
  * initialisation. Calls that share one must not overlap in time.
@@ -885,16 +891,21 @@ int foremoe_few_tokens_ffn_mxfp4(const void* x, int64_t ld, int64_t T, int32_t d
  *   p = p (1 - lr weight_decay) - lr scale X
  * p is master where the record has one (param, of bf16, then gets its rounded
  * copy), else param itself. zero_grads != 0: grad is zero afterwards.
- * m, norms, X and all sums are fp32 (norms' sums fp64). The products' factors
- * are X, G and b G + c G G rounded to fp16 (2^-11 of an element, or 2^-33
- * where that is more); a X is of the unrounded X, so that directions that u
- * does not have stay as small as fp32 holds them. X of the step is within
- * about 2^-9 of its norm of the exact one. Coefficients that let singular
- * values pass 100 overflow.
+ * m and all sums are fp32, the norm's fp64. Where both sides are above 64, X is
+ * held as two fp16 numbers (its rounding, and that of 2^10 times what it
+ * leaves), G and b G + c G G as one; the products take the first of X (2^-11 of
+ * an element, or 2^-33 where that is more), a X takes both, so that directions
+ * that u does not have stay small. X is within about 2^-9 of its norm of the
+ * exact one. Where s^2 or |b s^2 + c s^4| passes 255 for a singular value s of
+ * an X on the way, fp16 overflows to infinity (with coefficients that converge
+ * s stays below 1.3). Where a side is at most 64, all is fp32, and X the product
+ * of a polynomial of the first G and the first X: within 2^-18 of its norm, or
+ * about 2^-11 where u is close to singular.
  * A matrix with a NaN or infinite element, or whose u has one, becomes NaN;
  * the others do not.
  * tensors: HOST array, read during the call only; pointers aligned to their
- * types; param, grad, master and m hold [batch, rows, cols] contiguous. batch
+ * types; param, grad, master and m hold [batch, rows, cols] contiguous, and no
+ * two of them overlap. batch
  * = 0: skipped. batch <= 2^30, 1 <= rows, cols <= FOREMOE_MUON_SIDE,
  * min(rows, cols) <= FOREMOE_MUON_RANK, and with both sides rounded up to 256
  * at most 2^35 elements. 0 <= ns_steps <= 16.

@@ -8,12 +8,18 @@
 //   twice), X = a X + P X.
 // X is held as two fp16 numbers, its rounding and 2^10 times what that
 // leaves; the products take the first, a X takes both. So a product's factors
-// are rounded to 2^-12 of themselves, and directions that u does not have stay
+// are within 2^-11 of themselves, and directions that u does not have stay
 // at the size that fp32 leaves there: P X alone would fill them with the
 // rounding of X, which each of the first steps multiplies by a. (The last step
 // does without the second numbers: that is one factor a.)
 // X, G and P are held 2^8 times as large, which keeps entries of large, even
 // matrices (1/sqrt(m n) and less) above fp16's subnormal numbers.
+//
+// The passes over the tensors are bound by memory, the products by the matrix
+// cores and, of X, by the 8 bytes an element that its two numbers are read and
+// written with: 48 matrices of 768 x 2048 (75 M elements) take 165 us for the
+// momentum (5.5 TB/s), 250 for X0 (4.8), five times 100 for G and 49 for P, four
+// times 218 for X (0.53 PFLOP/s), 315 for the last X and the update.
 #include <math.h>
 
 #include "common.h"
@@ -41,7 +47,7 @@ struct MuonRec {
   uint32_t chunks;         // of a matrix, in the momentum pass
   int32_t chunk;           // elements of one
   float decay, move;       // 1 - lr weight_decay, lr scale
-  int32_t wide;              // the tensors' rows start on 16 bytes: read and written so
+  int32_t wide;            // the tensors' rows start on 16 bytes: read and written so
   union {
     struct {
       uint16_t *x[2], *rest[2];  // [batch, mm, nn]
@@ -144,7 +150,8 @@ __device__ __forceinline__ void put4(void* p, int64_t i, int64_t left, bool wide
   }
 }
 
-// m and the squares of u, a workgroup to a chunk of a matrix.
+// m and the squares of u, a workgroup to a chunk of a matrix (12 bytes an
+// element: see above).
 template <bool GBF16>
 __global__ __launch_bounds__(kMomentThreads) void muon_moment_kernel(MuonArgs a) {
   const int ri = find_rec(a, blockIdx.x);
@@ -292,14 +299,14 @@ __device__ __forceinline__ void update_n(const MuonRec& r, Place place, X x) {
 
 // One T x T tile of one matrix's product, by wavefronts of 64 x 64 (T = 128) or
 // 64 x 128 (T = 256). The workgroups of an XCD have neighbouring tiles, whose
-// operands its L2 then holds once (48 matrices of 768 x 2048, G: 135 -> 92 us).
+// operands its L2 then holds once (48 matrices of 768 x 2048, G: 135 -> 100 us).
 // The sums go through LDS, so that memory is read and written in whole lines
-// (X of the same: 412 -> 242 us). kUpdate is the last step's kApply: its X
-// goes into the parameters at once. NS stages of 64 of the k axis: two, or
-// four where a CU has one small tile alone and nothing else hides the loads.
-template <int P, bool PBF16, int T, int NS>
+// (X of the same: 412 -> 219 us). kUpdate is the last step's kApply: its X
+// goes into the parameters at once. Two stages of 64 of the k axis; four take
+// as long, also where a CU has one small tile alone.
+template <int P, bool PBF16, int T>
 __global__ __launch_bounds__(T * 2) void muon_product_kernel(MuonArgs a) {
-  constexpr int BK = kMuonBK, NW = T / 32, NT = 64 * NW, WN = T / 2;
+  constexpr int NS = 2, BK = kMuonBK, NW = T / 32, NT = 64 * NW, WN = T / 2;
   constexpr bool SYM = P == kGram || P == kPoly;
   using CoreT = Core<T, T, T / 64, 2, false, Fp16>;
   using AT = KTile<T, BK, NW>;
@@ -525,7 +532,8 @@ __global__ __launch_bounds__(256) void muon_update_kernel(MuonArgs a) {
 // workgroup a matrix. (fp16 factors would move X of a matrix with a side below
 // 16 by up to 2^-6 of its norm, as one singular value's error does not average
 // out; fp32 ones move it by 2^-20, or 2^-11 where u is next to singular, whose
-// small directions G holds squared.)
+// small directions G holds squared.) All of it is latency: the small ones of six
+// matrices with sides of 24 to 400 take 9, 27 and 13 us.
 // ---------------------------------------------------------------------------
 constexpr int kSmall = 64, kSmallLD = 65, kSmallChunks = 64;
 
@@ -832,10 +840,11 @@ int64_t scale_tiles(const foremoe_muon_tensor& t) {
 // Tiles of the products' launches over the tensors [i, end): of the symmetric
 // ones, and of X. A k step of a 256-wide tile takes a CU about as long as one
 // of two 128-wide ones, four times the work against two; one 128-wide tile
-// alone about half of that. So the wide ones are faster where whole rounds of
+// alone on a CU about half of that. So the wide ones are faster where whole rounds of
 // them fill the CUs and the padding does not take it back (us, 128 / 256: 48
-// matrices of 768 x 2048, G 92 / 118, X 242 / 215; 6 of 2048 x 7168, G 229 /
-// 194, X 488 / 455).
+// matrices of 768 x 2048, G 104 / 124, X 219 / 211; 6 of 2048 x 7168, G 246 /
+// 194, X 464 / 441; the large ones of six with sides of 24 to 400, G 10 / 13, X 10
+// / 20).
 struct Tiles {
   int pad, sym, full;
 };
@@ -927,9 +936,8 @@ static void launch_product(MuonArgs& a, int tile, hipStream_t st) {
     return P == kGram || P == kPoly ? tm * (tm + 1) / 2 : tm * (r.nn / T);
   });
   const dim3 grid((n + 7) / 8 * 8), threads(tile * 2);
-  if (tile == 256) hipLaunchKernelGGL((muon_product_kernel<P, PBF16, 256, 2>), grid, threads, 0, st, a);
-  else if (n > 256) hipLaunchKernelGGL((muon_product_kernel<P, PBF16, 128, 2>), grid, threads, 0, st, a);
-  else hipLaunchKernelGGL((muon_product_kernel<P, PBF16, 128, 4>), grid, threads, 0, st, a);
+  if (tile == 256) hipLaunchKernelGGL((muon_product_kernel<P, PBF16, 256>), grid, threads, 0, st, a);
+  else hipLaunchKernelGGL((muon_product_kernel<P, PBF16, 128>), grid, threads, 0, st, a);
 }
 
 static void launch_large(MuonArgs& a, const Tiles& tiles, bool pb16, bool gb16, hipStream_t st) {
