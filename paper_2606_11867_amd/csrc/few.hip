@@ -7,14 +7,14 @@
 //     use; a workgroup to a CU takes its even share of all units, a wavefront a
 //     unit or, where they are few, a part of its k axis.
 //   down: a workgroup takes its even share of the output columns, of every
-//     matrix in use, a wavefront up to 8 columns of one, or a part of their k
+//     matrix in use, a wavefront up to 16 columns of one, or a part of their k
 //     axis. So it holds a token's sum over its experts alone: no partial sums in
 //     memory, no counters, a fixed order.
 //
 // Bound by memory where many experts are picked: 64 tokens over 32 experts of
-// 7168 x 2048 in bf16 pick 28 of them, 2.45 GB, and take 313 and 208 us (5.2 and
-// 3.9 TB/s); 24 tokens of 8 of 128 experts of 2048 x 768 in 4 bits, 0.25 GB, 37 and
-// 34 us, of which a good part is each wavefront's wait for a unit's first weights.
+// 7168 x 2048 in bf16 pick 28 of them, 2.45 GB, and take 313 and 169 us (5.2 and
+// 4.8 TB/s); 24 tokens of 8 of 128 experts of 2048 x 768 in 4 bits, 0.25 GB, 37 and
+// 33 us, of which a good part is each wavefront's wait for a unit's first weights.
 // One token of 8 experts of 2048 x 768 takes 16 and 12 us, of which 12
 // would be its 75 MB: there the latency of a launch, of the ids and of the first
 // weights counts.
@@ -306,6 +306,7 @@ __device__ __forceinline__ int parts_for(int n, int nc, int each, int slots) {
 // takes its even share of them, a wavefront a unit or a part of its k axis.
 // ---------------------------------------------------------------------------
 constexpr int kFewThreads = 1024, kFewWaves = 16, kUpSlots = 1024, kUpStage = 72 << 10;
+static_assert(FOREMOE_FEW_PAIRS % kFewThreads == 0 && FOREMOE_MAX_SLOTS % kFewThreads == 0, "group_pairs");
 // Steps of weights in flight behind those that are multiplied: as many as the
 // registers of 16 wavefronts a CU hold beside NG groups of tokens.
 template <int WT, int NG>
@@ -313,7 +314,7 @@ constexpr int kAhead = WT == kFp4 ? 1 : (NG == 4 ? 2 : 4);
 template <int WT, int NG>
 constexpr int kAheadStaged = NG == 1 ? 4 : 2;  // (4 for both spills registers: 51 us of 24 tokens in 4 bits, 37 so)
 template <int WT, int NG>
-constexpr int kAheadDown = WT == kFp4 ? (NG == 1 ? 3 : 1) : (NG == 4 ? 2 : 4);
+constexpr int kAheadDown = WT == kFp4 ? (NG == 1 ? 2 : 1) : (NG == 4 ? 2 : 4);
 // Groups of tokens that a step of weights is multiplied with, at most.
 template <int WT>
 constexpr int kGroups = WT == kFp4 ? 2 : 4;
@@ -548,19 +549,20 @@ __global__ __launch_bounds__(kFewThreads) void few_up_kernel(FewArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// down and the sum over a token's experts. The 16 rows of an instruction are 8
-// output columns at two chunks of the k axis. Its 16 columns are the same two
-// chunks of PL planes of 8 / PL pairs (fp32 one plane; bf16 two, or for an fp32
-// output three and an empty one): of its products one row half by one column
-// half each is wanted.
+// down and the sum over a token's experts. The 16 rows of an instruction are
+// ROWS output columns: 16, or where a workgroup has no more than 8, those at two
+// chunks of the k axis. Its 16 columns are PL planes of ROWS / PL pairs (fp32 one
+// plane; bf16 two, or for an fp32 output three and an empty one), at the same two
+// chunks where ROWS is 8: then of its products one row half by one column half
+// each is wanted.
 // ---------------------------------------------------------------------------
-template <int WT, bool VEC, int PL, int NG>
+template <int WT, bool VEC, int ROWS, int PL, int NG>
 __device__ __forceinline__ void down_groups(const FewArgs& a, const Groups& G, int first, int end, const Stretch& s,
                                             float* yp) {
   using C = Chunk<WT>;
-  constexpr int P = 8 / PL;  // pairs of a group
+  constexpr int S = 16 / ROWS, P = ROWS / PL;  // pairs of a group
   const int lane = lane_id(), g = lane >> 4, r = lane & 15;
-  const int plane = (r & 7) / P;
+  const int plane = (r & (ROWS - 1)) / P;
   const uint32_t plane_bytes = (uint32_t)(a.T * a.K * a.Fp * C::ES);
   uint32_t tok[NG];
 #pragma unroll
@@ -570,32 +572,31 @@ __device__ __forceinline__ void down_groups(const FewArgs& a, const Groups& G, i
   }
   const Tokens h = tokens_at(a.h, plane_bytes * (WT == kF32 ? 1 : a.planes));
   f32x4 acc[NG];
-  stream_rows<WT, VEC, true, false, true, NG, kAheadDown<WT, NG>, 2>(s, a.F, h, tok, a.Fp, r >> 3, g, acc);
+  stream_rows<WT, VEC, true, false, true, NG, kAheadDown<WT, NG>, S>(s, a.F, h, tok, a.Fp, S == 2 ? r >> 3 : 0, g, acc);
 #pragma unroll
   for (int i = 0; i < NG; ++i)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      // row 4 g + e and column r of the even chunks, row + 8 and column + 8 of the odd
-      float v = acc[i][e];
-      v += __shfl(v, (lane + 40) & 63, 64);
-      if constexpr (PL >= 2) v += __shfl(v, (lane + 4) & 63, 64);  // the other planes
-      if constexpr (PL == 4) v += __shfl(v, (lane + 2) & 63, 64);
+      float v = acc[i][e];  // row 4 g + e, column r
+      if constexpr (S == 2) v += __shfl(v, (lane + 40) & 63, 64);  // of the odd chunks: row + 8, column + 8
+      if constexpr (PL >= 2) v += __shfl(v, (lane + ROWS / 2) & 63, 64);  // the other planes
+      if constexpr (PL == 4) v += __shfl(v, (lane + ROWS / 4) & 63, 64);
       const int q = first + P * i + r;
-      if (r < P && g < 2 && q < end) yp[q * 8 + 4 * g + e] = v;
+      if (r < P && 4 * g < ROWS && q < end) yp[q * ROWS + 4 * g + e] = v;
     }
 }
 
-template <int WT, bool VEC, int PL, int CAP>
+template <int WT, bool VEC, int ROWS, int PL, int CAP>
 __global__ __launch_bounds__(kFewThreads) void few_down_kernel(FewArgs a) {
   __shared__ Groups G;
-  __shared__ float yp[CAP * 8];  // [tile][part][place][8]
+  __shared__ float yp[CAP * ROWS];  // [tile][part][place][ROWS]
   group_pairs<kFewThreads>(a, G);
   const int tid = threadIdx.x, lane = lane_id();
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n_used = G.n_used, count = G.begin_used[n_used];
   using C = Chunk<WT>;
-  constexpr int P = 8 / PL;
-  const int r = lane & 15, nc = (a.F + 2 * C::K - 1) / (2 * C::K);  // pairs of chunks
+  constexpr int S = 16 / ROWS, P = ROWS / PL;
+  const int r = lane & 15, nc = (a.F + S * C::K - 1) / (S * C::K);  // steps of S chunks
   // this workgroup's tiles of a.width columns, as many at a time as their
   // sums have room
   const int t0 = a.tiles * (int)blockIdx.x, t1 = min(t0 + a.tiles, (a.d + a.width - 1) / a.width);
@@ -608,28 +609,28 @@ __global__ __launch_bounds__(kFewThreads) void few_down_kernel(FewArgs a) {
       const int w = __builtin_amdgcn_readfirstlane(G.used[c]);
       const int first = __builtin_amdgcn_readfirstlane(G.begin_used[c]), end = __builtin_amdgcn_readfirstlane(G.begin_used[c + 1]);
       const int col = (tile0 + tile) * a.width, cols = min(a.width, a.d - col);
-      const int64_t row = (int64_t)w * a.d + col + min(r & 7, cols - 1);
+      const int64_t row = (int64_t)w * a.d + col + min(r & (ROWS - 1), cols - 1);
       const char* rp = a.dn + (WT == kFp4 ? row * (a.F / 2) : row * a.F * C::ES);
       const uint8_t* sp = WT == kFp4 ? a.dn_scales + row * (a.F / kMxBlock) : nullptr;
-      const Stretch s{rp, sp, nc * part / parts * 2, nc * (part + 1) / parts * 2};
-      float* to = yp + (size_t)(tile * parts + part) * count * 8;
+      const Stretch s{rp, sp, nc * part / parts * S, nc * (part + 1) / parts * S};
+      float* to = yp + (size_t)(tile * parts + part) * count * ROWS;
       for (int at = first; at < end; at += kGroups<WT> * P) {
-        if (end - at <= P) down_groups<WT, VEC, PL, 1>(a, G, at, end, s, to);
-        else if (kGroups<WT> == 2 || end - at <= 2 * P) down_groups<WT, VEC, PL, 2>(a, G, at, end, s, to);
-        else down_groups<WT, VEC, PL, kGroups<WT>>(a, G, at, end, s, to);
+        if (end - at <= P) down_groups<WT, VEC, ROWS, PL, 1>(a, G, at, end, s, to);
+        else if (kGroups<WT> == 2 || end - at <= 2 * P) down_groups<WT, VEC, ROWS, PL, 2>(a, G, at, end, s, to);
+        else down_groups<WT, VEC, ROWS, PL, kGroups<WT>>(a, G, at, end, s, to);
       }
     }
     __syncthreads();
     const int c0 = tile0 * a.width, cols = min(nt * a.width, a.d - c0);
     for (int o = tid; o < a.T * cols; o += kFewThreads) {
       const int t = o / cols, j = o % cols;
-      const float* from = yp + (size_t)(j / a.width * parts) * count * 8 + j % a.width;
+      const float* from = yp + (size_t)(j / a.width * parts) * count * ROWS + j % a.width;
       float s = 0.0f;
       for (int k = 0; k < a.K; ++k) {
         const int q = G.place[t * a.K + k];
         if (q < 0) continue;
         float v = 0.0f;
-        for (int p = 0; p < parts; ++p) v += from[((size_t)p * count + q) * 8];
+        for (int p = 0; p < parts; ++p) v += from[((size_t)p * count + q) * ROWS];
         s = fmaf(a.gates[t * a.K + k], v, s);
       }
       const int64_t at = (int64_t)t * a.d + c0 + j;
@@ -640,18 +641,14 @@ __global__ __launch_bounds__(kFewThreads) void few_down_kernel(FewArgs a) {
   }
 }
 
-template <int WT, bool UP_VEC, bool DOWN_VEC>
-void launch_few(FewArgs a, hipStream_t st) {
-  const int pairs = a.T * a.K, cus = num_cus();
-  const int64_t units = (int64_t)((a.F + 7) / 8) * (pairs < a.W ? pairs : a.W);
-  hipLaunchKernelGGL((few_up_kernel<WT, UP_VEC>), dim3((unsigned)(units < cus ? units : cus)), dim3(kFewThreads), 0, st,
-                     a);
-  // an even share of the columns to every CU, in tiles of 8 at most
-  const int share = (a.d + cus - 1) / cus;
-  a.tiles = (share + 7) / 8;
+template <int WT, bool VEC, int ROWS>
+void launch_down(FewArgs a, int share, hipStream_t st) {
+  const int pairs = a.T * a.K;
+  a.tiles = (share + ROWS - 1) / ROWS;
   a.width = (share + a.tiles - 1) / a.tiles;
   const dim3 grid((a.d + a.tiles * a.width - 1) / (a.tiles * a.width));
-#define DOWN(PL, CAP) hipLaunchKernelGGL((few_down_kernel<WT, DOWN_VEC, PL, CAP>), grid, dim3(kFewThreads), 0, st, a)
+#define DOWN(PL, CAP) \
+  hipLaunchKernelGGL((few_down_kernel<WT, VEC, ROWS, PL, CAP>), grid, dim3(kFewThreads), 0, st, a)
   if constexpr (WT == kF32) {
     if (pairs <= 512) DOWN(1, 512);
     else DOWN(1, 2048);
@@ -663,6 +660,22 @@ void launch_few(FewArgs a, hipStream_t st) {
     else DOWN(4, 2048);
   }
 #undef DOWN
+}
+
+template <int WT, bool UP_VEC, bool DOWN_VEC>
+void launch_few(FewArgs a, hipStream_t st) {
+  const int pairs = a.T * a.K, cus = num_cus();
+  const int64_t units = (int64_t)((a.F + 7) / 8) * (pairs < a.W ? pairs : a.W);
+  hipLaunchKernelGGL((few_up_kernel<WT, UP_VEC>), dim3((unsigned)(units < cus ? units : cus)), dim3(kFewThreads), 0, st,
+                     a);
+  // an even share of the columns to every CU, in tiles of 16 at most, or of 8
+  // where it has no more: a tile's rows of weights are multiplied with every
+  // hidden row of their matrix, which come from the L2 again for each tile (us, 8
+  // / 16: 64 tokens over 28 experts of 7168 x 2048 209 / 169, 32 places of each of
+  // 8 such experts 297 / 164)
+  const int share = (a.d + cus - 1) / cus;
+  if (share > 8) launch_down<WT, DOWN_VEC, 16>(a, share, st);
+  else launch_down<WT, DOWN_VEC, 8>(a, share, st);
 }
 
 }  // namespace

@@ -96,6 +96,8 @@ SIZES = {
     "wide": dict(T=3, d=1056, F=1120, E=5, W=5, K=5),
     "pairs": dict(T=128, d=64, F=32, E=40, W=40, K=16),  # 2048 pairs
     "long-rows": dict(T=12, d=8192, F=64, E=3, W=3, K=2),  # past what the LDS holds
+    "wide-pairs": dict(T=128, d=2304, F=64, E=40, W=40, K=16),  # 2048 pairs, more than 8 columns a CU
+    "wide-share": dict(T=70, d=4128, F=192, E=32, W=4, K=4, dead=0.2),
     "long-and-crowded": dict(T=40, d=2048, F=72 * 32, E=2, W=2, K=2, dead=0.1),
     "many-experts": dict(T=5, d=64, F=64, E=1024, W=1024, K=3, widx=False),
 }
@@ -113,7 +115,7 @@ def test_few_tokens(gpu, name, w, out):
 
 @pytest.mark.parametrize("w", ["bf16", "f32"])
 @pytest.mark.parametrize("d,F,pad", [(1, 1, 0), (7, 3, 2), (33, 9, 0), (64, 31, 1), (65, 64, 0), (130, 257, 6), (104, 56, 8),
-                                     (96, 1, 0), (2, 100, 0)])
+                                     (96, 1, 0), (2, 100, 0), (4101, 33, 0)])
 def test_odd_sizes(gpu, w, d, F, pad):
     print(f"\n[case] few odd {w} d={d} F={F} pad={pad}", flush=True)
     rng = np.random.default_rng(d * 31 + F)
