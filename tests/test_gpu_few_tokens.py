@@ -211,3 +211,22 @@ def test_refused(gpu):
             bad()
     with pytest.raises(ForeMoEError):
         call(ws=torch.empty(64, dtype=torch.uint8, device=gpu))
+
+
+@pytest.mark.parametrize("w", ["bf16", "f32"])
+def test_far_weights(gpu, w):
+    """Weights past 2^32 bytes: the last matrix gives what it gives alone."""
+    from paper_2606_11867_amd import api
+    W, d, F = 100, 7168, 2048
+    print(f"\n[case] few {w}, {W} matrices of {d} x {F}", flush=True)
+    g = torch.Generator(device=gpu).manual_seed(8)
+    gu, dn = (torch.zeros(W, *s, dtype=DT[w], device=gpu) for s in ((2 * F, d), (d, F)))
+    pick = [0, W - 1]
+    for t in (gu, dn):
+        for i in pick:
+            t[i] = torch.randn(t.shape[1:], generator=g, device=gpu) * t.shape[2] ** -0.5
+    x = torch.randn(3, d, generator=g, device=gpu).to(DT[w])
+    ids = torch.tensor([[0, 1], [1, 0], [1, -1]], dtype=I32, device=gpu)
+    gates = torch.rand(3, 2, generator=g, device=gpu)
+    y = api.few_tokens_ffn(x, ids, gates, gu, dn, expert_widx=torch.tensor(pick, dtype=I32, device=gpu))
+    assert bool(y.any()) and torch.equal(y, api.few_tokens_ffn(x, ids, gates, gu[pick], dn[pick]))

@@ -236,3 +236,22 @@ def test_many_large_matrices(gpu, shape):
     q = torch.zeros_like(p)
     Muon([q], [g], lr=1.0, momentum=0.0, nesterov=False, scale=-1.0).step()
     assert torch.equal(p, q)
+
+
+def test_far_elements(gpu):
+    """More than 2^31 elements: the first and last matrix move as they do alone.
+    Either X is within about 2^-9 of its norm of the exact one."""
+    from paper_2606_11867_amd.optimizer import Muon
+    shape = (130, 4096, 4100)
+    print(f"\n[case] muon {shape}", flush=True)
+    g = torch.zeros(shape, device=gpu)
+    gen = torch.Generator(device=gpu).manual_seed(3)
+    for i in (0, 129):
+        g[i].normal_(generator=gen)
+    p = torch.zeros(shape, device=gpu)
+    Muon([p], [g], lr=1.0, momentum=0.0, nesterov=False, scale=-1.0).step()
+    assert not p[1:129].any()
+    for i in (0, 129):
+        q = torch.zeros(shape[1:], device=gpu)
+        Muon([q], [g[i]], lr=1.0, momentum=0.0, nesterov=False, scale=-1.0).step()
+        assert (p[i] - q).norm() <= 2.0 ** -8 * q.norm() and q.norm() > 30

@@ -293,3 +293,43 @@ def test_captured(gpu):
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(run()[:loads[-1]], y[:loads[-1]])
+
+
+def test_far_rows(gpu):
+    """More than 2^31 elements: the last rows are those of a call of their own."""
+    from paper_2606_11867_amd import api
+    rows, cols = (1 << 20) + 5, 2080
+    print(f"\n[case] quantize {rows}x{cols}", flush=True)
+    x = torch.empty(rows, cols, dtype=BF16, device=gpu)
+    x[:7].normal_(), x[7:-7].fill_(1.0), x[-7:].normal_()
+    q, tail, head = api.mxfp4_quantize(x), api.mxfp4_quantize(x[-7:]), api.mxfp4_quantize(x[:7])
+    for at, ref in ((slice(-7, None), tail), (slice(0, 7), head)):
+        assert torch.equal(q.codes[at], ref.codes) and torch.equal(q.scales[at], ref.scales)
+    v = api.mxfp4_values(q, dtype=BF16)
+    assert torch.equal(v[-7:], api.mxfp4_values(tail, dtype=BF16)) and bool((v[7:-7] == 1).all())
+
+
+def test_far_weights(gpu):
+    """Weights past 2^31 bytes: the last matrix gives what it gives alone."""
+    from paper_2606_11867_amd import api
+    W, d, F = 160, 7168, 2048
+    print(f"\n[case] ffn4 and few, {W} matrices of {d} x {F}", flush=True)
+    g = torch.Generator(device=gpu).manual_seed(7)
+    make = lambda r, n: api.MXFP4(  # noqa: E731
+        torch.randint(0, 256, (W, r, n // 2), generator=g, device=gpu, dtype=torch.uint8),
+        torch.randint(116, 120, (W, r, n // 32), generator=g, device=gpu, dtype=torch.uint8))
+    gu, dn = make(2 * F, d), make(d, F)
+    x = torch.randn(40, d, generator=g, device=gpu).to(BF16)
+    xq = api.mxfp4_quantize(x)
+    off = torch.tensor([0, 25, 40], dtype=torch.int32, device=gpu)
+    pick = [0, W - 1]
+    few_of = lambda q: api.MXFP4(q.codes[pick], q.scales[pick])  # noqa: E731
+    y = api.grouped_ffn_mxfp4_fwd(xq, off, torch.tensor(pick, dtype=torch.int32, device=gpu), gu, dn)
+    ref = api.grouped_ffn_mxfp4_fwd(xq, off, torch.tensor([0, 1], dtype=torch.int32, device=gpu), few_of(gu), few_of(dn))
+    assert bool(torch.isfinite(y).all()) and torch.equal(y, ref)
+    ids = torch.tensor([[0, 1], [1, 0], [1, -1]], dtype=torch.int32, device=gpu)
+    gates = torch.rand(3, 2, generator=g, device=gpu)
+    widx = torch.tensor(pick, dtype=torch.int32, device=gpu)
+    y = api.few_tokens_ffn(x[:3], ids, gates, gu, dn, expert_widx=widx)
+    ref = api.few_tokens_ffn(x[:3], ids, gates, few_of(gu), few_of(dn))
+    assert bool(torch.isfinite(y).all()) and torch.equal(y, ref)
