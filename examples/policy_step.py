@@ -6,7 +6,9 @@ framework's calls from end to end:
 
 The model is one MoE layer between a fixed embedding and a head, with random
 weights; the "rollout" is a fixed batch of tokens with advantages, whose
-routing the first pass records and every later step replays (Sec. 5). Run
+routing the first pass records and every later step replays (Sec. 5). The
+experts are updated by AdamW or by Muon; refresh() hands them to a rollout in 4
+bits, prompt() and decode() are its two ways through the layer. Run
 
     python examples/policy_step.py [steps]
 
@@ -22,7 +24,7 @@ import torch
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 
 from paper_2606_11867_amd import api  # noqa: E402
-from paper_2606_11867_amd.optimizer import AdamW  # noqa: E402
+from paper_2606_11867_amd.optimizer import AdamW, Muon  # noqa: E402
 
 BF16, F32 = torch.bfloat16, torch.float32
 
@@ -38,7 +40,7 @@ class PolicyStep:
     """Weights, workspaces and optimizers of the model, and its step."""
 
     def __init__(self, T=512, d=256, F=128, E=16, K=4, V=3000, dtype=BF16, state_bits=32, lr=3e-3, seed=0,
-                 device="cuda:0", entropy_coef=0.01, balance_coef=0.01):
+                 device="cuda:0", entropy_coef=0.01, balance_coef=0.01, muon=False):
         dev = torch.device(device)
         g = torch.Generator(device=dev).manual_seed(seed)
         self.T, self.d, self.F, self.E, self.K, self.V, self.dtype = T, d, F, E, K, V, dtype
@@ -62,9 +64,15 @@ class PolicyStep:
         self.ws, self.rws = api.workspace(T, K, E, dev), api.router_workspace(E, dev)
         self.fws, self.wws, self.lws = api.ffn_workspace(dev), api.wgrad_workspace(d, F, dev), api.logprobs_workspace(dev)
         kw = dict(lr=lr, weight_decay=0.01, state_bits=state_bits, zero_grads=True)
-        self.opts = [AdamW([self.gate_up, self.down, self.head], [self.d_gate_up, self.d_down, self.d_head], **kw),
-                     AdamW([self.router], [self.d_router], **kw)]
+        experts, d_experts = [self.gate_up, self.down], [self.d_gate_up, self.d_down]
+        if muon:  # gate and up of an expert are two matrices
+            self.opts = [Muon(experts, d_experts, lr=lr, weight_decay=0.01, parts=[2, 1], zero_grads=True),
+                         AdamW([self.head], [self.d_head], **kw), AdamW([self.router], [self.d_router], **kw)]
+        else:
+            self.opts = [AdamW([*experts, self.head], [*d_experts, self.d_head], **kw),
+                         AdamW([self.router], [self.d_router], **kw)]
         self.recorded = None  # the rollout's routing
+        self.rollout = None   # the rollout's experts, in 4 bits
 
     def forward(self):
         """Everything the backward needs; the loss is fwd["loss"]."""
@@ -115,13 +123,47 @@ class PolicyStep:
         return f["loss"]
 
 
+    def refresh(self):
+        """The experts in 4 bits, from the optimizer's masters where it has some;
+        into the same memory every time, which a captured rollout reads."""
+        experts = list((self.opts[0].masters or self.opts[0].params)[:2])
+        if self.rollout is None:
+            self.rollout = [api.mxfp4_quantize(t) for t in experts]
+        else:
+            for t, q in zip(experts, self.rollout):
+                api.mxfp4_quantize(t, out=q)
+
+    def _route(self, x):
+        return api.router_fwd(x.float() @ self.router.t(), self.K, stats=False)
+
+    def prompt(self, x):
+        """Logits of a prompt's tokens x [n, d] (bf16), by the grouped FFN in 4 bits."""
+        r, n = self._route(x), x.shape[0]
+        ws = api.workspace(n, self.K, self.E, x.device)
+        _, begin, _, offset = api.histogram_assign(r.ids, self.plan, ws)
+        x_perm, _, p2r = api.permute(x, r.ids, self.plan, begin, offset, n * self.K, ws)
+        y_perm = api.grouped_ffn_mxfp4_fwd(api.mxfp4_quantize(x_perm, n_rows=offset[-1:]), offset, self.plan.slot_widx,
+                                           *self.rollout)
+        return (x + api.combine(y_perm, p2r, r.gates, out_dtype=x.dtype)) @ self.head.t()
+
+    def decode(self, x):
+        """Logits of a decoding step's few tokens x [n, d]: the layer in two
+        launches, in 4 bits once refresh() has run."""
+        r = self._route(x)
+        experts = self.rollout or (self.gate_up, self.down)
+        return (x + api.few_tokens_ffn(x, r.ids, r.gates, *experts)) @ self.head.t()
+
+
 def main(steps=20):
-    for bits in (32, 8):
-        model = PolicyStep(state_bits=bits)
+    for bits, muon in ((32, False), (8, False), (32, True)):
+        model = PolicyStep(state_bits=bits, muon=muon)
         for i in range(steps):
             loss = model.step()
             if i % 5 == 0 or i == steps - 1:
-                print(f"{bits}-bit states, step {i}: loss {loss.item():.4f}")
+                print(f"{'Muon' if muon else f'{bits}-bit states'}, step {i}: loss {loss.item():.4f}")
+    model.refresh()
+    picked = model.prompt(model.x)[-4:].argmax(1), model.decode(model.x[-4:]).argmax(1)
+    print(f"rollout in 4 bits: {picked[0].tolist()} from the prompt, {picked[1].tolist()} decoding")
 
 
 if __name__ == "__main__":

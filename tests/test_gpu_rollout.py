@@ -6,6 +6,9 @@ after the weights have changed.
 Each part is compared with the oracle on the inputs that it was given, with the
 tolerances of its own tests; combine adds K products in fp32.
 """
+import importlib.util
+import os
+
 import numpy as np
 import pytest
 import torch
@@ -180,3 +183,48 @@ def test_graph_follows_the_weights(gpu):
         seen.append(y.clone())
         assert torch.equal(step(), seen[-1])
     assert not torch.equal(seen[0], seen[1])
+
+
+@pytest.fixture(scope="module")
+def example():
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "policy_step.py")
+    spec = importlib.util.spec_from_file_location("policy_step", path)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    return m
+
+
+@pytest.mark.parametrize("muon", [False, True])
+def test_example_rolls_out(gpu, example, muon):
+    """The example's layer: decoding in bf16, then steps, a refresh into the same
+    memory, prompt and decoding in 4 bits, the layer's part against the oracle."""
+    model = example.PolicyStep(T=96, d=256, F=128, E=6, K=2, V=301, muon=muon)
+    x = model.x[:24]
+    assert bool(torch.isfinite(model.decode(x)).all()) and model.rollout is None
+    model.step()
+    model.refresh()
+    first, at = [q.codes.clone() for q in model.rollout], [q.codes.data_ptr() for q in model.rollout]
+    before = model.gate_up.clone()
+    model.step()
+    assert not torch.equal(before, model.gate_up) and not model.d_gate_up.any()
+    model.refresh()
+    assert at == [q.codes.data_ptr() for q in model.rollout]
+    assert not all(torch.equal(a, q.codes) for a, q in zip(first, model.rollout))
+    assert model.prompt(x).shape == (24, 301) and bool(torch.isfinite(model.prompt(x)).all())
+    r = model._route(x)
+    vals = [R.mxfp4_values(q.codes.cpu().numpy(), q.scales.cpu().numpy()) for q in model.rollout]
+    for v, m in zip(vals, (model.opts[0].masters or model.opts[0].params)[:2]):
+        assert np.array_equal(v, R.mxfp4_values(*R.mxfp4_quantize(_np(m))))
+    ids, gates = r.ids.cpu().numpy(), _np(r.gates)
+    y = R.few_tokens(_np(x), ids, gates, *vals)
+    # the layer's output, its sum with x and the logits are each rounded to bf16
+    # (half a step of 2^-8); a product of 256 terms in fp32 is within 256 u of its
+    # magnitudes
+    lim = _limit(_np(x), ids, gates, *vals, None, y, "bf16")
+    hidden = _np(x) + y
+    lim += 2.0 ** -8 * (np.abs(hidden) + lim)
+    head = _np(model.head)
+    ref = hidden @ head.T
+    lim = lim @ np.abs(head).T + 256 * U * ((np.abs(hidden) + lim) @ np.abs(head).T)
+    lim += 2.0 ** -8 * (np.abs(ref) + lim)
+    assert np.all(np.abs(_np(model.decode(x)) - ref) <= lim)
