@@ -255,3 +255,17 @@ def test_far_elements(gpu):
         q = torch.zeros(shape[1:], device=gpu)
         Muon([q], [g[i]], lr=1.0, momentum=0.0, nesterov=False, scale=-1.0).step()
         assert (p[i] - q).norm() <= 2.0 ** -8 * q.norm() and q.norm() > 30
+
+
+def test_more_tensors_than_a_launch(gpu):
+    """60 tensors, small and large and empty ones in turn: three groups of
+    launches over one workspace."""
+    from paper_2606_11867_amd.optimizer import Muon
+    rng = np.random.default_rng(13)
+    shapes = [((0, 5, 6) if i % 10 == 3 else (70 + i, 90) if i % 3 == 0 else (2 + i, 40)) for i in range(60)]
+    gs = [torch.from_numpy(rng.standard_normal(s).astype(np.float32)).to(gpu) for s in shapes]
+    ps = [torch.zeros(s, device=gpu) for s in shapes]
+    Muon(ps, gs, lr=1.0, momentum=0.0, nesterov=False, scale=-1.0).step()
+    for p, g in zip(ps, gs):
+        if p.numel():
+            _x_close(_np(p), _np(g))
