@@ -893,16 +893,16 @@ int foremoe_few_tokens_ffn_mxfp4(const void* x, int64_t ld, int64_t T, int32_t d
  *   p = p (1 - lr weight_decay) - lr scale X
  * p is master where the record has one (param, of bf16, then gets its rounded
  * copy), else param itself. zero_grads != 0: grad is zero afterwards.
- * m and all sums are fp32, the norm's fp64. Where both sides are above 64, X is
+ * m and u are fp32, and so are all sums but the norm's, fp64. Where both sides are above 64, X is
  * held as two fp16 numbers (its rounding, and that of 2^10 times what it
  * leaves), G and b G + c G G as one; the products take the first of X (2^-11 of
  * an element, or 2^-33 where that is more), a X takes both, so that directions
  * that u does not have stay small. X is within about 2^-9 of its norm of the
  * exact one. Where s^2 or |b s^2 + c s^4| passes 255 for a singular value s of
  * an X on the way, fp16 overflows to infinity (with coefficients that converge
- * s stays below 1.3). Where a side is at most 64, all is fp32, and X the product
- * of a polynomial of the first G and the first X: within 2^-18 of its norm, or
- * about 2^-11 where u is close to singular.
+ * s stays below 1.3). Where a side is at most 64, all from u on is fp64, and the
+ * parameters are off by their own rounding, 2^-23 of X's norm, and by the
+ * rounding of fp64 that the steps multiply by a each, 2^-49 a^ns_steps.
  * A matrix with a NaN or infinite element, or whose u has one, becomes NaN;
  * the others do not.
  * tensors: HOST array, read during the call only; pointers aligned to their

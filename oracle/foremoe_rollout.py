@@ -111,8 +111,9 @@ def newton_schulz(x, coef, steps):
 
 
 def newton_schulz_held(x, coef, steps):
-    """The same with the roundings that the step's format has. A side of at most
-    64: G and the product of all M = a I + b G + c G G in fp32, X = Q X0. Else
+    """The same with the roundings that the step's format has, or coarser ones. A
+    side of at most 64: G and the product of all M = a I + b G + c G G in fp32, X =
+    Q X0 (the step has fp64 there, and forms G again after some steps). Else
     the products' factors in fp16, of X the first of two numbers; the last step
     does without the second (unless it is the first too)."""
     tall = x.shape[0] > x.shape[1]

@@ -55,10 +55,10 @@ struct MuonRec {
       double* squares;           // [batch, chunks]
     };
     struct {  // small matrices (m <= 64)
-      float* part;      // [batch, chunks, 64, 64]: of each chunk of columns u u^T over 2^(2 e)
-      int32_t* part_e;  // [batch, chunks]: e + 127
-      float* q;         // [batch, 64, 64]: Q
+      double* part;     // [batch, chunks, 10 tiles of 16 x 16]: of each chunk of columns u u^T
+      double* q;        // [batch, 64, 64]: Q
       double* inverse;  // [batch]: 1 / max(|u|, eps)
+      double* held;     // [batch, m, n]: X between two stages
     };
   };
 };
@@ -74,7 +74,9 @@ struct MuonArgs {
   int n_rec, nesterov, zero_grads, from;  // from: which X the launch reads
   int has_rest, put_rest;  // whether that X has its second numbers, and the written one
   uint32_t n_work;         // workgroups with work in a product's launch
-  int steps;
+  int steps;               // (of a stage, for small matrices)
+  int from_u, to_params;   // small matrices: whether the stage starts from u, and ends in the parameters
+  double coef[3];
   float momentum, a, b, c;
   double eps;
   const float* grad_scale;
@@ -525,24 +527,78 @@ __global__ __launch_bounds__(256) void muon_update_kernel(MuonArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// Matrices with a side of at most 64: three launches for all steps, in fp32.
-// With M = a I + b G + c G G, all of G, M and Q are polynomials of the first G
-// and commute: X = Q X0 with Q = M .. M, and the next G is M G M. So X is read
-// twice, for the first G and for Q X0, and the rest happens in the LDS of one
-// workgroup a matrix. (fp16 factors would move X of a matrix with a side below
-// 16 by up to 2^-6 of its norm, as one singular value's error does not average
-// out; fp32 ones move it by 2^-20, or 2^-11 where u is next to singular, whose
-// small directions G holds squared.) All of it is latency: the small ones of six
-// matrices with sides of 24 to 400 take 9, 27 and 13 us.
+// Matrices with a side of at most 64. With M = a I + b G + c G G, all of G, M
+// and Q are symmetric polynomials of the first G and commute: X = Q X0 with Q = M
+// .. M, and the next G is M G M. So X is read twice, for the first G and for
+// Q X0, and the rest happens in the LDS of one workgroup a matrix.
+//
+// All of it is fp64, and only so many steps at a time (a stage, see
+// small_stages): what G is off by where u has nothing, or next to nothing, is an
+// eigenvalue near 0 of either sign, which a step multiplies by a^2, where X itself
+// would have no such eigenvalue and grow by a. Once a negative one is no longer
+// small, M runs away with it. From an fp32 G that takes 8 to 10 steps of the
+// usual coefficients; from an fp64 one it stays below 2^-53 2^24, and the next
+// stage forms G again from X, which is held in fp64 in between. X comes out within
+// the rounding of fp32 whatever the rank of u and the number of steps (simulated:
+// 2^-24 of its norm after 16 steps, where the plain iteration in fp32 has filled
+// the empty directions). Latency bounds it: the small ones of six matrices with
+// sides of 24 to 400 take 8, 25 and 15 us (in fp32 9, 27 and 13).
 // ---------------------------------------------------------------------------
-constexpr int kSmall = 64, kSmallLD = 65, kSmallChunks = 64;
+constexpr int kSmall = 64, kSmallChunks = 64;
+constexpr int kSmallLD = 68;       // doubles of a row in LDS: 16 rows of 4 are 2 to a bank
+constexpr int kSmallTiles = 10;    // 16 x 16 tiles on and above the diagonal
+constexpr int kSmallThreads = 512; // of a matrix's steps: two wavefronts a SIMD
 
-// u of the 64 x 64 tile of the matrix whose first long index is l0, the small
-// side as rows, times `inv`, into LDS; zeros past the ends.
-template <bool GBF16, bool STORE_M>
-__device__ __forceinline__ void small_u(const MuonArgs& a, const MuonRec& r, int64_t base, int l0, double inv,
-                                        float (*u)[kSmallLD]) {
+typedef double f64x4 __attribute__((ext_vector_type(4)));
+typedef double SmallRow[kSmallLD];
+
+// Tile t of the upper triangle, column by column: those of a smaller matrix come first.
+__device__ __forceinline__ void small_tile(int t, int& ti, int& tj) {
+  tj = t < 1 ? 0 : t < 3 ? 1 : t < 6 ? 2 : 3;
+  ti = t - tj * (tj + 1) / 2;
+}
+
+// acc += that tile of A B^T, k below n (a multiple of 4). The matrix
+// instruction leaves row 4 q + lane / 16, column lane % 16 in element q.
+__device__ __forceinline__ f64x4 small_product(const SmallRow* A, const SmallRow* B, int ti, int tj, int n, f64x4 acc) {
+  const int lane = lane64(), l = lane & 15, h = lane >> 4;
+#pragma unroll 4
+  for (int k = 0; k < n; k += 4)
+    acc = __builtin_amdgcn_mfma_f64_16x16x4f64(A[16 * ti + l][k + h], B[16 * tj + l][k + h], acc, 0, 0, 0);
+  return acc;
+}
+
+// A tile of a symmetric matrix, on both sides of the diagonal: f(q, i, j) gives
+// element q. Of a tile on the diagonal the upper half counts, so that the matrix
+// is symmetric to the last bit and its rows serve as its columns.
+template <class F>
+__device__ __forceinline__ void small_put(SmallRow* M, int ti, int tj, F&& f) {
+  const int lane = lane64(), j = 16 * tj + (lane & 15);
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int i = 16 * ti + 4 * q + (lane >> 4);
+    const double v = f(q, i, j);
+    if (i <= j) M[i][j] = v, M[j][i] = v;
+  }
+}
+
+// The 64 x 64 tile of the matrix whose first long index is l0, the small side as
+// rows, into LDS; zeros past the ends. In the first stage it is u, times inv,
+// otherwise X. MOMENT: m is updated on the way, and nothing is scaled.
+template <bool GBF16, bool MOMENT>
+__device__ __forceinline__ void small_x(const MuonArgs& a, const MuonRec& r, int64_t matrix, int l0, double inv,
+                                        SmallRow* u) {
   const bool tall = r.rows > r.cols;
+  const int64_t base = matrix * (int64_t)r.rows * r.cols;
+  if (!a.from_u) {
+    const int m = tall ? r.cols : r.rows, n = tall ? r.rows : r.cols;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+      const int i = k * 4 + (threadIdx.x >> 6), j = threadIdx.x & 63;
+      u[i][j] = i < m && l0 + j < n ? r.held[base + (int64_t)i * n + l0 + j] : 0.0;
+    }
+    return;
+  }
   const float gs = a.grad_scale ? *a.grad_scale : 1.0f;
   const int r0 = tall ? l0 : 0, c0 = tall ? 0 : l0;
 #pragma unroll
@@ -554,12 +610,12 @@ __device__ __forceinline__ void small_u(const MuonArgs& a, const MuonRec& r, int
       const int64_t i = base + (int64_t)rr * r.cols + cc;
       float g[4] = {0, 0, 0, 0};
       get4<false>(r.m, i, left, r.wide, v);
-      if (STORE_M || a.nesterov) {
+      if (MOMENT || a.nesterov) {
         get4<GBF16>(r.grad, i, left, r.wide, g);
 #pragma unroll
         for (int e = 0; e < 4; ++e) g[e] *= gs;
       }
-      if constexpr (STORE_M) {
+      if constexpr (MOMENT) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = fmaf(a.momentum, v[e], g[e]);
         put4<false>(r.m, i, left, r.wide, v);
@@ -570,213 +626,175 @@ __device__ __forceinline__ void small_u(const MuonArgs& a, const MuonRec& r, int
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         if (a.nesterov) v[e] = fmaf(a.momentum, v[e], g[e]);
-        v[e] = e >= left ? 0.0f : (STORE_M ? v[e] : (float)((double)v[e] * inv));
+        if (e >= left) v[e] = 0.0f;
       }
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      if (tall) u[tc + e][tr] = v[e];
-      else u[tr][tc + e] = v[e];
+      const double x = MOMENT ? (double)v[e] : (double)v[e] * inv;
+      if (tall) u[tc + e][tr] = x;
+      else u[tr][tc + e] = x;
     }
   }
 }
 
-// A 32 x 32 quarter of A B (TRANS: A B^T) of LDS matrices, k below n: block
-// (wave / 2, wave % 2) of the wavefront, the sums as the matrix instruction
-// leaves them (row 8 (q / 4) + 4 (lane / 32) + q % 4, column lane % 32).
-template <bool TRANS>
-__device__ __forceinline__ f32x16 small_product(const float (*A)[kSmallLD], const float (*B)[kSmallLD], int n) {
-  const int lane = lane64(), wave = wave_id(), l = lane & 31, h = lane >> 5;
-  const int i = 32 * (wave >> 1) + l, j = 32 * (wave & 1) + l;
-  f32x16 acc;
-#pragma unroll
-  for (int q = 0; q < 16; ++q) acc[q] = 0.0f;
-#pragma unroll 8
-  for (int k = 0; k < n; k += 2)
-    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(A[i][k + h], TRANS ? B[j][k + h] : B[k + h][j], acc, 0, 0, 0);
-  return acc;
-}
-template <class F>
-__device__ __forceinline__ void small_each(F&& f) {  // f(q, row, column)
-  const int lane = lane64(), wave = wave_id();
-#pragma unroll
-  for (int q = 0; q < 16; ++q)
-    f(q, 32 * (wave >> 1) + 8 * (q / 4) + 4 * (lane >> 5) + q % 4, 32 * (wave & 1) + (lane & 31));
-}
-
-// The same by wavefronts of 16 x 16, for matrices with a side of at most 32.
-__device__ __forceinline__ f32x4 small_product16(const float (*A)[kSmallLD], const float (*B)[kSmallLD], int n) {
-  const int lane = lane64(), wave = wave_id(), l = lane & 15, h = lane >> 4;
-  const int i = 16 * (wave >> 1) + l, j = 16 * (wave & 1) + l;
-  f32x4 acc = {0, 0, 0, 0};
-#pragma unroll 4
-  for (int k = 0; k < n; k += 4) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(A[i][k + h], B[k + h][j], acc, 0, 0, 0);
-  return acc;
-}
-template <class F>
-__device__ __forceinline__ void small_each16(F&& f) {
-  const int lane = lane64(), wave = wave_id();
-#pragma unroll
-  for (int q = 0; q < 4; ++q) f(q, 16 * (wave >> 1) + 4 * (lane >> 4) + q, 16 * (wave & 1) + (lane & 15));
-}
-
-// m, and a chunk's part of u u^T. The sums are of u over a power of two that
-// the chunk's largest element gives, so that no square leaves the range of fp32.
+// A chunk's part of u u^T (squares of fp32 numbers are far inside fp64's range),
+// with m on the way, or of X X^T.
 template <bool GBF16>
 __global__ __launch_bounds__(256) void muon_small_gram_kernel(MuonArgs a) {
   const int ri = find_rec(a, blockIdx.x);
   const MuonRec& r = a.rec[ri];
   const uint32_t b = blockIdx.x - a.first.at[ri];
   const int64_t matrix = b / r.chunks, chunk = b % r.chunks;
-  const int n = r.rows > r.cols ? r.rows : r.cols;  // the long side, in tiles of 64
-  const int tiles = (n + 63) / 64, t0 = (int)(tiles * chunk / r.chunks), t1 = (int)(tiles * (chunk + 1) / r.chunks);
-  const int64_t base = matrix * (int64_t)r.rows * r.cols;
-  __shared__ float u[kSmall][kSmallLD];
-  __shared__ uint32_t most[4];
-  f32x16 acc;
+  const bool tall = r.rows > r.cols;
+  const int n = tall ? r.rows : r.cols, nt = ((tall ? r.cols : r.rows) + 15) / 16;
+  const int blocks = (n + 63) / 64;  // of the long side
+  const int b0 = (int)(blocks * chunk / r.chunks), b1 = (int)(blocks * (chunk + 1) / r.chunks);
+  const int wave = wave_id(), tiles = nt * (nt + 1) / 2;
+  __shared__ SmallRow u[kSmall];
+  f64x4 acc[3];
 #pragma unroll
-  for (int q = 0; q < 16; ++q) acc[q] = 0.0f;
-  int e = 0;  // biased exponent that the sums are over
-  for (int t = t0; t < t1; ++t) {
+  for (int p = 0; p < 3; ++p) acc[p] = f64x4{0, 0, 0, 0};
+  for (int t = b0; t < b1; ++t) {
     __syncthreads();
-    small_u<GBF16, true>(a, r, base, t * 64, 1.0, u);
+    small_x<GBF16, true>(a, r, matrix, t * 64, 1.0, u);
     __syncthreads();
-    uint32_t top = 0;
-    for (int i = threadIdx.x; i < 4096; i += 256) {
-      const uint32_t v = __float_as_uint(u[i >> 6][i & 63]) & 0x7fffffffu;
-      top = v > top ? v : top;
+#pragma unroll
+    for (int p = 0; p < 3; ++p) {
+      int ti, tj;
+      small_tile(wave + 4 * p, ti, tj);
+      if (wave + 4 * p < tiles) acc[p] = small_product(u, u, ti, tj, kSmall, acc[p]);
     }
-#pragma unroll
-    for (int o = 32; o; o >>= 1) {
-      const uint32_t v = __shfl_xor(top, o, 64);
-      top = v > top ? v : top;
-    }
-    if (lane64() == 0) most[wave_id()] = top;
-    __syncthreads();
-    top = 0;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) top = most[w] > top ? most[w] : top;
-    const int et = (int)(top >> 23);
-    if (et > e) {
-      const float down = ldexpf(1.0f, 2 * (e - et));
-#pragma unroll
-      for (int q = 0; q < 16; ++q) acc[q] *= down;
-      e = et;
-    }
-    for (int i = threadIdx.x; i < 4096; i += 256) u[i >> 6][i & 63] = ldexpf(u[i >> 6][i & 63], 127 - e);
-    __syncthreads();
-    const f32x16 s = small_product<true>(u, u, kSmall);
-#pragma unroll
-    for (int q = 0; q < 16; ++q) acc[q] += s[q];
   }
-  float* to = r.part + (matrix * r.chunks + chunk) * (kSmall * kSmall);
-  small_each([&](int q, int i, int j) { to[i * kSmall + j] = acc[q]; });
-  if (threadIdx.x == 0) r.part_e[matrix * r.chunks + chunk] = e;
+  double* to = r.part + (matrix * r.chunks + chunk) * (kSmallTiles * 256) + lane64();
+#pragma unroll
+  for (int p = 0; p < 3; ++p)
+    if (wave + 4 * p < tiles)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) to[(wave + 4 * p) * 256 + q * 64] = acc[p][q];
 }
 
-// All steps of a matrix in LDS. product(A, B) gives this wavefront's part of A
-// B, each(f) its elements.
-template <class Product, class Each>
-__device__ __forceinline__ void small_steps(const MuonArgs& a, float (*G)[kSmallLD], float (*M)[kSmallLD],
-                                            float (*S)[kSmallLD], float (*Q)[kSmallLD], Product product, Each each) {
-  for (int t = 0; t < a.steps; ++t) {
-    const auto s = product(G, G);
-    each([&](int q, int i, int j) { M[i][j] = (i == j ? a.a : 0.0f) + fmaf(a.b, G[i][j], a.c * s[q]); });
-    __syncthreads();
-    const auto nq = product(M, Q);
-    if (t + 1 < a.steps) {
-      const auto mg = product(M, G);
-      each([&](int q, int i, int j) { S[i][j] = mg[q]; });
-    }
-    __syncthreads();
-    each([&](int q, int i, int j) { Q[i][j] = nq[q]; });
-    if (t + 1 < a.steps) {
-      const auto ng = product(S, M);
-      each([&](int q, int i, int j) { G[i][j] = ng[q]; });
-    }
-    __syncthreads();
-  }
-}
-
-// Q and 1 / max(|u|, eps) of a matrix.
-__global__ __launch_bounds__(256) void muon_small_steps_kernel(MuonArgs a) {
+// Q of a stage, and in the first one 1 / max(|u|, eps).
+__global__ __launch_bounds__(kSmallThreads) void muon_small_steps_kernel(MuonArgs a) {
+  constexpr int NW = kSmallThreads / 64;
   const int ri = find_rec(a, blockIdx.x);
   const MuonRec& r = a.rec[ri];
   const int64_t matrix = blockIdx.x - a.first.at[ri];
-  const int m = r.rows < r.cols ? r.rows : r.cols, n = (m + 3) & ~3, tid = threadIdx.x;
-  __shared__ float G[kSmall][kSmallLD], M[kSmall][kSmallLD], S[kSmall][kSmallLD], Q[kSmall][kSmallLD];
-  const float* part = r.part + matrix * r.chunks * (kSmall * kSmall);
-  const int32_t* part_e = r.part_e + matrix * r.chunks;
-  const int lane = lane64();
-  const int mine = lane < (int)r.chunks ? part_e[lane] : 0;  // (at most 64 chunks)
-  int e = mine;
-#pragma unroll
-  for (int o = 32; o; o >>= 1) {
-    const int other = __shfl_xor(e, o, 64);
-    e = other > e ? other : e;
+  const int m = r.rows < r.cols ? r.rows : r.cols, n = (m + 3) & ~3, nt = (m + 15) / 16, tiles = nt * (nt + 1) / 2;
+  const int tid = threadIdx.x, lane = lane64(), wave = wave_id();
+  __shared__ SmallRow G[kSmall], M[kSmall], S[kSmall], Q[kSmall];
+  const double* part = r.part + matrix * r.chunks * (kSmallTiles * 256);
+  for (int o = tid; o < tiles * 256; o += kSmallThreads) {
+    double s = 0;
+#pragma unroll 8
+    for (int c = 0; c < (int)r.chunks; ++c) s += part[c * (kSmallTiles * 256) + o];
+    int ti, tj;
+    small_tile(o >> 8, ti, tj);
+    const int i = 16 * ti + (o >> 6 & 3) * 4 + (lane >> 4), j = 16 * tj + (lane & 15);
+    if (i <= j) G[i][j] = s, G[j][i] = s;
   }
-  const float scale = ldexpf(1.0f, 2 * (mine - e));
-  // this thread's elements: column tid % 64, rows tid / 64 + 4 k
-  const int col = tid & 63;
-  float s[16];
-#pragma unroll
-  for (int k = 0; k < 16; ++k) s[k] = 0.0f;
-#pragma unroll 4
-  for (int c = 0; c < (int)r.chunks; ++c) {
-    const float by = __shfl(scale, c, 64);
-#pragma unroll
-    for (int k = 0; k < 16; ++k) s[k] = fmaf(part[c * (kSmall * kSmall) + tid + 256 * k], by, s[k]);
-  }
-#pragma unroll
-  for (int k = 0; k < 16; ++k) G[(tid >> 6) + 4 * k][col] = s[k];
+  for (int o = tid; o < kSmall * kSmall; o += kSmallThreads) Q[o >> 6][o & 63] = (o >> 6) == (o & 63) ? 1.0 : 0.0;
   __syncthreads();
-  // |u|^2 over 2^(2 (e - 127)), summed in the same order by every thread
-  double trace = 0;
-  for (int i = 0; i < m; ++i) trace += G[i][i];
-  const double norm = e == 255 ? (double)NAN : ldexp(sqrt(trace), e - 127);
-  const double den = !(norm <= a.eps) ? norm : a.eps;
-  // nothing in it: no move; not finite: NaN everywhere
-  const double inv = den == 0 ? 0.0 : 1.0 / den;
-  const double by = ldexp(inv, e - 127);
-  __syncthreads();
+  if (a.from_u) {
+    // |u|^2, summed in the same order by every wavefront
+    double s = lane < m ? G[lane][lane] : 0.0;
 #pragma unroll
-  for (int k = 0; k < 16; ++k) {
-    const int row = (tid >> 6) + 4 * k;
-    G[row][col] = (float)(s[k] * by * by);
-    Q[row][col] = row == col ? 1.0f : 0.0f;
+    for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o, 64);
+    const double norm = sqrt(s);
+    const double den = !(norm <= a.eps) ? norm : a.eps;
+    // nothing in it: no move; not finite: NaN everywhere
+    const double inv = den == 0 ? 0.0 : (isinf(den) ? (double)NAN : 1.0 / den);
+    __syncthreads();
+    for (int o = tid; o < 16 * nt * 64; o += kSmallThreads)
+      if ((o & 63) < 16 * nt) G[o >> 6][o & 63] *= inv * inv;
+    if (tid == 0) r.inverse[matrix] = inv;
+    __syncthreads();
   }
-  __syncthreads();
-  if (m <= 32) {
-    // (elements past the matrix: zeros, but for the diagonal of M and Q)
-    small_steps(
-        a, G, M, S, Q, [&](auto A, auto B) { return small_product16(A, B, n); }, [&](auto f) { small_each16(f); });
-  } else {
-    small_steps(
-        a, G, M, S, Q, [&](auto A, auto B) { return small_product<false>(A, B, n); }, [&](auto f) { small_each(f); });
+  for (int t = 0; t < a.steps; ++t) {
+    const bool more = t + 1 < a.steps;
+    f64x4 q[2];
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      int ti, tj;
+      small_tile(wave + NW * p, ti, tj);
+      if (wave + NW * p >= tiles) continue;
+      const f64x4 s = small_product(G, G, ti, tj, n, f64x4{0, 0, 0, 0});
+      small_put(M, ti, tj, [&](int e, int i, int j) {
+        return (i == j ? a.coef[0] : 0.0) + fma(a.coef[1], G[i][j], a.coef[2] * s[e]);
+      });
+    }
+    __syncthreads();
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      int ti, tj;
+      small_tile(wave + NW * p, ti, tj);
+      if (wave + NW * p >= tiles) continue;
+      if (more) {
+        const f64x4 s = small_product(M, G, ti, tj, n, f64x4{0, 0, 0, 0});
+        small_put(S, ti, tj, [&](int e, int, int) { return s[e]; });
+      }
+      q[p] = small_product(M, Q, ti, tj, n, f64x4{0, 0, 0, 0});
+    }
+    __syncthreads();
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      int ti, tj;
+      small_tile(wave + NW * p, ti, tj);
+      if (wave + NW * p >= tiles) continue;
+      small_put(Q, ti, tj, [&](int e, int, int) { return q[p][e]; });
+      if (more) {
+        const f64x4 g = small_product(S, M, ti, tj, n, f64x4{0, 0, 0, 0});
+        small_put(G, ti, tj, [&](int e, int, int) { return g[e]; });
+      }
+    }
+    __syncthreads();
   }
-  for (int i = tid; i < kSmall * kSmall; i += 256) r.q[matrix * (kSmall * kSmall) + i] = Q[i >> 6][i & 63];
-  if (tid == 0) r.inverse[matrix] = inv;
+  for (int o = tid; o < kSmall * kSmall; o += kSmallThreads) r.q[matrix * (kSmall * kSmall) + o] = Q[o >> 6][o & 63];
 }
 
-// X = Q X0 for 64 of the long side, and the parameters.
+// X = Q X for 64 of the long side: into the parameters, or held for the next
+// stage in place of what it was.
 template <bool GBF16, bool PBF16>
-__global__ __launch_bounds__(256) void muon_small_update_kernel(MuonArgs a) {
+__global__ __launch_bounds__(256) void muon_small_apply_kernel(MuonArgs a) {
   const int ri = find_rec(a, blockIdx.x);
   const MuonRec& r = a.rec[ri];
   const uint32_t b = blockIdx.x - a.first.at[ri];
   const bool tall = r.rows > r.cols;
-  const int tiles = ((tall ? r.rows : r.cols) + 63) / 64, tid = threadIdx.x;
-  const int64_t matrix = b / tiles;
-  const int l0 = (int)(b % tiles) * 64, m = tall ? r.cols : r.rows, n = (m + 1) & ~1;
+  const int m = tall ? r.cols : r.rows, n = tall ? r.rows : r.cols;
+  const int blocks = (n + 63) / 64, tid = threadIdx.x, lane = lane64(), wave = wave_id();
+  const int64_t matrix = b / blocks;
+  const int l0 = (int)(b % blocks) * 64;
   const int64_t base = matrix * (int64_t)r.rows * r.cols;
-  __shared__ float u[kSmall][kSmallLD], Q[kSmall][kSmallLD];
+  __shared__ SmallRow u[kSmall], Q[kSmall];
   for (int i = tid; i < kSmall * kSmall; i += 256) Q[i >> 6][i & 63] = r.q[matrix * (kSmall * kSmall) + i];
-  small_u<GBF16, false>(a, r, base, l0, r.inverse[matrix], u);
+  small_x<GBF16, false>(a, r, matrix, l0, a.from_u ? r.inverse[matrix] : 1.0, u);
   __syncthreads();
-  const f32x16 x = small_product<false>(Q, u, n);
+  // rows 16 wave .. of X, all 64 columns
+  const int l = lane & 15, h = lane >> 4;
+  f64x4 x[4];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) x[c] = f64x4{0, 0, 0, 0};
+  if (16 * wave < m) {
+#pragma unroll 2
+    for (int k = 0; k < m; k += 4) {  // (u is zero past m)
+      const double q = Q[16 * wave + l][k + h];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) x[c] = __builtin_amdgcn_mfma_f64_16x16x4f64(q, u[k + h][16 * c + l], x[c], 0, 0, 0);
+    }
+  }
   __syncthreads();
-  small_each([&](int q, int i, int j) { u[i][j] = x[q] * kHeld; });
+#pragma unroll
+  for (int c = 0; c < 4; ++c)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) u[16 * wave + 4 * q + h][16 * c + l] = x[c][q];
   __syncthreads();
+  if (!a.to_params) {
+    for (int o = tid; o < m * 64; o += 256) {
+      const int i = o >> 6, j = o & 63;
+      if (l0 + j < n) r.held[base + (int64_t)i * n + l0 + j] = u[i][j];
+    }
+    return;
+  }
   const int r0 = tall ? l0 : 0, c0 = tall ? 0 : l0, i0 = tid >> 4, j = (tid & 15) * 4;
   update_n<PBF16, 4>(
       r,
@@ -787,8 +805,43 @@ __global__ __launch_bounds__(256) void muon_small_update_kernel(MuonArgs a) {
       [&](int k, float* v) {
         const int i = i0 + 16 * k;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = tall ? u[j + e][i] : u[i][j + e];
+        for (int e = 0; e < 4; ++e) v[e] = (float)(tall ? u[j + e][i] : u[i][j + e]) * kHeld;
       });
+}
+
+// ---------------------------------------------------------------------------
+// What the coefficients make of singular values, and the stages that follow.
+// ---------------------------------------------------------------------------
+// The largest |p + q l + r l^2| for l in [0, top].
+double most_of(double p, double q, double r, double top) {
+  const double v = fmax(fabs(p), fabs(p + (q + r * top) * top)), at = -q / (2 * r);
+  return at > 0 && at < top ? fmax(v, fabs(p + 0.5 * q * at)) : v;
+}
+
+// Stages of small matrices. An eigenvalue l of G becomes f(l) = l M(l)^2, so what
+// it is off by is multiplied by |f'| = |M(l)| |a + 3 b l + 5 c l^2| (a^2 near
+// 0). A stage ends before the product of the steps' largest passes 2^24.
+struct Stages {
+  int n, steps[16];
+};
+Stages small_stages(const double* coef, int ns_steps) {
+  const double a = coef[0], b = coef[1], c = coef[2];
+  Stages g{};
+  g.n = 1;
+  double s = 1.0, off = 1.0;  // singular values are at most s: 1 at first, as |X| is
+  for (int t = 0; t < ns_steps; ++t) {
+    const double top = s * s;
+    const double by = fmax(1.0, most_of(a, b, c, top) * most_of(a, 3 * b, 5 * c, top));
+    if (g.steps[g.n - 1] > 0 && !(off * by <= (double)(1 << 24))) ++g.n, off = 1.0;
+    off *= by, ++g.steps[g.n - 1];
+    // the largest |s M(s^2)|: at an end, or where a + 3 b l + 5 c l^2 is 0
+    double most = s * fabs(a + (b + c * top) * top);
+    const double h = 1.5 * b, d = h * h - 5 * c * a, t2 = -(h + copysign(sqrt(d), h));
+    for (double l : {t2 / (5 * c), a / t2})
+      if (l > 0 && l < top) most = fmax(most, sqrt(l) * fabs(a + (b + c * l) * l));
+    s = most;
+  }
+  return g;
 }
 
 int64_t pad_side(int64_t n, int tile) { return (n + tile - 1) / tile * tile; }
@@ -812,10 +865,10 @@ size_t lay_out(const foremoe_muon_tensor& t, int tile, size_t at, char* ws, Muon
     // parts of u u^T to be joined by one workgroup: 16, more for the longest
     const int64_t most = tiles < 256 ? 16 : kSmallChunks;
     q.chunks = (uint32_t)(tiles < most ? tiles : most);
-    q.part = (float*)take((size_t)t.batch * q.chunks * kSmall * kSmall * 4);
-    q.part_e = (int32_t*)take((size_t)t.batch * q.chunks * 4);
-    q.q = (float*)take((size_t)t.batch * kSmall * kSmall * 4);
+    q.part = (double*)take((size_t)t.batch * q.chunks * kSmallTiles * 256 * 8);
+    q.q = (double*)take((size_t)t.batch * kSmall * kSmall * 8);
     q.inverse = (double*)take((size_t)t.batch * 8);
+    q.held = (double*)take((size_t)t.batch * s * l * 8);
     if (r) *r = q;
     return at;
   }
@@ -914,17 +967,22 @@ static unsigned grid_of(MuonArgs& a, Count count) {
   return (unsigned)n;
 }
 
-static void launch_small(MuonArgs& a, bool pb16, bool gb16, hipStream_t st) {
-  unsigned n = grid_of(a, [](const MuonRec& r) { return (uint64_t)r.chunks; });
-  if (gb16) hipLaunchKernelGGL((muon_small_gram_kernel<true>), dim3(n), dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((muon_small_gram_kernel<false>), dim3(n), dim3(256), 0, st, a);
-  n = grid_of(a, [](const MuonRec&) { return (uint64_t)1; });
-  hipLaunchKernelGGL(muon_small_steps_kernel, dim3(n), dim3(256), 0, st, a);
-  n = grid_of(a, [](const MuonRec& r) { return (uint64_t)((r.rows > r.cols ? r.rows : r.cols) + 63) / 64; });
-  if (gb16 && pb16) hipLaunchKernelGGL((muon_small_update_kernel<true, true>), dim3(n), dim3(256), 0, st, a);
-  else if (gb16) hipLaunchKernelGGL((muon_small_update_kernel<true, false>), dim3(n), dim3(256), 0, st, a);
-  else if (pb16) hipLaunchKernelGGL((muon_small_update_kernel<false, true>), dim3(n), dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((muon_small_update_kernel<false, false>), dim3(n), dim3(256), 0, st, a);
+static void launch_small(MuonArgs& a, const Stages& stages, bool pb16, bool gb16, hipStream_t st) {
+  const int steps = a.steps;
+  for (int k = 0; k < stages.n; ++k) {
+    a.steps = stages.steps[k], a.from_u = k == 0, a.to_params = k + 1 == stages.n;
+    unsigned n = grid_of(a, [](const MuonRec& r) { return (uint64_t)r.chunks; });
+    if (gb16) hipLaunchKernelGGL((muon_small_gram_kernel<true>), dim3(n), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((muon_small_gram_kernel<false>), dim3(n), dim3(256), 0, st, a);
+    n = grid_of(a, [](const MuonRec&) { return (uint64_t)1; });
+    hipLaunchKernelGGL(muon_small_steps_kernel, dim3(n), dim3(kSmallThreads), 0, st, a);
+    n = grid_of(a, [](const MuonRec& r) { return (uint64_t)((r.rows > r.cols ? r.rows : r.cols) + 63) / 64; });
+    if (gb16 && pb16) hipLaunchKernelGGL((muon_small_apply_kernel<true, true>), dim3(n), dim3(256), 0, st, a);
+    else if (gb16) hipLaunchKernelGGL((muon_small_apply_kernel<true, false>), dim3(n), dim3(256), 0, st, a);
+    else if (pb16) hipLaunchKernelGGL((muon_small_apply_kernel<false, true>), dim3(n), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((muon_small_apply_kernel<false, false>), dim3(n), dim3(256), 0, st, a);
+  }
+  a.steps = steps;
 }
 
 // (a grid of a multiple of the XCDs: see xcd_virtual_id)
@@ -1027,6 +1085,8 @@ int foremoe_muon_step(const foremoe_muon_tensor* tensors, int32_t n_tensors, for
   MuonArgs a{};
   a.nesterov = nesterov != 0, a.zero_grads = zero_grads != 0, a.grad_scale = grad_scale, a.steps = ns_steps;
   a.momentum = (float)momentum, a.a = (float)coef[0], a.b = (float)coef[1], a.c = (float)coef[2], a.eps = eps;
+  for (int i = 0; i < 3; ++i) a.coef[i] = coef[i];
+  const Stages stages = small_stages(coef, ns_steps);
   const bool pb16 = param_dtype == FOREMOE_BF16, gb16 = grad_dtype == FOREMOE_BF16;
   hipStream_t st = (hipStream_t)stream;
   int rc = FOREMOE_OK;
@@ -1048,7 +1108,7 @@ int foremoe_muon_step(const foremoe_muon_tensor* tensors, int32_t n_tensors, for
         r.decay = (float)(1 - lr * t.weight_decay), r.move = (float)(lr * t.scale);
       }
       if (a.n_rec == 0) continue;
-      if (small) launch_small(a, pb16, gb16, st);
+      if (small) launch_small(a, stages, pb16, gb16, st);
       else launch_large(a, tiles, pb16, gb16, st);
       rc = check_launch("muon_step");
       if (rc != FOREMOE_OK) break;
