@@ -898,9 +898,9 @@ int foremoe_few_tokens_ffn_mxfp4(const void* x, int64_t ld, int64_t T, int32_t d
  * leaves), G and b G + c G G as one; the products take the first of X (2^-11 of
  * an element, or 2^-33 where that is more), a X takes both, so that directions
  * that u does not have stay small. X is within about 2^-9 of its norm of the
- * exact one. Where s^2 or |b s^2 + c s^4| passes 255 for a singular value s of
- * an X on the way, fp16 overflows to infinity (with coefficients that converge
- * s stays below 1.3). Where a side is at most 64, all from u on is fp64, and the
+ * exact one. Coefficients with which s^2 or |b s^2 + c s^4| could pass 250 for a
+ * singular value s of an X on the way, from s = 1 at most, are refused
+ * (FOREMOE_EUNSUPPORTED; with those that converge s stays below 1.3). Where a side is at most 64, all from u on is fp64, and the
  * parameters are off by their own rounding, 2^-23 of X's norm, and by the
  * rounding of fp64 that the steps multiply by a each, 2^-49 a^ns_steps.
  * A matrix with a NaN or infinite element, or whose u has one, becomes NaN;

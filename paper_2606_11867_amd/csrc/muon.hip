@@ -818,30 +818,53 @@ double most_of(double p, double q, double r, double top) {
   return at > 0 && at < top ? fmax(v, fabs(p + 0.5 * q * at)) : v;
 }
 
-// Stages of small matrices. An eigenvalue l of G becomes f(l) = l M(l)^2, so what
-// it is off by is multiplied by |f'| = |M(l)| |a + 3 b l + 5 c l^2| (a^2 near
-// 0). A stage ends before the product of the steps' largest passes 2^24.
+// One step on an X whose singular values are at most s.
+struct Reach {
+  double s;     // what they are at most afterwards: the largest |s M(s^2)|
+  double poly;  // the largest |b s^2 + c s^4|
+  double off;   // an eigenvalue l of G becomes f(l) = l M(l)^2: the largest |f'| = |M(l)| |a + 3 b l + 5 c l^2|, or 1
+};
+Reach reach(const double* coef, double s) {
+  const double a = coef[0], b = coef[1], c = coef[2], top = s * s;
+  Reach r;
+  r.poly = most_of(0.0, b, c, top);
+  r.off = fmax(1.0, most_of(a, b, c, top) * most_of(a, 3 * b, 5 * c, top));
+  // s M(s^2) is largest at an end, or where a + 3 b l + 5 c l^2 is 0
+  r.s = s * fabs(a + (b + c * top) * top);
+  const double h = 1.5 * b, t = -(h + copysign(sqrt(h * h - 5 * c * a), h));
+  for (double l : {t / (5 * c), a / t})
+    if (l > 0 && l < top) r.s = fmax(r.s, sqrt(l) * fabs(a + (b + c * l) * l));
+  return r;
+}
+
+// Stages of small matrices: what G is off by is multiplied by `off` each step (a^2
+// near 0). A stage ends before their product passes 2^24.
 struct Stages {
   int n, steps[16];
 };
 Stages small_stages(const double* coef, int ns_steps) {
-  const double a = coef[0], b = coef[1], c = coef[2];
   Stages g{};
   g.n = 1;
-  double s = 1.0, off = 1.0;  // singular values are at most s: 1 at first, as |X| is
+  double s = 1.0, off = 1.0;  // (|X| is 1 at first)
   for (int t = 0; t < ns_steps; ++t) {
-    const double top = s * s;
-    const double by = fmax(1.0, most_of(a, b, c, top) * most_of(a, 3 * b, 5 * c, top));
-    if (g.steps[g.n - 1] > 0 && !(off * by <= (double)(1 << 24))) ++g.n, off = 1.0;
-    off *= by, ++g.steps[g.n - 1];
-    // the largest |s M(s^2)|: at an end, or where a + 3 b l + 5 c l^2 is 0
-    double most = s * fabs(a + (b + c * top) * top);
-    const double h = 1.5 * b, d = h * h - 5 * c * a, t2 = -(h + copysign(sqrt(d), h));
-    for (double l : {t2 / (5 * c), a / t2})
-      if (l > 0 && l < top) most = fmax(most, sqrt(l) * fabs(a + (b + c * l) * l));
-    s = most;
+    const Reach r = reach(coef, s);
+    if (g.steps[g.n - 1] > 0 && !(off * r.off <= (double)(1 << 24))) ++g.n, off = 1.0;
+    off *= r.off, s = r.s, ++g.steps[g.n - 1];
   }
   return g;
+}
+
+// Whether G and P of large matrices stay within fp16, 2^8 times as large as they
+// are held: below 255.8, of which the format's roundings may take some.
+constexpr double kHalfMost = 250.0;
+bool within_half(const double* coef, int ns_steps) {
+  double s = 1.0;
+  for (int t = 0; t < ns_steps; ++t) {
+    const Reach r = reach(coef, s);
+    if (!(s * s <= kHalfMost && r.poly <= kHalfMost)) return false;
+    s = r.s;
+  }
+  return true;
 }
 
 int64_t pad_side(int64_t n, int tile) { return (n + tile - 1) / tile * tile; }
@@ -1062,13 +1085,13 @@ int foremoe_muon_step(const foremoe_muon_tensor* tensors, int32_t n_tensors, for
   REQUIRE(isfinite(eps) && eps >= 0, "muon_step: eps must be finite and not negative");
   REQUIRE(!misaligned(grad_scale, 4), "muon_step: grad_scale misaligned");
   const uintptr_t pb = param_dtype == FOREMOE_BF16 ? 2 : 4, gb = grad_dtype == FOREMOE_BF16 ? 2 : 4;
-  bool some = false;
+  bool some = false, large = false;
   for (int i = 0; i < n_tensors; ++i) {
     const foremoe_muon_tensor& t = tensors[i];
     const int rc = check_tensor(t, i);
     if (rc != FOREMOE_OK) return rc;
     if (t.batch == 0) continue;
-    some = true;
+    some = true, large = large || !is_small(t);
     REQUIRE(t.param && t.grad && t.m, "muon_step: tensor %d: NULL pointer", i);
     REQUIRE(!t.master || param_dtype == FOREMOE_BF16, "muon_step: tensor %d: a master goes with bf16 parameters", i);
     REQUIRE(isfinite(t.weight_decay) && isfinite(t.scale), "muon_step: tensor %d: weight decay or scale is not finite",
@@ -1077,6 +1100,11 @@ int foremoe_muon_step(const foremoe_muon_tensor* tensors, int32_t n_tensors, for
             "muon_step: tensor %d: misaligned pointer", i);
   }
   if (!some) return FOREMOE_OK;
+  if (large && !within_half(coef, ns_steps))
+    return set_error(FOREMOE_EUNSUPPORTED,
+                     "muon_step: %d steps of coef (%g, %g, %g) may pass %g on the way, which matrices with both sides "
+                     "above %d cannot hold",
+                     ns_steps, coef[0], coef[1], coef[2], kHalfMost, kSmall);
   REQUIRE(ws, "muon_step: workspace NULL");
   const size_t need = foremoe_muon_workspace_size(tensors, n_tensors);
   REQUIRE(ws_bytes >= need, "muon_step: workspace too small (%zu < %zu bytes)", ws_bytes, need);

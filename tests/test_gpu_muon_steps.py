@@ -146,3 +146,22 @@ def test_small_sides_captured(gpu):
         b.step()
         for x, y in zip((*pa, *a.states, *ga), (*pb, *b.states, *gb)):
             assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("coef,steps", [((15.0, 0.0, 0.0), 2), ((1.0, 125.0, 125.0), 1), ((4.0, -5.0, 2.03), 2)])
+def test_large_sides_up_to_the_range_of_fp16(gpu, coef, steps):
+    """The largest coefficients that are not refused, on the singular values that
+    they drive furthest: 1 alone, and 200 of up to 1."""
+    from paper_2606_11867_amd.optimizer import Muon
+    print(f"\n[case] muon, {steps} steps of {coef}", flush=True)
+    rng = np.random.default_rng(11)
+    for kind in ("rank 1", "steep", "full"):
+        u = matrix(rng, (200, 330), kind)
+        g = torch.from_numpy(u.astype(np.float32)).to(gpu)
+        p = torch.zeros_like(g)
+        Muon([p], [g], lr=1.0, momentum=0.0, nesterov=False, scale=-1.0, steps=steps, coefficients=coef).step()
+        u = u / np.linalg.norm(u)
+        exact, held = R.newton_schulz(u, coef, steps), R.newton_schulz_held(u, coef, steps)
+        # the format's roundings and fp32 sums in another order, as in test_gpu_muon.py
+        lim = 3 * np.linalg.norm(held - exact) + 2.0 ** -18 * np.linalg.norm(exact)
+        assert np.linalg.norm(_np(p) - exact) <= lim and lim <= 2.0 ** -8 * np.linalg.norm(exact), (kind, lim)
