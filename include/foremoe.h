@@ -893,22 +893,25 @@ int foremoe_few_tokens_ffn_mxfp4(const void* x, int64_t ld, int64_t T, int32_t d
  *   p = p (1 - lr weight_decay) - lr scale X
  * p is master where the record has one (param, of bf16, then gets its rounded
  * copy), else param itself. zero_grads != 0: grad is zero afterwards.
- * m and u are fp32, and so are all sums but the norm's, fp64. Where both sides are above 64, X is
- * held as two fp16 numbers (its rounding, and that of 2^10 times what it
- * leaves), G and b G + c G G as one; the products take the first of X (2^-11 of
- * an element, or 2^-33 where that is more), a X takes both, so that directions
- * that u does not have stay small. X is within about 2^-9 of its norm of the
- * exact one. Coefficients with which s^2 or |b s^2 + c s^4| could pass 250 for a
+ * m and u are fp32, and so are all sums but the norm's, fp64. Where both sides
+ * are above 64, X is held as two fp16 numbers (its rounding, and that of 2^10
+ * times what it leaves), G and b G + c G G as one; the products take the first
+ * of X (2^-11 of an element, or 2^-33 where that is more), a X takes both. With
+ * the usual coefficients X is off by 2^-8 of its norm after 5 steps and twice that
+ * after 16 at most (2^-9 and 2^-8 for Gaussian matrices); where u has empty
+ * directions they hold the rounding of X, which each step multiplies by a, 2^-22
+ * a^ns_steps in all: as with X in fp32, they are filled after some 12 steps of
+ * a = 3.4. Coefficients with which s^2 or |b s^2 + c s^4| could pass 250 for a
  * singular value s of an X on the way, from s = 1 at most, are refused
- * (FOREMOE_EUNSUPPORTED; with those that converge s stays below 1.3). Where a side is at most 64, all from u on is fp64, and the
- * parameters are off by their own rounding, 2^-23 of X's norm, and by the
- * rounding of fp64 that the steps multiply by a each, 2^-49 a^ns_steps.
+ * (FOREMOE_EUNSUPPORTED; with those that converge s stays below 1.3). Where a
+ * side is at most 64, all from u on is fp64, and the parameters are off by their
+ * own rounding, 2^-23 of X's norm, and by the rounding of fp64 that the steps
+ * multiply by a each, 2^-49 a^ns_steps.
  * A matrix with a NaN or infinite element, or whose u has one, becomes NaN;
  * the others do not.
  * tensors: HOST array, read during the call only; pointers aligned to their
  * types; param, grad, master and m hold [batch, rows, cols] contiguous, and no
- * two of them overlap. batch
- * = 0: skipped. batch <= 2^30, 1 <= rows, cols <= FOREMOE_MUON_SIDE,
+ * two of them overlap. batch = 0: skipped. batch <= 2^30, 1 <= rows, cols <= FOREMOE_MUON_SIDE,
  * min(rows, cols) <= FOREMOE_MUON_RANK, and with both sides rounded up to 256
  * at most 2^35 elements. 0 <= ns_steps <= 16.
  * coef: HOST array of 3.

@@ -10,8 +10,12 @@
 // leaves; the products take the first, a X takes both. So a product's factors
 // are within 2^-11 of themselves, and directions that u does not have stay
 // at the size that fp32 leaves there: P X alone would fill them with the
-// rounding of X, which each of the first steps multiplies by a. (The last step
-// does without the second numbers: that is one factor a.)
+// rounding of X, which each step multiplies by a. (The last step does without the
+// second numbers: that is one factor a.) Off the exact X by, of its norm, the plain
+// iteration in fp32 beside it (simulated, 130 x 300): Gaussian 2^-9.2 after 5
+// steps and 2^-7.7 after 16, 2^-19 and 2^-18; rank 5, 2^-10.3 after 5 steps and
+// 2^-15, 2^-9.7 after 8 and 2^-9.6, 2^-7.2 after 10 and 2^-6.1, and from 12 on
+// either has filled the empty directions.
 // X, G and P are held 2^8 times as large, which keeps entries of large, even
 // matrices (1/sqrt(m n) and less) above fp16's subnormal numbers.
 //

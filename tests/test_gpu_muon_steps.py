@@ -165,3 +165,29 @@ def test_large_sides_up_to_the_range_of_fp16(gpu, coef, steps):
         # the format's roundings and fp32 sums in another order, as in test_gpu_muon.py
         lim = 3 * np.linalg.norm(held - exact) + 2.0 ** -18 * np.linalg.norm(exact)
         assert np.linalg.norm(_np(p) - exact) <= lim and lim <= 2.0 ** -8 * np.linalg.norm(exact), (kind, lim)
+
+
+@pytest.mark.parametrize("steps", [5, 6, 8, 10, 12, 16])
+@pytest.mark.parametrize("shape", [(130, 300), (300, 130), (256, 256), (66, 70)])
+def test_large_sides(gpu, shape, steps):
+    """Both sides above 64: within what the header says, 2^-8 of the norm, twice
+    that after 16 steps, and 2^-22 a^steps for the rounding of X in directions
+    that u does not have; within three times what the oracle's model
+    of the format gives as long as that is small; and always a matrix whose
+    singular values the iteration bounds (by 1.2024)."""
+    from paper_2606_11867_amd.optimizer import Muon
+    print(f"\n[case] muon {shape}, {steps} steps", flush=True)
+    rng = np.random.default_rng(steps)
+    for kind in KINDS:
+        u = matrix(rng, shape, kind)
+        g = torch.from_numpy(u.astype(np.float32)).to(gpu)
+        p = torch.zeros_like(g)
+        Muon([p], [g], lr=1.0, momentum=0.0, nesterov=False, scale=-1.0, eps=0.0, steps=steps).step()
+        got, u = _np(p), u / np.linalg.norm(u)
+        exact, held = R.newton_schulz(u, USUAL, steps), R.newton_schulz_held(u, USUAL, steps)
+        n, fill = np.linalg.norm(exact), 2.0 ** -22 * USUAL[0] ** steps
+        off = np.linalg.norm(got - exact)
+        assert off <= 2.0 ** -8 * (1 + steps / 16) * n + fill, (kind, off, n)
+        if fill < 2.0 ** -6 * n:
+            assert off <= 3 * np.linalg.norm(held - exact) + 2.0 ** -18 * n, (kind, off, n)
+        assert np.linalg.norm(got, 2) <= 1.2024 * (1 + 2.0 ** -6), kind
