@@ -107,6 +107,13 @@ __device__ __forceinline__ int find_rec(const MuonArgs& a, uint32_t b) {
   return r;
 }
 
+// 1 / max(norm, eps). Nothing in the matrix: no move, also where 1 / eps is
+// infinite; not finite: NaN everywhere.
+__device__ __forceinline__ double inverse_norm(double norm, double eps) {
+  if (norm == 0) return 0.0;
+  return norm < INFINITY ? 1.0 / fmax(norm, eps) : (double)NAN;
+}
+
 // Four neighbours of a tensor, from element i on: at once (wide), or those
 // of them that are below n.
 template <bool BF16_T>
@@ -212,10 +219,7 @@ __global__ __launch_bounds__(256) void muon_scale_kernel(MuonArgs a) {
   for (uint32_t i = tid & 63; i < r.chunks; i += 64) s += r.squares[matrix * r.chunks + i];
 #pragma unroll
   for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o, 64);
-  const double norm = sqrt(s);
-  const double den = !(norm <= a.eps) ? norm : a.eps;
-  // nothing in it: no move; not finite: NaN everywhere
-  const double inv = den == 0 ? 0.0 : (isinf(den) ? (double)NAN : 1.0 / den);
+  const double inv = inverse_norm(sqrt(s), a.eps);
   const float gs = a.grad_scale ? *a.grad_scale : 1.0f;
   const int64_t base = matrix * (int64_t)r.rows * r.cols;
   // read along the source's rows
@@ -704,10 +708,7 @@ __global__ __launch_bounds__(kSmallThreads) void muon_small_steps_kernel(MuonArg
     double s = lane < m ? G[lane][lane] : 0.0;
 #pragma unroll
     for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o, 64);
-    const double norm = sqrt(s);
-    const double den = !(norm <= a.eps) ? norm : a.eps;
-    // nothing in it: no move; not finite: NaN everywhere
-    const double inv = den == 0 ? 0.0 : (isinf(den) ? (double)NAN : 1.0 / den);
+    const double inv = inverse_norm(sqrt(s), a.eps);
     __syncthreads();
     for (int o = tid; o < 16 * nt * 64; o += kSmallThreads)
       if ((o & 63) < 16 * nt) G[o >> 6][o & 63] *= inv * inv;

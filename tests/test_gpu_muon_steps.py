@@ -191,3 +191,25 @@ def test_large_sides(gpu, shape, steps):
         if fill < 2.0 ** -6 * n:
             assert off <= 3 * np.linalg.norm(held - exact) + 2.0 ** -18 * n, (kind, off, n)
         assert np.linalg.norm(got, 2) <= 1.2024 * (1 + 2.0 ** -6), kind
+
+
+@pytest.mark.parametrize("eps", [0.0, 5e-324, 1e-310, 1e-200, 1e-100, 1e-7, 1e300])
+@pytest.mark.parametrize("shape", [(3, 40, 50), (3, 90, 70)])
+def test_nothing_does_not_move_whatever_eps(gpu, shape, eps):
+    """The inverse of the least eps is infinite, and that of others squared; the
+    matrices beside the empty one go by the larger of their norm and eps."""
+    from paper_2606_11867_amd.optimizer import Muon
+    print(f"\n[case] muon {shape} eps={eps}", flush=True)
+    rng = np.random.default_rng(4)
+    u = np.stack([matrix(rng, shape[1:], "full") for _ in range(3)])
+    u[1] = 0.0
+    for steps in (0, 5, 13):
+        g = torch.from_numpy(u.astype(np.float32)).to(gpu)
+        p = torch.ones(shape, device=gpu)
+        Muon([p], [g], lr=1.0, momentum=0.0, nesterov=False, scale=-1.0, eps=eps, steps=steps).step()
+        assert bool((p[1] == 1.0).all())
+        for i in (0, 2):
+            exact = R.newton_schulz(u[i] / max(np.linalg.norm(u[i]), eps), USUAL, steps)
+            # X of its format, and p = 1 + X in fp32
+            lim = 2.0 ** -7 * np.linalg.norm(exact) + 2.0 ** -23 * np.linalg.norm(1 + exact)
+            assert np.linalg.norm(_np(p[i]) - 1 - exact) <= lim, (steps, i)
