@@ -861,8 +861,8 @@ int foremoe_grouped_ffn_mxfp4_fwd(const uint8_t* x_codes, const uint8_t* x_scale
  * as fast from 2 to 8 places of each picked expert on, and faster above.
  * The same call gives the same bits. How the sums over d and F are cut depends
  * on T, K and which experts are picked, so a token's may differ with the others
- * beside it by fp32 roundings. A NaN stays with the tokens that meet it; an
- * infinite element of Wd may give NaN where the sum would be infinite.
+ * beside it by fp32 roundings. A NaN or infinity stays with the tokens that meet
+ * it.
  * ws: foremoe_few_workspace_size(T, K, F) bytes for the hidden rows (one of
  * the largest T, K and F serves smaller calls), 256-byte aligned; needs no
  * initialisation. Calls that share one must not overlap in time.

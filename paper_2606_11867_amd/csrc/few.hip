@@ -579,8 +579,11 @@ __device__ __forceinline__ void down_groups(const FewArgs& a, const Groups& G, i
     for (int e = 0; e < 4; ++e) {
       float v = acc[i][e];  // row 4 g + e, column r
       if constexpr (S == 2) v += __shfl(v, (lane + 40) & 63, 64);  // of the odd chunks: row + 8, column + 8
-      if constexpr (PL >= 2) v += __shfl(v, (lane + ROWS / 2) & 63, 64);  // the other planes
-      if constexpr (PL == 4) v += __shfl(v, (lane + ROWS / 4) & 63, 64);
+      if constexpr (PL >= 2) {  // and the other planes, but for those of an infinite sum, which hold infinity times 0
+        float all = v + __shfl(v, (lane + ROWS / 2) & 63, 64);
+        if constexpr (PL == 4) all += __shfl(all, (lane + ROWS / 4) & 63, 64);
+        v = fabsf(v) < INFINITY ? all : v;
+      }
       const int q = first + P * i + r;
       if (r < P && 4 * g < ROWS && q < end) yp[q * ROWS + 4 * g + e] = v;
     }
