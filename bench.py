@@ -856,7 +856,8 @@ def planner_report(w, api, dev, n_micro: int, N_r: int = 4, C_max: int = 8) -> d
 
 TRAFFIC_RECORD = os.path.join(ROOT, "profiles", "traffic_qwen3_share.json")
 DISPATCH_SOURCES = ["paper_2606_11867_amd/csrc/dispatch.hip"]
-ROW_GEMM_SOURCES = ["paper_2606_11867_amd/csrc/grouped_gemm.hip", "paper_2606_11867_amd/csrc/row_units.h"]
+ROW_GEMM_SOURCES = ["paper_2606_11867_amd/csrc/grouped_gemm.hip", "paper_2606_11867_amd/csrc/mfma_tiles.h",
+                    "paper_2606_11867_amd/csrc/row_units.h"]
 # the kernels of every phase; a name that serves two phases is dispatched
 # once for each per micro-step, in this order (one-stream and overlapped
 # schedules alike)
