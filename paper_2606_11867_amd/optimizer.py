@@ -202,7 +202,8 @@ class Muon:
         if len(self._grads) != n:
             raise ValueError("params and grads differ in number")
         self.lr, self.momentum, self.nesterov, self.eps, self.steps = lr, momentum, bool(nesterov), eps, int(steps)
-        self.coefficients, self.zero_grads = tuple(coefficients), bool(zero_grads)
+        a, b, c = coefficients
+        self.coefficients, self.zero_grads = (a, b, c), bool(zero_grads)
         self.device = self._params[0].device
         bf16 = self._params[0].dtype == torch.bfloat16
         self._dtypes = self._params[0].dtype, self._grads[0].dtype
@@ -311,7 +312,8 @@ class Muon:
         if list(map(torch.Tensor.data_ptr, self._tensors)) != self._at or self._rates != (self._weight_decay,
                                                                                           self._scale):
             self._fill()
-        coef = (ctypes.c_double * 3)(*self.coefficients)
+        a, b, c = self.coefficients
+        coef = (ctypes.c_double * 3)(a, b, c)
         scale = _vec(grad_scale, 1, F32, "grad_scale", self.device)
         _call(self.device, self.lib.foremoe_muon_step, (
             self._records, len(self._params), self._pdt, self._gdt, self.lr, self.momentum, self.nesterov, self.steps,

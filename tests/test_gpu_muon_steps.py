@@ -213,3 +213,17 @@ def test_nothing_does_not_move_whatever_eps(gpu, shape, eps):
             # X of its format, and p = 1 + X in fp32
             lim = 2.0 ** -7 * np.linalg.norm(exact) + 2.0 ** -23 * np.linalg.norm(1 + exact)
             assert np.linalg.norm(_np(p[i]) - 1 - exact) <= lim, (steps, i)
+
+
+def test_coefficients_are_three(gpu):
+    """Two would leave the last at 0."""
+    from paper_2606_11867_amd.optimizer import Muon
+    p, g = torch.ones(8, 8, device=gpu), torch.ones(8, 8, device=gpu)
+    for bad in ((1.5, -0.5), (1.0, 2.0, 3.0, 4.0)):
+        with pytest.raises(ValueError):
+            Muon([p], [g], coefficients=bad)
+        opt = Muon([p], [g])
+        opt.coefficients = bad
+        with pytest.raises(ValueError):
+            opt.step()
+    assert bool((p == 1).all())
