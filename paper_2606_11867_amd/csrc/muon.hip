@@ -59,8 +59,8 @@ struct MuonRec {
       double* squares;           // [batch, chunks]
     };
     struct {  // small matrices (m <= 64)
-      double* part;     // [batch, chunks, 10 tiles of 16 x 16]: of each chunk of columns u u^T
-      double* q;        // [batch, 64, 64]: Q
+      double* part;     // [batch, chunks, tiles of 16 x 16 on and above the diagonal]: of each chunk of columns u u^T
+      double* q;        // [batch, whole tiles of rows and columns]: Q
       double* inverse;  // [batch]: 1 / max(|u|, eps)
       double* held;     // [batch, m, n]: X between two stages
     };
@@ -550,15 +550,18 @@ __global__ __launch_bounds__(256) void muon_update_kernel(MuonArgs a) {
 // the rounding of fp32 whatever the rank of u and the number of steps (simulated:
 // 2^-24 of its norm after 16 steps, where the plain iteration in fp32 has filled
 // the empty directions). Latency bounds it: the small ones of six matrices with
-// sides of 24 to 400 take 8, 25 and 15 us (in fp32 9, 27 and 13).
+// sides of 24 to 400 take 8, 25 and 13 us (in fp32 9, 27 and 13).
 // ---------------------------------------------------------------------------
 constexpr int kSmall = 64, kSmallChunks = 64;
 constexpr int kSmallLD = 68;       // doubles of a row in LDS: 16 rows of 4 are 2 to a bank
-constexpr int kSmallTiles = 10;    // 16 x 16 tiles on and above the diagonal
 constexpr int kSmallThreads = 512; // of a matrix's steps: two wavefronts a SIMD
 
 typedef double f64x4 __attribute__((ext_vector_type(4)));
 typedef double SmallRow[kSmallLD];
+
+// 16 x 16 tiles along a side of m, and of the upper triangle.
+__host__ __device__ __forceinline__ int small_tiles(int m) { return (m + 15) / 16; }
+__host__ __device__ __forceinline__ int small_upper(int m) { return small_tiles(m) * (small_tiles(m) + 1) / 2; }
 
 // Tile t of the upper triangle, column by column: those of a smaller matrix come first.
 __device__ __forceinline__ void small_tile(int t, int& ti, int& tj) {
@@ -655,10 +658,10 @@ __global__ __launch_bounds__(256) void muon_small_gram_kernel(MuonArgs a) {
   const uint32_t b = blockIdx.x - a.first.at[ri];
   const int64_t matrix = b / r.chunks, chunk = b % r.chunks;
   const bool tall = r.rows > r.cols;
-  const int n = tall ? r.rows : r.cols, nt = ((tall ? r.cols : r.rows) + 15) / 16;
+  const int n = tall ? r.rows : r.cols;
   const int blocks = (n + 63) / 64;  // of the long side
   const int b0 = (int)(blocks * chunk / r.chunks), b1 = (int)(blocks * (chunk + 1) / r.chunks);
-  const int wave = wave_id(), tiles = nt * (nt + 1) / 2;
+  const int wave = wave_id(), tiles = small_upper(tall ? r.cols : r.rows);
   __shared__ SmallRow u[kSmall];
   f64x4 acc[3];
 #pragma unroll
@@ -674,7 +677,7 @@ __global__ __launch_bounds__(256) void muon_small_gram_kernel(MuonArgs a) {
       if (wave + 4 * p < tiles) acc[p] = small_product(u, u, ti, tj, kSmall, acc[p]);
     }
   }
-  double* to = r.part + (matrix * r.chunks + chunk) * (kSmallTiles * 256) + lane64();
+  double* to = r.part + (matrix * r.chunks + chunk) * (tiles * 256) + lane64();
 #pragma unroll
   for (int p = 0; p < 3; ++p)
     if (wave + 4 * p < tiles)
@@ -688,20 +691,21 @@ __global__ __launch_bounds__(kSmallThreads) void muon_small_steps_kernel(MuonArg
   const int ri = find_rec(a, blockIdx.x);
   const MuonRec& r = a.rec[ri];
   const int64_t matrix = blockIdx.x - a.first.at[ri];
-  const int m = r.rows < r.cols ? r.rows : r.cols, n = (m + 3) & ~3, nt = (m + 15) / 16, tiles = nt * (nt + 1) / 2;
+  const int m = r.rows < r.cols ? r.rows : r.cols, n = (m + 3) & ~3, side = 16 * small_tiles(m);
+  const int tiles = small_upper(m);
   const int tid = threadIdx.x, lane = lane64(), wave = wave_id();
   __shared__ SmallRow G[kSmall], M[kSmall], S[kSmall], Q[kSmall];
-  const double* part = r.part + matrix * r.chunks * (kSmallTiles * 256);
+  const double* part = r.part + matrix * r.chunks * (tiles * 256);
   for (int o = tid; o < tiles * 256; o += kSmallThreads) {
     double s = 0;
 #pragma unroll 8
-    for (int c = 0; c < (int)r.chunks; ++c) s += part[c * (kSmallTiles * 256) + o];
+    for (int c = 0; c < (int)r.chunks; ++c) s += part[c * (tiles * 256) + o];
     int ti, tj;
     small_tile(o >> 8, ti, tj);
     const int i = 16 * ti + (o >> 6 & 3) * 4 + (lane >> 4), j = 16 * tj + (lane & 15);
     if (i <= j) G[i][j] = s, G[j][i] = s;
   }
-  for (int o = tid; o < kSmall * kSmall; o += kSmallThreads) Q[o >> 6][o & 63] = (o >> 6) == (o & 63) ? 1.0 : 0.0;
+  for (int o = tid; o < side * side; o += kSmallThreads) Q[o / side][o % side] = o / side == o % side ? 1.0 : 0.0;
   __syncthreads();
   if (a.from_u) {
     // |u|^2, summed in the same order by every wavefront
@@ -710,8 +714,7 @@ __global__ __launch_bounds__(kSmallThreads) void muon_small_steps_kernel(MuonArg
     for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o, 64);
     const double inv = inverse_norm(sqrt(s), a.eps);
     __syncthreads();
-    for (int o = tid; o < 16 * nt * 64; o += kSmallThreads)
-      if ((o & 63) < 16 * nt) G[o >> 6][o & 63] *= inv * inv;
+    for (int o = tid; o < side * side; o += kSmallThreads) G[o / side][o % side] *= inv * inv;
     if (tid == 0) r.inverse[matrix] = inv;
     __syncthreads();
   }
@@ -754,7 +757,7 @@ __global__ __launch_bounds__(kSmallThreads) void muon_small_steps_kernel(MuonArg
     }
     __syncthreads();
   }
-  for (int o = tid; o < kSmall * kSmall; o += kSmallThreads) r.q[matrix * (kSmall * kSmall) + o] = Q[o >> 6][o & 63];
+  for (int o = tid; o < side * side; o += kSmallThreads) r.q[matrix * (side * side) + o] = Q[o / side][o % side];
 }
 
 // X = Q X for 64 of the long side: into the parameters, or held for the next
@@ -771,7 +774,8 @@ __global__ __launch_bounds__(256) void muon_small_apply_kernel(MuonArgs a) {
   const int l0 = (int)(b % blocks) * 64;
   const int64_t base = matrix * (int64_t)r.rows * r.cols;
   __shared__ SmallRow u[kSmall], Q[kSmall];
-  for (int i = tid; i < kSmall * kSmall; i += 256) Q[i >> 6][i & 63] = r.q[matrix * (kSmall * kSmall) + i];
+  const int side = 16 * small_tiles(m);
+  for (int i = tid; i < side * side; i += 256) Q[i / side][i % side] = r.q[matrix * (side * side) + i];
   small_x<GBF16, false>(a, r, matrix, l0, a.from_u ? r.inverse[matrix] : 1.0, u);
   __syncthreads();
   // rows 16 wave .. of X, all 64 columns
@@ -893,8 +897,8 @@ size_t lay_out(const foremoe_muon_tensor& t, int tile, size_t at, char* ws, Muon
     // parts of u u^T to be joined by one workgroup: 16, more for the longest
     const int64_t most = tiles < 256 ? 16 : kSmallChunks;
     q.chunks = (uint32_t)(tiles < most ? tiles : most);
-    q.part = (double*)take((size_t)t.batch * q.chunks * kSmallTiles * 256 * 8);
-    q.q = (double*)take((size_t)t.batch * kSmall * kSmall * 8);
+    q.part = (double*)take((size_t)t.batch * q.chunks * small_upper((int)s) * 256 * 8);
+    q.q = (double*)take((size_t)t.batch * small_tiles((int)s) * small_tiles((int)s) * 256 * 8);
     q.inverse = (double*)take((size_t)t.batch * 8);
     q.held = (double*)take((size_t)t.batch * s * l * 8);
     if (r) *r = q;

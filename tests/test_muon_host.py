@@ -59,3 +59,20 @@ def test_coefficients(lib, coef):
         assert b"coef" in lib.foremoe_last_error()
     if coef == USUAL:
         assert call(lib, coef, 16, (4096, 4100)) == -1
+
+
+def test_workspace_of_small_matrices(lib):
+    """By their tiles of 16: a batch of as many tiny ones as are accepted fits beside them."""
+    from paper_2606_11867_amd import _lib
+
+    def size(batch, r, c):
+        return lib.foremoe_muon_workspace_size((_lib.MuonTensor * 1)(_lib.MuonTensor(None, None, None, None, batch, r, c,
+                                                                                    0.0, 1.0)), 1)
+
+    for (r, c), t, pieces in (((1, 1), 1, 1), ((16, 64), 1, 1), ((17, 65), 2, 2), ((64, 64), 4, 1), ((1000, 60), 4, 16),
+                              ((5, 1 << 20), 1, 64)):
+        for batch in (1, 7) if c > 100 else (1, 7, 1 << 19):
+            if batch == 1 << 19 and r > 256:
+                continue
+            need = batch * (2048 * (pieces * (t * (t + 1) // 2) + t * t) + 8 + 8 * r * c)
+            assert need <= size(batch, r, c) <= need + 4 * 256
