@@ -857,8 +857,10 @@ int foremoe_grouped_ffn_mxfp4_fwd(const uint8_t* x_codes, const uint8_t* x_scale
  * and x and the hidden rows below 3.7 GB (else FOREMOE_EUNSUPPORTED).
  * Pointers aligned to their types, w_* and codes to 16 bytes; _mxfp4: x's rows
  * to 16 bytes (ld a multiple of 8).
- * For few places an expert: with bf16 weights steps 1-5 by their own calls are
- * as fast from 2 to 8 places of each picked expert on, and faster above.
+ * For few places an expert: steps 1-5 by their own calls are as fast from some
+ * number of places of each picked expert on, and faster above: 2 to 8 with bf16
+ * weights, 8 to 16 with fp32 ones, and 1 to 4 with 4-bit ones where the rows
+ * may be in 4 bits too (foremoe_grouped_ffn_mxfp4_fwd).
  * The same call gives the same bits. How the sums over d and F are cut depends
  * on T, K and which experts are picked, so a token's may differ with the others
  * beside it by fp32 roundings. A NaN or infinity stays with the tokens that meet

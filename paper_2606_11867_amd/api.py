@@ -367,7 +367,8 @@ _SCORES = {"softmax": _lib.SOFTMAX, "sigmoid": _lib.SIGMOID}
 
 def _rows(t: torch.Tensor, name: str) -> int:
     """Checks a [rows, columns] device tensor whose rows are contiguous and do
-    not overlap; returns the elements from one row to the next."""
+    not overlap (without rows, its strides mean nothing and are not looked at);
+    returns the elements from one row to the next."""
     if not t.is_cuda:
         raise ValueError(f"{name}: expected a device tensor")
     if t.dim() != 2:
@@ -711,8 +712,9 @@ def few_tokens_ffn(x: torch.Tensor, ids: torch.Tensor, gates: torch.Tensor,
     [W, 2F, d], [W, d, F] of x's type or in 4 bits (then x is bf16). expert_widx
     [E] int32: which weights an expert has here, -1: none (its part of the sum
     is another rank's); without it expert e has weights e. Made for few places an
-    expert: from 2 to 8 on, permute, grouped_ffn_fwd and combine are as fast in
-    bf16. out_dtype: by default x's. ws: from few_tokens_workspace (one is made
+    expert: permute, grouped_ffn_fwd and combine are as fast from 2 to 8 places of
+    each picked one on in bf16, from 8 to 16 on in fp32, and, with rows in 4 bits
+    too, grouped_ffn_mxfp4_fwd from 1 to 4 on. out_dtype: by default x's. ws: from few_tokens_workspace (one is made
     when missing)."""
     ld = _rows(x, "x")
     T, d = x.shape

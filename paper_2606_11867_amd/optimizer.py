@@ -180,6 +180,9 @@ class Muon:
     scale: how far a step goes, lr times it; one for all, one per tensor, or
     None for 0.2 sqrt(max(rows, columns)) of the matrix, with which the move of
     an element is about as large as AdamW's.
+    coefficients, steps: of the iteration. A matrix with both sides above 64 is
+    iterated on in fp16 products; a step() whose coefficients could leave their
+    range is refused. How far the result is off goes by the steps: see the header.
     masters, zero_grads, weight_decay, and giving params and grads other
     memory: as AdamW. states: the momenta, fp32, used in place; None starts
     from zero. ws: scratch, by default the optimizer's own.
